@@ -84,14 +84,14 @@ typedef struct {
 } kvs_config;
 
 typedef struct {
-    uint64_t append_launches;     /* kernels launched by kvs_append                          */
-    uint64_t append_skipped;      /* kvs_append calls on sharing layers (no launch)          */
+    uint64_t append_launches;     /* kernels launched by kvs_append, kvs_append_rotary       */
+    uint64_t append_skipped;      /* the same on sharing layers (nothing appended)           */
     uint64_t attention_launches;  /* split-K kernels launched                                */
     uint64_t combine_launches;    /* combine kernels launched                                */
     uint64_t kv_bytes_read;       /* 2*B*Hkv*n*D*elem summed over attention calls            */
     uint64_t kv_bytes_appended;   /* 2*B*Hkv*n_new*D*elem summed over launched appends       */
-    uint64_t prefill_launches;    /* tensor-core prefill kernels launched                    */
-    uint64_t evict_launches;      /* kvs_evict calls that launched                           */
+    uint64_t prefill_launches;    /* kvs_prefill_attention and kvs_tree_attention calls      */
+    uint64_t evict_launches;      /* kvs_evict and kvs_accept_draft calls that launched      */
     uint64_t search_launches;     /* kernels launched by kvs_layer_distances / kvs_mean_cosine */
     uint64_t fused_appends;       /* kvs_decode_step calls whose append rode in the split-K kernel */
 } kvs_stats_t;
@@ -248,6 +248,95 @@ kvs_status kvs_prefill_attention(kvs_ctx* ctx, int32_t layer, const void* q, flo
  * Errors: STATE before bind or on an empty slot; INVALID_ARG for bad sizes or batch != cached batch. */
 kvs_status kvs_evict(kvs_ctx* ctx, int32_t layer, const int32_t* keep, const int32_t* n_keep,
                      int32_t keep_stride, int32_t batch, void* stream);
+
+/* ---- tokens enter the cache: norms, positions and storage in one pass -------------------------- */
+
+typedef struct {
+    int32_t rotary_dim;     /* rotated elements of a head: 0 (none) .. head_dim, a multiple of 16          */
+    int32_t interleaved;    /* 0: pair i is elements (i, i + rotary_dim/2); 1: elements (2i, 2i + 1)       */
+    float eps;              /* added to the mean square of the norm                                        */
+    const double* inv_freq; /* host, rotary_dim/2 entries: radians per position of every pair              */
+} kvs_rotary;
+
+/* kvs_append of new tokens whose queries and keys still lack their per-head norm and their position:
+ *   norm      x' = x / sqrt(mean(x^2) + eps) * weight, over the head (left out where the weight is NULL)
+ *   rotation  pair (x0, x1) of index i by the angle a = positions[b][t] * inv_freq[i]:
+ *             (x0 cos a - x1 sin a, x1 cos a + x0 sin a); elements from rotary_dim on are not rotated
+ * computed in fp32 (the angle in fp64, so that far positions keep their phase) and rounded to the storage type
+ * once.  Keys and values (the latter bit for bit) go to rows len .. len+n_new-1 of the layer's slot exactly as
+ * kvs_append stores them, queries to q_out, ready for the attention calls.  A layer whose cache is replaced has
+ * its queries processed and nothing else: k and v are not read and may be NULL, nothing is appended.
+ *   rot:       host, read during the call
+ *   q, k, v:   device, storage type, 16-byte aligned; token t of sequence b starts (b * n_new + t) * stride elements
+ *              in, its heads are contiguous: slices of one projection's output need no copy.  Strides are
+ *              multiples of 16 bytes and at least a token's row
+ *   positions: device, int32 [batch][n_new], any value (NULL only if rotary_dim is 0)
+ *   q_weight, k_weight: device, storage type [head_dim], 16-byte aligned, or NULL
+ *   q_out:     device, storage type [batch][n_new][n_q_heads][head_dim], 16-byte aligned; may be q itself where q
+ *              is packed (q_stride = n_q_heads * head_dim), must not overlap the inputs otherwise
+ * One launch.  Under KVS_OPT_REPLAY it counts as the layer's append of the step (n_new = 1).
+ * Errors: as kvs_append; INVALID_ARG for the above.                                                          */
+kvs_status kvs_append_rotary(kvs_ctx* ctx, int32_t layer, const kvs_rotary* rot, const void* q, int64_t q_stride,
+                             const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                             const void* q_weight, const void* k_weight, void* q_out, int32_t batch, int32_t n_new,
+                             void* stream);
+
+/* ---- verification of drafted tokens ------------------------------------------------------------- */
+
+/* Attention of a tree of drafted tokens.  The n_t drafts (1 .. 64) are the newest n_t rows of the cache the layer
+ * uses: append them first (on a sharing layer: the source layer's append), in any order of the tree.  Draft t sees
+ * every row before the drafts and those drafts j whose bit j is set in its mask word; bits from n_t on are ignored.
+ *   q:    device, [batch][n_t][n_q_heads][head_dim], storage type, 16-byte aligned
+ *   mask: device, uint64 [batch][n_t]; a draft that is to see itself has its own bit set.  NULL: draft t sees
+ *         drafts 0 .. t (a chain)
+ *   out:  device, same shape and type as q, 16-byte aligned.  The storage type, not float32 as in
+ *         kvs_decode_attention: 64 times the rows go on to the next matrix product in that type
+ * A draft that sees nothing at all (an empty context and an empty mask) gets zeros.  What a masked draft's rows hold
+ * (NaN of a padding token included) does not reach the result.  Works on ragged slots too: a unit's drafts are its
+ * own newest n_t rows.
+ * Errors: as kvs_decode_attention; INVALID_ARG if a unit holds fewer than n_t rows; STATE under KVS_OPT_REPLAY.  */
+kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* out, const uint64_t* mask, int32_t batch,
+                              int32_t n_t, void* stream);
+
+/* Keep the accepted drafts of every slot and forget the others: of a unit's newest n_draft rows, rows path[b][0],
+ * path[b][1], ... path[b][n_accept[b]-1] (numbers among the drafts, strictly ascending: ancestors come first) move
+ * to the front of the drafts, bit for bit, and the unit ends behind them.
+ *   path:     device, int32 [batch][path_stride], the same for all layers
+ *   n_accept: host, int32 [batch], each 0 .. n_draft and at most path_stride
+ * Where all sequences keep the same number a slot stays as it is; otherwise its units differ in length afterwards,
+ * as after kvs_evict (kvs_prefill_attention and kvs_truncate then refuse it).  One launch per slot.  A path that is
+ * not ascending or out of range cannot be seen by the host: the kernel leaves the row already there and sets the
+ * device status word to KVS_ERR_INVALID_ARG.
+ * Errors: STATE before bind, under KVS_OPT_REPLAY, or if a unit of some slot holds fewer than n_draft rows;
+ * INVALID_ARG for bad sizes, batch != cached batch, or counts that differ and leave some unit empty.              */
+kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stride, const int32_t* n_accept, int32_t n_draft,
+                            int32_t batch, void* stream);
+
+/* ---- reducing a cache by attention weight -------------------------------------------------------- */
+
+/* kvs_decode_attention that also adds up how much attention every cached row received:
+ *   total_out[b][h][j] = total_in[b][h][j] + sum over the group's G q-heads of softmax_j
+ * for every row j the unit holds; what lies behind them in total_out is left as it is.
+ *   total_in:  device, float32 [batch][n_kv_heads][total_stride], or NULL: zeros
+ *   total_out: the same layout; may be total_in itself, must not overlap it otherwise
+ *   total_stride: at least the slot's rows (under KVS_OPT_REPLAY: max_seq)
+ * The sums are made in a fixed order: the same call gives the same bits.  Two launches.
+ * Other arguments and errors: as kvs_decode_attention.                                                        */
+kvs_status kvs_decode_attention_weights(kvs_ctx* ctx, int32_t layer, const void* q, float* out, const float* total_in,
+                                        float* total_out, int32_t total_stride, int32_t batch, void* stream);
+
+/* Which rows a budget keeps: of every (sequence, kv-head) unit the newest n_recent rows and, of the others, the
+ * n_keep - n_recent with the largest totals (equal totals: the older row; -0 equals 0; NaN is below everything).
+ *   total:      device, float32 [batch][n_kv_heads][total_stride], total_stride at least the slot's rows
+ *   n_keep:     host, int32 [batch * n_kv_heads], each 1 .. the unit's rows, at least n_recent, at most keep_stride
+ *   keep:       device, int32 [batch][n_kv_heads][keep_stride]: the row numbers, ascending, as kvs_evict takes them
+ *   kept_total: device, float32, the layout of keep, or NULL: the rows' totals, i.e. the totals of the slot once
+ *               kvs_evict has applied the list; must not overlap total
+ * What lies behind a unit's n_keep entries is left as it is.  Nothing is evicted: the slot is not changed, and the
+ * layer may be a sharing one (its source's slot is meant).  One launch per 900 units.
+ * Errors: STATE before bind, on an empty slot, or under KVS_OPT_REPLAY; INVALID_ARG for the above.             */
+kvs_status kvs_select_rows(kvs_ctx* ctx, int32_t layer, const float* total, int32_t total_stride, const int32_t* n_keep,
+                           int32_t n_recent, int32_t* keep, float* kept_total, int32_t keep_stride, int32_t batch, void* stream);
 
 /* Rows cached for sequence b, kv-head h of the slot `layer` reads. */
 kvs_status kvs_unit_len(const kvs_ctx* ctx, int32_t layer, int32_t b, int32_t h, int32_t* len);

@@ -11,7 +11,29 @@ from .binding import (  # noqa: F401
     KVS_BF16, KVS_F32, KVS_OK, KVS_OPT_EARLY_START, KVS_OPT_FINISH_IN_KERNEL, KVS_OPT_HOST_CHUNKS, KVS_OPT_KERNEL, KVS_OPT_MAX_CTAS, KVS_OPT_REPLAY, KVS_OPT_WAIT_LIMIT_US, KvsError,
 )
 
-__all__ = ["binding", "SharedKVCache", "KvsError"]
+__all__ = ["binding", "SharedKVCache", "Rotary", "KvsError"]
+
+
+class Rotary:
+    """Rotary positions for ``append_rotary``: radians per position of every pair (``rotary_dim / 2`` numbers).
+
+    ``Rotary.from_theta(dim, theta)`` gives the usual ``theta ** (-2 i / dim)``.  ``interleaved``: pair i is elements
+    (2i, 2i + 1) of the head instead of (i, i + dim / 2).
+    """
+
+    def __init__(self, inv_freq, interleaved=False):
+        import ctypes
+
+        values = [float(x) for x in inv_freq]
+        self._array = (ctypes.c_double * max(len(values), 1))(*values)
+        self.rotary_dim, self.interleaved = 2 * len(values), int(bool(interleaved))
+
+    def _struct(self, eps):
+        return binding.kvs_rotary(self.rotary_dim, self.interleaved, eps, self._array)
+
+    @classmethod
+    def from_theta(cls, rotary_dim, theta=10000.0, interleaved=False):
+        return cls([theta ** (-2.0 * i / rotary_dim) for i in range(rotary_dim // 2)], interleaved)
 
 
 class SharedKVCache:
@@ -109,6 +131,93 @@ class SharedKVCache:
         assert keep.is_contiguous() and keep.dtype == self._torch.int32 and keep.ndim == 3
         counts = [int(x) for x in self._torch.as_tensor(n_keep).reshape(-1).tolist()]
         binding.kvs_evict(self.ctx, layer, keep, counts, keep.shape[2], keep.shape[0], self._stream())
+
+    def _token_stride(self, x, heads, shape):
+        """Elements between consecutive tokens of ``[batch][n_new][heads][head_dim]`` (heads contiguous)."""
+        assert x.dtype == self.dtype and x.shape == (*shape, heads, self.shape[3])
+        step = x.stride(1) if x.shape[1] > 1 else (x.stride(0) if x.shape[0] > 1 else heads * self.shape[3])
+        assert x.stride(3) == 1 and (heads == 1 or x.stride(2) == self.shape[3])
+        assert x.shape[0] == 1 or x.stride(0) == x.shape[1] * step, "tokens of all sequences must be evenly spaced"
+        return step
+
+    def append_rotary(self, layer, q, k, v, positions, rotary, q_weight=None, k_weight=None, eps=1e-6, out=None):
+        """New tokens: per-head RMS norm (where a weight is given) and rotary positions of q and k, k and v appended
+        to the layer's slot, the finished queries returned.  q, k, v: ``[batch][n_new][heads][head_dim]``, slices of
+        one projection's output allowed (k, v: None on a sharing layer); positions: int32 ``[batch][n_new]``."""
+        torch = self._torch
+        shape = q.shape[:2]
+        qs = self._token_stride(q, self.shape[1], shape)
+        ks = vs = 0
+        if k is not None:
+            ks, vs = self._token_stride(k, self.shape[2], shape), self._token_stride(v, self.shape[2], shape)
+        assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == shape)
+        for w in (q_weight, k_weight):
+            assert w is None or (w.dtype == self.dtype and w.is_contiguous() and w.numel() == self.shape[3])
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        assert out.is_contiguous() and out.dtype == self.dtype and out.shape == q.shape
+        binding.kvs_append_rotary(self.ctx, layer, rotary._struct(eps), q, qs, k, ks, v, vs, positions, q_weight, k_weight, out,
+                                  shape[0], shape[1], self._stream())
+        return out
+
+    def tree_attention(self, layer, q, mask=None, out=None):
+        """Attention of drafted tokens, the newest n_t rows of the cache.  q: ``[batch][n_t][n_q_heads][head_dim]``;
+        mask: int64 ``[batch][n_t]``, bit j of a word: the token sees draft j (None: a chain).  Returns q's type."""
+        torch = self._torch
+        assert q.is_contiguous() and q.dtype == self.dtype and q.ndim == 4 and q.shape[2:] == (self.shape[1], self.shape[3])
+        assert mask is None or (mask.dtype in (torch.int64, torch.uint64) and mask.is_contiguous() and mask.shape == q.shape[:2])
+        if out is None:
+            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
+        assert out.is_contiguous() and out.dtype == self.dtype and out.shape == q.shape
+        binding.kvs_tree_attention(self.ctx, layer, q, out, mask, q.shape[0], q.shape[1], self._stream())
+        return out
+
+    def accept_draft(self, path, n_accept, n_draft):
+        """Keep the accepted drafts in every slot.  path: int32 ``[batch][stride]`` draft numbers, ascending; n_accept:
+        how many of them each sequence keeps (host)."""
+        assert path.dtype == self._torch.int32 and path.is_contiguous() and path.ndim == 2 and len(n_accept) == path.shape[0]
+        binding.kvs_accept_draft(self.ctx, path, path.shape[1], [int(x) for x in n_accept], n_draft, path.shape[0], self._stream())
+
+    def decode_attention_weights(self, layer, q, total_in, total_out=None, out=None):
+        """``decode_attention`` that also returns, in ``total_out``, ``total_in`` (None: zeros) plus every row's softmax
+        weight summed over its group of q-heads: float32 ``[batch][n_kv_heads][stride]``; without ``total_out`` the
+        totals are updated in place."""
+        torch = self._torch
+        assert q.is_contiguous() and q.dtype == self.dtype and q.shape[1:] == (self.shape[1], self.shape[3])
+        if total_out is None:
+            total_out = total_in
+        for x in (total_in, total_out):
+            assert x is None or (x.dtype == torch.float32 and x.is_contiguous() and x.ndim == 3 and x.shape == total_out.shape)
+        assert total_out.shape[:2] == (q.shape[0], self.shape[2])
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.float32, device=self.device)
+        binding.kvs_decode_attention_weights(self.ctx, layer, q, out, total_in, total_out, total_out.shape[2], q.shape[0],
+                                             self._stream())
+        return out
+
+    def select_rows(self, layer, total, n_keep, n_recent, keep=None, kept_total=None):
+        """The rows a budget keeps: the newest n_recent and those with the largest totals.  total: float32
+        ``[batch][n_kv_heads][stride]``; n_keep: ``[batch][n_kv_heads]`` counts (host).  Returns the keep list ``evict``
+        takes, int32 ``[batch][n_kv_heads][max n_keep]``, and the rows' totals in the same layout."""
+        torch = self._torch
+        assert total.dtype == torch.float32 and total.is_contiguous() and total.ndim == 3 and total.shape[1] == self.shape[2]
+        counts = torch.as_tensor(n_keep).reshape(-1).tolist()
+        assert len(counts) == total.shape[0] * total.shape[1]
+        if keep is None:
+            keep = torch.zeros(*total.shape[:2], max(counts), dtype=torch.int32, device=self.device)
+        if kept_total is None:
+            kept_total = torch.zeros(keep.shape, dtype=torch.float32, device=self.device)
+        assert keep.is_contiguous() and keep.dtype == torch.int32 and keep.shape[:2] == total.shape[:2]
+        assert kept_total.is_contiguous() and kept_total.dtype == torch.float32 and kept_total.shape == keep.shape
+        binding.kvs_select_rows(self.ctx, layer, total, total.shape[2], counts, n_recent, keep, kept_total, keep.shape[2],
+                                total.shape[0], self._stream())
+        return keep, kept_total
+
+    def evict_by_weight(self, layer, total, n_keep, n_recent):
+        """``select_rows`` and ``evict`` in one: the layer's slot keeps n_keep rows per unit.  Returns their totals."""
+        keep, kept = self.select_rows(layer, total, n_keep, n_recent)
+        self.evict(layer, keep, n_keep)
+        return kept
 
     def unit_len(self, layer, b, h):
         return binding.kvs_unit_len(self.ctx, layer, b, h)

@@ -47,6 +47,7 @@ EXPORTS = (
     "kvs_replay_advance", "kvs_replay_commit", "kvs_decode_step",
     "kvs_clear_device_status", "kvs_selftest_wait_timeout", "kvs_truncate",
     "kvs_selftest_bounds", "kvs_selftest_stalled_copy", "kvs_trace_begin", "kvs_trace_end",
+    "kvs_append_rotary", "kvs_tree_attention", "kvs_accept_draft", "kvs_decode_attention_weights", "kvs_select_rows",
 )
 
 
@@ -66,6 +67,11 @@ class kvs_stats_t(ctypes.Structure):
         ("prefill_launches", ctypes.c_uint64), ("evict_launches", ctypes.c_uint64),
         ("search_launches", ctypes.c_uint64), ("fused_appends", ctypes.c_uint64),
     ]
+
+
+class kvs_rotary(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("inv_freq", ctypes.POINTER(ctypes.c_double))]
 
 
 _lib = None
@@ -118,6 +124,12 @@ def load() -> ctypes.CDLL:
         "kvs_selftest_stalled_copy": [vp, i32, vp, vp, i32, vp],
         "kvs_set_option": [vp, i32, i32],
         "kvs_last_launch": [vp, P(i32), P(i32), P(i32)],
+        "kvs_append_rotary": [vp, i32, P(kvs_rotary), vp, ctypes.c_int64, vp, ctypes.c_int64, vp, ctypes.c_int64, vp, vp, vp,
+                              vp, i32, i32, vp],
+        "kvs_tree_attention": [vp, i32, vp, vp, vp, i32, i32, vp],
+        "kvs_accept_draft": [vp, vp, i32, P(i32), i32, i32, vp],
+        "kvs_decode_attention_weights": [vp, i32, vp, vp, vp, vp, i32, i32, vp],
+        "kvs_select_rows": [vp, i32, vp, i32, P(i32), i32, vp, vp, i32, i32, vp],
         "kvs_read_roof": [vp, sz, vp, i32, vp],
     }
     for name, argtypes in sig.items():
@@ -211,6 +223,38 @@ def kvs_evict(ctx: int, layer: int, keep, n_keep, keep_stride: int, batch: int, 
     """keep: device int32 ``[batch][Hkv][keep_stride]``; n_keep: host sequence of batch*Hkv counts."""
     counts = (ctypes.c_int32 * len(n_keep))(*[int(x) for x in n_keep])
     _check(load().kvs_evict(ctx, layer, _ptr(keep), counts, keep_stride, batch, stream), "kvs_evict")
+
+
+def kvs_append_rotary(ctx: int, layer: int, rot: kvs_rotary, q, q_stride: int, k, k_stride: int, v, v_stride: int, positions,
+                      q_weight, k_weight, q_out, batch: int, n_new: int, stream: int = 0) -> None:
+    _check(load().kvs_append_rotary(ctx, layer, ctypes.byref(rot), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride,
+                                    _ptr(positions), _ptr(q_weight), _ptr(k_weight), _ptr(q_out), batch, n_new, stream),
+           "kvs_append_rotary")
+
+
+def kvs_tree_attention(ctx: int, layer: int, q, out, mask, batch: int, n_t: int, stream: int = 0) -> None:
+    """mask: device 64-bit words ``[batch][n_t]`` or None (a chain)."""
+    _check(load().kvs_tree_attention(ctx, layer, _ptr(q), _ptr(out), _ptr(mask), batch, n_t, stream), "kvs_tree_attention")
+
+
+def kvs_accept_draft(ctx: int, path, path_stride: int, n_accept, n_draft: int, batch: int, stream: int = 0) -> None:
+    """path: device int32 ``[batch][path_stride]``; n_accept: host sequence of ``batch`` counts."""
+    counts = (ctypes.c_int32 * len(n_accept))(*n_accept)
+    _check(load().kvs_accept_draft(ctx, _ptr(path), path_stride, counts, n_draft, batch, stream), "kvs_accept_draft")
+
+
+def kvs_decode_attention_weights(ctx: int, layer: int, q, out, total_in, total_out, total_stride: int, batch: int,
+                                 stream: int = 0) -> None:
+    _check(load().kvs_decode_attention_weights(ctx, layer, _ptr(q), _ptr(out), _ptr(total_in), _ptr(total_out), total_stride,
+                                               batch, stream), "kvs_decode_attention_weights")
+
+
+def kvs_select_rows(ctx: int, layer: int, total, total_stride: int, n_keep, n_recent: int, keep, kept_total, keep_stride: int,
+                    batch: int, stream: int = 0) -> None:
+    """n_keep: host sequence of batch*Hkv counts (or a ctypes int32 array of them)."""
+    counts = n_keep if isinstance(n_keep, ctypes.Array) else (ctypes.c_int32 * len(n_keep))(*n_keep)
+    _check(load().kvs_select_rows(ctx, layer, _ptr(total), total_stride, counts, n_recent, _ptr(keep), _ptr(kept_total),
+                                  keep_stride, batch, stream), "kvs_select_rows")
 
 
 def kvs_unit_len(ctx: int, layer: int, b: int, h: int) -> int:

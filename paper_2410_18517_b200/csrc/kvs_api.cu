@@ -84,8 +84,8 @@ struct kvs_ctx {
 
     // workspace carve-up (byte offsets)
     size_t off_status = 0, off_part_o = 0, off_part_ml = 0, off_stage_q = 0, off_stage_k = 0, off_stage_v = 0,
-           off_stage_out = 0, off_unit_len = 0, off_counts = 0, off_search = 0, off_replay = 0, off_flags = 0, ws_bytes = 0,
-           search_bytes = 0;
+           off_stage_out = 0, off_unit_len = 0, off_counts = 0, off_search = 0, off_replay = 0, off_flags = 0, off_scores = 0,
+           off_tree_o = 0, off_tree_ml = 0, ws_bytes = 0, search_bytes = 0;
 
     alignas(64) unsigned char tensor_map[128];  // TMA view of the pool (bf16 storage only), 64-row boxes
     alignas(64) unsigned char tensor_map_tail[128];   // the same view with 16-row boxes (partly filled tiles)
@@ -204,14 +204,24 @@ void layout_workspace(kvs_ctx* c) {
     off += kAlign;
     c->off_flags = off;         // one int per unit: "second piece written" (zero between launches)
     off = align_up(off + units * sizeof(int32_t), kAlign);
-    c->off_search = off;        // per-block partial sums of the strategy-search reductions
+    c->off_search = off;        // per-block partial sums of the strategy-search reductions, and more (below)
     {
         // at most one slot per layer, at most max_seq rows: enough for every strategy and length
         const size_t need = std::max(kvs::distance_scratch_bytes(f.n_layers <= kvs::kMaxLayersSearch ? f.n_layers : 4,
                                                                  2LL * f.n_kv_heads * f.max_seq * f.head_dim),
                                      (size_t)kvs::kCosineMaxBlocks * 3 * sizeof(double));
         c->search_bytes = need;
-        off = align_up(off + need, kAlign);
+        // The same bytes serve the other calls whose scratch lives no longer than the call (every kernel writes it
+        // only after its wait for the previous one):
+        // kvs_decode_attention_weights: one score per (sequence, q-head, row)
+        const size_t scores = (size_t)f.max_batch * f.n_q_heads * c->row_stride * sizeof(float);
+        c->off_scores = off;
+        // kvs_tree_attention: two cut pieces per thread block at most
+        const size_t tree_rows = (size_t)2 * kvs::kTreeMaxBlocks * kvs::tree_partial_rows(c->G);
+        const size_t tree_o = align_up(tree_rows * f.head_dim * sizeof(float), kAlign);
+        c->off_tree_o = off;
+        c->off_tree_ml = off + tree_o;
+        off = align_up(off + std::max(std::max(need, scores), tree_o + tree_rows * 2 * sizeof(float)), kAlign);
     }
     c->ws_bytes = off;
 }
@@ -225,6 +235,8 @@ cudaError_t init_device_once(int device) {
         g_init_err[device] = kvs::init_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_mma_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_prefill_kernels();
+        if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_tree_kernels();
+        if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_weights_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = resolve_static_scratch(device);
     });
     return g_init_err[device];
@@ -272,6 +284,8 @@ kvs_status check_attention(kvs_ctx* c, int layer, const void* q, const void* out
     return KVS_OK;
 }
 
+kvs_status appended(kvs_ctx* c, int slot, int batch, int n_new, cudaStream_t st);
+
 kvs_status do_append(kvs_ctx* c, int layer, const void* k, const void* v, int batch, int n_new, cudaStream_t st) {
     const int slot = c->slot_of_layer[layer];
     char* kp = c->pool + (size_t)(2 * slot) * c->plane_bytes;
@@ -282,7 +296,12 @@ kvs_status do_append(kvs_ctx* c, int layer, const void* k, const void* v, int ba
                            reinterpret_cast<int*>(c->ws + c->off_status), (long long)c->plane_bytes, take_early_start(c),
                            st) != cudaSuccess)
         return KVS_ERR_CUDA;
-    if (rag) {
+    return appended(c, slot, batch, n_new, st);
+}
+
+// Bookkeeping of a kernel just launched that stores n_new rows at the end of every unit of `slot`.
+kvs_status appended(kvs_ctx* c, int slot, int batch, int n_new, cudaStream_t st) {
+    if (c->ragged[slot]) {
         const int units = batch * c->cfg.n_kv_heads;
         if (kvs::launch_add_len(unit_len_dev(c, slot), n_new, units, c->opt_pdl != 0, st) != cudaSuccess)
             return KVS_ERR_CUDA;
@@ -321,12 +340,19 @@ bool choose_plan(const kvs_ctx* c, int units, int n, kvs::DecodePlan* plan) {
     return use_mma;
 }
 
+// Where kvs_decode_attention_weights reads and leaves the running totals of the rows' softmax weights.
+struct WeightTotals {
+    const float* in;     // nullptr: totals start at zero
+    float* out;
+    int stride;
+};
+
 // Split-K kernel + combine kernel of one layer, with the given plan and scratch.
 // With k_new / v_new the split-K kernel also appends that one row per unit (the slot's length must
 // already count it).
 kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int batch, const kvs::DecodePlan& plan,
                          bool use_mma, const AttentionScratch& scratch, cudaStream_t st, const void* k_new = nullptr,
-                         const void* v_new = nullptr) {
+                         const void* v_new = nullptr, const WeightTotals* totals = nullptr) {
     kvs::DecodeArgs a;
     a.q = q;
     a.kplane = c->pool + (size_t)(2 * slot) * c->plane_bytes;
@@ -357,7 +383,9 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int ba
         a.trace = c->trace_buf + (size_t)(c->trace_launch++) * kvs::kTraceLaunchWords;
     a.stall_tile = c->stall_tile >= 0 ? std::min<long long>(c->stall_tile, plan.T - 1) : -1;
     c->stall_tile = -1;
-    a.finish_in_kernel = c->opt_finish != 0 && kvs::can_finish_in_kernel(plan, a.units);
+    // with totals the unit's (max, sum) are needed beyond its output: always the separate finishing kernel
+    a.finish_in_kernel = c->opt_finish != 0 && kvs::can_finish_in_kernel(plan, a.units) && totals == nullptr;
+    a.scores = totals ? reinterpret_cast<float*>(c->ws + c->off_scores) : nullptr;
     a.flags = scratch.flags;
     if (scratch.tracked) {
         c->seq += a.finish_in_kernel ? 1 : 2;     // split-K kernel, then (unless it finishes the units itself) combine
@@ -372,7 +400,9 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int ba
         if (kvs::launch_decode_scalar(a, plan, st) != cudaSuccess) return KVS_ERR_CUDA;
     }
     if (!a.finish_in_kernel) {
-        if (kvs::launch_combine(a, plan, st) != cudaSuccess) return KVS_ERR_CUDA;
+        const cudaError_t e = totals ? kvs::launch_weights_finish(a, plan, totals->in, totals->out, totals->stride, st)
+                                     : kvs::launch_combine(a, plan, st);
+        if (e != cudaSuccess) return KVS_ERR_CUDA;
         c->stats.combine_launches += 1;
     }
     c->last_plan = plan;
@@ -415,7 +445,8 @@ kvs_status do_fused_step(kvs_ctx* c, int layer, const void* q, const void* k, co
     return KVS_OK;
 }
 
-kvs_status do_attention(kvs_ctx* c, int layer, const void* q, float* out, int batch, cudaStream_t st) {
+kvs_status do_attention(kvs_ctx* c, int layer, const void* q, float* out, int batch, cudaStream_t st,
+                        const WeightTotals* totals = nullptr) {
     const int slot = c->slot_of_layer[layer];
     kvs::DecodePlan plan;
     const bool use_mma = choose_plan(c, batch * c->cfg.n_kv_heads, c->slot_len[slot], &plan);
@@ -423,7 +454,25 @@ kvs_status do_attention(kvs_ctx* c, int layer, const void* q, float* out, int ba
                                       reinterpret_cast<float*>(c->ws + c->off_part_ml),
                                       reinterpret_cast<int*>(c->ws + c->off_flags),
                                       reinterpret_cast<int*>(c->ws + c->off_status), take_early_start(c), true};
-    return run_attention(c, slot, q, out, batch, plan, use_mma, scratch, st);
+    return run_attention(c, slot, q, out, batch, plan, use_mma, scratch, st, nullptr, nullptr, totals);
+}
+
+// Rows of unit `u` of `slot` as the host knows them.
+int unit_rows(const kvs_ctx* c, int slot, int u) { return c->ragged[slot] ? c->unit_len_host[slot][u] : c->slot_len[slot]; }
+
+// Whether every unit of the slot's first `batch` sequences holds at least `rows` rows.
+bool holds_rows(const kvs_ctx* c, int slot, int batch, int rows) {
+    if (!c->ragged[slot]) return c->slot_len[slot] >= rows;
+    for (int u = 0; u < batch * c->cfg.n_kv_heads; ++u)
+        if (c->unit_len_host[slot][u] < rows) return false;
+    return true;
+}
+
+// Every row of the slot may just have moved: nothing of it may be fetched early.
+void rows_moved(kvs_ctx* c, int slot) {
+    c->app_seq_prev[slot] = c->seq;
+    c->app_seq_latest[slot] = c->seq;
+    c->app_start_latest[slot] = 0;
 }
 
 }  // namespace
@@ -699,11 +748,236 @@ kvs_status kvs_evict(kvs_ctx* ctx, int32_t layer, const int32_t* keep, const int
     ctx->slot_len[slot] = longest;
     // every row of the slot may just have moved: nothing of it may be fetched early
     ctx->seq += 2;
-    ctx->app_seq_prev[slot] = ctx->seq;
-    ctx->app_seq_latest[slot] = ctx->seq;
-    ctx->app_start_latest[slot] = 0;
+    rows_moved(ctx, slot);
     ctx->stats.evict_launches += 1;
     ctx->counter_written = false;   // a plain launch: full dependency on everything before it
+    return KVS_OK;
+}
+
+kvs_status kvs_append_rotary(kvs_ctx* ctx, int32_t layer, const kvs_rotary* rot, const void* q, int64_t q_stride,
+                             const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* positions,
+                             const void* q_weight, const void* k_weight, void* q_out, int32_t batch, int32_t n_new,
+                             void* stream) {
+    bool sharing = false;
+    kvs_status s = check_append(ctx, layer, k, v, batch, n_new, &sharing);
+    if (s != KVS_OK) return s;
+    const kvs_config& f = ctx->cfg;
+    if (!rot || !q || !q_out) return KVS_ERR_INVALID_ARG;
+    if (rot->rotary_dim < 0 || rot->rotary_dim > f.head_dim || rot->rotary_dim % 16 != 0) return KVS_ERR_INVALID_ARG;
+    if (rot->interleaved != 0 && rot->interleaved != 1) return KVS_ERR_INVALID_ARG;
+    if (rot->rotary_dim > 0 && (!rot->inv_freq || !positions)) return KVS_ERR_INVALID_ARG;
+    for (int i = 0; i < rot->rotary_dim / 2; ++i)
+        if (!std::isfinite(rot->inv_freq[i])) return KVS_ERR_INVALID_ARG;
+    if (!(rot->eps >= 0.f) || std::isinf(rot->eps)) return KVS_ERR_INVALID_ARG;
+    if (((uintptr_t)q % 16) != 0 || ((uintptr_t)q_out % 16) != 0 || ((uintptr_t)positions % 4) != 0 ||
+        ((uintptr_t)q_weight % 16) != 0 || ((uintptr_t)k_weight % 16) != 0)
+        return KVS_ERR_INVALID_ARG;
+    // token strides: 16-byte vector loads, and no two tokens overlap
+    const int per = 16 / ctx->elem;
+    const long long q_row = (long long)f.n_q_heads * f.head_dim, kv_row = (long long)f.n_kv_heads * f.head_dim;
+    if (q_stride < q_row || q_stride % per != 0) return KVS_ERR_INVALID_ARG;
+    if (!sharing && (k_stride < kv_row || k_stride % per != 0 || v_stride < kv_row || v_stride % per != 0))
+        return KVS_ERR_INVALID_ARG;
+    if ((long long)batch * n_new > 0x7fffffffll) return KVS_ERR_INVALID_ARG;
+    if (q == q_out && q_stride != q_row && (long long)batch * n_new > 1) return KVS_ERR_INVALID_ARG;   // in place: packed rows only
+    DeviceGuard guard(f.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    const int slot = ctx->slot_of_layer[layer];
+    kvs::RotaryArgs r = {};
+    r.q = q;
+    r.q_stride = q_stride;
+    r.positions = positions;
+    r.q_weight = q_weight;
+    r.q_out = q_out;
+    r.batch = batch;
+    r.n_new = n_new;
+    r.Hq = f.n_q_heads;
+    r.D = f.head_dim;
+    r.dtype = f.dtype;
+    r.inv_freq = rot->inv_freq;
+    r.rotary_dim = rot->rotary_dim;
+    r.interleaved = rot->interleaved != 0;
+    r.eps = rot->eps;
+    r.status = reinterpret_cast<int*>(ctx->ws + ctx->off_status);
+    if (!sharing) {
+        r.k = k;
+        r.k_stride = k_stride;
+        r.v = v;
+        r.v_stride = v_stride;
+        r.k_weight = k_weight;
+        r.Hkv = f.n_kv_heads;
+        r.kplane = ctx->pool + (size_t)(2 * slot) * ctx->plane_bytes;
+        r.vplane = ctx->pool + (size_t)(2 * slot + 1) * ctx->plane_bytes;
+        r.row_stride = ctx->row_stride;
+        r.len0 = ctx->slot_len[slot];
+        r.capacity = f.max_seq;
+        r.unit_len = ctx->ragged[slot] ? unit_len_dev(ctx, slot) : nullptr;
+        r.n_extra = replay_counter(ctx);
+        r.plane_bytes = (long long)ctx->plane_bytes;
+    }
+    r.programmatic = take_early_start(ctx);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (kvs::launch_append_rotary(r, st) != cudaSuccess) return KVS_ERR_CUDA;
+    if (!sharing) return appended(ctx, slot, batch, n_new, st);
+    ctx->seq += 1;
+    ctx->stats.append_skipped += 1;
+    return KVS_OK;
+}
+
+kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* out, const uint64_t* mask, int32_t batch,
+                              int32_t n_t, void* stream) {
+    if (!ctx) return KVS_ERR_INVALID_ARG;
+    if (!ctx->bound || ctx->opt_replay) return KVS_ERR_STATE;
+    if (layer < 0 || layer >= ctx->cfg.n_layers || !q || !out) return KVS_ERR_INVALID_ARG;
+    if (batch < 1 || batch > ctx->cfg.max_batch || n_t < 1 || n_t > kvs::kTreeMaxTokens) return KVS_ERR_INVALID_ARG;
+    if (((uintptr_t)q % 16) != 0 || ((uintptr_t)out % 16) != 0 || ((uintptr_t)mask % 8) != 0) return KVS_ERR_INVALID_ARG;
+    const int slot = ctx->slot_of_layer[layer];
+    if (ctx->slot_len[slot] == 0) return KVS_ERR_STATE;
+    if (batch > ctx->cur_batch || !holds_rows(ctx, slot, batch, n_t)) return KVS_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    kvs::TreeArgs a;
+    a.q = q;
+    a.out = out;
+    a.mask = reinterpret_cast<const unsigned long long*>(mask);
+    a.kplane = ctx->pool + (size_t)(2 * slot) * ctx->plane_bytes;
+    a.vplane = ctx->pool + (size_t)(2 * slot + 1) * ctx->plane_bytes;
+    a.part_o = reinterpret_cast<float*>(ctx->ws + ctx->off_tree_o);
+    a.part_ml = reinterpret_cast<float*>(ctx->ws + ctx->off_tree_ml);
+    a.status = reinterpret_cast<int*>(ctx->ws + ctx->off_status);
+    a.n = ctx->slot_len[slot];
+    a.unit_len = ctx->ragged[slot] ? unit_len_dev(ctx, slot) : nullptr;
+    a.n_t = n_t;
+    a.units = batch * ctx->cfg.n_kv_heads;
+    a.B = batch;
+    a.Hq = ctx->cfg.n_q_heads;
+    a.Hkv = ctx->cfg.n_kv_heads;
+    a.G = ctx->G;
+    a.D = ctx->cfg.head_dim;
+    a.dtype = ctx->cfg.dtype;
+    a.row_stride = ctx->row_stride;
+    a.capacity = ctx->cfg.max_seq;
+    a.plane_bytes = (long long)ctx->plane_bytes;
+    a.scale_log2 = ctx->scale * 1.4426950408889634f;
+    a.wait_ns = 1000ull * (unsigned long long)ctx->opt_wait_us;
+    int launches = 0;
+    if (kvs::launch_tree(a, ctx->sm_count, ctx->opt_max_ctas, &launches, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+        return KVS_ERR_CUDA;
+    // a plain launch: it starts only after everything before it on the stream has finished
+    ctx->seq += launches;
+    ctx->last_splitk_seq = ctx->seq;
+    ctx->stats.prefill_launches += 1;
+    ctx->counter_written = false;
+    return KVS_OK;
+}
+
+kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stride, const int32_t* n_accept, int32_t n_draft,
+                            int32_t batch, void* stream) {
+    if (!ctx || !path || !n_accept) return KVS_ERR_INVALID_ARG;
+    if (!ctx->bound || ctx->opt_replay) return KVS_ERR_STATE;
+    if (n_draft < 1 || n_draft > kvs::kTreeMaxTokens || path_stride < 1) return KVS_ERR_INVALID_ARG;
+    if (((uintptr_t)path % 4) != 0) return KVS_ERR_INVALID_ARG;
+    if (ctx->cur_batch == 0) return KVS_ERR_STATE;
+    if (batch != ctx->cur_batch) return KVS_ERR_INVALID_ARG;
+    bool same = true;
+    for (int b = 0; b < batch; ++b) {
+        if (n_accept[b] < 0 || n_accept[b] > n_draft || n_accept[b] > path_stride) return KVS_ERR_INVALID_ARG;
+        same = same && n_accept[b] == n_accept[0];
+    }
+    const int Hkv = ctx->cfg.n_kv_heads, units = batch * Hkv;
+    for (int s = 0; s < ctx->n_slots; ++s) {
+        if (!holds_rows(ctx, s, batch, n_draft)) return KVS_ERR_STATE;
+        // a slot whose units differ in length has none that is empty
+        if (!same || ctx->ragged[s])
+            for (int u = 0; u < units; ++u)
+                if (unit_rows(ctx, s, u) - n_draft + n_accept[u / Hkv] < 1) return KVS_ERR_INVALID_ARG;
+    }
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    bool empty = true;
+    for (int s = 0; s < ctx->n_slots; ++s) {
+        const bool was = ctx->ragged[s] != 0, becomes = was || !same;
+        char* kp = ctx->pool + (size_t)(2 * s) * ctx->plane_bytes;
+        for (int b0 = 0; b0 < batch; b0 += kvs::AcceptCounts::kMax) {
+            const int seqs = std::min(batch - b0, (int)kvs::AcceptCounts::kMax);
+            kvs::AcceptCounts counts;
+            for (int i = 0; i < seqs; ++i) counts.n[i] = (unsigned char)n_accept[b0 + i];
+            if (kvs::launch_accept(kp, kp + ctx->plane_bytes, path, path_stride, counts, b0, seqs, Hkv, n_draft,
+                                   was ? -1 : ctx->slot_len[s], becomes ? unit_len_dev(ctx, s) : nullptr, becomes, ctx->row_bytes,
+                                   ctx->row_stride, reinterpret_cast<int*>(ctx->ws + ctx->off_status),
+                                   (long long)ctx->plane_bytes, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+                return KVS_ERR_CUDA;
+            ctx->seq += 1;
+        }
+        if (becomes) {
+            std::vector<int32_t> lens((size_t)ctx->cfg.max_batch * Hkv, 0);
+            int longest = 0;
+            for (int u = 0; u < units; ++u) {
+                lens[u] = unit_rows(ctx, s, u) - n_draft + n_accept[u / Hkv];
+                longest = std::max(longest, lens[u]);
+            }
+            ctx->unit_len_host[s] = lens;
+            ctx->ragged[s] = 1;
+            ctx->slot_len[s] = longest;
+        } else {
+            ctx->slot_len[s] += n_accept[0] - n_draft;
+        }
+        empty = empty && ctx->slot_len[s] == 0;
+        rows_moved(ctx, s);
+    }
+    if (empty) ctx->cur_batch = 0;
+    ctx->stats.evict_launches += 1;
+    ctx->counter_written = false;   // a plain launch: full dependency on everything before it
+    return KVS_OK;
+}
+
+kvs_status kvs_decode_attention_weights(kvs_ctx* ctx, int32_t layer, const void* q, float* out, const float* total_in,
+                                        float* total_out, int32_t total_stride, int32_t batch, void* stream) {
+    kvs_status s = check_attention(ctx, layer, q, out, batch);
+    if (s != KVS_OK) return s;
+    if (!total_out || ((uintptr_t)total_in % 4) != 0 || ((uintptr_t)total_out % 4) != 0) return KVS_ERR_INVALID_ARG;
+    // a recorded launch grows on the device: its totals need room for every row the slot can hold
+    if (total_stride < (ctx->opt_replay ? ctx->cfg.max_seq : ctx->slot_len[ctx->slot_of_layer[layer]])) return KVS_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    const WeightTotals totals = {total_in, total_out, total_stride};
+    return do_attention(ctx, layer, q, out, batch, static_cast<cudaStream_t>(stream), &totals);
+}
+
+kvs_status kvs_select_rows(kvs_ctx* ctx, int32_t layer, const float* total, int32_t total_stride, const int32_t* n_keep,
+                           int32_t n_recent, int32_t* keep, float* kept_total, int32_t keep_stride, int32_t batch, void* stream) {
+    if (!ctx || !total || !n_keep || !keep) return KVS_ERR_INVALID_ARG;
+    if (!ctx->bound || ctx->opt_replay) return KVS_ERR_STATE;
+    if (layer < 0 || layer >= ctx->cfg.n_layers || n_recent < 0 || keep_stride < 1) return KVS_ERR_INVALID_ARG;
+    if (((uintptr_t)total % 4) != 0 || ((uintptr_t)keep % 4) != 0 || ((uintptr_t)kept_total % 4) != 0) return KVS_ERR_INVALID_ARG;
+    const int slot = ctx->slot_of_layer[layer];
+    if (ctx->slot_len[slot] == 0) return KVS_ERR_STATE;
+    if (batch < 1 || batch > ctx->cur_batch || total_stride < ctx->slot_len[slot]) return KVS_ERR_INVALID_ARG;
+    const int units = batch * ctx->cfg.n_kv_heads;
+    for (int u = 0; u < units; ++u)
+        if (n_keep[u] < 1 || n_keep[u] > unit_rows(ctx, slot, u) || n_keep[u] < n_recent || n_keep[u] > keep_stride)
+            return KVS_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    kvs::SelectArgs a;
+    a.total = total;
+    a.keep = keep;
+    a.kept = kept_total;
+    a.total_stride = total_stride;
+    a.keep_stride = keep_stride;
+    a.n = ctx->slot_len[slot];
+    a.unit_len = ctx->ragged[slot] ? unit_len_dev(ctx, slot) : nullptr;
+    a.n_recent = n_recent;
+    for (int u0 = 0; u0 < units; u0 += kvs::SelectCounts::kMax) {
+        a.unit0 = u0;
+        a.units = std::min(units - u0, (int)kvs::SelectCounts::kMax);
+        kvs::SelectCounts counts;
+        for (int i = 0; i < a.units; ++i) counts.n[i] = n_keep[u0 + i];
+        if (kvs::launch_select(a, counts, static_cast<cudaStream_t>(stream)) != cudaSuccess) return KVS_ERR_CUDA;
+        ctx->seq += 1;
+    }
+    ctx->last_splitk_seq = ctx->seq;   // plain launches: everything before them has finished when they run
+    ctx->counter_written = false;
     return KVS_OK;
 }
 

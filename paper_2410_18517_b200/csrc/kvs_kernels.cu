@@ -294,9 +294,12 @@ struct ScalarKernelArgs {
     unsigned long long wait_ns;   // limit of every wait inside the kernel
     long long stall_tile;         // self-test only: the K/V copies of this tile are withheld (-1: none)
     unsigned long long* trace;    // tracing build: this launch's rows of time stamps, or nullptr
+    float* scores;                // W only: [units][G][row_stride] scores in the log2 domain
 };
 
-template <typename T, int D, int G>
+// W: every row's score is stored beside the ordinary work (kvs_decode_attention_weights normalises them once the
+// unit's maximum and sum are known): 4 G bytes written for each 2 * D * sizeof(T) read.
+template <typename T, int D, int G, bool W>
 __global__ void __launch_bounds__(ScalarShape<T, D, G>::THREADS, ScalarShape<T, D, G>::MIN_BLOCKS)
     decode_splitk_scalar(const ScalarKernelArgs a_in) {
     using S = ScalarShape<T, D, G>;
@@ -561,6 +564,11 @@ __global__ void __launch_bounds__(ScalarShape<T, D, G>::THREADS, ScalarShape<T, 
 #pragma unroll
                 for (int g = 0; g < GP; ++g) {
                     float sv = reduce_transpose<R, LPR / 2>(s[g], lig);
+                    if constexpr (W) {
+                        // 2^SH neighbouring lanes hold the same row: the first of them stores it
+                        if (mine_valid && (lig & ((1 << SH) - 1)) == 0)
+                            a.scores[(u * G + g0 + g) * a.row_stride + (long long)(ti0 + k) * TN + grp + NG * my_i] = sv;
+                    }
                     sv = mine_valid ? sv : -INFINITY;
                     float tmax = sv;
 #pragma unroll
@@ -891,30 +899,37 @@ cudaError_t launch_combine(const DecodeArgs& a, const DecodePlan& plan, cudaStre
 // --------------------------------------------------------------------------------------
 // Launch plumbing for the scalar kernel.
 // --------------------------------------------------------------------------------------
-template <typename T, int D, int G>
+template <typename T, int D, int G, bool W>
 static cudaError_t set_attr_one() {
-    cudaError_t e = cudaFuncSetAttribute(decode_splitk_scalar<T, D, G>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaError_t e = cudaFuncSetAttribute(decode_splitk_scalar<T, D, G, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          ScalarShape<T, D, G>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
     // the whole L1 / shared-memory array as shared memory, so that the combine kernel's blocks, launched
     // early behind this kernel, find room to become resident beside its blocks (see the tensor-core kernel)
-    return cudaFuncSetAttribute(decode_splitk_scalar<T, D, G>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    return cudaFuncSetAttribute(decode_splitk_scalar<T, D, G, W>, cudaFuncAttributePreferredSharedMemoryCarveout,
                                 cudaSharedmemCarveoutMaxShared);
+}
+
+template <typename T, int D, int G>
+static cudaError_t set_attr_both() {
+    const cudaError_t e = set_attr_one<T, D, G, false>();
+    return e != cudaSuccess ? e : set_attr_one<T, D, G, true>();
 }
 
 template <typename T, int D>
 static cudaError_t set_attr_groups() {
     cudaError_t e;
-    if ((e = set_attr_one<T, D, 1>()) != cudaSuccess) return e;
-    if ((e = set_attr_one<T, D, 2>()) != cudaSuccess) return e;
-    if ((e = set_attr_one<T, D, 4>()) != cudaSuccess) return e;
-    return set_attr_one<T, D, 8>();
+    if ((e = set_attr_both<T, D, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr_both<T, D, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_both<T, D, 4>()) != cudaSuccess) return e;
+    return set_attr_both<T, D, 8>();
 }
 
 template <typename T, int D, int G>
 static cudaError_t launch_scalar_one(const ScalarKernelArgs& ka, int NC, bool programmatic, cudaStream_t stream) {
-    return launch_kernel(decode_splitk_scalar<T, D, G>, dim3(NC), dim3(ScalarShape<T, D, G>::THREADS),
-                         ScalarShape<T, D, G>::SMEM_BYTES, stream, programmatic, ka);
+    using S = ScalarShape<T, D, G>;
+    return ka.scores ? launch_kernel(decode_splitk_scalar<T, D, G, true>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, programmatic, ka)
+                     : launch_kernel(decode_splitk_scalar<T, D, G, false>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, programmatic, ka);
 }
 
 template <typename T, int D>
@@ -967,6 +982,7 @@ cudaError_t launch_decode_scalar(const DecodeArgs& a, const DecodePlan& plan, cu
     ka.wait_ns = a.wait_ns;
     ka.stall_tile = a.stall_tile;
     ka.trace = a.trace;
+    ka.scores = a.scores;
     const bool pdl = a.programmatic;
     if (a.dtype == 0) {
         if (a.D == 128) return launch_scalar_groups<__nv_bfloat16, 128>(a.G, ka, plan.NC, pdl, stream);

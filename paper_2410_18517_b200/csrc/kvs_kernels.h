@@ -50,6 +50,9 @@ struct DecodeArgs {
     unsigned long long wait_ns;   // limit of every wait inside the split-K kernels
     long long stall_tile;    // self-test only: the K/V copies of this tile of the line are withheld (-1: none)
     unsigned long long* trace;    // tracing build only: this launch's [kTraceBlocks][kTraceSlots] words, or nullptr
+    // kvs_decode_attention_weights: where the split-K kernel leaves every row's score (log2 domain),
+    // [units][G][row_stride], or nullptr
+    float* scores = nullptr;
 };
 
 // Whether a launch of this plan over `units` units can finish inside the split-K kernel.
@@ -111,6 +114,100 @@ cudaError_t launch_append(const void* k, const void* v, void* kplane, void* vpla
                           int row_bytes, int row_stride, int len0, const int* unit_len, const int* n_extra, int capacity, int* status,
                           long long plane_bytes, bool programmatic, cudaStream_t stream);
 cudaError_t launch_replay_advance(int* n_extra, bool programmatic, cudaStream_t stream);
+
+// Rotary append (see kvs_rotary.cu).  Strides in elements between consecutive tokens.
+struct RotaryArgs {
+    const void* q;
+    const void* k;            // k, v unused when Hkv == 0 (a layer that shares its cache: queries only)
+    const void* v;
+    long long q_stride, k_stride, v_stride;
+    const int* positions;     // device, [batch][n_new]
+    const void* q_weight;     // device, [D], or nullptr: no norm
+    const void* k_weight;
+    void* q_out;              // [batch][n_new][Hq][D]
+    void* kplane;
+    void* vplane;
+    int batch, n_new, Hq, Hkv, D, dtype;
+    int row_stride, len0, capacity;
+    const int* unit_len;
+    const int* n_extra;
+    int* status;
+    long long plane_bytes;
+    const double* inv_freq;   // host, [rotary_dim / 2]
+    int rotary_dim;           // 0: no rotation
+    bool interleaved;
+    float eps;
+    bool programmatic;
+};
+cudaError_t launch_append_rotary(const RotaryArgs& r, cudaStream_t stream);
+
+// Attention of a tree of drafted tokens (see kvs_tree.cu).  The n_t queries of a sequence are the newest n_t rows
+// of its units; the G heads of a kv-head and the tokens form the rows of query tiles of `rows` rows.  A *team* of
+// m_tiles thread blocks walks a contiguous run of the line of key tiles (units * tiles per unit), block j of the
+// team with query tile j, so that the team reads every K/V tile at the same time.  A unit cut between teams
+// leaves one piece per team: piece slot 2 * team + 1 if it begins the unit, 2 * team otherwise.
+struct TreePlan {
+    int tokens;      // drafted tokens per query tile
+    int m_tiles;     // query tiles per unit
+    int key_rows;    // keys per tile
+    int tpu;         // key tiles per unit (of the longest unit)
+    long long T;     // key tiles of all units
+    int teams;
+};
+struct TreeArgs {
+    const void* q;                     // [B][n_t][Hq][D]
+    void* out;                         // same shape and type
+    const unsigned long long* mask;    // [B][n_t] or nullptr (token i sees tokens 0..i)
+    const void* kplane;
+    const void* vplane;
+    float* part_o;                     // [piece slot][m_tile][rows][D]
+    float* part_ml;                    // [piece slot][m_tile][rows][2]
+    int* status;
+    int n;                             // rows per unit, drafts included (longest unit of a ragged slot)
+    const int* unit_len;
+    int n_t, units, B, Hq, Hkv, G, D, dtype;
+    int row_stride, capacity;
+    long long plane_bytes;
+    float scale_log2;
+    unsigned long long wait_ns;
+};
+constexpr int kTreeMaxTokens = 64;
+constexpr int kTreeMaxBlocks = 320;    // thread blocks of one call; bounds the partial results
+constexpr int kTreeTileRows = 128;     // query rows of the largest tile
+inline int tree_partial_rows(int G) { return G * kTreeMaxTokens < kTreeTileRows ? G * kTreeMaxTokens : kTreeTileRows; }
+cudaError_t init_tree_kernels();
+cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* launches, cudaStream_t stream);
+
+// Running totals of softmax weights and the rows a budget keeps (see kvs_weights.cu).
+//   launch_weights_finish: merges the pieces of a split-K launch that stored its scores (out, as launch_combine)
+//   and adds every row's weight, summed over the group's heads, to its total
+cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, const float* total_in, float* total_out,
+                                  int total_stride, cudaStream_t stream);
+struct SelectCounts {
+    static constexpr int kMax = 900;   // units per launch
+    int n[kMax];                       // rows to keep
+};
+struct SelectArgs {
+    const float* total;       // [units][total_stride]
+    int* keep;                // [units][keep_stride]
+    float* kept;              // [units][keep_stride] or nullptr
+    int total_stride, keep_stride;
+    int n;                    // rows per unit
+    const int* unit_len;
+    int n_recent;
+    int unit0, units;         // units of this launch
+};
+cudaError_t init_weights_kernels();
+cudaError_t launch_select(const SelectArgs& a, const SelectCounts& counts, cudaStream_t stream);
+
+// Accepted drafts of one slot move to the front of its draft rows (see kvs_tree.cu).
+struct AcceptCounts {
+    static constexpr int kMax = 2048;  // sequences per launch
+    unsigned char n[kMax];             // accepted drafts, 0 .. kTreeMaxTokens
+};
+cudaError_t launch_accept(void* kplane, void* vplane, const int* path, int path_stride, const AcceptCounts& counts,
+                          int seq0, int seqs, int Hkv, int n_draft, int len, int* unit_len, bool write_len, int row_bytes,
+                          int row_stride, int* status, long long plane_bytes, cudaStream_t stream);
 
 // Ragged slots (rows evicted by an outside intra-layer method).
 //   launch_evict:   per unit u, rows keep[u*keep_stride + j], j < counts[u], move to rows 0..counts[u]-1

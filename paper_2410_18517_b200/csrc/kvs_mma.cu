@@ -143,11 +143,16 @@ struct MmaKernelArgs {
     unsigned long long wait_ns;   // limit of every wait inside the kernel
     long long stall_tile;         // self-test only: the K/V copies of this tile are withheld (-1: none)
     unsigned long long* trace;    // tracing build: this launch's rows of time stamps, or nullptr
+    float* scores;                // W only: [units][G][row_stride] scores in the log2 domain
 };
 
 // G (q-heads per kv-head, 1..8) is a run-time argument: it only selects which rows of the padded
 // 16-row M side are real, so one kernel per head size serves every group size.
-template <int D, int BIG>
+// W (kvs_decode_attention_weights): every row's scores are stored too, and the softmax weights go into the second
+// contraction as three bf16 terms instead of two: its result stands beside totals that are exact to fp32 rounding,
+// and two terms leave 1.5e-6 of the output, three 3e-7 (n = 256, normal draws); the extra products are hidden
+// behind the stream of K and V.
+template <int D, int BIG, bool W>
 __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
     decode_splitk_mma(const __grid_constant__ CUtensorMap tmap, const __grid_constant__ CUtensorMap tmap_tail,
                       const MmaKernelArgs a_in) {
@@ -431,6 +436,14 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
                         s[blk][nb][j] = tok < valid ? s[blk][nb][j] * a.scale_log2 : -INFINITY;
                         tmax = fmaxf(tmax, s[blk][nb][j]);
                     }
+                if constexpr (W) {
+                    if (row < G) {
+                        float* dst = a.scores + (u * G + row) * a.row_stride + (long long)(ti0 + k) * TN + tok0 + quad * 2;
+#pragma unroll
+                        for (int nb = 0; nb < 2; ++nb)      // rows up to the row stride, a multiple of 128, are scratch
+                            if (tok0 < valid) *reinterpret_cast<float2*>(dst + nb * 8) = make_float2(s[blk][nb][0], s[blk][nb][1]);
+                    }
+                }
             }
             // ---- one online-softmax update for row `row` over the warp's tokens of this tile ----
             tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 1));
@@ -466,6 +479,13 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
                 const uint32_t phi_lo = pack_bf16(h00, h01), phi_hi = pack_bf16(h10, h11);
                 const uint32_t plo_lo = pack_bf16(p[blk][0][0] - h00, p[blk][0][1] - h01);
                 const uint32_t plo_hi = pack_bf16(p[blk][1][0] - h10, p[blk][1][1] - h11);
+                uint32_t pll_lo = 0, pll_hi = 0;      // W: the third term
+                if constexpr (W) {
+                    const float r00 = p[blk][0][0] - h00, r01 = p[blk][0][1] - h01;
+                    const float r10 = p[blk][1][0] - h10, r11 = p[blk][1][1] - h11;
+                    pll_lo = pack_bf16(r00 - bf16_round(r00), r01 - bf16_round(r01));
+                    pll_hi = pack_bf16(r10 - bf16_round(r10), r11 - bf16_round(r11));
+                }
                 // Four column blocks at a time: their P_hi products are issued before their P_lo products, so
                 // that an MMA never waits for the one just before it (same accumulator).
                 const int t = tok0 + (((lane >> 3) & 1) << 3) + (lane & 7);
@@ -490,6 +510,13 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
                     for (int x = 0; x < 2; ++x) {
                         mma_bf16_upper(o[2 * (nbp + x)][0], o[2 * (nbp + x)][1], plo_lo, plo_hi, b[x][0], b[x][1]);
                         mma_bf16_upper(o[2 * (nbp + x) + 1][0], o[2 * (nbp + x) + 1][1], plo_lo, plo_hi, b[x][2], b[x][3]);
+                    }
+                    if constexpr (W) {
+#pragma unroll
+                        for (int x = 0; x < 2; ++x) {
+                            mma_bf16_upper(o[2 * (nbp + x)][0], o[2 * (nbp + x)][1], pll_lo, pll_hi, b[x][0], b[x][1]);
+                            mma_bf16_upper(o[2 * (nbp + x) + 1][0], o[2 * (nbp + x) + 1][1], pll_lo, pll_hi, b[x][2], b[x][3]);
+                        }
                     }
                 }
             }
@@ -570,34 +597,38 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
     }
 }
 
-template <int D, int BIG>
+template <int D, int BIG, bool W>
 cudaError_t set_attr() {
-    cudaError_t e = cudaFuncSetAttribute(decode_splitk_mma<D, BIG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaError_t e = cudaFuncSetAttribute(decode_splitk_mma<D, BIG, W>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                          MmaShape<D, BIG>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
     // All of the SM's L1 / shared-memory array as shared memory: the kernel gains nothing from L1
     // (its loads are bulk copies), and the blocks of the small kernels launched early behind it
     // (combine) only become resident beside it if the carve-out has room for them.  Measured: with
     // the default carve-out a footprint of 157 KiB instead of 142 KiB cost 2.8 us per layer.
-    return cudaFuncSetAttribute(decode_splitk_mma<D, BIG>, cudaFuncAttributePreferredSharedMemoryCarveout,
+    return cudaFuncSetAttribute(decode_splitk_mma<D, BIG, W>, cudaFuncAttributePreferredSharedMemoryCarveout,
                                 cudaSharedmemCarveoutMaxShared);
 }
 
 template <int D, int BIG>
 cudaError_t launch_one(const CUtensorMap& tm, const CUtensorMap& tm_tail, const MmaKernelArgs& ka, int NC, bool pdl,
                        cudaStream_t stream) {
-    return launch_kernel(decode_splitk_mma<D, BIG>, dim3(NC), dim3(kMmaThreads), MmaShape<D, BIG>::SMEM_BYTES, stream, pdl, tm,
-                         tm_tail, ka);
+    return ka.scores ? launch_kernel(decode_splitk_mma<D, BIG, true>, dim3(NC), dim3(kMmaThreads), MmaShape<D, BIG>::SMEM_BYTES,
+                                     stream, pdl, tm, tm_tail, ka)
+                     : launch_kernel(decode_splitk_mma<D, BIG, false>, dim3(NC), dim3(kMmaThreads), MmaShape<D, BIG>::SMEM_BYTES,
+                                     stream, pdl, tm, tm_tail, ka);
 }
 
 }  // namespace
 
 cudaError_t init_mma_kernels() {
     cudaError_t e;
-    if ((e = set_attr<128, 0>()) != cudaSuccess || (e = set_attr<128, 1>()) != cudaSuccess ||
-        (e = set_attr<64, 0>()) != cudaSuccess)
+    if ((e = set_attr<128, 0, false>()) != cudaSuccess || (e = set_attr<128, 1, false>()) != cudaSuccess ||
+        (e = set_attr<64, 0, false>()) != cudaSuccess || (e = set_attr<64, 1, false>()) != cudaSuccess ||
+        (e = set_attr<128, 0, true>()) != cudaSuccess || (e = set_attr<128, 1, true>()) != cudaSuccess ||
+        (e = set_attr<64, 0, true>()) != cudaSuccess)
         return e;
-    return set_attr<64, 1>();
+    return set_attr<64, 1, true>();
 }
 
 // Tensor map over the whole pool seen as [total_rows][D] bf16, box = 64 columns x 64 rows (or, with
@@ -669,6 +700,7 @@ cudaError_t launch_decode_mma(const DecodeArgs& a, const DecodePlan& plan, const
     ka.wait_ns = a.wait_ns;
     ka.stall_tile = a.stall_tile;
     ka.trace = a.trace;
+    ka.scores = a.scores;
     if (a.G < 1 || a.G > 8) return cudaErrorInvalidValue;
     const bool big = plan.tile_rows * a.D * 2 == kMmaBigTileBytes && kMmaBigTileBytes != kMmaTileBytes;
     if (a.D == 128)

@@ -1,0 +1,354 @@
+// Attention of a tree of drafted tokens over a cache, its combine step, and the move that keeps the accepted drafts.
+//
+// The n_t queries of a sequence sit on the newest n_t rows of its units.  Query (token t, head g) of a kv-head sees
+// every row before the drafts and those drafts whose bit is set in mask[t]:
+//   out = sum_j p_j V_j / sum_j p_j,   p_j = 2^(s_j - m),  s_j = q . K_j * scale * log2(e),  m = max over visible j
+// and 0 where nothing is visible.  The result has the storage type: as many as 64 rows per head go into the next
+// matrix product in that type, and the rounding (one, at the end) is that type's half step.
+//
+// A masked draft contributes nothing whatever its row holds: its score is replaced, not added to, and its value row
+// is left out of the sum (0 * infinity would be NaN).  Padding tokens of a batch may hold anything.
+#include <algorithm>
+
+#include "kvs_device.cuh"
+#include "kvs_kernels.h"
+
+namespace kvs {
+
+namespace {
+
+constexpr int kTreeThreads = 256;
+constexpr int kTreeRows = 32;    // query rows per tile of the fp32 kernel
+constexpr int kTreeKeys = 64;    // keys per tile
+
+__host__ __device__ __forceinline__ long long first_tile(long long c, long long T, int teams) { return c * T / teams; }
+__host__ __device__ __forceinline__ int team_of_tile(long long gt, long long T, int teams) {
+    return (int)(((gt + 1) * teams + T - 1) / T - 1);
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(T* dst, const float4& v);
+template <>
+__device__ __forceinline__ void store4<float>(float* dst, const float4& v) { *reinterpret_cast<float4*>(dst) = v; }
+template <>
+__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* dst, const float4& v) {
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+}
+
+struct TreeKernelArgs {
+    TreeArgs a;
+    TreePlan p;
+};
+
+// --------------------------------------------------------------------------------------
+// fp32 FMA kernel.  32 query rows x 64 keys per step; thread (ty, tx) owns rows 2 ty, 2 ty + 1 and, of the
+// scores, keys tx + 16 i, of the output, columns 4 tx + 64 c: every operand comes from shared memory as float4 and
+// the 16 lanes of a row reduce its softmax with shuffles.
+// --------------------------------------------------------------------------------------
+template <int D>
+struct TreeShape {
+    static constexpr int LD = D + 4;       // row stride of Q and K in shared memory: eight rows hit eight bank quads
+    static constexpr int SMEM_BYTES = (kTreeRows * LD + kTreeKeys * LD + kTreeKeys * D + kTreeRows * kTreeKeys) * 4 + kTreeRows * 8;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __grid_constant__ TreeKernelArgs ka) {
+    using S = TreeShape<D>;
+    constexpr int EPL = 16 / (int)sizeof(T), LPR = D / EPL, CB = D / 64;
+    const TreeArgs& a = ka.a;
+    const TreePlan& p = ka.p;
+    extern __shared__ __align__(16) float smem_f[];
+    float* Qs = smem_f;
+    float* Ks = Qs + kTreeRows * S::LD;
+    float* Vs = Ks + kTreeKeys * S::LD;
+    float* Ps = Vs + kTreeKeys * D;
+    unsigned long long* sees = reinterpret_cast<unsigned long long*>(Ps + kTreeRows * kTreeKeys);
+
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int team = blockIdx.x / p.m_tiles, mt = blockIdx.x - team * p.m_tiles;
+    const int tok0 = mt * p.tokens, rows = min(p.tokens, a.n_t - tok0) * a.G;
+    const unsigned long long all = a.n_t >= 64 ? ~0ull : (1ull << a.n_t) - 1;
+    const long long t1 = first_tile(team + 1, p.T, p.teams);
+
+    for (long long gt = first_tile(team, p.T, p.teams); gt < t1;) {
+        const long long u = gt / p.tpu;
+        const int ti0 = (int)(gt - u * p.tpu);
+        const int piece = (int)min((long long)(p.tpu - ti0), t1 - gt);
+        gt += piece;
+        const int n = a.unit_len ? min(a.unit_len[u], a.capacity) : a.n;
+        const int nt = (n + kTreeKeys - 1) / kTreeKeys;          // key tiles the unit really has
+        const int te = min(ti0 + piece, nt);
+        if (ti0 >= te) continue;                                 // the piece lies past a ragged unit's end
+        const int b = (int)(u / a.Hkv), hk = (int)(u - (long long)b * a.Hkv);
+        const int ctx = n - a.n_t;                               // rows every query sees
+        const T* K = reinterpret_cast<const T*>(a.kplane) + u * a.row_stride * (long long)D;
+        const T* V = reinterpret_cast<const T*>(a.vplane) + u * a.row_stride * (long long)D;
+        __syncthreads();                                         // the previous piece's readers are done
+        for (int i = tid; i < kTreeRows * LPR; i += kTreeThreads) {
+            const int r = i / LPR, c = i - r * LPR;
+            float f[EPL];
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) f[e] = 0.f;
+            if (r < rows) {
+                const long long off = (((long long)b * a.n_t + tok0 + r / a.G) * a.Hq + hk * a.G + r % a.G) * D + c * EPL;
+                Unpack<T>::run(*reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + off), f);
+            }
+#pragma unroll
+            for (int e = 0; e < EPL; e += 4)
+                *reinterpret_cast<float4*>(Qs + r * S::LD + c * EPL + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+        }
+        if (tid < kTreeRows) {
+            const int t = tok0 + tid / a.G;
+            unsigned long long w = 0;
+            if (tid < rows) w = a.mask ? a.mask[(long long)b * a.n_t + t] & all : (t >= 63 ? ~0ull : (2ull << t) - 1);
+            sees[tid] = w;
+        }
+        float m[2] = {-1.0e30f, -1.0e30f}, l[2] = {0.f, 0.f};
+        float4 o[2][CB];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int c = 0; c < CB; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+
+        for (int ti = ti0; ti < te; ++ti) {
+            const int key0 = ti * kTreeKeys;
+            __syncthreads();
+            for (int i = tid; i < 2 * kTreeKeys * LPR; i += kTreeThreads) {
+                const bool isv = i >= kTreeKeys * LPR;
+                const int ii = isv ? i - kTreeKeys * LPR : i;
+                const int r = ii / LPR, c = ii - r * LPR;
+                float f[EPL];
+#pragma unroll
+                for (int e = 0; e < EPL; ++e) f[e] = 0.f;
+                if (key0 + r < n && KVS_BOUNDS_OK(((u * a.row_stride + key0 + r) * (long long)D + c * EPL) * (int)sizeof(T), 16,
+                                                  a.plane_bytes, a.status))
+                    Unpack<T>::run(*reinterpret_cast<const uint4*>((isv ? V : K) + (long long)(key0 + r) * D + c * EPL), f);
+                float* dst = isv ? Vs + r * D : Ks + r * S::LD;
+#pragma unroll
+                for (int e = 0; e < EPL; e += 4)
+                    *reinterpret_cast<float4*>(dst + c * EPL + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+            }
+            __syncthreads();
+            float s[2][4];
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[r][i] = 0.f;
+#pragma unroll 4
+            for (int d = 0; d < D; d += 4) {
+                float4 qv[2], kv[4];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) qv[r] = *reinterpret_cast<const float4*>(Qs + (2 * ty + r) * S::LD + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) kv[i] = *reinterpret_cast<const float4*>(Ks + (tx + 16 * i) * S::LD + d);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        s[r][i] = fmaf(qv[r].x, kv[i].x, s[r][i]);
+                        s[r][i] = fmaf(qv[r].y, kv[i].y, s[r][i]);
+                        s[r][i] = fmaf(qv[r].z, kv[i].z, s[r][i]);
+                        s[r][i] = fmaf(qv[r].w, kv[i].w, s[r][i]);
+                    }
+            }
+            const bool masked = key0 + kTreeKeys > ctx;          // the tile holds drafts or ends past the unit
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                bool vis[4];
+                float mx = -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = key0 + tx + 16 * i;
+                    vis[i] = !masked || j < ctx || (j < n && (sees[2 * ty + r] >> (j - ctx) & 1ull));
+                    s[r][i] = vis[i] ? s[r][i] * a.scale_log2 : -INFINITY;
+                    mx = fmaxf(mx, s[r][i]);
+                }
+#pragma unroll
+                for (int off = 8; off >= 1; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+                const float m_new = fmaxf(m[r], mx);
+                const float alpha = fast_exp2(m[r] - m_new);
+                m[r] = m_new;
+                l[r] *= alpha;
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    o[r][c].x *= alpha; o[r][c].y *= alpha; o[r][c].z *= alpha; o[r][c].w *= alpha;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = vis[i] ? fast_exp2(s[r][i] - m_new) : 0.f;
+                    l[r] += w;
+                    Ps[(2 * ty + r) * kTreeKeys + tx + 16 * i] = w;
+                }
+            }
+            __syncwarp();                                        // a row's weights are written and read by one warp
+#pragma unroll 4
+            for (int j = 0; j < kTreeKeys; ++j) {
+                const float w0 = Ps[(2 * ty) * kTreeKeys + j], w1 = Ps[(2 * ty + 1) * kTreeKeys + j];
+#pragma unroll
+                for (int c = 0; c < CB; ++c) {
+                    const float4 v = *reinterpret_cast<const float4*>(Vs + j * D + 64 * c + 4 * tx);
+                    if (!masked || w0 != 0.f) {
+                        o[0][c].x = fmaf(w0, v.x, o[0][c].x); o[0][c].y = fmaf(w0, v.y, o[0][c].y);
+                        o[0][c].z = fmaf(w0, v.z, o[0][c].z); o[0][c].w = fmaf(w0, v.w, o[0][c].w);
+                    }
+                    if (!masked || w1 != 0.f) {
+                        o[1][c].x = fmaf(w1, v.x, o[1][c].x); o[1][c].y = fmaf(w1, v.y, o[1][c].y);
+                        o[1][c].z = fmaf(w1, v.z, o[1][c].z); o[1][c].w = fmaf(w1, v.w, o[1][c].w);
+                    }
+                }
+            }
+        }
+        const bool whole = ti0 == 0 && te == nt;
+        const long long slot = 2ll * team + (ti0 == 0 ? 1 : 0);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+#pragma unroll
+            for (int off = 8; off >= 1; off >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], off);
+            const int row = 2 * ty + r;
+            if (row >= rows) continue;
+            if (whole) {
+                const float inv = l[r] > 0.f || l[r] != l[r] ? 1.0f / l[r] : 0.f;    // nothing visible: 0
+                T* dst = reinterpret_cast<T*>(a.out) + (((long long)b * a.n_t + tok0 + row / a.G) * a.Hq + hk * a.G + row % a.G) * D;
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+                    store4<T>(dst + 64 * c + 4 * tx, make_float4(o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv));
+            } else {
+                const long long pr = (slot * p.m_tiles + mt) * kTreeRows + row;
+#pragma unroll
+                for (int c = 0; c < CB; ++c) *reinterpret_cast<float4*>(a.part_o + pr * D + 64 * c + 4 * tx) = o[r][c];
+                if (tx == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(m[r], l[r]);
+            }
+        }
+    }
+}
+
+// --------------------------------------------------------------------------------------
+// Combine: one warp per (unit, token, head) of a unit that was cut between teams: the pieces, in team order.
+// --------------------------------------------------------------------------------------
+constexpr int kTreeCombineWarps = 8;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const __grid_constant__ TreeKernelArgs ka, int tile_rows) {
+    constexpr int VEC = D / 32;
+    const TreeArgs& a = ka.a;
+    const TreePlan& p = ka.p;
+    pdl_wait();
+    const long long item = (long long)blockIdx.x * kTreeCombineWarps + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, per_unit = a.n_t * a.G;
+    if (item >= (long long)a.units * per_unit) return;
+    const long long u = item / per_unit;
+    const int q = (int)(item - u * per_unit), t = q / a.G, g = q - t * a.G;
+    const int mt = t / p.tokens, row = (t - mt * p.tokens) * a.G + g;
+    const int n = a.unit_len ? min(a.unit_len[u], a.capacity) : a.n;
+    const int nt = (n + p.key_rows - 1) / p.key_rows;
+    const int c0 = team_of_tile(u * p.tpu, p.T, p.teams), c1 = team_of_tile(u * p.tpu + nt - 1, p.T, p.teams);
+    if (c0 == c1) return;                                        // finished by its one team
+    float M = -1.0e30f, den = 0.f, acc[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+    for (int c = c0; c <= c1; ++c) {
+        const long long pr = ((2ll * c + (c == c0 ? 1 : 0)) * p.m_tiles + mt) * tile_rows + row;
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + pr * 2);
+        const float m_new = fmaxf(M, ml.x);
+        const float w0 = fast_exp2(M - m_new), w1 = fast_exp2(ml.x - m_new);
+        M = m_new;
+        den = fmaf(w1, ml.y, w0 * den);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[e] = fmaf(w1, a.part_o[pr * D + lane * VEC + e], w0 * acc[e]);
+    }
+    const float inv = den > 0.f || den != den ? 1.0f / den : 0.f;
+    const int b = (int)(u / a.Hkv), hk = (int)(u - (long long)b * a.Hkv);
+    T* dst = reinterpret_cast<T*>(a.out) + (((long long)b * a.n_t + t) * a.Hq + hk * a.G + g) * D + lane * VEC;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+        if constexpr (sizeof(T) == 2) dst[e] = __float2bfloat16_rn(acc[e] * inv);
+        else dst[e] = acc[e] * inv;
+    }
+}
+
+// --------------------------------------------------------------------------------------
+// Accepted drafts: rows base + path[i] -> base + i of every unit, i < n_acc (path strictly ascending: path[i] >= i).
+// One block per unit; all of a unit's rows go through shared memory, K and then V, so that no row is read after it was
+// written.  An entry that is not ascending or out of range sets the status word to 1 and keeps the row already there.
+// --------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* vplane, const int* __restrict__ path, int path_stride,
+                                                           const __grid_constant__ AcceptCounts counts, int seq0, int Hkv,
+                                                           int n_draft, int len, int* unit_len, bool write_len, int row_vecs,
+                                                           int row_stride, int* status, long long plane_vecs) {
+    __shared__ uint4 buf[kTreeMaxTokens * 32];     // 64 rows of up to 512 bytes
+    const int b = seq0 + blockIdx.x / Hkv, cnt = counts.n[blockIdx.x / Hkv];
+    const long long u = (long long)seq0 * Hkv + blockIdx.x;
+    // (a slot that becomes ragged with this call has no lengths on the device yet)
+    const int base = (unit_len && !(write_len && len >= 0) ? unit_len[u] : len) - n_draft;
+    const int* list = path + (long long)b * path_stride;
+    for (int kv = 0; kv < 2; ++kv) {
+        uint4* rows = reinterpret_cast<uint4*>(kv == 0 ? kplane : vplane) + (u * row_stride + base) * row_vecs;
+        __syncthreads();
+        for (int i = threadIdx.x; i < cnt * row_vecs; i += blockDim.x) {
+            const int j = i / row_vecs, v = i - j * row_vecs;
+            int src = list[j];
+            if (src < j || src >= n_draft || (j > 0 && list[j - 1] >= src)) {
+                if (v == 0) atomicExch(status, 1);
+                src = j;
+            }
+            if (!KVS_BOUNDS_OK((u * row_stride + base + src) * (long long)row_vecs, row_vecs, plane_vecs, status)) continue;
+            buf[i] = rows[(long long)src * row_vecs + v];
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < cnt * row_vecs; i += blockDim.x)
+            if (KVS_BOUNDS_OK((u * row_stride + base) * (long long)row_vecs + i, 1, plane_vecs, status)) rows[i] = buf[i];
+    }
+    if (write_len && threadIdx.x == 0) unit_len[u] = base + cnt;
+}
+
+template <typename T, int D>
+cudaError_t launch_fma(const TreeKernelArgs& ka, bool cut, cudaStream_t stream) {
+    tree_attention_fma<T, D><<<ka.p.teams * ka.p.m_tiles, kTreeThreads, TreeShape<D>::SMEM_BYTES, stream>>>(ka);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || !cut) return e;
+    const long long items = (long long)ka.a.units * ka.a.n_t * ka.a.G;
+    const unsigned grid = (unsigned)((items + kTreeCombineWarps - 1) / kTreeCombineWarps);
+    return launch_kernel(tree_combine_kernel<T, D>, dim3(grid), dim3(kTreeCombineWarps * 32), 0, stream, true, ka, kTreeRows);
+}
+
+}  // namespace
+
+cudaError_t init_tree_kernels() {
+    cudaError_t e;
+    if ((e = cudaFuncSetAttribute(tree_attention_fma<float, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<128>::SMEM_BYTES)) != cudaSuccess ||
+        (e = cudaFuncSetAttribute(tree_attention_fma<float, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<64>::SMEM_BYTES)) != cudaSuccess ||
+        (e = cudaFuncSetAttribute(tree_attention_fma<__nv_bfloat16, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<128>::SMEM_BYTES)) != cudaSuccess)
+        return e;
+    return cudaFuncSetAttribute(tree_attention_fma<__nv_bfloat16, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<64>::SMEM_BYTES);
+}
+
+cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* launches, cudaStream_t stream) {
+    TreeKernelArgs ka;
+    ka.a = a;
+    TreePlan& p = ka.p;
+    p.tokens = std::min(a.n_t, kTreeRows / a.G);
+    p.m_tiles = (a.n_t + p.tokens - 1) / p.tokens;
+    p.key_rows = kTreeKeys;
+    p.tpu = (a.n + kTreeKeys - 1) / kTreeKeys;
+    p.T = (long long)a.units * p.tpu;
+    int blocks = std::min(2 * sm_count, kTreeMaxBlocks);
+    if (max_ctas > 0) blocks = std::min(blocks, max_ctas);
+    p.teams = (int)std::min<long long>(p.T, std::max(1, blocks / p.m_tiles));
+    // some unit is cut unless every team boundary falls on a unit boundary
+    const bool cut = a.units % p.teams != 0;
+    *launches = cut ? 2 : 1;
+    if (a.dtype == 0) return a.D == 128 ? launch_fma<__nv_bfloat16, 128>(ka, cut, stream) : launch_fma<__nv_bfloat16, 64>(ka, cut, stream);
+    return a.D == 128 ? launch_fma<float, 128>(ka, cut, stream) : launch_fma<float, 64>(ka, cut, stream);
+}
+
+cudaError_t launch_accept(void* kplane, void* vplane, const int* path, int path_stride, const AcceptCounts& counts,
+                          int seq0, int seqs, int Hkv, int n_draft, int len, int* unit_len, bool write_len, int row_bytes,
+                          int row_stride, int* status, long long plane_bytes, cudaStream_t stream) {
+    accept_draft_kernel<<<(unsigned)(seqs * Hkv), 256, 0, stream>>>(
+        static_cast<char*>(kplane), static_cast<char*>(vplane), path, path_stride, counts, seq0, Hkv, n_draft, len, unit_len,
+        write_len, row_bytes / 16, row_stride, status, plane_bytes / 16);
+    return cudaGetLastError();
+}
+
+}  // namespace kvs
