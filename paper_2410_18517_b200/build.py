@@ -13,8 +13,8 @@ LIB_BOUNDS = os.path.join(HERE, "libkvs_bounds.so")
 # the same sources with -DKVS_TRACE: the attention kernels stamp a per-block timeline (kvs_trace_begin)
 LIB_TRACE = os.path.join(HERE, "libkvs_trace.so")
 SOURCES = ["kvs_api.cu", "kvs_kernels.cu", "kvs_mma.cu", "kvs_prefill.cu", "kvs_prefill_f32.cu", "kvs_search.cu",
-           "kvs_rotary.cu", "kvs_tree.cu", "kvs_weights.cu"]
-HEADERS = ["kvs_device.cuh", "kvs_kernels.h", os.path.join("..", "..", "include", "kvs.h")]
+           "kvs_rotary.cu", "kvs_tree.cu", "kvs_tree_tc.cu", "kvs_weights.cu"]
+HEADERS = ["kvs_device.cuh", "kvs_umma.cuh", "kvs_kernels.h", os.path.join("..", "..", "include", "kvs.h")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

@@ -828,6 +828,7 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
                               int32_t n_t, void* stream) {
     if (!ctx) return KVS_ERR_INVALID_ARG;
     if (!ctx->bound || ctx->opt_replay) return KVS_ERR_STATE;
+    if (ctx->cfg.dtype == KVS_BF16 && !ctx->have_tensor_map) return KVS_ERR_STATE;
     if (layer < 0 || layer >= ctx->cfg.n_layers || !q || !out) return KVS_ERR_INVALID_ARG;
     if (batch < 1 || batch > ctx->cfg.max_batch || n_t < 1 || n_t > kvs::kTreeMaxTokens) return KVS_ERR_INVALID_ARG;
     if (((uintptr_t)q % 16) != 0 || ((uintptr_t)out % 16) != 0 || ((uintptr_t)mask % 8) != 0) return KVS_ERR_INVALID_ARG;
@@ -860,6 +861,10 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
     a.plane_bytes = (long long)ctx->plane_bytes;
     a.scale_log2 = ctx->scale * 1.4426950408889634f;
     a.wait_ns = 1000ull * (unsigned long long)ctx->opt_wait_us;
+    a.pool_map = ctx->tensor_map;
+    const long long plane_rows = (long long)ctx->cfg.max_batch * ctx->cfg.n_kv_heads * ctx->row_stride;
+    a.krow0 = plane_rows * (2 * slot);
+    a.vrow0 = plane_rows * (2 * slot + 1);
     int launches = 0;
     if (kvs::launch_tree(a, ctx->sm_count, ctx->opt_max_ctas, &launches, static_cast<cudaStream_t>(stream)) != cudaSuccess)
         return KVS_ERR_CUDA;

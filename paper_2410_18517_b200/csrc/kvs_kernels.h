@@ -149,6 +149,7 @@ cudaError_t launch_append_rotary(const RotaryArgs& r, cudaStream_t stream);
 struct TreePlan {
     int tokens;      // drafted tokens per query tile
     int m_tiles;     // query tiles per unit
+    int tile_rows;   // rows a query tile takes in the partial results
     int key_rows;    // keys per tile
     int tpu;         // key tiles per unit (of the longest unit)
     long long T;     // key tiles of all units
@@ -170,12 +171,18 @@ struct TreeArgs {
     long long plane_bytes;
     float scale_log2;
     unsigned long long wait_ns;
+    const void* pool_map;              // tensor map of the pool (bf16), 64-row boxes
+    long long krow0, vrow0;            // first row of the slot's planes in the pool-wide row numbering
 };
 constexpr int kTreeMaxTokens = 64;
 constexpr int kTreeMaxBlocks = 320;    // thread blocks of one call; bounds the partial results
 constexpr int kTreeTileRows = 128;     // query rows of the largest tile
 inline int tree_partial_rows(int G) { return G * kTreeMaxTokens < kTreeTileRows ? G * kTreeMaxTokens : kTreeTileRows; }
 cudaError_t init_tree_kernels();
+// the tensor-core kernel (bf16; see kvs_tree_tc.cu); launch_tree chooses and adds the combine step
+cudaError_t init_tree_tc_kernels();
+void plan_tree_tc(const TreeArgs& a, int blocks, TreePlan* plan);
+cudaError_t launch_tree_tc(const TreeArgs& a, const TreePlan& plan, cudaStream_t stream);
 cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* launches, cudaStream_t stream);
 
 // Running totals of softmax weights and the rows a budget keeps (see kvs_weights.cu).

@@ -30,11 +30,6 @@ template <typename T>
 __device__ __forceinline__ void store4(T* dst, const float4& v);
 template <>
 __device__ __forceinline__ void store4<float>(float* dst, const float4& v) { *reinterpret_cast<float4*>(dst) = v; }
-template <>
-__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* dst, const float4& v) {
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
-    *reinterpret_cast<uint2*>(dst) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-}
 
 struct TreeKernelArgs {
     TreeArgs a;
@@ -214,7 +209,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
                 for (int c = 0; c < CB; ++c)
                     store4<T>(dst + 64 * c + 4 * tx, make_float4(o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv));
             } else {
-                const long long pr = (slot * p.m_tiles + mt) * kTreeRows + row;
+                const long long pr = (slot * p.m_tiles + mt) * p.tile_rows + row;
 #pragma unroll
                 for (int c = 0; c < CB; ++c) *reinterpret_cast<float4*>(a.part_o + pr * D + 64 * c + 4 * tx) = o[r][c];
                 if (tx == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(m[r], l[r]);
@@ -229,7 +224,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
 constexpr int kTreeCombineWarps = 8;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const __grid_constant__ TreeKernelArgs ka, int tile_rows) {
+__global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const __grid_constant__ TreeKernelArgs ka) {
     constexpr int VEC = D / 32;
     const TreeArgs& a = ka.a;
     const TreePlan& p = ka.p;
@@ -248,7 +243,7 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
     for (int c = c0; c <= c1; ++c) {
-        const long long pr = ((2ll * c + (c == c0 ? 1 : 0)) * p.m_tiles + mt) * tile_rows + row;
+        const long long pr = ((2ll * c + (c == c0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + row;
         const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + pr * 2);
         const float m_new = fmaxf(M, ml.x);
         const float w0 = fast_exp2(M - m_new), w1 = fast_exp2(ml.x - m_new);
@@ -303,13 +298,10 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* v
 }
 
 template <typename T, int D>
-cudaError_t launch_fma(const TreeKernelArgs& ka, bool cut, cudaStream_t stream) {
-    tree_attention_fma<T, D><<<ka.p.teams * ka.p.m_tiles, kTreeThreads, TreeShape<D>::SMEM_BYTES, stream>>>(ka);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || !cut) return e;
+cudaError_t launch_combine_one(const TreeKernelArgs& ka, cudaStream_t stream) {
     const long long items = (long long)ka.a.units * ka.a.n_t * ka.a.G;
     const unsigned grid = (unsigned)((items + kTreeCombineWarps - 1) / kTreeCombineWarps);
-    return launch_kernel(tree_combine_kernel<T, D>, dim3(grid), dim3(kTreeCombineWarps * 32), 0, stream, true, ka, kTreeRows);
+    return launch_kernel(tree_combine_kernel<T, D>, dim3(grid), dim3(kTreeCombineWarps * 32), 0, stream, true, ka);
 }
 
 }  // namespace
@@ -317,29 +309,42 @@ cudaError_t launch_fma(const TreeKernelArgs& ka, bool cut, cudaStream_t stream) 
 cudaError_t init_tree_kernels() {
     cudaError_t e;
     if ((e = cudaFuncSetAttribute(tree_attention_fma<float, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<128>::SMEM_BYTES)) != cudaSuccess ||
-        (e = cudaFuncSetAttribute(tree_attention_fma<float, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<64>::SMEM_BYTES)) != cudaSuccess ||
-        (e = cudaFuncSetAttribute(tree_attention_fma<__nv_bfloat16, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<128>::SMEM_BYTES)) != cudaSuccess)
+        (e = cudaFuncSetAttribute(tree_attention_fma<float, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<64>::SMEM_BYTES)) != cudaSuccess)
         return e;
-    return cudaFuncSetAttribute(tree_attention_fma<__nv_bfloat16, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<64>::SMEM_BYTES);
+    return init_tree_tc_kernels();
 }
 
 cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* launches, cudaStream_t stream) {
     TreeKernelArgs ka;
     ka.a = a;
     TreePlan& p = ka.p;
-    p.tokens = std::min(a.n_t, kTreeRows / a.G);
-    p.m_tiles = (a.n_t + p.tokens - 1) / p.tokens;
-    p.key_rows = kTreeKeys;
-    p.tpu = (a.n + kTreeKeys - 1) / kTreeKeys;
-    p.T = (long long)a.units * p.tpu;
     int blocks = std::min(2 * sm_count, kTreeMaxBlocks);
     if (max_ctas > 0) blocks = std::min(blocks, max_ctas);
-    p.teams = (int)std::min<long long>(p.T, std::max(1, blocks / p.m_tiles));
+    cudaError_t e;
+    if (a.dtype == 0) {
+        plan_tree_tc(a, blocks, &p);
+        e = launch_tree_tc(a, p, stream);
+    } else {
+        p.tokens = std::min(a.n_t, kTreeRows / a.G);
+        p.m_tiles = (a.n_t + p.tokens - 1) / p.tokens;
+        p.tile_rows = kTreeRows;
+        p.key_rows = kTreeKeys;
+        p.tpu = (a.n + kTreeKeys - 1) / kTreeKeys;
+        p.T = (long long)a.units * p.tpu;
+        p.teams = (int)std::min<long long>(p.T, std::max(1, blocks / p.m_tiles));
+        const unsigned grid = (unsigned)(p.teams * p.m_tiles);
+        if (a.D == 128) tree_attention_fma<float, 128><<<grid, kTreeThreads, TreeShape<128>::SMEM_BYTES, stream>>>(ka);
+        else tree_attention_fma<float, 64><<<grid, kTreeThreads, TreeShape<64>::SMEM_BYTES, stream>>>(ka);
+        e = cudaGetLastError();
+    }
     // some unit is cut unless every team boundary falls on a unit boundary
     const bool cut = a.units % p.teams != 0;
     *launches = cut ? 2 : 1;
-    if (a.dtype == 0) return a.D == 128 ? launch_fma<__nv_bfloat16, 128>(ka, cut, stream) : launch_fma<__nv_bfloat16, 64>(ka, cut, stream);
-    return a.D == 128 ? launch_fma<float, 128>(ka, cut, stream) : launch_fma<float, 64>(ka, cut, stream);
+    if (e != cudaSuccess || !cut) return e;
+    if (a.dtype == 0)
+        return a.D == 128 ? launch_combine_one<__nv_bfloat16, 128>(ka, stream)
+                          : launch_combine_one<__nv_bfloat16, 64>(ka, stream);
+    return a.D == 128 ? launch_combine_one<float, 128>(ka, stream) : launch_combine_one<float, 64>(ka, stream);
 }
 
 cudaError_t launch_accept(void* kplane, void* vplane, const int* path, int path_stride, const AcceptCounts& counts,

@@ -207,6 +207,24 @@ def test_tree_on_ragged_units_and_smaller_batch(dtype):
     cache.check_canaries()
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,B,n,n_t", [(32, 32, 128, 8, 4112, 16), (32, 8, 128, 4, 8224, 32), (24, 8, 64, 3, 700, 20)])
+def test_tree_many_calls_in_flight_give_the_same_bits(Hq, Hkv, D, B, n, n_t):
+    """Two caches used in turn without a wait: the last tiles' clean-up must not meet a copy or a product in flight."""
+    cases = []
+    for i in range(2):
+        cache, _, _ = filled(Hq, Hkv, D, B, n, "bf16", seed=10 * i + 1, cls=SharedKVCache)
+        words = [ref.random_tree(np.random.default_rng(b + i), n_t) for b in range(B)]
+        words = [[0 if t > 3 * b + 2 else w & ((8 << 3 * b) - 1) for t, w in enumerate(row)] for b, row in enumerate(words)]
+        cases.append((cache, normal(5 + i, "bf16", B, n_t, Hq, D), torch.tensor([ref.to_int64(w) for w in words]).cuda()))
+    first = [c.tree_attention(0, q, m) for c, q, m in cases]
+    outs = [[c.tree_attention(0, q, m) for c, q, m in cases] for _ in range(40)]
+    for pair in outs:
+        for a, b in zip(pair, first):
+            assert torch.equal(a, b)
+    (cache, q, m), out = cases[0], first[0]
+    check_tree(cache, 0, q[:1], m[:1].tolist(), out[:1])
+
+
 def test_tree_bits_behind_the_last_draft_are_ignored_and_out_rows_stay():
     cache, _, _ = filled(8, 2, 128, 2, 90, "bf16")
     words = [ref.random_tree(np.random.default_rng(b), 11) for b in range(2)]
