@@ -3,11 +3,11 @@
 //
 // One thread block = one query tile (up to 128 rows: the G heads of as many drafts as fit) walking over key tiles
 // of 64; two blocks share an SM.
-//   warp 8 (one lane)  TMA producer: the query tile per piece, K and V tiles, kTcStages stages each
-//   warp 9 (one lane)  MMA issuer:   S = Q K^T into one of two score buffers (S of tile j+1 runs during the softmax of
+//   warp 4 (one lane)  TMA producer: the query tile per piece, K and V tiles, kTcStages stages each
+//   warp 5 (one lane)  MMA issuer:   S = Q K^T into one of two score buffers (S of tile j+1 runs during the softmax of
 //                                    tile j), O += P V with P as bf16 read from tensor memory
-//   warps 0..7         softmax: two threads per query row (= tensor-memory lane), 32 keys of the tile each; warps
-//                      whose lanes hold no query row stay out of it
+//   warps 0..3         softmax: one thread per query row (= tensor-memory lane), all 64 keys of the tile; warps whose
+//                      lanes hold no query row stay out of it
 // P goes into the second contraction as one bf16 term (each weight off by at most 2^-8 of itself, the sum of the weights
 // kept in fp32 from the unrounded ones): the result is rounded to bf16 anyway, and a second term would add half again to the
 // tensor work of wide trees, which the tensor pipe bounds.
@@ -25,7 +25,7 @@ namespace kvs {
 
 namespace {
 
-constexpr int kTcSoftmaxWarps = 8;
+constexpr int kTcSoftmaxWarps = 4;
 constexpr int kTcThreads = (kTcSoftmaxWarps + 2) * 32;
 constexpr int kTcKeys = 64;
 constexpr int kTcStages = 2;
@@ -38,8 +38,7 @@ struct TcShape {
     static constexpr int HALVES = D / 64;
     static constexpr int Q_BYTES = HALVES * kTcQBlock;
     static constexpr int KV_BYTES = HALVES * kTcKvBlock;
-    static constexpr int OC = D / 2;             // output columns per softmax thread
-    static constexpr int SMEM_BYTES = 1024 + Q_BYTES + 2 * kTcStages * KV_BYTES + 512 + 6 * kTreeTileRows * 4;
+    static constexpr int SMEM_BYTES = 1024 + Q_BYTES + 2 * kTcStages * KV_BYTES + 512;
 };
 
 struct TreeTcArgs {
@@ -80,21 +79,38 @@ struct Pieces {
 
 // p = 2^(x * scale - m_ref) of 16 scores as bf16 pairs, 0 where the key's bit in `vis` is not set (MASK).
 template <bool MASK, int OFF>
-__device__ __forceinline__ float weights_chunk(const float (&x)[32], float scale_log2, float m_ref, uint32_t vis, uint32_t (&w)[8]) {
+__device__ __forceinline__ float weights_chunk(const float (&x)[64], float scale_log2, float m_ref, unsigned long long vis,
+                                               uint32_t (&w)[8]) {
     const float2 sc = make_float2(scale_log2, scale_log2), nm = make_float2(-m_ref, -m_ref);
+    const uint32_t bits = (uint32_t)(vis >> OFF);
     float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
         const float2 t = __ffma2_rn(make_float2(x[OFF + i], x[OFF + i + 1]), sc, nm);
         float2 p = make_float2(fast_exp2(t.x), fast_exp2(t.y));
         if (MASK) {
-            p.x = (vis >> (OFF + i)) & 1u ? p.x : 0.f;
-            p.y = (vis >> (OFF + i + 1)) & 1u ? p.y : 0.f;
+            p.x = (bits >> i) & 1u ? p.x : 0.f;
+            p.y = (bits >> (i + 1)) & 1u ? p.y : 0.f;
         }
         sum = __fadd2_rn(sum, p);
         w[i >> 1] = pack2_bf16(p.x, p.y);
     }
     return sum.x + sum.y;
+}
+
+// The weights of a tile's 64 keys, as they go to tensor memory (key k -> column k / 2 at `taddr`); returns their sum.
+template <bool MASK>
+__device__ __forceinline__ float weights_tile(const float (&x)[64], float scale_log2, float m_ref, unsigned long long vis, uint32_t taddr) {
+    uint32_t w[8];
+    float l = weights_chunk<MASK, 0>(x, scale_log2, m_ref, vis, w);
+    tmem_st8(taddr, w);
+    l += weights_chunk<MASK, 16>(x, scale_log2, m_ref, vis, w);
+    tmem_st8(taddr + 8, w);
+    l += weights_chunk<MASK, 32>(x, scale_log2, m_ref, vis, w);
+    tmem_st8(taddr + 16, w);
+    l += weights_chunk<MASK, 48>(x, scale_log2, m_ref, vis, w);
+    tmem_st8(taddr + 24, w);
+    return l;
 }
 
 __device__ __forceinline__ uint32_t nonfinite16(uint32_t w) {      // mask of the halves of w that are Inf or NaN
@@ -119,7 +135,6 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     uint64_t* o_full = bars + 2;       // [2] by tile parity: the tile's PV is in O
     uint64_t* s_full = bars + 4;       // [2] per score buffer
     uint64_t* p_full = bars + 6;       // [2] one arrival per active softmax thread
-    uint64_t* pair_bar = bars + 8;     // [4] the two warps that share 32 query rows
     uint64_t* drain = bars + 12;
     uint64_t* k_full = bars + 16;      // [NS] each
     uint64_t* k_empty = k_full + NS;
@@ -128,20 +143,17 @@ __global__ void __launch_bounds__(kTcThreads, 2)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(v_empty + NS);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);    // [2]; the second bounds the drains
     volatile int* broken = abort_flag + 2;                                        // [2] by piece parity
-    float* exch_m = reinterpret_cast<float*>(bars + 64);    // [2 tile parities][2 key halves][128] row maxima
-    float* exch_l = exch_m + 4 * kTreeTileRows;             // [2 key halves][128] row sums
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int team = blockIdx.x / p.m_tiles, mt = blockIdx.x - team * p.m_tiles;
     const int tok0 = mt * p.tokens, rows = min(p.tokens, a.n_t - tok0) * a.G;
     const int quarters = (p.tokens * a.G + 31) / 32;        // tensor-memory lane quarters that hold query rows
-    const uint32_t active = quarters * 64;                  // softmax threads at work
+    const uint32_t active = quarters * 32;                  // softmax threads at work
 
     if (tid == 0) {
         for (int i = 0; i < 16 + 4 * NS; ++i) mbar_init(&bars[i], 1);
         mbar_init(&p_full[0], active);
         mbar_init(&p_full[1], active);
-        for (int i = 0; i < 4; ++i) mbar_init(&pair_bar[i], 64);
         abort_flag[0] = abort_flag[1] = broken[0] = broken[1] = 0;
         fence_mbar_init();
     }
@@ -263,17 +275,16 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                 mbar_wait_bounded(drain, 0, abort_flag + 1, a.status, a.wait_ns);
             }
         }
-    } else if ((warp & 3) < quarters) {
+    } else if (warp < quarters) {
         // ------------------------------ softmax / output rows ------------------------------
-        const int w4 = warp & 3, hf = warp >> 2;             // tensor-memory lane quarter, key half of a tile
-        const int r = w4 * 32 + lane;                        // query row in the tile = tensor-memory lane
-        const uint32_t lane_addr = (uint32_t)(w4 * 32) << 16;
-        const uint32_t to = tmem_o + lane_addr + hf * S::OC;
-        const int tok = tok0 + min(r, rows - 1) / a.G, g = min(r, rows - 1) % a.G;    // rows past the last repeat it
+        const int r = tid;                                   // query row in the tile = tensor-memory lane
+        const uint32_t lane_addr = (uint32_t)(warp * 32) << 16;
+        const uint32_t to = tmem_o + lane_addr;
+        const bool real = r < rows;                          // lanes past the last row hold no query: their scores are junk
+        const int tok = tok0 + min(r, rows - 1) / a.G, g = min(r, rows - 1) % a.G;
         const unsigned long long all = a.n_t >= 64 ? ~0ull : (1ull << a.n_t) - 1;
         auto wait = [&](uint64_t* bar, uint32_t ph) { return mbar_wait_bounded(bar, ph & 1u, abort_flag, a.status, a.wait_ns); };
         int t = 0, pc = 0;
-        uint32_t pp = 0;                                     // phases used so far of pair_bar[w4]
         bool ok = true;
         for (Pieces pi(x, team); ok && pi.next(); ++pc) {
             const int b = (int)(pi.u / a.Hkv), hk = (int)(pi.u - (long long)b * a.Hkv);
@@ -283,24 +294,29 @@ __global__ void __launch_bounds__(kTcThreads, 2)
             float m_ref = -1.0e30f, l = 0.f;                 // p is taken relative to m_ref (log2 domain)
             for (int j = 0; j < pi.nt; ++j, ++t) {
                 const int sbuf = t & 1;
-                const int key_t = (pi.ti0 + j) * kTcKeys, key0 = key_t + hf * 32;
-                const bool mask = key_t + kTcKeys > ctx;     // the tile holds drafts or rows past the end
+                const int key0 = (pi.ti0 + j) * kTcKeys;
+                const bool mask = key0 + kTcKeys > ctx;      // the tile holds drafts or rows past the end
                 ok = wait(&s_full[sbuf], t >> 1);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t vis = 0xffffffffu;
+                const uint32_t sb = tmem_s + lane_addr + sbuf * kTcKeys;
+                float xs[64];
+                __syncwarp();                                // the warp's tensor-memory accesses are made together
+                tmem_ld64(sb, xs);
+                unsigned long long vis = ~0ull;
+                float mx = -INFINITY;
                 if (mask) {
                     const int off = key0 - ctx;
-                    if (off >= 0) vis = off < 64 ? (uint32_t)(sees >> off) : 0u;
-                    else if (off > -32) vis = (uint32_t)(sees << -off) | ((1u << -off) - 1u);
+                    if (off >= 0) vis = off < 64 ? sees >> off : 0ull;
+                    else if (off > -64) vis = sees << -off | ((1ull << -off) - 1ull);
                     // Clean the V tile (see the head of this file).  Only behind the wait above: S of this tile is
                     // done, so PV of the tile that had this V stage before is too, and v_full cannot be a phase
                     // behind the one waited for.
                     const int st = t % NS;
                     ok = wait(&v_full[st], t / NS);
                     if (!ok) break;
-                    for (int i = (hf * quarters + w4) * 32 + lane; i < kKv / 16; i += active) {
-                        const int key = key_t + (i * 16 % kTcKvBlock) / 128;
+                    for (int i = tid; i < kKv / 16; i += active) {
+                        const int key = key0 + (i * 16 % kTcKvBlock) / 128;
                         if (key < ctx) continue;
                         uint4* q4 = reinterpret_cast<uint4*>(sV + st * kKv + i * 16);
                         uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -314,32 +330,21 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                         *q4 = v;
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
-                const uint32_t sb = tmem_s + lane_addr + sbuf * kTcKeys;
-                float xs[32];
-                tmem_ld32(sb + hf * 32, xs);
-                // row maximum of the visible scores: own half, then the partner warp's through shared memory.  After
-                // the pair barrier both halves of S have been read, so P may overwrite it.
-                float mx = -INFINITY;
-                if (mask) {
+                    __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) mx = fmaxf(mx, (vis >> i) & 1u ? xs[i] : -INFINITY);
+                    for (int i = 0; i < 64; ++i) mx = fmaxf(mx, (vis >> i) & 1ull ? xs[i] : -INFINITY);
                 } else {
+                    float m4[4] = {xs[0], xs[1], xs[2], xs[3]};
 #pragma unroll
-                    for (int i = 0; i < 32; i += 2) mx = fmax3(mx, xs[i], xs[i + 1]);
+                    for (int i = 4; i < 60; i += 8)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) m4[c] = fmax3(m4[c], xs[i + c], xs[i + 4 + c]);
+                    mx = fmax3(fmax3(m4[0], m4[1], fmaxf(m4[2], m4[3])), fmaxf(xs[60], xs[61]), fmaxf(xs[62], xs[63]));
                 }
-                float* em = exch_m + sbuf * 2 * kTreeTileRows;
-                em[hf * kTreeTileRows + r] = mx;
-                tc_fence_before();
-                mbar_arrive(&pair_bar[w4]);
-                ok = wait(&pair_bar[w4], pp);
-                ++pp;
-                if (!ok) break;
-                tc_fence_after();
-                mx = fmaxf(mx, em[(hf ^ 1) * kTreeTileRows + r]) * a.scale_log2;
+                mx *= a.scale_log2;
                 // The reference maximum only moves when the new one is more than 8 (a factor 256) above it; then
                 // the output row and the sum so far are rescaled, once every PV issued so far has landed in O.
-                const bool grow = mx > m_ref + 8.0f;
+                const bool grow = real && mx > m_ref + 8.0f;
                 if (__any_sync(0xffffffffu, grow)) {
                     const float m_new = grow ? mx : m_ref;
                     const float alpha = fast_exp2(m_ref - m_new);
@@ -347,29 +352,19 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                         ok = wait(&o_full[(t - 1) & 1], (uint32_t)(t - 1) >> 1);
                         if (!ok) break;
                         tc_fence_after();
+                        __syncwarp();
 #pragma unroll 1
-                        for (int c = 0; c < S::OC / 8; ++c) tmem_scale8(to + c * 8, alpha);
+                        for (int c = 0; c < D; c += 32) tmem_scale32(to + c, alpha);
                     }
                     l *= alpha;
                     m_ref = m_new;
                 }
-                uint32_t w[8];
-                l += mask ? weights_chunk<true, 0>(xs, a.scale_log2, m_ref, vis, w) : weights_chunk<false, 0>(xs, a.scale_log2, m_ref, vis, w);
-                tmem_st8(sb + hf * 16, w);                   // key k of the tile -> column k / 2
-                l += mask ? weights_chunk<true, 16>(xs, a.scale_log2, m_ref, vis, w) : weights_chunk<false, 16>(xs, a.scale_log2, m_ref, vis, w);
-                tmem_st8(sb + hf * 16 + 8, w);
+                l += mask ? weights_tile<true>(xs, a.scale_log2, m_ref, vis, sb) : weights_tile<false>(xs, a.scale_log2, m_ref, vis, sb);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 mbar_arrive(&p_full[sbuf]);
             }
             if (!ok) break;
-            // the row's sum is the two halves' sums (both relative to the same reference maximum)
-            exch_l[hf * kTreeTileRows + r] = l;
-            mbar_arrive(&pair_bar[w4]);
-            ok = wait(&pair_bar[w4], pp);
-            ++pp;
-            if (!ok) break;
-            l += exch_l[(hf ^ 1) * kTreeTileRows + r];
             // the last tile's PV group is behind every other MMA of the piece on the pipe
             ok = wait(&o_full[(t - 1) & 1], (uint32_t)(t - 1) >> 1);
             if (!ok) break;
@@ -379,15 +374,16 @@ __global__ void __launch_bounds__(kTcThreads, 2)
             const long long orow = ((long long)b * a.n_t + tok) * a.Hq + hk * a.G + g;
             const long long prow = ((2ll * team + (pi.ti0 == 0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + r;
 #pragma unroll 1
-            for (int c = 0; c < S::OC; c += 32) {
+            for (int c = 0; c < D; c += 32) {
                 float o[32];
+                __syncwarp();
                 tmem_ld32(to + c, o);
                 if (patch) {
                     // a draft row this query sees holds Inf or NaN: its elements go into the sum as they are
                     for (int d = 0; d < a.n_t; ++d) {
                         const int key = ctx + d;
                         if (!(sees >> d & 1ull) || key < pi.ti0 * kTcKeys || key >= (pi.ti0 + pi.nt) * kTcKeys) continue;
-                        const __nv_bfloat16* vr = reinterpret_cast<const __nv_bfloat16*>(a.vplane) + (pi.u * a.row_stride + key) * D + hf * S::OC + c;
+                        const __nv_bfloat16* vr = reinterpret_cast<const __nv_bfloat16*>(a.vplane) + (pi.u * a.row_stride + key) * D + c;
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
                             const float v = __bfloat162float(vr[i]);
@@ -395,20 +391,19 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                         }
                     }
                 }
-                if (r >= rows) continue;
-                if (pi.whole) {
-                    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + orow * D + hf * S::OC + c);
+                if (real && pi.whole) {
+                    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + orow * D + c);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         dst[i] = make_uint4(pack2_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack2_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
                                             pack2_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack2_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
-                } else {
-                    float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + hf * S::OC + c);
+                } else if (real) {
+                    float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
             }
-            if (!pi.whole && hf == 0 && r < rows) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(m_ref, l);
+            if (!pi.whole && real) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(m_ref, l);
             tc_fence_before();      // the next piece's first PV waits for this thread's arrival on p_full
         }
     }
