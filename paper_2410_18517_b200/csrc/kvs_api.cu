@@ -862,6 +862,7 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
     a.scale_log2 = ctx->scale * 1.4426950408889634f;
     a.wait_ns = 1000ull * (unsigned long long)ctx->opt_wait_us;
     a.pool_map = ctx->tensor_map;
+    a.pool_map_tail = ctx->tensor_map_tail;
     const long long plane_rows = (long long)ctx->cfg.max_batch * ctx->cfg.n_kv_heads * ctx->row_stride;
     a.krow0 = plane_rows * (2 * slot);
     a.vrow0 = plane_rows * (2 * slot + 1);

@@ -143,8 +143,8 @@ cudaError_t launch_append_rotary(const RotaryArgs& r, cudaStream_t stream);
 
 // Attention of a tree of drafted tokens (see kvs_tree.cu).  The n_t queries of a sequence are the newest n_t rows
 // of its units; the G heads of a kv-head and the tokens form the rows of query tiles of `rows` rows.  A *team* of
-// m_tiles thread blocks walks a contiguous run of the line of key tiles (units * tiles per unit), block j of the
-// team with query tile j, so that the team reads every K/V tile at the same time.  A unit cut between teams
+// thread blocks that covers the m_tiles query tiles walks a contiguous run of the line of key tiles (units * tiles per
+// unit), each block with its own query tile (tensor cores: two), so that the team reads every K/V tile at the same time.  A unit cut between teams
 // leaves one piece per team: piece slot 2 * team + 1 if it begins the unit, 2 * team otherwise.
 struct TreePlan {
     int tokens;      // drafted tokens per query tile
@@ -171,7 +171,8 @@ struct TreeArgs {
     long long plane_bytes;
     float scale_log2;
     unsigned long long wait_ns;
-    const void* pool_map;              // tensor map of the pool (bf16), 64-row boxes
+    const void* pool_map;              // tensor maps of the pool (bf16): 64-row boxes, 16-row boxes
+    const void* pool_map_tail;
     long long krow0, vrow0;            // first row of the slot's planes in the pool-wide row numbering
 };
 constexpr int kTreeMaxTokens = 64;

@@ -318,7 +318,8 @@ cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* laun
     TreeKernelArgs ka;
     ka.a = a;
     TreePlan& p = ka.p;
-    int blocks = std::min(2 * sm_count, kTreeMaxBlocks);
+    // blocks per SM: two of the fp32 kernel, one of the tensor-core kernel (all of its shared and tensor memory)
+    int blocks = std::min(a.dtype == 0 ? sm_count : 2 * sm_count, kTreeMaxBlocks);
     if (max_ctas > 0) blocks = std::min(blocks, max_ctas);
     cudaError_t e;
     if (a.dtype == 0) {
