@@ -861,6 +861,7 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
     a.plane_bytes = (long long)ctx->plane_bytes;
     a.scale_log2 = ctx->scale * 1.4426950408889634f;
     a.wait_ns = 1000ull * (unsigned long long)ctx->opt_wait_us;
+    a.programmatic = take_early_start(ctx);
     a.pool_map = ctx->tensor_map;
     a.pool_map_tail = ctx->tensor_map_tail;
     const long long plane_rows = (long long)ctx->cfg.max_batch * ctx->cfg.n_kv_heads * ctx->row_stride;
@@ -869,11 +870,10 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
     int launches = 0;
     if (kvs::launch_tree(a, ctx->sm_count, ctx->opt_max_ctas, &launches, static_cast<cudaStream_t>(stream)) != cudaSuccess)
         return KVS_ERR_CUDA;
-    // a plain launch: it starts only after everything before it on the stream has finished
+    // like a split-K kernel, the attention kernel lets its successor start only after its own wait
+    ctx->last_splitk_seq = ctx->seq + 1;
     ctx->seq += launches;
-    ctx->last_splitk_seq = ctx->seq;
     ctx->stats.prefill_launches += 1;
-    ctx->counter_written = false;
     return KVS_OK;
 }
 

@@ -171,6 +171,7 @@ struct TreeArgs {
     long long plane_bytes;
     float scale_log2;
     unsigned long long wait_ns;
+    bool programmatic;                 // launch with programmatic stream serialization (early start, explicit wait)
     const void* pool_map;              // tensor maps of the pool (bf16): 64-row boxes, 16-row boxes
     const void* pool_map_tail;
     long long krow0, vrow0;            // first row of the slot's planes in the pool-wide row numbering

@@ -65,6 +65,8 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
     const int tok0 = mt * p.tokens, rows = min(p.tokens, a.n_t - tok0) * a.G;
     const unsigned long long all = a.n_t >= 64 ? ~0ull : (1ull << a.n_t) - 1;
     const long long t1 = first_tile(team + 1, p.T, p.teams);
+    pdl_wait();
+    pdl_launch_dependents();
 
     for (long long gt = first_tile(team, p.T, p.teams); gt < t1;) {
         const long long u = gt / p.tpu;
@@ -219,41 +221,66 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
 }
 
 // --------------------------------------------------------------------------------------
-// Combine: one warp per (unit, token, head) of a unit that was cut between teams: the pieces, in team order.
+// Combine: one warp per (unit, token, head) of a unit that was cut between teams; the pieces in team order.  Lane c
+// fetches the (max, sum) of piece c, so that all of them take one round trip to L2, and the output vectors follow eight at
+// a time: with one piece after the other (three dependent loads each) 17 pieces took 13 us, now 4.
 // --------------------------------------------------------------------------------------
-constexpr int kTreeCombineWarps = 8;
+constexpr int kTreeCombineWarps = 4;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const __grid_constant__ TreeKernelArgs ka) {
     constexpr int VEC = D / 32;
+    struct __align__(VEC * 4) Vec {
+        float v[VEC];
+    };
     const TreeArgs& a = ka.a;
     const TreePlan& p = ka.p;
-    pdl_wait();
     const long long item = (long long)blockIdx.x * kTreeCombineWarps + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31, per_unit = a.n_t * a.G;
-    if (item >= (long long)a.units * per_unit) return;
-    const long long u = item / per_unit;
-    const int q = (int)(item - u * per_unit), t = q / a.G, g = q - t * a.G;
+    const bool there = item < (long long)a.units * per_unit;
+    const int u = there ? (int)(item / per_unit) : 0;
+    const int q = there ? (int)(item - (long long)u * per_unit) : 0, t = q / a.G, g = q - t * a.G;
     const int mt = t / p.tokens, row = (t - mt * p.tokens) * a.G + g;
+    pdl_wait();
+    if (!there) return;
     const int n = a.unit_len ? min(a.unit_len[u], a.capacity) : a.n;
     const int nt = (n + p.key_rows - 1) / p.key_rows;
-    const int c0 = team_of_tile(u * p.tpu, p.T, p.teams), c1 = team_of_tile(u * p.tpu + nt - 1, p.T, p.teams);
-    if (c0 == c1) return;                                        // finished by its one team
-    float M = -1.0e30f, den = 0.f, acc[VEC];
+    const long long first = (long long)u * p.tpu;
+    const int c0 = team_of_tile(first, p.T, p.teams), np = team_of_tile(first + nt - 1, p.T, p.teams) - c0 + 1;
+    if (np == 1) return;                                         // finished by its one team
+    // piece c of the unit: slot 2 (c0 + c), the first one 2 c0 + 1
+    auto where = [&](int c) { return ((2ll * (c0 + c) + (c == 0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + row; };
+    float M = -1.0e30f;
+    for (int cb = 0; cb < np; cb += 32)
+        if (cb + lane < np) M = fmaxf(M, a.part_ml[where(cb + lane) * 2]);
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    float den = 0.f, acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-    for (int c = c0; c <= c1; ++c) {
-        const long long pr = ((2ll * c + (c == c0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + row;
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + pr * 2);
-        const float m_new = fmaxf(M, ml.x);
-        const float w0 = fast_exp2(M - m_new), w1 = fast_exp2(ml.x - m_new);
-        M = m_new;
-        den = fmaf(w1, ml.y, w0 * den);
+    for (int cb = 0; cb < np; cb += 32) {
+        const float2 ml = cb + lane < np ? *reinterpret_cast<const float2*>(a.part_ml + where(cb + lane) * 2) : make_float2(-1.0e30f, 0.f);
+        const float w = cb + lane < np ? fast_exp2(ml.x - M) : 0.f;
+        den = fmaf(w, ml.y, den);
+        const int cnt = min(32, np - cb);
+        for (int j = 0; j < cnt; j += 8) {
+            Vec x[8];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] = fmaf(w1, a.part_o[pr * D + lane * VEC + e], w0 * acc[e]);
+            for (int i = 0; i < 8; ++i)
+                if (j + i < cnt) x[i] = reinterpret_cast<const Vec*>(a.part_o + where(cb + j + i) * D)[lane];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float wi = __shfl_sync(0xffffffffu, w, j + i);
+                if (j + i < cnt)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[e] = fmaf(wi, x[i].v[e], acc[e]);
+            }
+        }
     }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
     const float inv = den > 0.f || den != den ? 1.0f / den : 0.f;
-    const int b = (int)(u / a.Hkv), hk = (int)(u - (long long)b * a.Hkv);
+    const int b = u / a.Hkv, hk = u - b * a.Hkv;
     T* dst = reinterpret_cast<T*>(a.out) + (((long long)b * a.n_t + t) * a.Hq + hk * a.G + g) * D + lane * VEC;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
@@ -318,8 +345,7 @@ cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* laun
     TreeKernelArgs ka;
     ka.a = a;
     TreePlan& p = ka.p;
-    // blocks per SM: two of the fp32 kernel, one of the tensor-core kernel (all of its shared and tensor memory)
-    int blocks = std::min(a.dtype == 0 ? sm_count : 2 * sm_count, kTreeMaxBlocks);
+    int blocks = std::min(2 * sm_count, kTreeMaxBlocks);     // two per SM of either kernel
     if (max_ctas > 0) blocks = std::min(blocks, max_ctas);
     cudaError_t e;
     if (a.dtype == 0) {
@@ -334,9 +360,10 @@ cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* laun
         p.T = (long long)a.units * p.tpu;
         p.teams = (int)std::min<long long>(p.T, std::max(1, blocks / p.m_tiles));
         const unsigned grid = (unsigned)(p.teams * p.m_tiles);
-        if (a.D == 128) tree_attention_fma<float, 128><<<grid, kTreeThreads, TreeShape<128>::SMEM_BYTES, stream>>>(ka);
-        else tree_attention_fma<float, 64><<<grid, kTreeThreads, TreeShape<64>::SMEM_BYTES, stream>>>(ka);
-        e = cudaGetLastError();
+        e = a.D == 128 ? launch_kernel(tree_attention_fma<float, 128>, dim3(grid), dim3(kTreeThreads), TreeShape<128>::SMEM_BYTES, stream,
+                                       a.programmatic, ka)
+                       : launch_kernel(tree_attention_fma<float, 64>, dim3(grid), dim3(kTreeThreads), TreeShape<64>::SMEM_BYTES, stream,
+                                       a.programmatic, ka);
     }
     // some unit is cut unless every team boundary falls on a unit boundary
     const bool cut = a.units % p.teams != 0;

@@ -1,17 +1,23 @@
 // Attention of a tree of drafted tokens on the 5th-generation tensor cores (bf16 storage, head size 64 or 128).
 // The mathematics and the masks are those of kvs_tree.cu.
 //
-// One thread block per SM with two softmax *slots*, each with its own scores and output in tensor memory:
-//   warps 0..3 / 4..7  softmax of slot 0 / 1: one thread per query row (= tensor-memory lane), the 128 keys of a key
-//                      tile; warps whose lanes hold no query row stay out of it
-//   warp 8 (one lane)  TMA producer: query tiles per piece, K and V tiles through one ring (K0 V0 K1 V1 ...)
-//   warp 9 (one lane)  MMA issuer: S(0) S(1), then PV(k) S(k+2) ..., step k belonging to slot k & 1, so that the
-//                      tensor pipe works for one slot while the other slot's softmax runs
-// Two query tiles (more than 128 rows per kv-head): the slots take one each and every K/V tile serves both, which
-// halves the shared-memory traffic of the copies.  One query tile: the slots take alternate key tiles and their two
-// results are merged at the end (a slot's threads can read the other's output: same tensor-memory lanes).
-// 128-key tiles, because an S product of N = 64 keys reads 6 KiB of shared memory per 32 tensor cycles, more than
-// the 128 bytes a cycle there are; N = 128 reads just that.
+// One thread block = one query tile (up to 128 rows: the G heads of as many drafts as fit) walking over key tiles
+// of 64; two blocks share an SM, so that one block's softmax runs beside the other's products.
+//   warps 0..3         softmax: one thread per query row (= tensor-memory lane), the 64 keys of a tile; warps whose
+//                      lanes hold no query row stay out of it
+//   warp 4 (one lane)  TMA producer: the query tile per piece; K and V tiles through one ring (K0 V0 K1 V1 ...)
+//   warp 5             MMA issuer: S = Q K^T into one of two score buffers (S of tile t+1 runs during the softmax of
+//                      tile t), O += P V with P as bf16 read from tensor memory.  The whole warp walks the tiles and an
+//                      elected lane issues: operands are then in uniform registers (issued from a one-lane branch the
+//                      sixteen MMAs of a 128-key tile took 1700 cycles instead of 1200)
+// Bound: up to 128 query rows per kv-head HBM (32 heads, B = 8, n = 4096, 16 drafts: 537 MB in 85 us, 6.3 TB/s); above
+// that shared memory: a 64-key tile costs 32 KiB of copies, 48 KiB of S operands (Q is read again for every tile) and
+// 16 KiB of V, 768 cycles at 128 bytes a cycle, 1536 for the two blocks of an SM, of the 2000 that a tile takes (32q/8kv,
+// B = 4, n = 32768, 64 drafts: 256 rows per kv-head, 137 us).
+// Measured against this layout there: one block per SM whose two softmax groups take a query tile each and share K/V tiles
+// of 128 keys (two thirds of that traffic), 156 us against 147, because a score buffer is free only after the product
+// that reads its weights and S then waits for softmax, PV and S in a row; a quarter of the exp2 by a polynomial on the
+// FMA pipe, 151; two stages per operand instead of the ring of five, 147.
 // P goes into the second contraction as one bf16 term (each weight off by at most 2^-8 of itself, the sum of the weights
 // kept in fp32 from the unrounded ones): the result is rounded to bf16 anyway, and a second term would add half again to the
 // tensor work of wide trees, which the tensor pipe bounds.
@@ -29,24 +35,23 @@ namespace kvs {
 
 namespace {
 
-constexpr int kTcSlotWarps = 4;
-constexpr int kTcThreads = (2 * kTcSlotWarps + 4) * 32;   // three warpgroups: two of softmax, one of producer and issuer
-// A softmax thread holds a tile's 128 scores, more than the 168 registers a thread of twelve warps is launched with allow
-// beside the rest: the third warpgroup hands its share over.  2 * 128 * 224 + 128 * 56 = 384 * 168 registers.
-constexpr int kTcSoftmaxRegs = 224, kTcOtherRegs = 56;
-constexpr int kTcKeys = 128;
+constexpr int kTcSoftmaxWarps = 4;
+constexpr int kTcThreads = (kTcSoftmaxWarps + 2) * 32;
+constexpr int kTcKeys = 64;
 constexpr int kTcQBlock = kTreeTileRows * 128;   // one swizzled block of Q: 128 rows x 64 bf16 columns
-constexpr int kTcKvBlock = kTcKeys * 128;        // one swizzled block of K or V: 128 rows x 64 bf16 columns
-constexpr int kTcBoxRows = 64, kTcTailRows = 16; // rows per copy: whole boxes, and the partly filled end of a unit
-constexpr uint32_t kTcTmemCols = 512;            // slot s: scores [256 s, 256 s + 128), output [256 s + 128, 256 s + 128 + D)
+constexpr int kTcKvBlock = kTcKeys * 128;        // one swizzled block of K or V: 64 rows x 64 bf16 columns
+constexpr int kTcTailRows = 16;                  // rows per copy at the partly filled end of a unit
+constexpr uint32_t kTcTmemCols = 256;            // two score buffers [0,64), [64,128); O: [128,128+D)
 
 template <int D>
 struct TcShape {
     static constexpr int HALVES = D / 64;
-    static constexpr int Q_BYTES = HALVES * kTcQBlock;           // one query tile
+    static constexpr int Q_BYTES = HALVES * kTcQBlock;
     static constexpr int KV_BYTES = HALVES * kTcKvBlock;
-    static constexpr int RING = 10 / HALVES;                     // K and V buffers: 160 KiB
-    static constexpr int SMEM_BYTES = 2 * Q_BYTES + RING * KV_BYTES + 512 + 4 * kTreeTileRows * 4;
+    // K and V buffers: as many as leave room for two blocks (and the 1 KiB the system keeps of each) on an SM's 228 KiB
+    static constexpr int RING = HALVES == 2 ? 5 : 12;
+    static constexpr int SMEM_BYTES = Q_BYTES + RING * KV_BYTES + 512;
+    static_assert(2 * (SMEM_BYTES + 1024) <= 228 * 1024, "two blocks per SM");
 };
 
 struct TreeTcArgs {
@@ -83,32 +88,6 @@ struct Pieces {
         }
         return false;
     }
-};
-
-// The steps of a block: step k is one key tile of one slot (k & 1).
-struct Steps {
-    Pieces pi;
-    bool two;          // two query tiles: two steps per key tile
-    int pc = -1;       // piece
-    int i = 0, n = 0;  // step within the piece, steps of the piece
-    int k = -1;        // step of the block
-    int t0 = 0;        // key tiles of earlier pieces
-    __device__ Steps(const TreeTcArgs& args, int team, bool two_) : pi(args, team), two(two_) {}
-    __device__ bool next() {
-        if (++i >= n) {
-            if (pc >= 0) t0 += pi.nt;
-            if (!pi.next()) return false;
-            ++pc;
-            i = 0;
-            n = two ? 2 * pi.nt : pi.nt;
-        }
-        ++k;
-        return true;
-    }
-    __device__ int tile() const { return two ? i >> 1 : i; }                 // key tile within the piece
-    __device__ bool first() const { return i < 2; }                          // the slot's first step of the piece
-    __device__ bool last_use() const { return !two || (i & 1); }             // of the key tile
-    __device__ bool last() const { return i == n - 1; }
 };
 
 // The weights p = 2^(x * scale - m_ref) of 32 scores, 0 where the key's bit in `vis` is not set (MASK), as they go to
@@ -164,12 +143,11 @@ __device__ __forceinline__ unsigned long long visible64(unsigned long long sees,
 }
 
 template <int D>
-__global__ void __launch_bounds__(kTcThreads, 1)
+__global__ void __launch_bounds__(kTcThreads, 2)
     tree_attention_tc(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_kv,
                       const __grid_constant__ CUtensorMap tmap_tail, const __grid_constant__ TreeTcArgs x) {
     using S = TcShape<D>;
     constexpr int NB = S::RING, kKv = S::KV_BYTES;
-    static_assert(2 * 128 * kTcSoftmaxRegs + 128 * kTcOtherRegs <= kTcThreads * 168, "registers at launch");
     const TreeArgs& a = x.a;
     const TreePlan& p = x.p;
     extern __shared__ __align__(1024) unsigned char sQ[];       // the 128-byte swizzle counts from 1024-byte boundaries
@@ -177,36 +155,35 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (threadIdx.x == 0) atomicExch(a.status, kDevBounds);
         return;
     }
-    unsigned char* ring = sQ + 2 * S::Q_BYTES;
+    unsigned char* ring = sQ + S::Q_BYTES;
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + NB * kKv);
-    uint64_t* q_full = bars;           // [2]
-    uint64_t* q_free = bars + 2;       // [2] every S of a piece is done
-    uint64_t* o_full = bars + 4;       // [2] per slot: the step's PV is in the slot's output
-    uint64_t* s_full = bars + 6;       // [2] per slot
-    uint64_t* p_full = bars + 8;       // [2] per slot: one arrival per active softmax thread
-    uint64_t* epi = bars + 10;         // all active softmax threads (one query tile only)
-    uint64_t* drain = bars + 11;
-    uint64_t* full = bars + 12;        // [NB]
+    uint64_t* q_full = bars;
+    uint64_t* q_free = bars + 1;       // every S of a piece is done
+    uint64_t* o_full = bars + 2;       // [2] by tile parity: the tile's PV is in O
+    uint64_t* s_full = bars + 4;       // [2] per score buffer
+    uint64_t* p_full = bars + 6;       // [2] one arrival per active softmax thread
+    uint64_t* drain = bars + 8;
+    uint64_t* full = bars + 9;         // [NB]
     uint64_t* empty = full + NB;       // [NB]
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(empty + NB);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 2);    // [2]; the second bounds the drains
     volatile int* broken = abort_flag + 2;                                        // [2] by piece parity
-    float2* exch = reinterpret_cast<float2*>(bars + 64);                          // [2 slots][128 rows] maximum, sum
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int pairs = (p.m_tiles + 1) / 2;
-    const int team = blockIdx.x / pairs, mt0 = 2 * (blockIdx.x - team * pairs);
-    const bool two = mt0 + 1 < p.m_tiles;
+    const int team = blockIdx.x / p.m_tiles, mt = blockIdx.x - team * p.m_tiles;
+    const int tok0 = mt * p.tokens, rows = min(p.tokens, a.n_t - tok0) * a.G;
     const int quarters = (p.tokens * a.G + 31) / 32;        // tensor-memory lane quarters that hold query rows
-    const uint32_t active = quarters * 32;                  // softmax threads at work per slot
+    const uint32_t active = quarters * 32;                  // softmax threads at work
 
     if (tid == 0) {
-        for (int i = 0; i < 12 + 2 * NB; ++i) mbar_init(&bars[i], 1);
+        for (int i = 0; i < 9 + 2 * NB; ++i) mbar_init(&bars[i], 1);
         mbar_init(&p_full[0], active);
         mbar_init(&p_full[1], active);
-        mbar_init(epi, 2 * active);
         abort_flag[0] = abort_flag[1] = broken[0] = broken[1] = 0;
         fence_mbar_init();
+        prefetch_map(&tmap_q);
+        prefetch_map(&tmap_kv);
+        prefetch_map(&tmap_tail);
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
@@ -218,29 +195,29 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    const uint32_t tmem_s = tmem_base, tmem_o = tmem_base + 128;
+    pdl_wait();                  // everything above runs beside the end of the previous kernel
+    pdl_launch_dependents();
 
-    // Key tile t of the block has K in ring entry 2 t and V in 2 t + 1; entry e lies in buffer e % NB, and its
-    // barriers are then in phase (e / NB) & 1.  A piece's queries: buffer and barrier qi, phase qp.
+    // Every role keeps its own count t of key tiles done in earlier pieces.  Tile t has K in ring entry 2 t and V in
+    // 2 t + 1 and uses score buffer t & 1; entry e lies in buffer e % NB, whose barriers are then in phase (e / NB) & 1.
     auto wait = [&](uint64_t* bar, uint32_t ph) { return mbar_wait_bounded(bar, ph & 1u, abort_flag, a.status, a.wait_ns); };
-    if (warp >= 2 * kTcSlotWarps) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcOtherRegs));
-    if (warp == 2 * kTcSlotWarps) {
+    if (warp == kTcSoftmaxWarps) {
         // ------------------------------ TMA producer ------------------------------
         if (lane == 0) {
             const uint32_t q_bytes = (uint32_t)(S::HALVES * p.tokens * a.G * 128);
-            int e = 0, pc = 0;               // ring entries issued, pieces
-            int q_done = 0;                  // pieces whose queries were issued
+            int e = 0, pc = 0, q_done = 0;   // ring entries, pieces, pieces whose queries were issued
             bool ok = true;
             for (Pieces pi(x, team); ok && pi.next(); ++pc) {
                 const int b = pi.u / a.Hkv, hk = pi.u - b * a.Hkv;
-                const int qi = two ? 0 : pc & 1, qn = two ? pc : pc >> 1;
                 for (int j = 0; j < pi.nt && ok; ++j) {
                     const int row0 = (pi.ti0 + j) * kTcKeys;
-                    const int rows = min(kTcKeys, pi.n - row0);
-                    const int boxes = rows / kTcBoxRows, tails = (rows - boxes * kTcBoxRows + kTcTailRows - 1) / kTcTailRows;
-                    const uint32_t bytes = (uint32_t)(boxes * kTcBoxRows + tails * kTcTailRows) * S::HALVES * 128;
+                    const int rows_t = min(kTcKeys, pi.n - row0);
+                    // a whole tile in one box per half, a partly filled one in 16-row boxes, only those that hold rows
+                    const int tails = rows_t < kTcKeys ? (rows_t + kTcTailRows - 1) / kTcTailRows : 0;
+                    const uint32_t bytes = (uint32_t)(tails ? tails * kTcTailRows : kTcKeys) * S::HALVES * 128;
                     long long row = (long long)pi.u * a.row_stride + row0;
-                    if (!KVS_BOUNDS_OK(row, boxes * kTcBoxRows + tails * kTcTailRows, x.plane_rows, a.status)) row = 0;
+                    if (!KVS_BOUNDS_OK(row, tails ? tails * kTcTailRows : kTcKeys, x.plane_rows, a.status)) row = 0;
                     for (int kv = 0; kv < 2; ++kv) {
                         const int st = e % NB;
                         if (e >= NB) ok = wait(&empty[st], e / NB - 1);
@@ -250,22 +227,17 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 #pragma unroll
                         for (int h = 0; h < S::HALVES; ++h) {
                             unsigned char* dst = ring + st * kKv + h * kTcKvBlock;
-                            for (int i = 0; i < boxes; ++i)
-                                tma_load_2d_pf(dst + i * kTcBoxRows * 128, &tmap_kv, h * 64, y + i * kTcBoxRows, &full[st]);
+                            if (!tails) tma_load_2d_pf(dst, &tmap_kv, h * 64, y, &full[st]);
                             for (int i = 0; i < tails; ++i)
-                                tma_load_2d_pf(dst + (boxes * kTcBoxRows + i * kTcTailRows) * 128, &tmap_tail, h * 64,
-                                               y + boxes * kTcBoxRows + i * kTcTailRows, &full[st]);
+                                tma_load_2d_pf(dst + i * kTcTailRows * 128, &tmap_tail, h * 64, y + i * kTcTailRows, &full[st]);
                         }
                         ++e;
                         if (kv == 0 && j == 0) {      // the queries, behind the piece's first K tile
-                            if (qn >= 1) ok = wait(&q_free[qi], qn - 1);
+                            if (pc >= 1) ok = wait(q_free, pc - 1);
                             if (!ok) break;
-                            mbar_arrive_expect_tx(&q_full[qi], two ? 2 * q_bytes : q_bytes);
-                            for (int m = 0; m < (two ? 2 : 1); ++m)
+                            mbar_arrive_expect_tx(q_full, q_bytes);
 #pragma unroll
-                                for (int h = 0; h < S::HALVES; ++h)
-                                    tma_load_4d(sQ + (two ? m : qi) * S::Q_BYTES + h * kTcQBlock, &tmap_q, h * 64, hk * a.G,
-                                                (mt0 + m) * p.tokens, b, &q_full[qi]);
+                            for (int h = 0; h < S::HALVES; ++h) tma_load_4d(sQ + h * kTcQBlock, &tmap_q, h * 64, hk * a.G, tok0, b, q_full);
                             ++q_done;
                         }
                     }
@@ -276,126 +248,118 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                 // block's shared memory when it exits.
                 for (int j = max(0, e - NB); j < e; ++j)
                     mbar_wait_bounded(&full[j % NB], (uint32_t)(j / NB) & 1u, abort_flag + 1, a.status, a.wait_ns);
-                for (int j = max(0, q_done - 2); j < q_done; ++j) {
-                    const int qi = two ? 0 : j & 1, qn = two ? j : j >> 1;
-                    if (!two || j == q_done - 1)
-                        mbar_wait_bounded(&q_full[qi], (uint32_t)qn & 1u, abort_flag + 1, a.status, a.wait_ns);
-                }
+                if (q_done > 0) mbar_wait_bounded(q_full, (uint32_t)(q_done - 1) & 1u, abort_flag + 1, a.status, a.wait_ns);
             }
         }
-    } else if (warp == 2 * kTcSlotWarps + 1) {
+    } else if (warp == kTcSoftmaxWarps + 1) {
         // ------------------------------ MMA issuer ------------------------------
-        // The pipe runs one thread's MMAs in issue order: S(k+2) overwrites its slot's scores only after PV(k) has
-        // read the weights that lie over them.  The whole warp walks the steps, one elected lane issues.
+        // Order on the tensor pipe: S_0, then per tile t: S_{t+1}, PV_t.  The pipe runs one thread's MMAs in issue
+        // order, so S_{t+1} overwrites its buffer only after PV_{t-1} has read P_{t-1} from it.
         const uint32_t idesc_s = instr_desc_bf16(0, kTcKeys);
         const uint32_t idesc_o = instr_desc_bf16(1, D);
         const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_base, 0);
         const bool leader = elect_one();
-        auto all_wait = [&](uint64_t* bar, uint32_t ph) { return __all_sync(0xffffffffu, wait(bar, ph)) != 0; };   // one answer for the warp
         // descriptors of the buffers' starts; steps inside a buffer are added in units of 16 bytes
         const uint64_t q_desc = smem_desc_sw128(smem_u32(sQ), 16, 1024);
         const uint64_t k_desc = smem_desc_sw128(smem_u32(ring), 16, 1024);
         // V is MN-major: 64 head-dim columns contiguous per key row, the other 64 (D = 128) one column block (LBO)
         // away; 8-key groups 1024 bytes (SBO) apart
         const uint64_t v_desc = smem_desc_sw128(smem_u32(ring), kTcKvBlock, 1024);
-        auto issue_s = [&](const Steps& s) {
-            const int qi = two ? 0 : s.pc & 1, qn = two ? s.pc : s.pc >> 1;
-            const int e = 2 * (s.t0 + s.tile()), st = e % NB;
-            if (s.i == 0 && !all_wait(&q_full[qi], qn)) return false;
-            if (!all_wait(&full[st], e / NB)) return false;
-            tc_fence_after();
-            const uint64_t q = q_desc + (uint32_t)(two ? s.k & 1 : qi) * (S::Q_BYTES / 16);
+        auto all_wait = [&](uint64_t* bar, uint32_t ph) { return __all_sync(0xffffffffu, wait(bar, ph)) != 0; };   // one answer for the warp
+        auto issue_s = [&](int t, bool last) {
+            const int st = 2 * t % NB;
             const uint64_t k = k_desc + (uint32_t)st * (kKv / 16);
-            const uint32_t d = tmem + (s.k & 1) * 256;
+            const uint32_t d = tmem + (t & 1) * kTcKeys;
             if (leader) {
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
-                    umma_bf16(d, q + ((ks >> 2) * kTcQBlock + (ks & 3) * 32) / 16, k + ((ks >> 2) * kTcKvBlock + (ks & 3) * 32) / 16,
+                    umma_bf16(d, q_desc + ((ks >> 2) * kTcQBlock + (ks & 3) * 32) / 16, k + ((ks >> 2) * kTcKvBlock + (ks & 3) * 32) / 16,
                               idesc_s, ks > 0);
-                umma_commit(&s_full[s.k & 1]);
-                if (s.last_use()) umma_commit(&empty[st]);
-                if (s.last()) umma_commit(&q_free[qi]);
+                umma_commit(&s_full[t & 1]);
+                umma_commit(&empty[st]);
+                if (last) umma_commit(q_free);
             }
             __syncwarp();
-            return true;
         };
-        Steps sa(x, team, two), sp(x, team, two);     // next S, next PV
-        bool more = sa.next(), ok = true;
-        for (int i = 0; i < 2 && ok && more; ++i) {
-            ok = issue_s(sa);
-            more = sa.next();
-        }
-        while (ok && sp.next()) {
-            const int e = 2 * (sp.t0 + sp.tile()) + 1, st = e % NB, slot = sp.k & 1;
-            ok = all_wait(&p_full[slot], sp.k >> 1) && all_wait(&full[st], e / NB);
+        int t = 0, pc = 0;
+        bool ok = true;
+        for (Pieces pi(x, team); ok && pi.next(); ++pc) {
+            ok = all_wait(q_full, pc) && all_wait(&full[2 * t % NB], 2 * t / NB);
             if (!ok) break;
             tc_fence_after();
-            const uint64_t v = v_desc + (uint32_t)st * (kKv / 16);
-            const uint32_t o = tmem + slot * 256 + 128, w = tmem + slot * 256, add = !sp.first();
-            if (leader) {
+            issue_s(t, pi.nt == 1);
+            for (int j = 0; j < pi.nt; ++j, ++t) {
+                if (j + 1 < pi.nt) {
+                    ok = all_wait(&full[(2 * t + 2) % NB], (2 * t + 2) / NB);
+                    if (!ok) break;
+                    tc_fence_after();
+                    issue_s(t + 1, j + 2 == pi.nt);
+                }
+                const int st = (2 * t + 1) % NB;
+                ok = all_wait(&full[st], (2 * t + 1) / NB) && all_wait(&p_full[t & 1], t >> 1);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t v = v_desc + (uint32_t)st * (kKv / 16);
+                const uint32_t o = tmem + 128, w = tmem + (t & 1) * kTcKeys;
+                if (leader) {
 #pragma unroll
-                for (int ks = 0; ks < kTcKeys / 16; ++ks) umma_bf16_ts(o, w + ks * 8, v + ks * 16 * 128 / 16, idesc_o, ks > 0 ? 1 : add);
-                umma_commit(&o_full[slot]);
-                if (sp.last_use()) umma_commit(&empty[st]);
-            }
-            __syncwarp();
-            if (more) {
-                ok = issue_s(sa);
-                more = sa.next();
+                    for (int ks = 0; ks < kTcKeys / 16; ++ks) umma_bf16_ts(o, w + ks * 8, v + ks * 16 * 128 / 16, idesc_o, ks > 0 ? 1 : j > 0);
+                    umma_commit(&o_full[t & 1]);
+                    umma_commit(&empty[st]);
+                }
+                __syncwarp();
             }
         }
         if (!ok && leader) {     // the MMAs already issued must be done before the block gives its memory back
             umma_commit(drain);
             mbar_wait_bounded(drain, 0, abort_flag + 1, a.status, a.wait_ns);
         }
-    }
-    } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcSoftmaxRegs));
-    if ((warp & 3) < quarters) {
+    } else if (warp < quarters) {
         // ------------------------------ softmax / output rows ------------------------------
-        const int slot = warp >> 2;
-        const int r = tid & 127;                             // query row in the tile = tensor-memory lane
-        const int mt = mt0 + (two ? slot : 0), tok0 = mt * p.tokens;
-        const int rows = min(p.tokens, a.n_t - tok0) * a.G;
-        const uint32_t lanes = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t ts = lanes + slot * 256, to = ts + 128;
+        const int r = tid;                                   // query row in the tile = tensor-memory lane
+        const uint32_t lane_addr = (uint32_t)(warp * 32) << 16;
+        const uint32_t to = tmem_o + lane_addr;
         const bool real = r < rows;                          // lanes past the last row hold no query: their scores are junk
         const int tok = tok0 + min(r, rows - 1) / a.G, g = min(r, rows - 1) % a.G;
         const unsigned long long all = a.n_t >= 64 ? ~0ull : (1ull << a.n_t) - 1;
-        int k0 = 0, t0 = 0, pc = 0;                          // steps, key tiles, pieces before this one
-        uint32_t ep = 0;                                     // phases used of epi
+        int t = 0, pc = 0;
         bool ok = true;
         for (Pieces pi(x, team); ok && pi.next(); ++pc) {
             const int b = pi.u / a.Hkv, hk = pi.u - b * a.Hkv;
             const int ctx = pi.n - a.n_t;                    // rows every query sees
             const unsigned long long sees =
                 a.mask ? a.mask[(long long)b * a.n_t + tok] & all : (tok >= 63 ? ~0ull : (2ull << tok) - 1);
-            const int steps = two ? 2 * pi.nt : pi.nt;
             float m_ref = -1.0e30f, l = 0.f;                 // p is taken relative to m_ref (log2 domain)
-            const int i0 = (k0 ^ slot) & 1;                  // the slot's first step of the piece
-            for (int i = i0; i < steps; i += 2) {
-                const int c = (k0 + i) >> 1;                 // the slot's count of steps
-                const int tile = two ? i >> 1 : i;
-                const int key0 = (pi.ti0 + tile) * kTcKeys;
+            for (int j = 0; j < pi.nt; ++j, ++t) {
+                const int sbuf = t & 1;
+                const int key0 = (pi.ti0 + j) * kTcKeys;
                 const bool mask = key0 + kTcKeys > ctx;      // the tile holds drafts or rows past the end
-                ok = wait(&s_full[slot], c);
+                ok = wait(&s_full[sbuf], t >> 1);
                 if (!ok) break;
                 tc_fence_after();
-                unsigned long long vx = ~0ull, vy = ~0ull;
+                const uint32_t sb = tmem_s + lane_addr + sbuf * kTcKeys;
+                // Both halves of the scores are asked for at once: beside running MMAs, which read and write tensor
+                // memory through the same ports, a load takes 250 to 400 cycles.
+                float x0[32], x1[32];
+                __syncwarp();                                // the warp's tensor-memory accesses are made together
+                tmem_ld32_issue(sb, x0);
+                tmem_ld32_issue(sb + 32, x1);
+                tmem_ld_wait(x0);
+                tmem_ld_wait(x1);
+                unsigned long long vis = ~0ull;
+                float mx;
                 if (mask) {
-                    vx = visible64(sees, key0 - ctx);
-                    vy = visible64(sees, key0 + 64 - ctx);
+                    vis = visible64(sees, key0 - ctx);
                     // Clean the V tile (see the head of this file).  Only behind the wait above: S of this tile is
-                    // done, so the ring entry that had this V buffer before was released and filled again in
-                    // order, and its barrier cannot be a phase behind the one waited for.  (With two query tiles
-                    // both slots clean the same tile: they write the same values.)
-                    const int e = 2 * (t0 + tile) + 1, st = e % NB;
-                    ok = wait(&full[st], e / NB);
+                    // done, so whatever had this buffer before has been used, and its barrier cannot be a phase
+                    // behind the one waited for.
+                    const int st = (2 * t + 1) % NB;
+                    ok = wait(&full[st], (2 * t + 1) / NB);
                     if (!ok) break;
-                    for (int v16 = r; v16 < kKv / 16; v16 += active) {
-                        const int key = key0 + (v16 * 16 % kTcKvBlock) / 128;
+                    for (int i = tid; i < kKv / 16; i += active) {
+                        const int key = key0 + (i * 16 % kTcKvBlock) / 128;
                         if (key < ctx) continue;
-                        uint4* q4 = reinterpret_cast<uint4*>(ring + st * kKv + v16 * 16);
+                        uint4* q4 = reinterpret_cast<uint4*>(ring + st * kKv + i * 16);
                         uint4 v = make_uint4(0u, 0u, 0u, 0u);
                         if (key < pi.n) {
                             v = *q4;
@@ -407,135 +371,82 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                         *q4 = v;
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    mx = fmaxf(max32<true>(x0, (uint32_t)vis), max32<true>(x1, (uint32_t)(vis >> 32)));
+                } else {
+                    mx = fmaxf(max32<false>(x0, 0u), max32<false>(x1, 0u));
                 }
-                // All of the scores are asked for at once: beside running MMAs, which read and write tensor memory
-                // through the same ports, a load takes 250 to 400 cycles.
-                float x0[32], x1[32], x2[32], x3[32];
-                __syncwarp();                                // the warp's tensor-memory accesses are made together
-                tmem_ld32_issue(ts, x0);
-                tmem_ld32_issue(ts + 32, x1);
-                tmem_ld32_issue(ts + 64, x2);
-                tmem_ld32_issue(ts + 96, x3);
-                tmem_ld_wait(x0);
-                tmem_ld_wait(x1);
-                tmem_ld_wait(x2);
-                tmem_ld_wait(x3);
-                float mx;
-                if (mask)
-                    mx = fmaxf(fmaxf(max32<true>(x0, (uint32_t)vx), max32<true>(x1, (uint32_t)(vx >> 32))),
-                               fmaxf(max32<true>(x2, (uint32_t)vy), max32<true>(x3, (uint32_t)(vy >> 32))));
-                else
-                    mx = fmaxf(fmaxf(max32<false>(x0, 0u), max32<false>(x1, 0u)), fmaxf(max32<false>(x2, 0u), max32<false>(x3, 0u)));
                 mx *= a.scale_log2;
                 // The reference maximum only moves when the new one is more than 8 (a factor 256) above it; then
-                // the output row and the sum so far are rescaled.  (S of this step is done, so PV of the slot's
-                // step before it is too: nothing is being added to the output.)
+                // the output row and the sum so far are rescaled, once every PV issued so far has landed in O.
                 const bool grow = real && mx > m_ref + 8.0f;
                 if (__any_sync(0xffffffffu, grow)) {
                     const float m_new = grow ? mx : m_ref;
                     const float alpha = fast_exp2(m_ref - m_new);
-                    if (i > i0) {
+                    if (j > 0) {
+                        ok = wait(&o_full[(t - 1) & 1], (uint32_t)(t - 1) >> 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        __syncwarp();
 #pragma unroll 1
-                        for (int cc = 0; cc < D; cc += 8) tmem_scale8(to + cc, alpha);
+                        for (int c = 0; c < D; c += 32) tmem_scale32(to + c, alpha);
                     }
                     l *= alpha;
                     m_ref = m_new;
                 }
                 if (mask) {
-                    l += weights32<true>(x0, a.scale_log2, m_ref, (uint32_t)vx, ts);
-                    l += weights32<true>(x1, a.scale_log2, m_ref, (uint32_t)(vx >> 32), ts + 16);
-                    l += weights32<true>(x2, a.scale_log2, m_ref, (uint32_t)vy, ts + 32);
-                    l += weights32<true>(x3, a.scale_log2, m_ref, (uint32_t)(vy >> 32), ts + 48);
+                    l += weights32<true>(x0, a.scale_log2, m_ref, (uint32_t)vis, sb);
+                    l += weights32<true>(x1, a.scale_log2, m_ref, (uint32_t)(vis >> 32), sb + 16);
                 } else {
-                    l += weights32<false>(x0, a.scale_log2, m_ref, 0u, ts);
-                    l += weights32<false>(x1, a.scale_log2, m_ref, 0u, ts + 16);
-                    l += weights32<false>(x2, a.scale_log2, m_ref, 0u, ts + 32);
-                    l += weights32<false>(x3, a.scale_log2, m_ref, 0u, ts + 48);
+                    l += weights32<false>(x0, a.scale_log2, m_ref, 0u, sb);
+                    l += weights32<false>(x1, a.scale_log2, m_ref, 0u, sb + 16);
                 }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
-                mbar_arrive(&p_full[slot]);
+                mbar_arrive(&p_full[sbuf]);
             }
             if (!ok) break;
-            const bool has = i0 < steps;
-            if (has) {
-                const int last = i0 + (steps - 1 - i0) / 2 * 2;
-                ok = wait(&o_full[slot], (uint32_t)(k0 + last) >> 1);
-                if (!ok) break;
-                tc_fence_after();
-            }
-            float w0 = 1.f, w1 = 0.f;          // weights of the own and the other slot's output
-            bool other = false;
-            if (!two) {
-                exch[slot * kTreeTileRows + r] = make_float2(m_ref, l);
-                tc_fence_before();
-                mbar_arrive(epi);
-                ok = wait(epi, ep);
-                ++ep;
-                if (!ok) break;
-                tc_fence_after();
-                const float2 ml = exch[(slot ^ 1) * kTreeTileRows + r];
-                const float m_new = fmaxf(m_ref, ml.x);
-                w0 = fast_exp2(m_ref - m_new);
-                w1 = fast_exp2(ml.x - m_new);
-                other = steps >= 2 || !has;
-                l = has ? (other ? fmaf(w0, l, w1 * ml.y) : l) : ml.y;
-                m_ref = m_new;
-            }
+            // the last tile's PV group is behind every other MMA of the piece on the pipe
+            ok = wait(&o_full[(t - 1) & 1], (uint32_t)(t - 1) >> 1);
+            if (!ok) break;
+            tc_fence_after();
             const bool patch = broken[pc & 1] == pc + 1;
             const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;        // nothing visible: 0
             const long long orow = ((long long)b * a.n_t + tok) * a.Hq + hk * a.G + g;
             const long long prow = ((2ll * team + (pi.ti0 == 0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + r;
-            // one query tile: each slot's threads write half of the columns
-            const int c0 = two ? 0 : slot * (D / 2), c1 = two ? D : c0 + D / 2;
 #pragma unroll 1
-            for (int cc = c0; cc < c1; cc += 32) {
+            for (int c = 0; c < D; c += 32) {
                 float o[32];
                 __syncwarp();
-                if (has) tmem_ld32(to + cc, o);
-                if (other) {
-                    float o2[32];
-                    tmem_ld32(lanes + (slot ^ 1) * 256 + 128 + cc, o2);
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) o[j] = has ? fmaf(w1, o2[j], w0 * o[j]) : o2[j];
-                }
+                tmem_ld32(to + c, o);
                 if (patch) {
                     // a draft row this query sees holds Inf or NaN: its elements go into the sum as they are
                     for (int d = 0; d < a.n_t; ++d) {
                         const int key = ctx + d;
                         if (!(sees >> d & 1ull) || key < pi.ti0 * kTcKeys || key >= (pi.ti0 + pi.nt) * kTcKeys) continue;
-                        const __nv_bfloat16* vr = reinterpret_cast<const __nv_bfloat16*>(a.vplane) + ((long long)pi.u * a.row_stride + key) * D + cc;
+                        const __nv_bfloat16* vr = reinterpret_cast<const __nv_bfloat16*>(a.vplane) + ((long long)pi.u * a.row_stride + key) * D + c;
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const float v = __bfloat162float(vr[j]);
-                            if (!isfinite(v)) o[j] += v;
+                        for (int i = 0; i < 32; ++i) {
+                            const float v = __bfloat162float(vr[i]);
+                            if (!isfinite(v)) o[i] += v;
                         }
                     }
                 }
                 if (real && pi.whole) {
-                    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + orow * D + cc);
+                    uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + orow * D + c);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        dst[j] = make_uint4(pack2_bf16(o[8 * j] * inv, o[8 * j + 1] * inv), pack2_bf16(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
-                                            pack2_bf16(o[8 * j + 4] * inv, o[8 * j + 5] * inv), pack2_bf16(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
+                    for (int i = 0; i < 4; ++i)
+                        dst[i] = make_uint4(pack2_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack2_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
+                                            pack2_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack2_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
                 } else if (real) {
-                    float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + cc);
+                    float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) dst[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                    for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
             }
-            if (!pi.whole && real && (two || slot == 0)) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(m_ref, l);
-            tc_fence_before();      // the slot's first PV of the next piece waits for this thread's arrival on p_full
-            if (!two) {             // ... and, as both slots' threads read both outputs, for the other slot's too
-                mbar_arrive(epi);
-                ok = wait(epi, ep);
-                ++ep;
-                tc_fence_after();
-            }
-            k0 += steps;
-            t0 += pi.nt;
+            if (!pi.whole && real) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(m_ref, l);
+            tc_fence_before();      // the next piece's first PV waits for this thread's arrival on p_full
         }
-    }
     }
     // every thread of every role ends here; tensor memory is released by the warp that took it
     tc_fence_before();
@@ -563,7 +474,7 @@ void plan_tree_tc(const TreeArgs& a, int blocks, TreePlan* p) {
     p->key_rows = kTcKeys;
     p->tpu = (a.n + kTcKeys - 1) / kTcKeys;
     p->T = (long long)a.units * p->tpu;
-    p->teams = (int)std::min<long long>(p->T, std::max(1, blocks / ((p->m_tiles + 1) / 2)));
+    p->teams = (int)std::min<long long>(p->T, std::max(1, blocks / p->m_tiles));
 }
 
 cudaError_t launch_tree_tc(const TreeArgs& a, const TreePlan& plan, cudaStream_t stream) {
@@ -588,10 +499,9 @@ cudaError_t launch_tree_tc(const TreeArgs& a, const TreePlan& plan, cudaStream_t
     x.vrow0 = a.vrow0;
     const CUtensorMap& tkv = *reinterpret_cast<const CUtensorMap*>(a.pool_map);
     const CUtensorMap& tail = *reinterpret_cast<const CUtensorMap*>(a.pool_map_tail);
-    const unsigned blocks = (unsigned)(plan.teams * ((plan.m_tiles + 1) / 2));
-    if (a.D == 128) tree_attention_tc<128><<<blocks, kTcThreads, TcShape<128>::SMEM_BYTES, stream>>>(tq, tkv, tail, x);
-    else tree_attention_tc<64><<<blocks, kTcThreads, TcShape<64>::SMEM_BYTES, stream>>>(tq, tkv, tail, x);
-    return cudaGetLastError();
+    const dim3 blocks((unsigned)(plan.teams * plan.m_tiles)), threads(kTcThreads);
+    return a.D == 128 ? launch_kernel(tree_attention_tc<128>, blocks, threads, TcShape<128>::SMEM_BYTES, stream, a.programmatic, tq, tkv, tail, x)
+                      : launch_kernel(tree_attention_tc<64>, blocks, threads, TcShape<64>::SMEM_BYTES, stream, a.programmatic, tq, tkv, tail, x);
 }
 
 }  // namespace kvs

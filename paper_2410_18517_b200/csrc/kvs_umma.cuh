@@ -23,6 +23,11 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* tmap, 
         : "memory");
 }
 
+// Fetch a tensor map ahead of its first use.
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tmap) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
+}
+
 // Shared-memory matrix descriptor, 128-byte swizzle: start address, leading and stride byte
 // offsets in 16-byte units, descriptor version 1, layout type 2 (128-byte swizzle).
 __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
