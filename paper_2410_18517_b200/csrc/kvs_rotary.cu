@@ -10,9 +10,11 @@
 // formed in fp64, reduced to half a turn there, and only the remainder goes to fp32 (one fp64 product per
 // (token, pair), shared by all heads of the token).
 //
-// Bound: HBM for prompts (each byte read and written once), launch latency for decode steps.  One block per
-// token (several where a token has many heads): a head row is read by row_bytes / 16 lanes, 16 bytes each; the block
-// issues its loads before it works out the cos / sin table, so that the table's latency hides behind them.
+// Bound: HBM for prompts (each byte read and written once), launch latency for decode steps.  A head row is read by
+// D / 8 lanes of eight elements each: four neighbours and the four they are rotated with, so that no value has to cross
+// lanes but the norm's sum (a layout of 16 contiguous bytes per lane needs eight shuffles a row for that).  A block
+// takes several tokens of a long prompt: its threads work out one (token, pair) angle each while the first rows are on
+// their way, and every block needs the table's latency only once.
 #include <algorithm>
 
 #include "kvs_device.cuh"
@@ -23,7 +25,8 @@ namespace kvs {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotVecs = 4;      // 16-byte vectors a thread has in flight
+constexpr int kRotRows = 4;      // head rows a group of lanes has in flight
+constexpr int kRotTokens = 4;    // tokens per block of a long prompt
 
 struct RotaryKernelArgs {
     const char* q;
@@ -38,6 +41,7 @@ struct RotaryKernelArgs {
     char* vplane;
     int Hq, Hkv;                                // Hkv = 0: queries only (a layer that shares its cache)
     int n_new;
+    int tokens;                                 // batch * n_new
     int row_stride;
     int len0;
     const int* unit_len;
@@ -50,137 +54,185 @@ struct RotaryKernelArgs {
     double turns[64];                           // inv_freq[i] / 2 pi
 };
 
+// Four elements of storage: 8 (bf16) or 16 (fp32) bytes.
 template <typename T>
-__device__ __forceinline__ uint4 pack_row(const float (&f)[16 / sizeof(T)]) {
-    uint4 r;
-    if constexpr (sizeof(T) == 2) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
-            w[i] = *reinterpret_cast<const uint32_t*>(&p);
-        }
-        r = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-        r = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+struct Quad;
+template <>
+struct Quad<__nv_bfloat16> {
+    uint2 v;
+    __device__ __forceinline__ void unpack(float* f) const {
+        f[0] = __uint_as_float(v.x << 16);
+        f[1] = __uint_as_float(v.x & 0xffff0000u);
+        f[2] = __uint_as_float(v.y << 16);
+        f[3] = __uint_as_float(v.y & 0xffff0000u);
     }
-    return r;
-}
+    __device__ __forceinline__ void pack(const float* f) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(f[0], f[1]), hi = __floats2bfloat162_rn(f[2], f[3]);
+        v = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    }
+};
+template <>
+struct Quad<float> {
+    float4 v;
+    __device__ __forceinline__ void unpack(float* f) const {
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    }
+    __device__ __forceinline__ void pack(const float* f) { v = make_float4(f[0], f[1], f[2], f[3]); }
+};
 
-// INTERLEAVED: pairs are neighbours (2i, 2i+1); else pair i is (i, i + half), half a multiple of a lane's elements.
-template <typename T, int D, bool INTERLEAVED>
-__global__ void __launch_bounds__(kRotThreads) append_rotary_kernel(const __grid_constant__ RotaryKernelArgs a) {
-    constexpr int EPL = 16 / (int)sizeof(T);
-    constexpr int LPR = D / EPL;
+// INTERLEAVED: pairs are neighbours (2i, 2i+1); else pair i is (i, i + half).  TOKENS: tokens per block.
+template <typename T, int D, bool INTERLEAVED, int TOKENS>
+__global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __grid_constant__ RotaryKernelArgs a) {
+    constexpr int LPR = D / 8;                    // lanes per head row, two quads each
     constexpr int ROWS = kRotThreads / LPR;       // head rows the block works on at once
     constexpr int RB = D * (int)sizeof(T);
-    __shared__ float2 cs[D / 2];
+    constexpr int QB = 4 * (int)sizeof(T);        // bytes of a quad
+    __shared__ float2 cs[TOKENS][D / 2];
     pdl_launch_dependents();
-    pdl_wait();
-    const int extra = a.n_extra ? *a.n_extra : 0;    // replayed launch: the slot has grown since it was recorded
-    const long long tok = blockIdx.x;
-    const int b = (int)(tok / a.n_new), t = (int)(tok - (long long)b * a.n_new);
     const int heads = a.Hq + 2 * a.Hkv;
     const int lig = threadIdx.x % LPR, slot = threadIdx.x / LPR;
-    // this block's share of the token's head rows (blockIdx.y of gridDim.y)
-    const int r0 = (int)((long long)heads * blockIdx.y / gridDim.y), r1 = (int)((long long)heads * (blockIdx.y + 1) / gridDim.y);
-    bool table = false;
-    for (int rb = r0; rb < r1; rb += ROWS * kRotVecs) {
-        uint4 raw[kRotVecs];
+    // This lane's two quads of a row: its pairs' first and second elements; the quads that are not rotated are dealt
+    // out to the lanes left over.  Interleaved pairs lie inside a quad.
+    const int hq = a.half / 4;                    // quads of first elements
+    int c0, c1;
+    bool turn0, turn1;
+    if (INTERLEAVED) {
+        c0 = lig;
+        c1 = lig + LPR;
+        turn0 = c0 < 2 * hq;
+        turn1 = c1 < 2 * hq;
+    } else {
+        turn0 = turn1 = lig < hq;
+        c0 = turn0 ? lig : hq + lig;                              // 2 hq + (lig - hq)
+        c1 = turn0 ? lig + hq : hq + lig + (LPR - hq);            // as many quads further on as are left over
+    }
+    const int passes = (heads + ROWS - 1) / ROWS;
+    const int tok0 = blockIdx.x * TOKENS, ntok = min(TOKENS, a.tokens - tok0);
+    const int items = ntok * passes;
+    pdl_wait();
+    const int extra = a.n_extra ? *a.n_extra : 0;    // replayed launch: the slot has grown since it was recorded
+    Quad<T> wq0 = {}, wq1 = {}, wk0 = {}, wk1 = {};
+    if (a.q_weight != nullptr) {
+        wq0 = *reinterpret_cast<const Quad<T>*>(a.q_weight + c0 * QB);
+        wq1 = *reinterpret_cast<const Quad<T>*>(a.q_weight + c1 * QB);
+    }
+    if (a.k_weight != nullptr) {
+        wk0 = *reinterpret_cast<const Quad<T>*>(a.k_weight + c0 * QB);
+        wk1 = *reinterpret_cast<const Quad<T>*>(a.k_weight + c1 * QB);
+    }
+    for (int it = 0; it < items; it += kRotRows) {
+        Quad<T> raw[kRotRows][2];
 #pragma unroll
-        for (int i = 0; i < kRotVecs; ++i) {
-            const int r = rb + i * ROWS + slot;
-            raw[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < r1) {
+        for (int i = 0; i < kRotRows; ++i) {
+            const int tk = (it + i) / passes, r = (it + i - tk * passes) * ROWS + slot;
+            if (it + i < items && r < heads) {
+                const long long tok = tok0 + tk;
                 const char* src = r < a.Hq ? a.q + tok * a.q_stride + (long long)r * RB
                                  : r < a.Hq + a.Hkv ? a.k + tok * a.k_stride + (long long)(r - a.Hq) * RB
                                                     : a.v + tok * a.v_stride + (long long)(r - a.Hq - a.Hkv) * RB;
-                raw[i] = *reinterpret_cast<const uint4*>(src + lig * 16);
+                raw[i][0] = *reinterpret_cast<const Quad<T>*>(src + c0 * QB);
+                raw[i][1] = *reinterpret_cast<const Quad<T>*>(src + c1 * QB);
             }
         }
-        if (!table) {
-            for (int i = threadIdx.x; i < a.half; i += kRotThreads) {
-                double turn = (double)a.positions[tok] * a.turns[i];
+        if (it == 0) {
+            for (int i = threadIdx.x; i < ntok * a.half; i += kRotThreads) {
+                const int tk = i / a.half, pr = i - tk * a.half;
+                double turn = (double)a.positions[tok0 + tk] * a.turns[pr];
                 turn -= rint(turn);
                 float sn, cn;
                 sincospif(2.0f * (float)turn, &sn, &cn);
-                cs[i] = make_float2(cn, sn);
+                cs[tk][pr] = make_float2(cn, sn);
             }
             __syncthreads();
-            table = true;
         }
 #pragma unroll
-        for (int i = 0; i < kRotVecs; ++i) {
-            // (whole warps agree on r >= r1 only by chance: the exchange below needs every lane, the store is guarded)
-            const int r = rb + i * ROWS + slot;
+        for (int i = 0; i < kRotRows; ++i) {
+            const int tk = (it + i) / passes, r = (it + i - tk * passes) * ROWS + slot;
+            const bool there = it + i < items && r < heads;
             const bool is_v = r >= a.Hq + a.Hkv;
-            uint4 res = raw[i];
-            float x[EPL];
-            Unpack<T>::run(raw[i], x);
-            const char* w = r < a.Hq ? a.q_weight : a.k_weight;
-            float ss = 0.f;
+            float x[8];
+            raw[i][0].unpack(x);
+            raw[i][1].unpack(x + 4);
+            const int which = r < a.Hq ? 0 : 1;
+            if ((which == 0 ? a.q_weight : a.k_weight) != nullptr) {
+                float ss = 0.f;
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) ss = fmaf(x[e], x[e], ss);
+                for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+                // (lanes of one row take this branch together; the mask names them)
+                const uint32_t group = LPR == 16 ? 0xffffu << (threadIdx.x & 16) : 0xffu << (threadIdx.x & 24);
 #pragma unroll
-            for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            if (w != nullptr) {
+                for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor_sync(group, ss, o);
                 const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
-                float wf[EPL];
-                Unpack<T>::run(*reinterpret_cast<const uint4*>(w + lig * 16), wf);
+                float wf[8];
+                const Quad<T> w0 = which == 0 ? wq0 : wk0, w1 = which == 0 ? wq1 : wk1;
+                w0.unpack(wf);
+                w1.unpack(wf + 4);
 #pragma unroll
-                for (int e = 0; e < EPL; ++e) x[e] = x[e] * inv * wf[e];
+                for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * wf[e];
             }
-            if constexpr (INTERLEAVED) {
+            if (!there) continue;
+            if (!is_v) {
+                if constexpr (INTERLEAVED) {
 #pragma unroll
-                for (int e = 0; e < EPL; e += 2) {
-                    const int p = (lig * EPL + e) / 2;
-                    if (p < a.half) {
-                        const float2 c = cs[p];
-                        const float x0 = x[e], x1 = x[e + 1];
-                        x[e] = x0 * c.x - x1 * c.y;
-                        x[e + 1] = x1 * c.x + x0 * c.y;
+                    for (int q = 0; q < 2; ++q)
+                        if (q == 0 ? turn0 : turn1) {
+                            const float4 c = *reinterpret_cast<const float4*>(&cs[tk][2 * (q == 0 ? c0 : c1)]);   // two pairs
+                            float* y = x + 4 * q;
+                            const float y0 = y[0], y1 = y[1], y2 = y[2], y3 = y[3];
+                            y[0] = y0 * c.x - y1 * c.y;
+                            y[1] = y1 * c.x + y0 * c.y;
+                            y[2] = y2 * c.z - y3 * c.w;
+                            y[3] = y3 * c.z + y2 * c.w;
+                        }
+                } else if (turn0) {
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const float4 c = *reinterpret_cast<const float4*>(&cs[tk][4 * c0 + 2 * q]);               // two pairs
+                        const float a0 = x[2 * q], a1 = x[2 * q + 1], b0 = x[4 + 2 * q], b1 = x[5 + 2 * q];
+                        x[2 * q] = a0 * c.x - b0 * c.y;
+                        x[4 + 2 * q] = b0 * c.x + a0 * c.y;
+                        x[2 * q + 1] = a1 * c.z - b1 * c.w;
+                        x[5 + 2 * q] = b1 * c.z + a1 * c.w;
                     }
                 }
-            } else {
-                const int hl = a.half / EPL;           // lanes that hold first elements of pairs
-                const bool first = lig < hl;
-                const int partner = first ? lig + hl : (lig < 2 * hl ? lig - hl : lig);
-                float y[EPL];
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) y[e] = __shfl_sync(0xffffffffu, x[e], partner, LPR);
-                if (lig < 2 * hl) {
-                    const int p = (first ? lig : lig - hl) * EPL;
-#pragma unroll
-                    for (int e = 0; e < EPL; ++e) {
-                        const float2 c = cs[p + e];
-                        x[e] = first ? x[e] * c.x - y[e] * c.y : x[e] * c.x + y[e] * c.y;
-                    }
-                }
+                raw[i][0].pack(x);
+                raw[i][1].pack(x + 4);
             }
-            if (!is_v) res = pack_row<T>(x);
-            if (r >= r1) continue;
+            const int tok = tok0 + tk;
+            char* dst;
             if (r < a.Hq) {
-                *reinterpret_cast<uint4*>(a.q_out + (tok * a.Hq + r) * RB + lig * 16) = res;
+                dst = a.q_out + ((long long)tok * a.Hq + r) * RB;
             } else {
-                const int h = is_v ? r - a.Hq - a.Hkv : r - a.Hq;
-                const long long u = (long long)b * a.Hkv + h;
-                const int row = (a.unit_len ? a.unit_len[u] : a.len0) + (a.unit_len ? 0 : extra) + t;
+                const int b = tok / a.n_new, t = tok - b * a.n_new;
+                const int u = b * a.Hkv + (is_v ? r - a.Hq - a.Hkv : r - a.Hq);
+                const int row = (a.unit_len ? a.unit_len[u] : a.len0 + extra) + t;
                 if (row >= a.capacity) {               // only a replay that outran the capacity gets here
                     if (lig == 0) atomicExch(a.status, 4);
                     continue;
                 }
-                const long long dst = (u * a.row_stride + row) * (long long)RB + lig * 16;
-                if (!KVS_BOUNDS_OK(dst, 16, a.plane_bytes, a.status)) continue;
-                *reinterpret_cast<uint4*>((is_v ? a.vplane : a.kplane) + dst) = res;
+                const long long off = ((long long)u * a.row_stride + row) * RB;
+                if (!KVS_BOUNDS_OK(off, RB, a.plane_bytes, a.status)) continue;
+                dst = (is_v ? a.vplane : a.kplane) + off;
             }
+            *reinterpret_cast<Quad<T>*>(dst + c0 * QB) = raw[i][0];
+            *reinterpret_cast<Quad<T>*>(dst + c1 * QB) = raw[i][1];
         }
     }
 }
 
+template <typename T, int D, int TOKENS>
+cudaError_t launch_one(const RotaryKernelArgs& ka, bool interleaved, bool pdl, cudaStream_t stream) {
+    const dim3 grid((unsigned)((ka.tokens + TOKENS - 1) / TOKENS)), block(kRotThreads);
+    return interleaved ? launch_kernel(append_rotary_kernel<T, D, true, TOKENS>, grid, block, 0, stream, pdl, ka)
+                       : launch_kernel(append_rotary_kernel<T, D, false, TOKENS>, grid, block, 0, stream, pdl, ka);
+}
+
+// Several tokens per block once that still leaves every SM its four blocks; below, one token per block spreads the
+// few tokens there are (decode, 8 tokens) over as many SMs.
 template <typename T, int D>
-cudaError_t launch_one(const RotaryKernelArgs& ka, bool interleaved, dim3 grid, bool pdl, cudaStream_t stream) {
-    return interleaved ? launch_kernel(append_rotary_kernel<T, D, true>, grid, dim3(kRotThreads), 0, stream, pdl, ka)
-                       : launch_kernel(append_rotary_kernel<T, D, false>, grid, dim3(kRotThreads), 0, stream, pdl, ka);
+cudaError_t launch_tokens(const RotaryKernelArgs& ka, bool interleaved, bool pdl, cudaStream_t stream) {
+    return ka.tokens >= kRotTokens * 4 * 148 ? launch_one<T, D, kRotTokens>(ka, interleaved, pdl, stream)
+                                             : launch_one<T, D, 1>(ka, interleaved, pdl, stream);
 }
 
 }  // namespace
@@ -213,13 +265,12 @@ cudaError_t launch_append_rotary(const RotaryArgs& r, cudaStream_t stream) {
     ka.half = r.rotary_dim / 2;
     ka.eps = r.eps;
     for (int i = 0; i < 64; ++i) ka.turns[i] = i < ka.half ? r.inv_freq[i] * 0.15915494309189533577 : 0.0;   // 1 / 2 pi
-    const long long tokens = (long long)r.batch * r.n_new;
-    const dim3 grid((unsigned)tokens, 1);
+    ka.tokens = r.batch * r.n_new;
     if (r.dtype == 0)
-        return r.D == 128 ? launch_one<__nv_bfloat16, 128>(ka, r.interleaved, grid, r.programmatic, stream)
-                          : launch_one<__nv_bfloat16, 64>(ka, r.interleaved, grid, r.programmatic, stream);
-    return r.D == 128 ? launch_one<float, 128>(ka, r.interleaved, grid, r.programmatic, stream)
-                      : launch_one<float, 64>(ka, r.interleaved, grid, r.programmatic, stream);
+        return r.D == 128 ? launch_tokens<__nv_bfloat16, 128>(ka, r.interleaved, r.programmatic, stream)
+                          : launch_tokens<__nv_bfloat16, 64>(ka, r.interleaved, r.programmatic, stream);
+    return r.D == 128 ? launch_tokens<float, 128>(ka, r.interleaved, r.programmatic, stream)
+                      : launch_tokens<float, 64>(ka, r.interleaved, r.programmatic, stream);
 }
 
 }  // namespace kvs
