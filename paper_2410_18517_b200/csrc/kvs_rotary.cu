@@ -25,8 +25,7 @@ namespace kvs {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotRows = 4;      // head rows a group of lanes has in flight
-constexpr int kRotTokens = 4;    // tokens per block of a long prompt
+constexpr int kRotTokens = 4;    // tokens per block of a long prompt: as many rows a group of lanes has in flight
 
 struct RotaryKernelArgs {
     const char* q;
@@ -87,7 +86,8 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
     constexpr int ROWS = kRotThreads / LPR;       // head rows the block works on at once
     constexpr int RB = D * (int)sizeof(T);
     constexpr int QB = 4 * (int)sizeof(T);        // bytes of a quad
-    __shared__ float2 cs[TOKENS][D / 2];
+    __shared__ __align__(16) float2 cs[TOKENS][D / 2];
+    __shared__ int seq[TOKENS], row_in[TOKENS];
     pdl_launch_dependents();
     const int heads = a.Hq + 2 * a.Hkv;
     const int lig = threadIdx.x % LPR, slot = threadIdx.x / LPR;
@@ -108,33 +108,30 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
     }
     const int passes = (heads + ROWS - 1) / ROWS;
     const int tok0 = blockIdx.x * TOKENS, ntok = min(TOKENS, a.tokens - tok0);
-    const int items = ntok * passes;
+    // grid.y = 1: the block goes through all passes; else each block has one of them
+    const int pass0 = gridDim.y == 1 ? 0 : blockIdx.y, pass1 = gridDim.y == 1 ? passes : pass0 + 1;
     pdl_wait();
     const int extra = a.n_extra ? *a.n_extra : 0;    // replayed launch: the slot has grown since it was recorded
-    Quad<T> wq0 = {}, wq1 = {}, wk0 = {}, wk1 = {};
-    if (a.q_weight != nullptr) {
-        wq0 = *reinterpret_cast<const Quad<T>*>(a.q_weight + c0 * QB);
-        wq1 = *reinterpret_cast<const Quad<T>*>(a.q_weight + c1 * QB);
-    }
-    if (a.k_weight != nullptr) {
-        wk0 = *reinterpret_cast<const Quad<T>*>(a.k_weight + c0 * QB);
-        wk1 = *reinterpret_cast<const Quad<T>*>(a.k_weight + c1 * QB);
-    }
-    for (int it = 0; it < items; it += kRotRows) {
-        Quad<T> raw[kRotRows][2];
+    for (int pass = pass0; pass < pass1; ++pass) {
+        // A group of lanes keeps its head row of the pass for all tokens of the block.
+        const int r = pass * ROWS + slot;
+        const bool is_q = r < a.Hq, is_v = r >= a.Hq + a.Hkv, there = r < heads;
+        const int h = is_q ? r : (is_v ? r - a.Hq - a.Hkv : r - a.Hq);
+        const long long step = is_q ? a.q_stride : (is_v ? a.v_stride : a.k_stride);
+        const char* src = (is_q ? a.q : (is_v ? a.v : a.k)) + tok0 * step + (long long)h * RB;
+        const char* w = is_q ? a.q_weight : (is_v ? nullptr : a.k_weight);
+        Quad<T> raw[TOKENS][2], w0 = {}, w1 = {};
 #pragma unroll
-        for (int i = 0; i < kRotRows; ++i) {
-            const int tk = (it + i) / passes, r = (it + i - tk * passes) * ROWS + slot;
-            if (it + i < items && r < heads) {
-                const long long tok = tok0 + tk;
-                const char* src = r < a.Hq ? a.q + tok * a.q_stride + (long long)r * RB
-                                 : r < a.Hq + a.Hkv ? a.k + tok * a.k_stride + (long long)(r - a.Hq) * RB
-                                                    : a.v + tok * a.v_stride + (long long)(r - a.Hq - a.Hkv) * RB;
-                raw[i][0] = *reinterpret_cast<const Quad<T>*>(src + c0 * QB);
-                raw[i][1] = *reinterpret_cast<const Quad<T>*>(src + c1 * QB);
+        for (int i = 0; i < TOKENS; ++i)
+            if (there && i < ntok) {
+                raw[i][0] = *reinterpret_cast<const Quad<T>*>(src + i * step + c0 * QB);
+                raw[i][1] = *reinterpret_cast<const Quad<T>*>(src + i * step + c1 * QB);
             }
+        if (w != nullptr) {
+            w0 = *reinterpret_cast<const Quad<T>*>(w + c0 * QB);
+            w1 = *reinterpret_cast<const Quad<T>*>(w + c1 * QB);
         }
-        if (it == 0) {
+        if (pass == pass0) {
             for (int i = threadIdx.x; i < ntok * a.half; i += kRotThreads) {
                 const int tk = i / a.half, pr = i - tk * a.half;
                 double turn = (double)a.positions[tok0 + tk] * a.turns[pr];
@@ -143,40 +140,42 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
                 sincospif(2.0f * (float)turn, &sn, &cn);
                 cs[tk][pr] = make_float2(cn, sn);
             }
+            if (threadIdx.x < ntok) {
+                // where the token's row of unit 0 of its sequence goes (a ragged slot adds the unit's length later)
+                const int tok = tok0 + threadIdx.x, b = tok / a.n_new, t = tok - b * a.n_new;
+                seq[threadIdx.x] = b;
+                row_in[threadIdx.x] = t + (a.unit_len ? 0 : a.len0 + extra);
+            }
             __syncthreads();
         }
+        if (!there) continue;
 #pragma unroll
-        for (int i = 0; i < kRotRows; ++i) {
-            const int tk = (it + i) / passes, r = (it + i - tk * passes) * ROWS + slot;
-            const bool there = it + i < items && r < heads;
-            const bool is_v = r >= a.Hq + a.Hkv;
-            float x[8];
-            raw[i][0].unpack(x);
-            raw[i][1].unpack(x + 4);
-            const int which = r < a.Hq ? 0 : 1;
-            if ((which == 0 ? a.q_weight : a.k_weight) != nullptr) {
-                float ss = 0.f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
-                // (lanes of one row take this branch together; the mask names them)
-                const uint32_t group = LPR == 16 ? 0xffffu << (threadIdx.x & 16) : 0xffu << (threadIdx.x & 24);
-#pragma unroll
-                for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor_sync(group, ss, o);
-                const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
-                float wf[8];
-                const Quad<T> w0 = which == 0 ? wq0 : wk0, w1 = which == 0 ? wq1 : wk1;
-                w0.unpack(wf);
-                w1.unpack(wf + 4);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * wf[e];
-            }
-            if (!there) continue;
+        for (int i = 0; i < TOKENS; ++i) {
+            if (i >= ntok) break;
             if (!is_v) {
+                float x[8];
+                raw[i][0].unpack(x);
+                raw[i][1].unpack(x + 4);
+                if (w != nullptr) {
+                    float ss = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+                    // (the lanes of a row come here together, other rows of the warp perhaps not)
+                    const uint32_t group = LPR == 16 ? 0xffffu << (threadIdx.x & 16) : 0xffu << (threadIdx.x & 24);
+#pragma unroll
+                    for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor_sync(group, ss, o);
+                    const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
+                    float wf[8];
+                    w0.unpack(wf);
+                    w1.unpack(wf + 4);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * wf[e];
+                }
                 if constexpr (INTERLEAVED) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q)
                         if (q == 0 ? turn0 : turn1) {
-                            const float4 c = *reinterpret_cast<const float4*>(&cs[tk][2 * (q == 0 ? c0 : c1)]);   // two pairs
+                            const float4 c = *reinterpret_cast<const float4*>(&cs[i][2 * (q == 0 ? c0 : c1)]);   // two pairs
                             float* y = x + 4 * q;
                             const float y0 = y[0], y1 = y[1], y2 = y[2], y3 = y[3];
                             y[0] = y0 * c.x - y1 * c.y;
@@ -187,7 +186,7 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
                 } else if (turn0) {
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
-                        const float4 c = *reinterpret_cast<const float4*>(&cs[tk][4 * c0 + 2 * q]);               // two pairs
+                        const float4 c = *reinterpret_cast<const float4*>(&cs[i][4 * c0 + 2 * q]);               // two pairs
                         const float a0 = x[2 * q], a1 = x[2 * q + 1], b0 = x[4 + 2 * q], b1 = x[5 + 2 * q];
                         x[2 * q] = a0 * c.x - b0 * c.y;
                         x[4 + 2 * q] = b0 * c.x + a0 * c.y;
@@ -198,14 +197,12 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
                 raw[i][0].pack(x);
                 raw[i][1].pack(x + 4);
             }
-            const int tok = tok0 + tk;
             char* dst;
-            if (r < a.Hq) {
-                dst = a.q_out + ((long long)tok * a.Hq + r) * RB;
+            if (is_q) {
+                dst = a.q_out + ((long long)(tok0 + i) * a.Hq + r) * RB;
             } else {
-                const int b = tok / a.n_new, t = tok - b * a.n_new;
-                const int u = b * a.Hkv + (is_v ? r - a.Hq - a.Hkv : r - a.Hq);
-                const int row = (a.unit_len ? a.unit_len[u] : a.len0 + extra) + t;
+                const int u = seq[i] * a.Hkv + h;
+                const int row = row_in[i] + (a.unit_len ? a.unit_len[u] : 0);
                 if (row >= a.capacity) {               // only a replay that outran the capacity gets here
                     if (lig == 0) atomicExch(a.status, 4);
                     continue;
@@ -221,18 +218,19 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
 }
 
 template <typename T, int D, int TOKENS>
-cudaError_t launch_one(const RotaryKernelArgs& ka, bool interleaved, bool pdl, cudaStream_t stream) {
-    const dim3 grid((unsigned)((ka.tokens + TOKENS - 1) / TOKENS)), block(kRotThreads);
+cudaError_t launch_one(const RotaryKernelArgs& ka, bool interleaved, int passes, bool pdl, cudaStream_t stream) {
+    const dim3 grid((unsigned)((ka.tokens + TOKENS - 1) / TOKENS), (unsigned)passes), block(kRotThreads);
     return interleaved ? launch_kernel(append_rotary_kernel<T, D, true, TOKENS>, grid, block, 0, stream, pdl, ka)
                        : launch_kernel(append_rotary_kernel<T, D, false, TOKENS>, grid, block, 0, stream, pdl, ka);
 }
 
-// Several tokens per block once that still leaves every SM its four blocks; below, one token per block spreads the
-// few tokens there are (decode, 8 tokens) over as many SMs.
+// Several tokens per block, and all head rows of a token in it, once that still leaves every SM its four blocks; below,
+// one token per block and a block for every pass over its heads spread the few rows there are over the SMs.
 template <typename T, int D>
 cudaError_t launch_tokens(const RotaryKernelArgs& ka, bool interleaved, bool pdl, cudaStream_t stream) {
-    return ka.tokens >= kRotTokens * 4 * 148 ? launch_one<T, D, kRotTokens>(ka, interleaved, pdl, stream)
-                                             : launch_one<T, D, 1>(ka, interleaved, pdl, stream);
+    if (ka.tokens >= kRotTokens * 4 * 148) return launch_one<T, D, kRotTokens>(ka, interleaved, 1, pdl, stream);
+    const int rows = kRotThreads / (D / 8);
+    return launch_one<T, D, 1>(ka, interleaved, (ka.Hq + 2 * ka.Hkv + rows - 1) / rows, pdl, stream);
 }
 
 }  // namespace
