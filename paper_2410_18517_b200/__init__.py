@@ -27,9 +27,13 @@ class Rotary:
         values = [float(x) for x in inv_freq]
         self._array = (ctypes.c_double * max(len(values), 1))(*values)
         self.rotary_dim, self.interleaved = 2 * len(values), int(bool(interleaved))
+        self._structs = {}
 
     def _struct(self, eps):
-        return binding.kvs_rotary(self.rotary_dim, self.interleaved, eps, self._array)
+        s = self._structs.get(eps)
+        if s is None:
+            s = self._structs[eps] = binding.kvs_rotary(self.rotary_dim, self.interleaved, eps, self._array)
+        return s
 
     @classmethod
     def from_theta(cls, rotary_dim, theta=10000.0, interleaved=False):
@@ -49,9 +53,12 @@ class SharedKVCache:
 
         self._torch = torch
         self.device = torch.device("cuda", device)
+        # the current stream's handle without a Stream object around it, where this torch has it
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
         self.shape = (n_layers, n_q_heads, n_kv_heads, head_dim)
         self.max_batch = max_batch
+        self._planes = {}           # views handed out by plane(): the pool stays where it is
         self.ctx = binding.kvs_create(n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq,
                                       KVS_BF16 if dtype == "bf16" else KVS_F32, softmax_scale, device)
         try:
@@ -76,6 +83,7 @@ class SharedKVCache:
             binding.kvs_destroy(self.ctx)
             self.ctx = None
             self.pool = self.workspace = None
+            self._planes = {}
 
     def __del__(self):
         try:
@@ -84,6 +92,8 @@ class SharedKVCache:
             pass
 
     def _stream(self) -> int:
+        if self._raw_stream is not None:
+            return self._raw_stream(self.device.index)
         return self._torch.cuda.current_stream(self.device).cuda_stream
 
     def append(self, layer, k=None, v=None, batch=None, n_new=None):
@@ -132,32 +142,39 @@ class SharedKVCache:
         counts = [int(x) for x in self._torch.as_tensor(n_keep).reshape(-1).tolist()]
         binding.kvs_evict(self.ctx, layer, keep, counts, keep.shape[2], keep.shape[0], self._stream())
 
-    def _token_stride(self, x, heads, shape):
+    def _token_stride(self, x, heads, batch, n_new):
         """Elements between consecutive tokens of ``[batch][n_new][heads][head_dim]`` (heads contiguous)."""
-        assert x.dtype == self.dtype and x.shape == (*shape, heads, self.shape[3])
-        step = x.stride(1) if x.shape[1] > 1 else (x.stride(0) if x.shape[0] > 1 else heads * self.shape[3])
-        assert x.stride(3) == 1 and (heads == 1 or x.stride(2) == self.shape[3])
-        assert x.shape[0] == 1 or x.stride(0) == x.shape[1] * step, "tokens of all sequences must be evenly spaced"
-        return step
+        D = self.shape[3]
+        b, t, h, d = x.shape
+        sb, st, sh, sd = x.stride()
+        assert x.dtype is self.dtype and b == batch and t == n_new and h == heads and d == D
+        assert sd == 1 and (sh == D or heads == 1), "a token's heads must be contiguous"
+        if t == 1:
+            return sb if b > 1 else heads * D
+        assert b == 1 or sb == t * st, "tokens of all sequences must be evenly spaced"
+        return st
 
     def append_rotary(self, layer, q, k, v, positions, rotary, q_weight=None, k_weight=None, eps=1e-6, out=None):
         """New tokens: per-head RMS norm (where a weight is given) and rotary positions of q and k, k and v appended
         to the layer's slot, the finished queries returned.  q, k, v: ``[batch][n_new][heads][head_dim]``, slices of
         one projection's output allowed (k, v: None on a sharing layer); positions: int32 ``[batch][n_new]``."""
         torch = self._torch
-        shape = q.shape[:2]
-        qs = self._token_stride(q, self.shape[1], shape)
+        batch, n_new = q.shape[0], q.shape[1]
+        _, Hq, Hkv, D = self.shape
+        qs = self._token_stride(q, Hq, batch, n_new)
         ks = vs = 0
         if k is not None:
-            ks, vs = self._token_stride(k, self.shape[2], shape), self._token_stride(v, self.shape[2], shape)
-        assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and positions.shape == shape)
+            ks, vs = self._token_stride(k, Hkv, batch, n_new), self._token_stride(v, Hkv, batch, n_new)
+        assert positions is None or (positions.dtype is torch.int32 and positions.is_contiguous() and
+                                     positions.shape == q.shape[:2])
         for w in (q_weight, k_weight):
-            assert w is None or (w.dtype == self.dtype and w.is_contiguous() and w.numel() == self.shape[3])
+            assert w is None or (w.dtype is self.dtype and w.is_contiguous() and w.numel() == D)
         if out is None:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        assert out.is_contiguous() and out.dtype == self.dtype and out.shape == q.shape
+            out = torch.empty((batch, n_new, Hq, D), dtype=self.dtype, device=self.device)
+        else:
+            assert out.is_contiguous() and out.dtype is self.dtype and out.shape == q.shape
         binding.kvs_append_rotary(self.ctx, layer, rotary._struct(eps), q, qs, k, ks, v, vs, positions, q_weight, k_weight, out,
-                                  shape[0], shape[1], self._stream())
+                                  batch, n_new, self._stream())
         return out
 
     def tree_attention(self, layer, q, mask=None, out=None):
@@ -167,8 +184,9 @@ class SharedKVCache:
         assert q.is_contiguous() and q.dtype == self.dtype and q.ndim == 4 and q.shape[2:] == (self.shape[1], self.shape[3])
         assert mask is None or (mask.dtype in (torch.int64, torch.uint64) and mask.is_contiguous() and mask.shape == q.shape[:2])
         if out is None:
-            out = torch.empty(q.shape, dtype=self.dtype, device=self.device)
-        assert out.is_contiguous() and out.dtype == self.dtype and out.shape == q.shape
+            out = torch.empty_like(q)
+        else:
+            assert out.is_contiguous() and out.dtype == self.dtype and out.shape == q.shape
         binding.kvs_tree_attention(self.ctx, layer, q, out, mask, q.shape[0], q.shape[1], self._stream())
         return out
 
@@ -201,10 +219,10 @@ class SharedKVCache:
         takes, int32 ``[batch][n_kv_heads][max n_keep]``, and the rows' totals in the same layout."""
         torch = self._torch
         assert total.dtype == torch.float32 and total.is_contiguous() and total.ndim == 3 and total.shape[1] == self.shape[2]
-        counts = torch.as_tensor(n_keep).reshape(-1).tolist()
-        assert len(counts) == total.shape[0] * total.shape[1]
+        counts = torch.as_tensor(n_keep, dtype=torch.int32, device="cpu").contiguous()
+        assert counts.numel() == total.shape[0] * total.shape[1]
         if keep is None:
-            keep = torch.zeros(*total.shape[:2], max(counts), dtype=torch.int32, device=self.device)
+            keep = torch.zeros(*total.shape[:2], int(counts.max()), dtype=torch.int32, device=self.device)
         if kept_total is None:
             kept_total = torch.zeros(keep.shape, dtype=torch.float32, device=self.device)
         assert keep.is_contiguous() and keep.dtype == torch.int32 and keep.shape[:2] == total.shape[:2]
@@ -258,10 +276,15 @@ class SharedKVCache:
 
     def plane(self, slot, kv):
         """View of plane (slot, kv) as ``[max_batch][n_kv_heads][row_stride][head_dim]``."""
+        view = self._planes.get((slot, kv))
+        if view is not None:
+            return view
         off = binding.kvs_plane_offset(self.ctx, slot, kv)
         nxt = binding.kvs_plane_offset(self.ctx, 0, 1)
         rs = binding.kvs_row_stride(self.ctx)
-        return self.pool[off:off + nxt].view(self.dtype).view(-1, self.shape[2], rs, self.shape[3])
+        view = self.pool[off:off + nxt].view(self.dtype).view(-1, self.shape[2], rs, self.shape[3])
+        self._planes[slot, kv] = view
+        return view
 
     # plain forwards
     def num_slots(self):

@@ -129,7 +129,7 @@ def load() -> ctypes.CDLL:
         "kvs_tree_attention": [vp, i32, vp, vp, vp, i32, i32, vp],
         "kvs_accept_draft": [vp, vp, i32, P(i32), i32, i32, vp],
         "kvs_decode_attention_weights": [vp, i32, vp, vp, vp, vp, i32, i32, vp],
-        "kvs_select_rows": [vp, i32, vp, i32, P(i32), i32, vp, vp, i32, i32, vp],
+        "kvs_select_rows": [vp, i32, vp, i32, vp, i32, vp, vp, i32, i32, vp],
         "kvs_read_roof": [vp, sz, vp, i32, vp],
     }
     for name, argtypes in sig.items():
@@ -157,11 +157,11 @@ def _ptr(x) -> int | None:
     """Raw address of a torch tensor / numpy array / int / None."""
     if x is None:
         return None
-    if isinstance(x, int):
-        return x
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr()
-    return x.ctypes.data
+    except AttributeError:
+        pass
+    return x if isinstance(x, int) else x.ctypes.data
 
 
 def kvs_status_string(status: int) -> str:
@@ -251,8 +251,8 @@ def kvs_decode_attention_weights(ctx: int, layer: int, q, out, total_in, total_o
 
 def kvs_select_rows(ctx: int, layer: int, total, total_stride: int, n_keep, n_recent: int, keep, kept_total, keep_stride: int,
                     batch: int, stream: int = 0) -> None:
-    """n_keep: host sequence of batch*Hkv counts (or a ctypes int32 array of them)."""
-    counts = n_keep if isinstance(n_keep, ctypes.Array) else (ctypes.c_int32 * len(n_keep))(*n_keep)
+    """n_keep: host sequence of batch*Hkv counts, or a contiguous int32 CPU tensor of them."""
+    counts = n_keep.data_ptr() if hasattr(n_keep, "data_ptr") else (ctypes.c_int32 * len(n_keep))(*n_keep)
     _check(load().kvs_select_rows(ctx, layer, _ptr(total), total_stride, counts, n_recent, _ptr(keep), _ptr(kept_total),
                                   keep_stride, batch, stream), "kvs_select_rows")
 

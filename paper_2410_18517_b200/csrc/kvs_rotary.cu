@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
     constexpr int ROWS = kRotThreads / LPR;       // head rows the block works on at once
     constexpr int RB = D * (int)sizeof(T);
     constexpr int QB = 4 * (int)sizeof(T);        // bytes of a quad
-    __shared__ __align__(16) float2 cs[TOKENS][D / 2];
+    // cos and sin apart: the lanes' 16-byte reads then hit different banks
+    __shared__ __align__(16) float cos_t[TOKENS][D / 2], sin_t[TOKENS][D / 2];
     __shared__ int seq[TOKENS], row_in[TOKENS];
     pdl_launch_dependents();
     const int heads = a.Hq + 2 * a.Hkv;
@@ -138,7 +139,8 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
                 turn -= rint(turn);
                 float sn, cn;
                 sincospif(2.0f * (float)turn, &sn, &cn);
-                cs[tk][pr] = make_float2(cn, sn);
+                cos_t[tk][pr] = cn;
+                sin_t[tk][pr] = sn;
             }
             if (threadIdx.x < ntok) {
                 // where the token's row of unit 0 of its sequence goes (a ragged slot adds the unit's length later)
@@ -149,6 +151,11 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
             __syncthreads();
         }
         if (!there) continue;
+        float wf[8];
+        w0.unpack(wf);
+        w1.unpack(wf + 4);
+        char* q_dst = a.q_out + ((long long)tok0 * a.Hq + r) * RB;      // (used where the row is a query's)
+        const long long q_step = (long long)a.Hq * RB;
 #pragma unroll
         for (int i = 0; i < TOKENS; ++i) {
             if (i >= ntok) break;
@@ -165,33 +172,26 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
 #pragma unroll
                     for (int o = LPR / 2; o >= 1; o >>= 1) ss += __shfl_xor_sync(group, ss, o);
                     const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
-                    float wf[8];
-                    w0.unpack(wf);
-                    w1.unpack(wf + 4);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = x[e] * inv * wf[e];
                 }
                 if constexpr (INTERLEAVED) {
 #pragma unroll
-                    for (int q = 0; q < 2; ++q)
-                        if (q == 0 ? turn0 : turn1) {
-                            const float4 c = *reinterpret_cast<const float4*>(&cs[i][2 * (q == 0 ? c0 : c1)]);   // two pairs
-                            float* y = x + 4 * q;
-                            const float y0 = y[0], y1 = y[1], y2 = y[2], y3 = y[3];
-                            y[0] = y0 * c.x - y1 * c.y;
-                            y[1] = y1 * c.x + y0 * c.y;
-                            y[2] = y2 * c.z - y3 * c.w;
-                            y[3] = y3 * c.z + y2 * c.w;
+                    for (int q = 0; q < 4; ++q)
+                        if (q < 2 ? turn0 : turn1) {
+                            const int pr = 2 * (q < 2 ? c0 : c1) + (q & 1);
+                            const float c = cos_t[i][pr], sn = sin_t[i][pr], f = x[2 * q], g = x[2 * q + 1];
+                            x[2 * q] = f * c - g * sn;
+                            x[2 * q + 1] = g * c + f * sn;
                         }
                 } else if (turn0) {
+                    const float4 c4 = *reinterpret_cast<const float4*>(&cos_t[i][4 * c0]), s4 = *reinterpret_cast<const float4*>(&sin_t[i][4 * c0]);
+                    const float c[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const float4 c = *reinterpret_cast<const float4*>(&cs[i][4 * c0 + 2 * q]);               // two pairs
-                        const float a0 = x[2 * q], a1 = x[2 * q + 1], b0 = x[4 + 2 * q], b1 = x[5 + 2 * q];
-                        x[2 * q] = a0 * c.x - b0 * c.y;
-                        x[4 + 2 * q] = b0 * c.x + a0 * c.y;
-                        x[2 * q + 1] = a1 * c.z - b1 * c.w;
-                        x[5 + 2 * q] = b1 * c.z + a1 * c.w;
+                    for (int q = 0; q < 4; ++q) {
+                        const float f = x[q], g = x[4 + q];
+                        x[q] = f * c[q] - g * sn[q];
+                        x[4 + q] = g * c[q] + f * sn[q];
                     }
                 }
                 raw[i][0].pack(x);
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
             }
             char* dst;
             if (is_q) {
-                dst = a.q_out + ((long long)(tok0 + i) * a.Hq + r) * RB;
+                dst = q_dst + i * q_step;
             } else {
                 const int u = seq[i] * a.Hkv + h;
                 const int row = row_in[i] + (a.unit_len ? a.unit_len[u] : 0);

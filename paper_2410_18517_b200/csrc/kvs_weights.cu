@@ -12,12 +12,13 @@ namespace {
 // Finish of a decode step that stored its scores s_gj (log2 domain) beside the split-K pieces:
 //   out[g]   = sum_c w_c o_c / L_g,   w_c = 2^(m_c - M_g),  M_g = max_c m_c,  L_g = sum_c w_c l_c
 //   total[j] += sum_g 2^(s_gj - M_g) / L_g          (heads in order: no atomics, the same bits every time)
-// Blocks 0 .. chunks-1 of a unit take 1024 rows each, blocks chunks .. chunks+G-1 one head's output each; every
-// block works M and L out for itself from the pieces' (max, sum) pairs, which are few and in L2.
+// Blocks 0 .. chunks-1 of a unit take a run of rows each, blocks chunks .. chunks+G-1 one head's output each; every
+// block works M and L out for itself from the pieces' (max, sum) pairs, which are few and in L2, while its first scores
+// are on their way.  A thread takes four neighbouring rows and asks for all heads' scores at once.
 // Bound: HBM / L2 for the scores and totals, (4 G + 8) bytes per row beside the step's 4 D or 8 D bytes.
 // --------------------------------------------------------------------------------------
 constexpr int kFinishThreads = 256;
-constexpr int kFinishRows = 1024;
+constexpr int kFinishRows = 4 * kFinishThreads;    // rows per turn of a block
 
 struct FinishArgs {
     const float* part_o;
@@ -28,6 +29,8 @@ struct FinishArgs {
     float* out;
     long long T;
     int total_stride, row_stride, G, tpu, NC, n, tile_rows, units, cap, chunks;
+    int turns;                 // turns of a block: it takes turns * kFinishRows rows
+    bool vec;                  // totals can be read and written four at a time
     const int* n_extra;
     const int* unit_len;
 };
@@ -53,6 +56,18 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
     const int c0 = block_of_tile(u * a.tpu, a.T, a.NC);
     const int np = block_of_tile((u + 1) * a.tpu - 1, a.T, a.NC) - c0 + 1;
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + (u + c0) * a.G;    // piece c, head g: ml[c * G + g]
+    const int n = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
+    const float* sc = a.scores + u * a.G * a.row_stride;
+    const long long tot = u * (long long)a.total_stride;
+    // (a score array's rows are padded to the planes' row stride, a multiple of 128: reading four at a time is safe)
+    float4 s[8];
+    auto fetch = [&](int j) {
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            if (g < a.G && j < n) s[g] = *reinterpret_cast<const float4*>(sc + (long long)g * a.row_stride + j);
+    };
+    const int j_first = part * a.turns * kFinishRows + 4 * threadIdx.x;
+    if (part < a.chunks) fetch(j_first);
     if (warp < a.G) {
         float M = -1.0e30f, L = 0.f;
         for (int c = lane; c < np; c += 32) M = fmaxf(M, ml[c * a.G + warp].x);
@@ -71,16 +86,32 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
     }
     __syncthreads();
     if (part < a.chunks) {
-        const int n = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
-        const float* sc = a.scores + u * a.G * a.row_stride;
-        const long long tot = u * (long long)a.total_stride;
-#pragma unroll
-        for (int i = 0; i < kFinishRows / kFinishThreads; ++i) {
-            const int j = part * kFinishRows + i * kFinishThreads + threadIdx.x;
+        for (int turn = 0; turn < a.turns; ++turn) {
+            const int j = j_first + turn * kFinishRows;
             if (j >= n) break;
-            float sum = 0.f;
-            for (int g = 0; g < a.G; ++g) sum = fmaf(fast_exp2(sc[(long long)g * a.row_stride + j] - s_max[g]), s_inv[g], sum);
-            a.total_out[tot + j] = a.total_in ? a.total_in[tot + j] + sum : sum;
+            if (turn > 0) fetch(j);
+            float t[4] = {0.f, 0.f, 0.f, 0.f};
+            const bool vec = a.vec && j + 4 <= n;
+            if (a.total_in != nullptr) {
+                if (vec) *reinterpret_cast<float4*>(t) = *reinterpret_cast<const float4*>(a.total_in + tot + j);
+                else
+                    for (int i = 0; i < 4 && j + i < n; ++i) t[i] = a.total_in[tot + j + i];
+            }
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+                if (g < a.G) {
+                    const float M = s_max[g], inv = s_inv[g];
+                    sum[0] = fmaf(fast_exp2(s[g].x - M), inv, sum[0]);
+                    sum[1] = fmaf(fast_exp2(s[g].y - M), inv, sum[1]);
+                    sum[2] = fmaf(fast_exp2(s[g].z - M), inv, sum[2]);
+                    sum[3] = fmaf(fast_exp2(s[g].w - M), inv, sum[3]);
+                }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) t[i] += sum[i];
+            if (vec) *reinterpret_cast<float4*>(a.total_out + tot + j) = *reinterpret_cast<const float4*>(t);
+            else
+                for (int i = 0; i < 4 && j + i < n; ++i) a.total_out[tot + j + i] = t[i];
         }
         return;
     }
@@ -110,13 +141,16 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
 // --------------------------------------------------------------------------------------
 // Selection: of a unit's n rows keep the newest n_recent and, of the others, the n_keep - n_recent with the largest
 // totals; equal totals go to the older row, NaN counts below everything.  The list comes out ascending.
-// Radix select on order-preserving 32-bit keys, eight bits per pass from the top: after four passes the key of the last
-// row kept is known exactly, and how many rows with that very key stay.  One block per unit; a warp then walks its own
-// contiguous stretch of rows twice (count, write), so that one scan over the 32 warps orders the whole list.
+// Radix select on order-preserving 32-bit keys, 11 + 11 + 10 bits from the top, by histograms in shared memory: after three
+// passes the key of the last row kept is known exactly, and how many rows with that very key stay.  One block per
+// unit; a warp owns IPT * 32 neighbouring rows, lane l the rows 32 i + l, in registers: loads and stores are
+// contiguous, and one vote orders 32 rows.  What pads a unit's end has the lowest key and the highest row numbers, so it
+// is never reached.  Bound: instruction issue, some 40 for 32 rows.
+// (Keys in shared memory and a list of the first bin's keys for the later passes: 100 for 32 rows, 53 us for 640 units
+// of 8192 rows; neighbouring rows in one thread: the loads of a warp then touch 32 lines each, 47 us.)
 // --------------------------------------------------------------------------------------
 constexpr int kSelectThreads = 1024;
-constexpr int kSelectWarps = kSelectThreads / 32;
-constexpr int kSelectCached = 49152;     // keys a block holds in shared memory; longer units are read again per pass
+constexpr int kSelectBins = 2048;
 
 __device__ __forceinline__ uint32_t order_key(float x) {
     if (x != x) return 0u;                            // NaN: below minus infinity (whose key is 0x007fffff)
@@ -124,119 +158,173 @@ __device__ __forceinline__ uint32_t order_key(float x) {
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-__global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const SelectArgs a, const __grid_constant__ SelectCounts counts,
-                                                                     int cached) {
-    extern __shared__ uint32_t cache[];
-    __shared__ int hist[256];
-    __shared__ int warp_gt[kSelectWarps], warp_eq[kSelectWarps];
+// The total a key was made from; of zeros and NaN, which lose their sign and payload in the key, the total itself.  (Read
+// again for every row kept, each store waited for its load: 35 us instead of 27 for 640 units of 8192 rows.)
+__device__ __forceinline__ float total_of(uint32_t key, const float* from) {
+    if (key == 0x80000000u || key == 0u) return *from;
+    return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
+}
+
+// IPT: rows per lane.  ONE: a unit fits one tile of blockDim.x * IPT rows, which stays in registers; otherwise (units of
+// more than 32768 rows) the tiles are read again for every step.
+template <int IPT, bool ONE>
+__global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const SelectArgs a, const __grid_constant__ SelectCounts counts) {
+    __shared__ int hist[kSelectBins];
+    __shared__ int warp_gt[32], warp_eq[32];
     __shared__ uint32_t s_prefix;
     __shared__ int s_need;
     const long long u = a.unit0 + blockIdx.x;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, threads = blockDim.x, warps = threads >> 5;
     const int n = a.unit_len ? a.unit_len[u] : a.n;
     const int want = counts.n[blockIdx.x] - a.n_recent;     // rows chosen by total
     const int old = n - a.n_recent;                         // rows they are chosen from
     const float* total = a.total + u * a.total_stride;
-    const bool held = old <= cached;
-    if (held) {
-        for (int j = tid; j < old; j += kSelectThreads) cache[j] = order_key(total[j]);
-    }
-    auto key = [&](int j) { return held ? cache[j] : order_key(total[j]); };
-    if (tid == 0) {
-        s_prefix = 0;
-        s_need = want;
-    }
-    __syncthreads();
-    // `need` rows are still to be taken among the keys that begin with `prefix`
-    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-        for (int i = tid; i < 256; i += kSelectThreads) hist[i] = 0;
-        __syncthreads();
-        const uint32_t prefix = s_prefix;
-        for (int j = tid; j < old; j += kSelectThreads) {
-            const uint32_t k = key(j);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
-        }
-        __syncthreads();
-        if (warp == 0) {
-            // lane i holds the counts of digits 255 - 8 i .. 248 - 8 i: largest first
-            int c[8], sum = 0;
+    const int tile = threads * IPT, first = warp * 32 * IPT + lane;
+    uint32_t key[IPT];
+    auto load = [&](int base) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                c[i] = hist[255 - 8 * lane - i];
-                sum += c[i];
-            }
-            int before = sum;
+        for (int i = 0; i < IPT; ++i) {
+            const int j = base + first + 32 * i;
+            key[i] = __float_as_uint(j < old ? total[j] : __uint_as_float(0x7fffffffu));
+        }
+#pragma unroll
+        for (int i = 0; i < IPT; ++i) key[i] = order_key(__uint_as_float(key[i]));
+    };
+    // the digit of the `need`-th largest key in hist[0 .. 2^bits): called by warp 0
+    auto find = [&](uint32_t prefix, int low, int bits) {
+        // lane i first sums the 64 (32) digits of the i-th largest run, then the warp looks into the run it is in
+        const int run = 1 << (bits - 5), need = s_need;
+        int top0 = (1 << bits) - 1, before = 0;                      // digits top0, top0 - 1, ...; rows above them
+        for (int level = 0; level < 2; ++level) {
+            const int width = level == 0 ? run : run / 32, top = top0 - width * lane;
+            int sum = 0;
+#pragma unroll 8
+            for (int i = 0; i < width; ++i) sum += hist[top - ((i + lane) & (width - 1))];     // (rotated: other banks)
+            int upto = sum;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, before, o);
-                if (lane >= o) before += y;
+                const int y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
             }
-            before -= sum;
-            const int need = s_need;
-            __syncwarp();
+            const int at = __ffs(__ballot_sync(0xffffffffu, before + upto >= need)) - 1;
+            before += __shfl_sync(0xffffffffu, upto - sum, at);
+            top0 -= width * at;
+        }
+        if (run == 64 && before + hist[top0] < need) before += hist[top0--];
+        __syncwarp();
+        if (lane == 0) {
+            s_prefix = prefix | (uint32_t)top0 << low;
+            s_need = need - before;
+        }
+    };
+    if (want > 0) {
+        if (ONE) load(0);
+        if (tid == 0) s_need = want;
+        uint32_t prefix = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (before < need && before + c[i] >= need) {      // exactly one digit of one lane
-                    s_prefix = prefix | (uint32_t)(255 - 8 * lane - i) << shift;
-                    s_need = need - before;
-                }
-                before += c[i];
+        for (int pass = 0; pass < 3; ++pass) {
+            const int low = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
+            for (int i = tid; i < kSelectBins; i += threads) hist[i] = 0;
+            __syncthreads();
+            for (int base = 0; base < old; base += tile) {
+                if (!ONE) load(base);
+#pragma unroll
+                for (int i = 0; i < IPT; ++i)
+                    if (pass == 0 || (key[i] ^ prefix) >> (low + bits & 31) == 0u) atomicAdd(&hist[key[i] >> low & ((1u << bits) - 1u)], 1);
             }
+            __syncthreads();
+            if (warp == 0) find(prefix, low, bits);
+            __syncthreads();
+            prefix = s_prefix;
         }
-        __syncthreads();
     }
-    const uint32_t last = s_prefix;        // the smallest key kept; of the rows that have it the first `ties` stay
-    const int ties = want > 0 ? s_need : 0;
-    // contiguous stretches per warp, in multiples of 32 rows
-    const int per = ((old + kSelectWarps - 1) / kSelectWarps + 31) / 32 * 32;
-    const int j0 = min(old, warp * per), j1 = min(old, j0 + per);
-    int gt = 0, eq = 0;
-    if (want > 0)
-        for (int j = j0; j < j1; j += 32) {
-            const uint32_t k = j + lane < j1 ? key(j + lane) : 0u;
-            const bool in = j + lane < j1;
-            gt += __popc(__ballot_sync(0xffffffffu, in && k > last));
-            eq += __popc(__ballot_sync(0xffffffffu, in && k == last));
-        }
-    if (lane == 0) {
-        warp_gt[warp] = gt;
-        warp_eq[warp] = eq;
-    }
-    __syncthreads();
-    int eq_before = 0, pos = 0;
-    for (int w = 0; w < warp; ++w) {
-        pos += warp_gt[w];
-        eq_before += warp_eq[w];
-    }
-    pos += min(eq_before, ties);
     int* keep = a.keep + u * a.keep_stride;
     float* kept = a.kept ? a.kept + u * a.keep_stride : nullptr;
-    const uint32_t below = (1u << lane) - 1;
-    if (want > 0)
-        for (int j = j0; j < j1; j += 32) {
-            const bool in = j + lane < j1;
-            const uint32_t k = in ? key(j + lane) : 0u;
-            const uint32_t meq = __ballot_sync(0xffffffffu, in && k == last);
-            const bool take = in && (k > last || (k == last && eq_before + __popc(meq & below) < ties));
-            const uint32_t mt = __ballot_sync(0xffffffffu, take);
-            if (take) {
-                const int p = pos + __popc(mt & below);
-                keep[p] = j + lane;
-                if (kept) kept[p] = total[j + lane];
+    if (want > 0) {
+        const uint32_t last = s_prefix;    // the smallest key kept; of the rows that have it the first `ties` stay
+        const int ties = s_need;
+        const uint32_t below = (1u << lane) - 1u;
+        int gt_done = 0, eq_done = 0;      // rows of earlier tiles
+        for (int base = 0; base < old; base += tile) {
+            if (!ONE) load(base);
+            int gt = 0, eq = 0;
+#pragma unroll
+            for (int i = 0; i < IPT; ++i) {
+                gt += key[i] > last ? 1 : 0;
+                eq += key[i] == last ? 1 : 0;
             }
-            pos += __popc(mt);
-            eq_before += __popc(meq);
+            gt = __reduce_add_sync(0xffffffffu, gt);
+            eq = __reduce_add_sync(0xffffffffu, eq);
+            if (lane == 0) {
+                warp_gt[warp] = gt;
+                warp_eq[warp] = eq;
+            }
+            __syncthreads();
+            int gt_w = lane < warps ? warp_gt[lane] : 0, eq_w = lane < warps ? warp_eq[lane] : 0;
+            const int gt_all = __reduce_add_sync(0xffffffffu, gt_w), eq_all = __reduce_add_sync(0xffffffffu, eq_w);
+            gt_w = __reduce_add_sync(0xffffffffu, lane < warp ? gt_w : 0);
+            eq_w = __reduce_add_sync(0xffffffffu, lane < warp ? eq_w : 0);
+            int seen = eq_done + eq_w;                               // rows with the last key before this warp's turn
+            int pos = gt_done + gt_w + min(seen, ties);
+            const float* from = total + base + first;
+            if (seen + eq <= ties || seen >= ties) {                 // the warp's rows with the last key stay all, or none
+                const uint32_t least = seen < ties || eq == 0 ? last : last + 1u;
+#pragma unroll
+                for (int i = 0; i < IPT; ++i) {
+                    const bool take = key[i] >= least;
+                    const uint32_t taken = __ballot_sync(0xffffffffu, take);
+                    if (take) {
+                        const int at = pos + __popc(taken & below);
+                        keep[at] = base + first + 32 * i;
+                        if (kept) kept[at] = total_of(key[i], from + 32 * i);
+                    }
+                    pos += __popc(taken);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < IPT; ++i) {
+                    const uint32_t same = __ballot_sync(0xffffffffu, key[i] == last);
+                    const bool take = key[i] > last || (key[i] == last && seen + __popc(same & below) < ties);
+                    const uint32_t taken = __ballot_sync(0xffffffffu, take);
+                    if (take) {
+                        const int at = pos + __popc(taken & below);
+                        keep[at] = base + first + 32 * i;
+                        if (kept) kept[at] = total_of(key[i], from + 32 * i);
+                    }
+                    pos += __popc(taken);
+                    seen += __popc(same);
+                }
+            }
+            gt_done += gt_all;
+            eq_done += eq_all;
+            if (!ONE) __syncthreads();     // warp_gt, warp_eq are written again
         }
-    for (int j = old + tid; j < n; j += kSelectThreads) {
+    }
+    for (int j = old + tid; j < n; j += threads) {
         keep[want + j - old] = j;
         if (kept) kept[want + j - old] = total[j];
     }
 }
 
+template <int IPT, bool ONE>
+cudaError_t select_attr() {
+    return cudaFuncSetAttribute(select_rows_kernel<IPT, ONE>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+}
+
+template <int IPT, bool ONE>
+cudaError_t launch_select_one(const SelectArgs& a, const SelectCounts& counts, int old, cudaStream_t stream) {
+    // no more warps than the longest unit has rows for
+    const long long warps = std::max(1, (old + 32 * IPT - 1) / (32 * IPT));
+    select_rows_kernel<IPT, ONE><<<(unsigned)a.units, (unsigned)std::min<long long>(kSelectThreads, 32 * warps), 0, stream>>>(a, counts);
+    return cudaGetLastError();
+}
+
 }  // namespace
 
 cudaError_t init_weights_kernels() {
-    return cudaFuncSetAttribute(select_rows_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSelectCached * 4);
+    cudaError_t e = select_attr<8, true>();
+    if (e == cudaSuccess) e = select_attr<32, true>();
+    return e == cudaSuccess ? select_attr<16, false>() : e;
 }
 
 cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, const float* total_in, float* total_out,
@@ -260,16 +348,22 @@ cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, c
     f.cap = a.capacity;
     f.n_extra = a.n_extra;
     f.unit_len = a.unit_len;
-    f.chunks = ((a.n_extra ? a.capacity : a.n) + kFinishRows - 1) / kFinishRows;
+    const int turns = ((a.n_extra ? a.capacity : a.n) + kFinishRows - 1) / kFinishRows;      // of a unit's longest run of rows
+    // several turns per block once eight blocks per SM are there without (640 units of 8192 rows: 2 blocks each)
+    f.turns = (int)std::min<long long>(turns, std::max<long long>(1, (long long)a.units * turns / (8 * 148)));
+    f.chunks = (turns + f.turns - 1) / f.turns;
+    f.vec = total_stride % 4 == 0 && (uintptr_t)total_in % 16 == 0 && (uintptr_t)total_out % 16 == 0;
     const dim3 grid((unsigned)(a.units * (f.chunks + a.G)));
     return a.D == 128 ? launch_kernel(weights_finish_kernel<128>, grid, dim3(kFinishThreads), 0, stream, a.programmatic, f)
                       : launch_kernel(weights_finish_kernel<64>, grid, dim3(kFinishThreads), 0, stream, a.programmatic, f);
 }
 
 cudaError_t launch_select(const SelectArgs& a, const SelectCounts& counts, cudaStream_t stream) {
-    const int cached = std::min(kSelectCached, std::max(0, a.n - a.n_recent));
-    select_rows_kernel<<<(unsigned)a.units, kSelectThreads, (size_t)cached * 4, stream>>>(a, counts, cached);
-    return cudaGetLastError();
+    const int old = std::max(0, a.n - a.n_recent);     // of the longest unit
+    // 256 threads up to 2048 rows (latency), then 32 rows per lane: blocks small enough that an SM holds several
+    if (old <= 2048) return launch_select_one<8, true>(a, counts, old, stream);
+    if (old <= 32 * kSelectThreads) return launch_select_one<32, true>(a, counts, old, stream);
+    return launch_select_one<16, false>(a, counts, old, stream);
 }
 
 }  // namespace kvs
