@@ -221,22 +221,23 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
 }
 
 // --------------------------------------------------------------------------------------
-// Combine: one warp per (unit, token, head) of a unit that was cut between teams; the pieces in team order.  Lane c
-// fetches the (max, sum) of piece c, so that all of them take one round trip to L2, and the output vectors follow eight at
-// a time: with one piece after the other (three dependent loads each) 17 pieces took 13 us, now 4.
+// Combine of the units that were cut between teams, per (unit, token, head).  Lane c fetches the (max, sum) of piece c, so
+// that all of them take one round trip to L2, and the output vectors follow eight at a time (one piece after the
+// other, three dependent loads each: 13 us for 17 pieces, now 7).  One warp per item, or (LONG) a block of four warps, warp w with pieces w, w + 4, ..., added in warp order: a fixed order either way.
 // --------------------------------------------------------------------------------------
 constexpr int kTreeCombineWarps = 4;
 
-template <typename T, int D>
+template <typename T, int D, bool LONG>
 __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const __grid_constant__ TreeKernelArgs ka) {
-    constexpr int VEC = D / 32;
+    constexpr int VEC = D / 32, STEP = LONG ? kTreeCombineWarps : 1;
     struct __align__(VEC * 4) Vec {
         float v[VEC];
     };
+    __shared__ float s_max[kTreeCombineWarps], s_den[kTreeCombineWarps], s_acc[LONG ? kTreeCombineWarps : 1][D];
     const TreeArgs& a = ka.a;
     const TreePlan& p = ka.p;
-    const long long item = (long long)blockIdx.x * kTreeCombineWarps + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31, per_unit = a.n_t * a.G;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per_unit = a.n_t * a.G;
+    const long long item = LONG ? blockIdx.x : (long long)blockIdx.x * kTreeCombineWarps + warp;
     const bool there = item < (long long)a.units * per_unit;
     const int u = there ? (int)(item / per_unit) : 0;
     const int q = there ? (int)(item - (long long)u * per_unit) : 0, t = q / a.G, g = q - t * a.G;
@@ -248,21 +249,30 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     const long long first = (long long)u * p.tpu;
     const int c0 = team_of_tile(first, p.T, p.teams), np = team_of_tile(first + nt - 1, p.T, p.teams) - c0 + 1;
     if (np == 1) return;                                         // finished by its one team
-    // piece c of the unit: slot 2 (c0 + c), the first one 2 c0 + 1
-    auto where = [&](int c) { return ((2ll * (c0 + c) + (c == 0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + row; };
+    // this warp's pieces, c = 0 .. mine-1; piece i of the unit: slot 2 (c0 + i), the first one 2 c0 + 1
+    const int w0 = LONG ? warp : 0, mine = (np - w0 + STEP - 1) / STEP;
+    auto where = [&](int c) {
+        const int i = w0 + c * STEP;
+        return ((2ll * (c0 + i) + (i == 0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + row;
+    };
     float M = -1.0e30f;
-    for (int cb = 0; cb < np; cb += 32)
-        if (cb + lane < np) M = fmaxf(M, a.part_ml[where(cb + lane) * 2]);
+    for (int cb = 0; cb < mine; cb += 32)
+        if (cb + lane < mine) M = fmaxf(M, a.part_ml[where(cb + lane) * 2]);
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    if (LONG) {
+        if (lane == 0) s_max[warp] = M;
+        __syncthreads();
+        M = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
+    }
     float den = 0.f, acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-    for (int cb = 0; cb < np; cb += 32) {
-        const float2 ml = cb + lane < np ? *reinterpret_cast<const float2*>(a.part_ml + where(cb + lane) * 2) : make_float2(-1.0e30f, 0.f);
-        const float w = cb + lane < np ? fast_exp2(ml.x - M) : 0.f;
+    for (int cb = 0; cb < mine; cb += 32) {
+        const float2 ml = cb + lane < mine ? *reinterpret_cast<const float2*>(a.part_ml + where(cb + lane) * 2) : make_float2(-1.0e30f, 0.f);
+        const float w = cb + lane < mine ? fast_exp2(ml.x - M) : 0.f;
         den = fmaf(w, ml.y, den);
-        const int cnt = min(32, np - cb);
+        const int cnt = min(32, mine - cb);
         for (int j = 0; j < cnt; j += 8) {
             Vec x[8];
 #pragma unroll
@@ -279,6 +289,19 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     }
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+    if (LONG) {
+        if (lane == 0) s_den[warp] = den;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s_acc[warp][lane * VEC + e] = acc[e];
+        __syncthreads();
+        if (warp != 0) return;
+#pragma unroll
+        for (int w = 1; w < kTreeCombineWarps; ++w) {
+            den += s_den[w];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[e] += s_acc[LONG ? w : 0][lane * VEC + e];
+        }
+    }
     const float inv = den > 0.f || den != den ? 1.0f / den : 0.f;
     const int b = u / a.Hkv, hk = u - b * a.Hkv;
     T* dst = reinterpret_cast<T*>(a.out) + (((long long)b * a.n_t + t) * a.Hq + hk * a.G + g) * D + lane * VEC;
@@ -327,8 +350,12 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* v
 template <typename T, int D>
 cudaError_t launch_combine_one(const TreeKernelArgs& ka, cudaStream_t stream) {
     const long long items = (long long)ka.a.units * ka.a.n_t * ka.a.G;
-    const unsigned grid = (unsigned)((items + kTreeCombineWarps - 1) / kTreeCombineWarps);
-    return launch_kernel(tree_combine_kernel<T, D>, dim3(grid), dim3(kTreeCombineWarps * 32), 0, stream, true, ka);
+    // four warps per item where a unit may have more than 16 pieces and the items are few enough that their latency
+    // counts (one unit of 8192 rows, 64 items: 22.5 us with one warp, 14.5 with four; 2048 items of 20 pieces: 25 and 29)
+    const bool many = ka.p.teams / ka.a.units + 2 > 16 && items <= 8 * 148;
+    const dim3 block(kTreeCombineWarps * 32), grid((unsigned)(many ? items : (items + kTreeCombineWarps - 1) / kTreeCombineWarps));
+    return many ? launch_kernel(tree_combine_kernel<T, D, true>, grid, block, 0, stream, true, ka)
+                : launch_kernel(tree_combine_kernel<T, D, false>, grid, block, 0, stream, true, ka);
 }
 
 }  // namespace
