@@ -137,10 +137,12 @@ __global__ void __launch_bounds__(kRotThreads, 4) append_rotary_kernel(const __g
                 const int tk = i / a.half, pr = i - tk * a.half;
                 double turn = (double)a.positions[tok0 + tk] * a.turns[pr];
                 turn -= rint(turn);
+                // the angle as hi + lo: rounding it to fp32 alone would cost as much again as the functions' own error
+                const float hi = (float)turn, lo = (float)(turn - (double)hi) * 6.2831853f;
                 float sn, cn;
-                sincospif(2.0f * (float)turn, &sn, &cn);
-                cos_t[tk][pr] = cn;
-                sin_t[tk][pr] = sn;
+                sincospif(2.0f * hi, &sn, &cn);
+                cos_t[tk][pr] = fmaf(-sn, lo, cn);
+                sin_t[tk][pr] = fmaf(cn, lo, sn);
             }
             if (threadIdx.x < ntok) {
                 // where the token's row of unit 0 of its sequence goes (a ragged slot adds the unit's length later)

@@ -1,0 +1,102 @@
+"""The serving operators' checks and tables that need no device: refusals before memory is bound, the Rotary table, and
+the reference the GPU tests use against independent restatements."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import operators_reference as ref
+from paper_2410_18517_b200 import Rotary
+from paper_2410_18517_b200 import binding as kb
+from paper_2410_18517_b200 import build as kbuild
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    kbuild.build()
+
+
+def refused(status, fn, *args):
+    with pytest.raises(kb.KvsError) as e:
+        fn(*args)
+    assert e.value.status == status
+
+
+def test_state_and_null_refusals():
+    c = kb.kvs_create(2, 8, 2, 64, 2, 100, kb.KVS_BF16, 0.0, 0)
+    rot = kb.kvs_rotary(0, 0, 1e-6, None)
+    p = 1 << 20                                  # never read: the context has no memory
+    refused(kb.KVS_ERR_STATE, kb.kvs_append_rotary, c, 0, rot, p, 512, p, 128, p, 128, None, None, None, p, 1, 1)
+    refused(kb.KVS_ERR_STATE, kb.kvs_tree_attention, c, 0, p, p, None, 1, 1)
+    refused(kb.KVS_ERR_STATE, kb.kvs_accept_draft, c, p, 1, [1], 1, 1)
+    refused(kb.KVS_ERR_STATE, kb.kvs_decode_attention_weights, c, 0, p, p, None, p, 100, 1)
+    refused(kb.KVS_ERR_STATE, kb.kvs_select_rows, c, 0, p, 100, [1, 1], 0, p, None, 1, 1)
+    kb.kvs_destroy(c)
+    for fn, args in ((kb.kvs_append_rotary, (0, rot, p, 512, p, 128, p, 128, None, None, None, p, 1, 1)), (kb.kvs_tree_attention, (0, p, p, None, 1, 1)),
+                     (kb.kvs_accept_draft, (p, 1, [1], 1, 1)), (kb.kvs_decode_attention_weights, (0, p, p, None, p, 100, 1)),
+                     (kb.kvs_select_rows, (0, p, 100, [1], 0, p, None, 1, 1))):
+        refused(kb.KVS_ERR_INVALID_ARG, fn, None, *args)
+
+
+def test_rotary_table():
+    r = Rotary.from_theta(64, 500000.0, interleaved=True)
+    s = r._struct(1e-5)
+    assert s.rotary_dim == 64 and s.interleaved == 1 and abs(s.eps - 1e-5) < 1e-11
+    assert [s.inv_freq[i] for i in range(32)] == [500000.0 ** (-2.0 * i / 64) for i in range(32)]
+    assert r._struct(1e-5) is s and r._struct(1e-6) is not s
+    assert ctypes.sizeof(kb.kvs_rotary) == 24
+
+
+def test_workspace_serves_every_call():
+    """The scratch of the calls that share the search reductions' bytes fits the workspace of small and of wide shapes."""
+    for Hq, Hkv, D, B, n, dt in ((1, 1, 64, 1, 1, kb.KVS_F32), (64, 8, 128, 4, 300, kb.KVS_BF16), (8, 8, 64, 200, 9000, kb.KVS_BF16)):
+        c = kb.kvs_create(1, Hq, Hkv, D, B, n, dt, 0.0, 0)
+        _, ws = kb.kvs_required_bytes(c)
+        rows = min(128, Hq // Hkv * 64)
+        assert ws >= B * Hq * kb.kvs_row_stride(c) * 4 and ws >= 2 * 320 * rows * (D + 2) * 4
+        kb.kvs_destroy(c)
+
+
+def test_reference_attention_against_torch():
+    g = torch.Generator().manual_seed(0)
+    q, K, V = (torch.randn(*s, generator=g, dtype=torch.float64) for s in ((5, 2, 16), (9, 16), (9, 16)))
+    sees = torch.rand(5, 9, generator=g) < 0.6
+    sees[:, 0] = True
+    out, p, _, _ = ref.attend(q, K, V, sees)
+    want = torch.nn.functional.scaled_dot_product_attention(q.transpose(0, 1), K.expand(2, 9, 16), V.expand(2, 9, 16), attn_mask=sees)
+    assert (out - want.transpose(0, 1)).abs().max() < 1e-12 and (p.sum(-1) - 1).abs().max() < 1e-12
+    out, _, _, _ = ref.attend(q, K, V, torch.zeros(5, 9, dtype=torch.bool))
+    assert not out.any()
+
+
+def test_reference_rotation_is_relative():
+    """Dot products of rotated vectors depend on the distance alone; norms do not change."""
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(1, 2, 1, 32, generator=g, dtype=torch.float64)
+    freq = [100.0 ** (-i / 16) for i in range(16)]
+    for inter in (False, True):
+        dots = []
+        for base in (0, 1000003):
+            y, _ = ref.norm_rope(x, None, torch.tensor([[base, base + 7]]), freq, inter, 0.0)
+            assert (y.norm(dim=-1) - x.norm(dim=-1)).abs().max() < 1e-9
+            dots.append(float((y[0, 0, 0] * y[0, 1, 0]).sum()))
+        assert abs(dots[0] - dots[1]) < 1e-8
+    y, _ = ref.norm_rope(x, torch.ones(32), torch.zeros(1, 2), freq, False, 0.0)
+    assert ((y * y).mean(-1) - 1).abs().max() < 1e-12
+
+
+def test_reference_selection_and_trees():
+    total = [3.0, float("nan"), 3.0, -0.0, 0.0, float("inf"), -1.0, 5.0]
+    assert ref.select(total, 8, 3, 1) == [0, 5, 7] and ref.select(total, 8, 8, 0) == list(range(8))
+    assert ref.select(total, 8, 5, 0) == [0, 2, 3, 5, 7] and ref.select(total, 8, 2, 2) == [6, 7]
+    rng = np.random.default_rng(0)
+    for n_t in (1, 5, 64):
+        words = ref.random_tree(rng, n_t)
+        for t, w in enumerate(words):
+            assert w >> t & 1 and w < 2 << t
+            for j in range(t):
+                assert not (w >> j & 1) or words[j] & ~w == 0          # ancestors bring their own ancestors
+        assert [x & (1 << 64) - 1 for x in ref.to_int64(words)] == words
+    assert math.isclose(ref.weight_error(0.0, 1), 2 * 120 * ref.U + 2 * ref.EXP2 + 2 * ref.U)
