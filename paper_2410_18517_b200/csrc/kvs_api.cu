@@ -911,7 +911,7 @@ kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stri
             if (kvs::launch_accept(kp, kp + ctx->plane_bytes, path, path_stride, counts, b0, seqs, Hkv, n_draft,
                                    was ? -1 : ctx->slot_len[s], becomes ? unit_len_dev(ctx, s) : nullptr, becomes, ctx->row_bytes,
                                    ctx->row_stride, reinterpret_cast<int*>(ctx->ws + ctx->off_status),
-                                   (long long)ctx->plane_bytes, static_cast<cudaStream_t>(stream)) != cudaSuccess)
+                                   (long long)ctx->plane_bytes, take_early_start(ctx), static_cast<cudaStream_t>(stream)) != cudaSuccess)
                 return KVS_ERR_CUDA;
             ctx->seq += 1;
         }
@@ -933,7 +933,6 @@ kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stri
     }
     if (empty) ctx->cur_batch = 0;
     ctx->stats.evict_launches += 1;
-    ctx->counter_written = false;   // a plain launch: full dependency on everything before it
     return KVS_OK;
 }
 

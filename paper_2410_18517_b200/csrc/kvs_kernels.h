@@ -216,7 +216,7 @@ struct AcceptCounts {
 };
 cudaError_t launch_accept(void* kplane, void* vplane, const int* path, int path_stride, const AcceptCounts& counts,
                           int seq0, int seqs, int Hkv, int n_draft, int len, int* unit_len, bool write_len, int row_bytes,
-                          int row_stride, int* status, long long plane_bytes, cudaStream_t stream);
+                          int row_stride, int* status, long long plane_bytes, bool programmatic, cudaStream_t stream);
 
 // Ragged slots (rows evicted by an outside intra-layer method).
 //   launch_evict:   per unit u, rows keep[u*keep_stride + j], j < counts[u], move to rows 0..counts[u]-1

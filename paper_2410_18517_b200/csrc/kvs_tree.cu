@@ -242,6 +242,7 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     const int u = there ? (int)(item / per_unit) : 0;
     const int q = there ? (int)(item - (long long)u * per_unit) : 0, t = q / a.G, g = q - t * a.G;
     const int mt = t / p.tokens, row = (t - mt * p.tokens) * a.G + g;
+    pdl_launch_dependents();
     pdl_wait();
     if (!there) return;
     const int n = a.unit_len ? min(a.unit_len[u], a.capacity) : a.n;
@@ -322,6 +323,7 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* v
                                                            int n_draft, int len, int* unit_len, bool write_len, int row_vecs,
                                                            int row_stride, int* status, long long plane_vecs) {
     __shared__ uint4 buf[kTreeMaxTokens * 32];     // 64 rows of up to 512 bytes
+    pdl_wait();
     const int b = seq0 + blockIdx.x / Hkv, cnt = counts.n[blockIdx.x / Hkv];
     const long long u = (long long)seq0 * Hkv + blockIdx.x;
     // (a slot that becomes ragged with this call has no lengths on the device yet)
@@ -404,11 +406,10 @@ cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* laun
 
 cudaError_t launch_accept(void* kplane, void* vplane, const int* path, int path_stride, const AcceptCounts& counts,
                           int seq0, int seqs, int Hkv, int n_draft, int len, int* unit_len, bool write_len, int row_bytes,
-                          int row_stride, int* status, long long plane_bytes, cudaStream_t stream) {
-    accept_draft_kernel<<<(unsigned)(seqs * Hkv), 256, 0, stream>>>(
-        static_cast<char*>(kplane), static_cast<char*>(vplane), path, path_stride, counts, seq0, Hkv, n_draft, len, unit_len,
-        write_len, row_bytes / 16, row_stride, status, plane_bytes / 16);
-    return cudaGetLastError();
+                          int row_stride, int* status, long long plane_bytes, bool programmatic, cudaStream_t stream) {
+    return launch_kernel(accept_draft_kernel, dim3((unsigned)(seqs * Hkv)), dim3(256), 0, stream, programmatic, static_cast<char*>(kplane),
+                         static_cast<char*>(vplane), path, path_stride, counts, seq0, Hkv, n_draft, len, unit_len, write_len,
+                         row_bytes / 16, row_stride, status, plane_bytes / 16);
 }
 
 }  // namespace kvs

@@ -17,7 +17,8 @@
 // Measured against this layout there: one block per SM whose two softmax groups take a query tile each and share K/V tiles
 // of 128 keys (two thirds of that traffic), 156 us against 147, because a score buffer is free only after the product
 // that reads its weights and S then waits for softmax, PV and S in a row; a quarter of the exp2 by a polynomial on the
-// FMA pipe, 151; two stages per operand instead of the ring of five, 147.
+// FMA pipe, 151; two stages per operand instead of the ring of five, 147; one block per SM with 128-key tiles, two score
+// buffers and two threads per row, 177.
 // P goes into the second contraction as one bf16 term (each weight off by at most 2^-8 of itself, the sum of the weights
 // kept in fp32 from the unrounded ones): the result is rounded to bf16 anyway, and a second term would add half again to the
 // tensor work of wide trees, which the tensor pipe bounds.
