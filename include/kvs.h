@@ -289,8 +289,8 @@ kvs_status kvs_append_rotary(kvs_ctx* ctx, int32_t layer, const kvs_rotary* rot,
  *   q:    device, [batch][n_t][n_q_heads][head_dim], storage type, 16-byte aligned
  *   mask: device, uint64 [batch][n_t]; a draft that is to see itself has its own bit set.  NULL: draft t sees
  *         drafts 0 .. t (a chain)
- *   out:  device, same shape and type as q, 16-byte aligned.  The storage type, not float32 as in
- *         kvs_decode_attention: 64 times the rows go on to the next matrix product in that type
+ *   out:  device, same shape and type as q, 16-byte aligned, not overlapping it.  The storage type, not float32 as
+ *         in kvs_decode_attention: 64 times the rows go on to the next matrix product in that type
  * A draft that sees nothing at all (an empty context and an empty mask) gets zeros.  What a masked draft's rows hold
  * (NaN of a padding token included) does not reach the result.  Works on ragged slots too: a unit's drafts are its
  * own newest n_t rows.
@@ -303,6 +303,7 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
  * to the front of the drafts, bit for bit, and the unit ends behind them.
  *   path:     device, int32 [batch][path_stride], the same for all layers
  *   n_accept: host, int32 [batch], each 0 .. n_draft and at most path_stride
+ * The rejected drafts' rows are cleared (kvs_truncate leaves rows as they are: fine for drafts whose rows are finite).
  * Where all sequences keep the same number a slot stays as it is; otherwise its units differ in length afterwards,
  * as after kvs_evict (kvs_prefill_attention and kvs_truncate then refuse it).  One launch per slot.  A path that is
  * not ascending or out of range cannot be seen by the host: the kernel leaves the row already there and sets the
@@ -316,7 +317,8 @@ kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stri
 
 /* kvs_decode_attention that also adds up how much attention every cached row received:
  *   total_out[b][h][j] = total_in[b][h][j] + sum over the group's G q-heads of softmax_j
- * for every row j the unit holds; what lies behind them in total_out is left as it is.
+ * for every row j the unit holds (a row appended since the last call starts from what total_in holds in its place:
+ * zero it); what lies behind them in total_out is left as it is.
  *   total_in:  device, float32 [batch][n_kv_heads][total_stride], or NULL: zeros
  *   total_out: the same layout; may be total_in itself, must not overlap it otherwise
  *   total_stride: at least the slot's rows (under KVS_OPT_REPLAY: max_seq)

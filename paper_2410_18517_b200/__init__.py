@@ -142,12 +142,17 @@ class SharedKVCache:
         counts = [int(x) for x in self._torch.as_tensor(n_keep).reshape(-1).tolist()]
         binding.kvs_evict(self.ctx, layer, keep, counts, keep.shape[2], keep.shape[0], self._stream())
 
+    def _here(self, *tensors):
+        """Whether the tensors (None: left out) live on the cache's device."""
+        index = self.device.index
+        return all(x is None or x.get_device() == index for x in tensors)
+
     def _token_stride(self, x, heads, batch, n_new):
         """Elements between consecutive tokens of ``[batch][n_new][heads][head_dim]`` (heads contiguous)."""
         D = self.shape[3]
         b, t, h, d = x.shape
         sb, st, sh, sd = x.stride()
-        assert x.dtype is self.dtype and b == batch and t == n_new and h == heads and d == D
+        assert x.dtype is self.dtype and b == batch and t == n_new and h == heads and d == D and self._here(x)
         assert sd == 1 and (sh == D or heads == 1), "a token's heads must be contiguous"
         if t == 1:
             return sb if b > 1 else heads * D
@@ -169,6 +174,7 @@ class SharedKVCache:
                                      positions.shape == q.shape[:2])
         for w in (q_weight, k_weight):
             assert w is None or (w.dtype is self.dtype and w.is_contiguous() and w.numel() == D)
+        assert self._here(positions, q_weight, k_weight, out)
         if out is None:
             out = torch.empty((batch, n_new, Hq, D), dtype=self.dtype, device=self.device)
         else:
@@ -183,6 +189,7 @@ class SharedKVCache:
         torch = self._torch
         assert q.is_contiguous() and q.dtype == self.dtype and q.ndim == 4 and q.shape[2:] == (self.shape[1], self.shape[3])
         assert mask is None or (mask.dtype in (torch.int64, torch.uint64) and mask.is_contiguous() and mask.shape == q.shape[:2])
+        assert self._here(q, mask, out)
         if out is None:
             out = torch.empty_like(q)
         else:
@@ -194,6 +201,7 @@ class SharedKVCache:
         """Keep the accepted drafts in every slot.  path: int32 ``[batch][stride]`` draft numbers, ascending; n_accept:
         how many of them each sequence keeps (host)."""
         assert path.dtype == self._torch.int32 and path.is_contiguous() and path.ndim == 2 and len(n_accept) == path.shape[0]
+        assert self._here(path)
         binding.kvs_accept_draft(self.ctx, path, path.shape[1], [int(x) for x in n_accept], n_draft, path.shape[0], self._stream())
 
     def decode_attention_weights(self, layer, q, total_in, total_out=None, out=None):
@@ -206,9 +214,11 @@ class SharedKVCache:
             total_out = total_in
         for x in (total_in, total_out):
             assert x is None or (x.dtype == torch.float32 and x.is_contiguous() and x.ndim == 3 and x.shape == total_out.shape)
-        assert total_out.shape[:2] == (q.shape[0], self.shape[2])
+        assert total_out.shape[:2] == (q.shape[0], self.shape[2]) and self._here(q, total_in, total_out, out)
         if out is None:
             out = torch.empty(q.shape, dtype=torch.float32, device=self.device)
+        else:
+            assert out.is_contiguous() and out.dtype == torch.float32 and out.shape == q.shape
         binding.kvs_decode_attention_weights(self.ctx, layer, q, out, total_in, total_out, total_out.shape[2], q.shape[0],
                                              self._stream())
         return out
@@ -227,13 +237,19 @@ class SharedKVCache:
             kept_total = torch.zeros(keep.shape, dtype=torch.float32, device=self.device)
         assert keep.is_contiguous() and keep.dtype == torch.int32 and keep.shape[:2] == total.shape[:2]
         assert kept_total.is_contiguous() and kept_total.dtype == torch.float32 and kept_total.shape == keep.shape
+        assert self._here(total, keep, kept_total)
         binding.kvs_select_rows(self.ctx, layer, total, total.shape[2], counts, n_recent, keep, kept_total, keep.shape[2],
                                 total.shape[0], self._stream())
         return keep, kept_total
 
-    def evict_by_weight(self, layer, total, n_keep, n_recent):
-        """``select_rows`` and ``evict`` in one: the layer's slot keeps n_keep rows per unit.  Returns their totals."""
-        keep, kept = self.select_rows(layer, total, n_keep, n_recent)
+    def evict_by_weight(self, layer, total, n_keep, n_recent, stride=None):
+        """``select_rows`` and ``evict`` in one: the layer's slot keeps n_keep rows per unit.  Returns their totals,
+        zeros behind them up to ``stride`` entries per unit (None: the largest n_keep; the slot's capacity leaves room
+        for rows appended later)."""
+        keep = None
+        if stride is not None:
+            keep = self._torch.zeros(*total.shape[:2], stride, dtype=self._torch.int32, device=self.device)
+        keep, kept = self.select_rows(layer, total, n_keep, n_recent, keep)
         self.evict(layer, keep, n_keep)
         return kept
 

@@ -832,6 +832,7 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
     if (layer < 0 || layer >= ctx->cfg.n_layers || !q || !out) return KVS_ERR_INVALID_ARG;
     if (batch < 1 || batch > ctx->cfg.max_batch || n_t < 1 || n_t > kvs::kTreeMaxTokens) return KVS_ERR_INVALID_ARG;
     if (((uintptr_t)q % 16) != 0 || ((uintptr_t)out % 16) != 0 || ((uintptr_t)mask % 8) != 0) return KVS_ERR_INVALID_ARG;
+    if (q == out) return KVS_ERR_INVALID_ARG;   // one block's result would overwrite another's queries
     const int slot = ctx->slot_of_layer[layer];
     if (ctx->slot_len[slot] == 0) return KVS_ERR_STATE;
     if (batch > ctx->cur_batch || !holds_rows(ctx, slot, batch, n_t)) return KVS_ERR_INVALID_ARG;
@@ -898,11 +899,23 @@ kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stri
             for (int u = 0; u < units; ++u)
                 if (unit_rows(ctx, s, u) - n_draft + n_accept[u / Hkv] < 1) return KVS_ERR_INVALID_ARG;
     }
+    // the lengths of the slots whose units will differ, before anything is launched
+    std::vector<std::vector<int32_t>> lens;
+    try {
+        lens.resize(ctx->n_slots);
+        for (int s = 0; s < ctx->n_slots; ++s) {
+            if (same && !ctx->ragged[s]) continue;
+            lens[s].assign((size_t)ctx->cfg.max_batch * Hkv, 0);
+            for (int u = 0; u < units; ++u) lens[s][u] = unit_rows(ctx, s, u) - n_draft + n_accept[u / Hkv];
+        }
+    } catch (const std::bad_alloc&) {
+        return KVS_ERR_OOM;
+    }
     DeviceGuard guard(ctx->cfg.device);
     if (!guard.ok) return KVS_ERR_CUDA;
     bool empty = true;
     for (int s = 0; s < ctx->n_slots; ++s) {
-        const bool was = ctx->ragged[s] != 0, becomes = was || !same;
+        const bool was = ctx->ragged[s] != 0, becomes = !lens[s].empty();
         char* kp = ctx->pool + (size_t)(2 * s) * ctx->plane_bytes;
         for (int b0 = 0; b0 < batch; b0 += kvs::AcceptCounts::kMax) {
             const int seqs = std::min(batch - b0, (int)kvs::AcceptCounts::kMax);
@@ -916,15 +929,9 @@ kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stri
             ctx->seq += 1;
         }
         if (becomes) {
-            std::vector<int32_t> lens((size_t)ctx->cfg.max_batch * Hkv, 0);
-            int longest = 0;
-            for (int u = 0; u < units; ++u) {
-                lens[u] = unit_rows(ctx, s, u) - n_draft + n_accept[u / Hkv];
-                longest = std::max(longest, lens[u]);
-            }
-            ctx->unit_len_host[s] = lens;
+            ctx->unit_len_host[s].swap(lens[s]);
             ctx->ragged[s] = 1;
-            ctx->slot_len[s] = longest;
+            ctx->slot_len[s] = *std::max_element(ctx->unit_len_host[s].begin(), ctx->unit_len_host[s].begin() + units);
         } else {
             ctx->slot_len[s] += n_accept[0] - n_draft;
         }

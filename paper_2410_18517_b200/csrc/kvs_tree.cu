@@ -316,7 +316,8 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
 // --------------------------------------------------------------------------------------
 // Accepted drafts: rows base + path[i] -> base + i of every unit, i < n_acc (path strictly ascending: path[i] >= i).
 // One block per unit; all of a unit's rows go through shared memory, K and then V, so that no row is read after it was
-// written.  An entry that is not ascending or out of range sets the status word to 1 and keeps the row already there.
+// written.  The rows of the rejected drafts are cleared: what lies past a unit's end stays finite, whatever they held.  An
+// entry that is not ascending or out of range sets the status word to 1 and keeps the row already there.
 // --------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* vplane, const int* __restrict__ path, int path_stride,
                                                            const __grid_constant__ AcceptCounts counts, int seq0, int Hkv,
@@ -345,6 +346,8 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* v
         __syncthreads();
         for (int i = threadIdx.x; i < cnt * row_vecs; i += blockDim.x)
             if (KVS_BOUNDS_OK((u * row_stride + base) * (long long)row_vecs + i, 1, plane_vecs, status)) rows[i] = buf[i];
+        for (int i = cnt * row_vecs + threadIdx.x; i < n_draft * row_vecs; i += blockDim.x)
+            if (KVS_BOUNDS_OK((u * row_stride + base) * (long long)row_vecs + i, 1, plane_vecs, status)) rows[i] = make_uint4(0u, 0u, 0u, 0u);
     }
     if (write_len && threadIdx.x == 0) unit_len[u] = base + cnt;
 }
@@ -356,8 +359,8 @@ cudaError_t launch_combine_one(const TreeKernelArgs& ka, cudaStream_t stream) {
     // counts (one unit of 8192 rows, 64 items: 22.5 us with one warp, 14.5 with four; 2048 items of 20 pieces: 25 and 29)
     const bool many = ka.p.teams / ka.a.units + 2 > 16 && items <= 8 * 148;
     const dim3 block(kTreeCombineWarps * 32), grid((unsigned)(many ? items : (items + kTreeCombineWarps - 1) / kTreeCombineWarps));
-    return many ? launch_kernel(tree_combine_kernel<T, D, true>, grid, block, 0, stream, true, ka)
-                : launch_kernel(tree_combine_kernel<T, D, false>, grid, block, 0, stream, true, ka);
+    return many ? launch_kernel(tree_combine_kernel<T, D, true>, grid, block, 0, stream, ka.a.programmatic, ka)
+                : launch_kernel(tree_combine_kernel<T, D, false>, grid, block, 0, stream, ka.a.programmatic, ka);
 }
 
 }  // namespace

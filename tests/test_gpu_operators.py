@@ -339,6 +339,29 @@ def test_accept_reports_a_bad_path():
     cache.check_canaries()
 
 
+@pytest.mark.parametrize("how", ["accept", "truncate"])
+@pytest.mark.parametrize("dtype,Hq", [("bf16", 8), ("bf16", 2), ("f32", 8)])
+def test_broken_drafts_leave_no_trace(how, dtype, Hq):
+    """Padding drafts whose rows are NaN, rejected or rolled back: the rows past the end share the last tile with rows that
+    decode attention reads."""
+    cache, _, _ = filled(Hq, 2, 128, 2, 70, dtype, extra=12)
+    good = normal(5, dtype, 2, 3, 2, 128)
+    bad = torch.full((2, 6, 2, 128), float("nan"), dtype=DT[dtype], device="cuda")
+    rows = torch.cat((good, bad), 1)
+    cache.append(0, rows, rows)
+    if how == "accept":
+        cache.accept_draft(torch.arange(3).int().expand(2, 3).contiguous().cuda(), [3, 3], 9)
+        assert torch.isfinite(cache.plane(0, 0)[:2, :, :80].float()).all() and torch.isfinite(cache.plane(0, 1)[:2, :, :80].float()).all()
+    else:
+        cache.truncate(73)
+    q = normal(6, dtype, 2, Hq, 128)
+    total = torch.zeros(2, 2, 82, device="cuda")
+    out = cache.decode_attention_weights(0, q, total)
+    check_weights(cache, 0, q, torch.zeros_like(total), total, out, 82)
+    assert torch.allclose(out, cache.decode_attention(0, q), rtol=0, atol=2e-5)
+    check_tree(cache, 0, q[:, None].contiguous(), [[1]] * 2, cache.tree_attention(0, q[:, None].contiguous()))
+
+
 # ------------------------------------------------------------------------------------------ rotary append
 
 def check_rotary(got, x, w, pos, inv_freq, interleaved, eps):
@@ -628,6 +651,15 @@ def test_select_odd_values():
         _select_case(cache, total, [[k]], 0)
 
 
+def test_select_on_ragged_units():
+    cache, _, _ = filled(4, 2, 64, 2, 300, "bf16", extra=9)
+    keep = torch.arange(300, dtype=torch.int32).expand(2, 2, 300).contiguous().cuda()
+    cache.evict(0, keep, [[1, 300], [33, 150]])
+    total = torch.rand(2, 2, 309, generator=torch.Generator().manual_seed(2)).cuda()
+    _select_case(cache, total, [[1, 40], [33, 7]], 1)
+    _select_case(cache, total, [[1, 300], [2, 150]], 0)
+
+
 def test_select_more_units_than_one_launch_takes():
     B, Hkv, n = 60, 16, 40                                               # 960 units
     cache = SharedKVCache(1, 16, 16, 64, B, n, "bf16")
@@ -644,7 +676,8 @@ def test_evict_by_weight_keeps_what_the_selection_says():
     for i in range(3):
         cache.decode_attention_weights(0, normal(40 + i, "bf16", B, Hq, D), total)
     counts = [[100, 37], [400, 64]]
-    kept = cache.evict_by_weight(0, total, counts, 16)
+    kept = cache.evict_by_weight(0, total, counts, 16, stride=n + 3)
+    assert kept.shape == (B, Hkv, n + 3)
     for b in range(B):
         for h in range(Hkv):
             rows = ref.select(total[b, h].tolist(), n, counts[b][h], 16)
@@ -791,9 +824,10 @@ def test_refusals_leave_everything_as_it_was():
     pool = cache.pool.clone()
 
     t = kb.kvs_tree_attention
-    for args in ((2, p, p, p, 2, 4), (-1, p, p, p, 2, 4), (0, None, p, p, 2, 4), (0, p, None, p, 2, 4), (0, p + 2, p, p, 2, 4),
-                 (0, p, p + 8, p, 2, 4), (0, p, p, p + 4, 2, 4), (0, p, p, p, 3, 4), (0, p, p, p, 0, 4), (0, p, p, p, 4, 4),
-                 (0, p, p, p, 2, 0), (0, p, p, p, 2, 65), (0, p, p, p, 2, 21)):
+    r_ = p + 65536
+    for args in ((2, p, r_, p, 2, 4), (-1, p, r_, p, 2, 4), (0, None, r_, p, 2, 4), (0, p, None, p, 2, 4), (0, p + 2, r_, p, 2, 4),
+                 (0, p, r_ + 8, p, 2, 4), (0, p, r_, p + 4, 2, 4), (0, p, r_, p, 3, 4), (0, p, r_, p, 0, 4), (0, p, r_, p, 4, 4),
+                 (0, p, p + 65536, p, 2, 0), (0, p, p + 65536, p, 2, 65), (0, p, p + 65536, p, 2, 21), (0, p, p, p, 2, 4)):
         refused(A, t, c, *args)
 
     f = kb.kvs_accept_draft
@@ -836,7 +870,7 @@ def test_refusals_leave_everything_as_it_was():
         refused(A, s, c, *args)
 
     cache.set_option(KVS_OPT_REPLAY, 1)
-    refused(S, t, c, 0, p, p, p, 2, 4)
+    refused(S, t, c, 0, p, r_, p, 2, 4)
     refused(S, f, c, p, 4, [1, 1], 4, 2)
     refused(S, s, c, 0, p, 20, [1] * 4, 0, o, None, 20, 2)
     refused(A, d, c, 0, p, o, None, o, 20, 2)           # a recorded step needs totals for max_seq rows
@@ -846,10 +880,26 @@ def test_refusals_leave_everything_as_it_was():
     assert torch.equal(pool, cache.pool) and cache.seq_len(0) == 20 and cache.device_status() == 0
 
 
+def test_tensors_of_another_device_are_refused():
+    cache, _, _ = filled(8, 2, 64, 2, 20, "bf16", extra=4)
+    q = normal(1, "bf16", 2, 1, 8, 64)
+    kv = normal(2, "bf16", 2, 1, 2, 64)
+    pos = torch.zeros(2, 1, dtype=torch.int32)
+    total = torch.zeros(2, 2, 24)
+    rot = Rotary.from_theta(64)
+    for call in (lambda: cache.append_rotary(0, q, kv, kv, pos, rot), lambda: cache.append_rotary(0, q.cpu(), kv, kv, pos.cuda(), rot),
+                 lambda: cache.append_rotary(0, q, kv, kv.cpu(), pos.cuda(), rot), lambda: cache.tree_attention(0, q.cpu()),
+                 lambda: cache.tree_attention(0, q, torch.zeros(2, 1, dtype=torch.int64)), lambda: cache.accept_draft(pos, [1, 1], 1),
+                 lambda: cache.decode_attention_weights(0, q[:, 0].contiguous(), total), lambda: cache.select_rows(0, total, [[1, 1]] * 2, 0)):
+        with pytest.raises(AssertionError):
+            call()
+    assert cache.seq_len(0) == 20
+
+
 def test_refusals_on_empty_slots():
     cache, _, _ = filled(8, 2, 64, 2, 0, "bf16", extra=4)
     p = torch.zeros(4096, dtype=torch.uint8, device="cuda").data_ptr()
-    refused(kb.KVS_ERR_STATE, kb.kvs_tree_attention, cache.ctx, 0, p, p, None, 2, 1)
+    refused(kb.KVS_ERR_STATE, kb.kvs_tree_attention, cache.ctx, 0, p, p + 2048, None, 2, 1)
     refused(kb.KVS_ERR_STATE, kb.kvs_accept_draft, cache.ctx, p, 4, [1, 1], 1, 2)
     refused(kb.KVS_ERR_STATE, kb.kvs_decode_attention_weights, cache.ctx, 0, p, p, None, p, 4, 2)
     refused(kb.KVS_ERR_STATE, kb.kvs_select_rows, cache.ctx, 0, p, 4, [1] * 4, 0, p, None, 4, 2)
