@@ -473,6 +473,17 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
             for (int blk = 0; blk < BPW; ++blk) {
                 const int tok0 = (warp * BPW + blk) * 16;
                 if (tok0 >= valid) continue;
+                if (tok0 + 16 > valid) {
+                    // The last block of a unit: value rows past the end may hold anything (0 * NaN is not 0), so they are
+                    // cleared in the staged tile, which only this warp reads here; the fence orders the stores before
+                    // the copy that refills the stage.
+                    for (int i = lane; i < 16 * S::HALVES * 8; i += 32) {
+                        const int r = tok0 + (i >> 3) / S::HALVES, half = (i >> 3) % S::HALVES;
+                        if (r >= valid) *reinterpret_cast<uint4*>(const_cast<unsigned char*>(ks) + kTile + half * (TN * 128) + r * 128 + (i & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
                 // P = P_hi + P_lo as A fragments (k = tokens): klo = tokens 0..7, khi = tokens 8..15
                 const float h00 = bf16_round(p[blk][0][0]), h01 = bf16_round(p[blk][0][1]);
                 const float h10 = bf16_round(p[blk][1][0]), h11 = bf16_round(p[blk][1][1]);
@@ -488,10 +499,6 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
                 }
                 // Four column blocks at a time: their P_hi products are issued before their P_lo products, so
                 // that an MMA never waits for the one just before it (same accumulator).
-                // In the last block of a unit this lane's tokens quad * 2, quad * 2 + 1 (and 8 further on) may lie past its end.
-                const int left = valid - tok0;
-                const uint32_t keep0 = (quad * 2 < left ? 0xffffu : 0u) | (quad * 2 + 1 < left ? 0xffff0000u : 0u);
-                const uint32_t keep1 = (quad * 2 + 8 < left ? 0xffffu : 0u) | (quad * 2 + 9 < left ? 0xffff0000u : 0u);
                 const int t = tok0 + (((lane >> 3) & 1) << 3) + (lane & 7);
                 const uint32_t rowaddr = vs_u32 + t * 128;
                 const int sw = t & 7;
@@ -504,10 +511,6 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
                         const int half = chunkg >> 3;
                         const int chunk = chunkg & 7;
                         ldmatrix_x4_trans(b[x], rowaddr + half * (TN * 128) + ((chunk ^ sw) << 4));
-                        if (left < 16) {      // rows past the unit's end may hold anything: 0 * NaN is not 0
-                            b[x][0] &= keep0; b[x][2] &= keep0;
-                            b[x][1] &= keep1; b[x][3] &= keep1;
-                        }
                     }
 #pragma unroll
                     for (int x = 0; x < 2; ++x) {
