@@ -45,10 +45,10 @@ FALLBACK_HBM_GBS = 6650.0
 # of the captured launch; traffic grows in proportion to it, so the bench scales by that
 # ratio.  A record is used only while the kernel sources still hash to `sha256`.
 NCU_TRAFFIC = {
-    1: {"files": ("kvs_kernels.cu", "kvs_device.cuh"), "dram_bytes": 1557.51e6, "kv_bytes": 1552.55e6,
-        "sha256": "a6b6b4437657743776030cf2ad57be5b9385213ccd1d31712ac119e110e59e81"},
-    2: {"files": ("kvs_mma.cu", "kvs_device.cuh"), "dram_bytes": 541.22e6, "kv_bytes": 536.90e6,
-        "sha256": "e8e9a2c490fd7d0a26c8ceb3a470e7f81085cdd57c3752f23dd2b1a41da37fca"},
+    1: {"files": ("kvs_kernels.cu", "kvs_device.cuh"), "dram_bytes": 1558.49e6, "kv_bytes": 1552.55e6,
+        "sha256": "4e9e2db4a1d641464cd5a2542d77d47eccbeeee4092bf9641ecce864faec99d3"},
+    2: {"files": ("kvs_mma.cu", "kvs_device.cuh"), "dram_bytes": 541.89e6, "kv_bytes": 536.90e6,
+        "sha256": "949ae9641d02cdb5efbd95dd34539e87157c5e24b7ce905ee82dfac38fa6746a"},
 }
 
 

@@ -10,15 +10,16 @@
 //                      tile t), O += P V with P as bf16 read from tensor memory.  The whole warp walks the tiles and an
 //                      elected lane issues: operands are then in uniform registers (issued from a one-lane branch the
 //                      sixteen MMAs of a 128-key tile took 1700 cycles instead of 1200)
-// Bound: up to 128 query rows per kv-head HBM (32 heads, B = 8, n = 4096, 16 drafts: 537 MB in 85 us, 6.3 TB/s); above
-// that shared memory: a 64-key tile costs 32 KiB of copies, 48 KiB of S operands (Q is read again for every tile) and
-// 16 KiB of V, 768 cycles at 128 bytes a cycle, 1536 for the two blocks of an SM, of the 2000 that a tile takes (32q/8kv,
-// B = 4, n = 32768, 64 drafts: 256 rows per kv-head, 137 us).
-// Measured against this layout there: one block per SM whose two softmax groups take a query tile each and share K/V tiles
-// of 128 keys (two thirds of that traffic), 156 us against 147, because a score buffer is free only after the product
-// that reads its weights and S then waits for softmax, PV and S in a row; a quarter of the exp2 by a polynomial on the
-// FMA pipe, 151; two stages per operand instead of the ring of five, 147; one block per SM with 128-key tiles, two score
-// buffers and two threads per row, 177.
+// Bound: up to 128 query rows per kv-head HBM (32 heads, B = 8, n = 4096, 16 drafts: 537 MB in 85 us, 6.3 TB/s).  Above
+// that no single unit is full: at 256 rows (32q/8kv, B = 4, n = 32768, 64 drafts: 133 us, 1.03 PFLOP/s) the tensor pipe and
+// the special-function unit are busy 59 % of the time each, a softmax warp's 64 keys take 1700 cycles of which the
+// exponentials alone are 820 beside the other block's, and an S product of 64 keys reads 6 KiB of shared memory per
+// 32 tensor cycles, more than the 128 bytes a cycle there are (Q is read again for every tile).
+// Measured against this layout at 256 rows, where it takes 147 us with the combine step: one block per SM whose two softmax
+// groups take a query tile each and share K/V tiles of 128 keys, 156 us (a score buffer is free only after the product
+// that reads its weights, and S then waits for softmax, PV and S in a row); one block per SM with 128-key tiles, two
+// score buffers and two threads per row, 177; a quarter of the exp2 by a polynomial on the FMA pipe, 151; two stages per
+// operand instead of the ring of five, 147; K/V fetched before the wait for the previous kernel, 150.
 // P goes into the second contraction as one bf16 term (each weight off by at most 2^-8 of itself, the sum of the weights
 // kept in fp32 from the unrounded ones): the result is rounded to bf16 anyway, and a second term would add half again to the
 // tensor work of wide trees, which the tensor pipe bounds.
