@@ -235,6 +235,7 @@ cudaError_t init_device_once(int device) {
         g_init_err[device] = kvs::init_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_mma_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_prefill_kernels();
+        if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_rotary_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_tree_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_weights_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = resolve_static_scratch(device);
@@ -798,6 +799,7 @@ kvs_status kvs_append_rotary(kvs_ctx* ctx, int32_t layer, const kvs_rotary* rot,
     r.rotary_dim = rot->rotary_dim;
     r.interleaved = rot->interleaved != 0;
     r.eps = rot->eps;
+    r.sm_count = ctx->sm_count;
     r.status = reinterpret_cast<int*>(ctx->ws + ctx->off_status);
     if (!sharing) {
         r.k = k;

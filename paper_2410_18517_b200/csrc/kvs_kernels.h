@@ -137,8 +137,10 @@ struct RotaryArgs {
     int rotary_dim;           // 0: no rotation
     bool interleaved;
     float eps;
+    int sm_count;
     bool programmatic;
 };
+cudaError_t init_rotary_kernels();
 cudaError_t launch_append_rotary(const RotaryArgs& r, cudaStream_t stream);
 
 // Attention of a tree of drafted tokens (see kvs_tree.cu).  The n_t queries of a sequence are the newest n_t rows

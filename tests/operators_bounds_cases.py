@@ -43,6 +43,8 @@ def main():
         for n, n_t in ((1, 1), (63, 2), (64, 64), (125, 17), (700, 33)):
             for ctas in (0, 3):
                 step(*shape, n, n_t, ctas)
+    t.test_append_rotary_of_long_prompts(*t.ROT_LONG[0])
+    t.test_append_rotary_of_long_prompts(*t.ROT_LONG[3])
     print("ALL OPERATOR BOUNDS CASES PASSED", kb.LIB_PATH)
     return 0
 

@@ -407,6 +407,44 @@ def test_append_rotary(dtype, Hq, Hkv, D, B, n0, n_new, dim, inter, norm, fused,
     cache.check_canaries()
 
 
+# long prompts: token rows of 8 KB and more, several hundred tokens
+ROT_LONG = [
+    ("bf16", 32, 8, 128, 2, 3, 1801, 128, False, True, True, 0), ("bf16", 40, 40, 128, 1, 1, 900, 128, True, True, False, 7),
+    ("bf16", 49, 7, 64, 1, 0, 1333, 32, True, True, True, 0), ("f32", 14, 7, 128, 3, 5, 700, 96, False, False, True, 100000),
+    ("f32", 8, 8, 128, 1, 0, 1000, 0, False, True, False, 0), ("bf16", 128, 16, 128, 1, 0, 907, 128, False, True, True, 0),
+    ("bf16", 128, 128, 128, 1, 0, 901, 128, False, True, True, 0),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,B,n0,n_new,dim,inter,norm,fused,first", ROT_LONG)
+def test_append_rotary_of_long_prompts(dtype, Hq, Hkv, D, B, n0, n_new, dim, inter, norm, fused, first):
+    test_append_rotary(dtype, Hq, Hkv, D, B, n0, n_new, dim, inter, norm, fused, first)
+
+
+def test_append_rotary_of_long_prompts_in_place_on_sharing_layers_and_ragged_slots():
+    B, n, Hq, Hkv, D = 2, 611, 32, 4, 128
+    freq = [10000.0 ** (-i / 64) for i in range(64)]
+    pos = (torch.arange(n)[None] + 11 * torch.arange(B)[:, None]).int().cuda()
+    cache, k0, v0 = filled(Hq, Hkv, D, B, 20, "bf16", extra=n + 2, L=2, share_map=[0, 0])
+    keep = torch.arange(20, dtype=torch.int32).expand(B, Hkv, 20).contiguous().cuda()
+    kept = [[3, 20, 1, 9], [7, 11, 20, 2]]
+    cache.evict(0, keep, kept)
+    q, k, v = (normal(i, "bf16", B, n, h, D) for i, h in ((3, Hq), (4, Hkv), (5, Hkv)))
+    w = normal(6, "bf16", D)
+    x = q.clone()
+    cache.append_rotary(0, x, k, v, pos, Rotary(freq), w, None, out=x)
+    check_rotary(x, q, w, pos, freq, False, 1e-6)
+    assert torch.equal(cache.append_rotary(1, q, None, None, pos, Rotary(freq), w), x)
+    for b in range(B):
+        for h in range(Hkv):
+            K, V = rows_of(cache, 0, b, h)
+            m = kept[b][h]
+            assert K.shape[0] == m + n and torch.equal(V[m:], v[b, :, h]) and torch.equal(K[:m], k0[b, :m, h])
+            check_rotary(K[None, m:, None], k[b:b + 1, :, h:h + 1], None, pos[b:b + 1], freq, False, 1e-6)
+    assert cache.device_status() == 0
+    cache.check_canaries()
+
+
 def test_append_rotary_in_place_and_one_weight_only():
     cache, _, _ = filled(8, 2, 128, 2, 4, "bf16", extra=8)
     q, k, v = (normal(i, "bf16", 2, 3, h, 128) for i, h in ((1, 8), (2, 2), (3, 2)))
