@@ -53,6 +53,7 @@ class SharedKVCache:
 
         self._torch = torch
         self.device = torch.device("cuda", device)
+        self._index = device
         # the current stream's handle without a Stream object around it, where this torch has it
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         self.dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
@@ -93,7 +94,7 @@ class SharedKVCache:
 
     def _stream(self) -> int:
         if self._raw_stream is not None:
-            return self._raw_stream(self.device.index)
+            return self._raw_stream(self._index)
         return self._torch.cuda.current_stream(self.device).cuda_stream
 
     def append(self, layer, k=None, v=None, batch=None, n_new=None):
@@ -144,19 +145,21 @@ class SharedKVCache:
 
     def _here(self, *tensors):
         """Whether the tensors (None: left out) live on the cache's device."""
-        index = self.device.index
-        return all(x is None or x.get_device() == index for x in tensors)
+        index = self._index
+        for x in tensors:
+            if x is not None and x.get_device() != index:
+                return False
+        return True
 
     def _token_stride(self, x, heads, batch, n_new):
         """Elements between consecutive tokens of ``[batch][n_new][heads][head_dim]`` (heads contiguous)."""
         D = self.shape[3]
-        b, t, h, d = x.shape
+        assert x.shape == (batch, n_new, heads, D) and x.dtype is self.dtype and x.get_device() == self._index
         sb, st, sh, sd = x.stride()
-        assert x.dtype is self.dtype and b == batch and t == n_new and h == heads and d == D and self._here(x)
         assert sd == 1 and (sh == D or heads == 1), "a token's heads must be contiguous"
-        if t == 1:
-            return sb if b > 1 else heads * D
-        assert b == 1 or sb == t * st, "tokens of all sequences must be evenly spaced"
+        if n_new == 1:
+            return sb if batch > 1 else heads * D
+        assert batch == 1 or sb == n_new * st, "tokens of all sequences must be evenly spaced"
         return st
 
     def append_rotary(self, layer, q, k, v, positions, rotary, q_weight=None, k_weight=None, eps=1e-6, out=None):
