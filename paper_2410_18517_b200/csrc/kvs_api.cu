@@ -982,6 +982,7 @@ kvs_status kvs_select_rows(kvs_ctx* ctx, int32_t layer, const float* total, int3
     a.n = ctx->slot_len[slot];
     a.unit_len = ctx->ragged[slot] ? unit_len_dev(ctx, slot) : nullptr;
     a.n_recent = n_recent;
+    a.sm_count = ctx->sm_count;
     for (int u0 = 0; u0 < units; u0 += kvs::SelectCounts::kMax) {
         a.unit0 = u0;
         a.units = std::min(units - u0, (int)kvs::SelectCounts::kMax);

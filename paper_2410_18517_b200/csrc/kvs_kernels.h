@@ -207,6 +207,7 @@ struct SelectArgs {
     const int* unit_len;
     int n_recent;
     int unit0, units;         // units of this launch
+    int sm_count;
 };
 cudaError_t init_weights_kernels();
 cudaError_t launch_select(const SelectArgs& a, const SelectCounts& counts, cudaStream_t stream);

@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
 // totals; equal totals go to the older row, NaN counts below everything.  The list comes out ascending.
 // Radix select on order-preserving 32-bit keys, 11 + 11 + 10 bits from the top, by histograms in shared memory: after three
 // passes the key of the last row kept is known exactly, and how many rows with that very key stay.  One block per
-// unit; a warp owns IPT * 32 neighbouring rows, lane l the rows 32 i + l, in registers: loads and stores are
+// unit, or a cluster of blocks where units are few and long; a warp owns IPT * 32 neighbouring rows, lane l the rows 32 i + l, in registers: loads and stores are
 // contiguous, and one vote orders 32 rows.  What pads a unit's end has the lowest key and the highest row numbers, so it
 // is never reached.  Bound: instruction issue, some 40 for 32 rows.
 // (Keys in shared memory and a list of the first bin's keys for the later passes: 100 for 32 rows, 53 us for 640 units
@@ -151,6 +151,7 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
 // --------------------------------------------------------------------------------------
 constexpr int kSelectThreads = 1024;
 constexpr int kSelectBins = 2048;
+constexpr int kSelectCluster = 8;
 
 __device__ __forceinline__ uint32_t order_key(float x) {
     if (x != x) return 0u;                            // NaN: below minus infinity (whose key is 0x007fffff)
@@ -165,18 +166,49 @@ __device__ __forceinline__ float total_of(uint32_t key, const float* from) {
     return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key);
 }
 
-// IPT: rows per lane.  ONE: a unit fits one tile of blockDim.x * IPT rows, which stays in registers; otherwise (units of
-// more than 32768 rows) the tiles are read again for every step.
-template <int IPT, bool ONE>
-__global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const SelectArgs a, const __grid_constant__ SelectCounts counts) {
-    __shared__ int hist[kSelectBins];
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// The same place of another block's shared memory.
+__device__ __forceinline__ uint32_t in_block(const void* p, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ int4 ld_cluster4(uint32_t at) {
+    int4 v;
+    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_cluster4(uint32_t at, const int4& v) {
+    asm volatile("st.shared::cluster.v4.s32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ int2 ld_cluster2(uint32_t at) {
+    int2 v;
+    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
+}
+
+// IPT: rows per lane.  SPREAD: the blocks of a cluster share a unit, block r takes the r-th tile of blockDim.x * IPT rows.  Each sums
+// its share of the digits over all blocks' histograms and hands all blocks the sums (every block summing every digit: 16.4
+// us instead of 12.6 for eight blocks on 32768 rows); before it writes it takes the earlier blocks' counts.
+// ONE: a unit fits the tile (or the cluster's tiles), which stays in registers; otherwise the tiles are read again for every
+// step.
+template <int IPT, bool ONE, bool SPREAD>
+__global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const SelectArgs a, const __grid_constant__ SelectCounts counts, int cluster) {
+    static_assert(ONE || !SPREAD, "a cluster's blocks take one tile each");
+    // (a spread unit's passes have a histogram each: the other blocks may still read the last one's)
+    __shared__ __align__(16) int hists[SPREAD ? 3 : 1][kSelectBins];
+    __shared__ __align__(16) int merged[SPREAD ? kSelectBins : 4];
     __shared__ int warp_gt[32], warp_eq[32];
+    __shared__ __align__(8) int block_counts[2];
     __shared__ uint32_t s_prefix;
     __shared__ int s_need;
-    const long long u = a.unit0 + blockIdx.x;
+    const int unit = SPREAD ? blockIdx.x / cluster : blockIdx.x, rank = SPREAD ? blockIdx.x - unit * cluster : 0;
+    const long long u = a.unit0 + unit;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, threads = blockDim.x, warps = threads >> 5;
     const int n = a.unit_len ? a.unit_len[u] : a.n;
-    const int want = counts.n[blockIdx.x] - a.n_recent;     // rows chosen by total
+    const int want = counts.n[unit] - a.n_recent;     // rows chosen by total
     const int old = n - a.n_recent;                         // rows they are chosen from
     const float* total = a.total + u * a.total_stride;
     const int tile = threads * IPT, first = warp * 32 * IPT + lane;
@@ -190,8 +222,8 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
 #pragma unroll
         for (int i = 0; i < IPT; ++i) key[i] = order_key(__uint_as_float(key[i]));
     };
-    // the digit of the `need`-th largest key in hist[0 .. 2^bits): called by warp 0
-    auto find = [&](uint32_t prefix, int low, int bits) {
+    // the digit of the s_need-th largest key in hist[0 .. 2^bits): called by warp 0
+    auto find = [&](const int* hist, uint32_t prefix, int low, int bits) {
         // lane i first sums the 64 (32) digits of the i-th largest run, then the warp looks into the run it is in
         const int run = 1 << (bits - 5), need = s_need;
         int top0 = (1 << bits) - 1, before = 0;                      // digits top0, top0 - 1, ...; rows above them
@@ -218,22 +250,39 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
         }
     };
     if (want > 0) {
-        if (ONE) load(0);
+        if (ONE) load(rank * tile);
         if (tid == 0) s_need = want;
         uint32_t prefix = 0;
 #pragma unroll
         for (int pass = 0; pass < 3; ++pass) {
             const int low = pass == 0 ? 21 : (pass == 1 ? 10 : 0), bits = pass == 2 ? 10 : 11;
+            int* hist = hists[SPREAD ? pass : 0];
             for (int i = tid; i < kSelectBins; i += threads) hist[i] = 0;
             __syncthreads();
-            for (int base = 0; base < old; base += tile) {
+            for (int base = 0; base < (ONE ? 1 : old); base += tile) {
                 if (!ONE) load(base);
 #pragma unroll
                 for (int i = 0; i < IPT; ++i)
                     if (pass == 0 || (key[i] ^ prefix) >> (low + bits & 31) == 0u) atomicAdd(&hist[key[i] >> low & ((1u << bits) - 1u)], 1);
             }
+            if constexpr (SPREAD) {
+                cluster_sync();
+                // each block sums a share of the digits over all blocks and hands every block the sums
+                const int part = (1 << bits) / cluster;
+                for (int i = 4 * tid; i < part; i += 4 * threads) {
+                    const int at = rank * part + i;
+                    int4 sum = make_int4(0, 0, 0, 0);
+#pragma unroll 4
+                    for (int r = 0; r < cluster; ++r) {
+                        const int4 x = ld_cluster4(in_block(hist + at, r));
+                        sum.x += x.x, sum.y += x.y, sum.z += x.z, sum.w += x.w;
+                    }
+                    for (int r = 0; r < cluster; ++r) st_cluster4(in_block(merged + at, r), sum);
+                }
+                cluster_sync();
+            }
             __syncthreads();
-            if (warp == 0) find(prefix, low, bits);
+            if (warp == 0) find(SPREAD ? merged : hist, prefix, low, bits);
             __syncthreads();
             prefix = s_prefix;
         }
@@ -245,7 +294,8 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
         const int ties = s_need;
         const uint32_t below = (1u << lane) - 1u;
         int gt_done = 0, eq_done = 0;      // rows of earlier tiles
-        for (int base = 0; base < old; base += tile) {
+        const int base0 = rank * tile;
+        for (int base = base0; base < (ONE ? base0 + 1 : old); base += tile) {
             if (!ONE) load(base);
             int gt = 0, eq = 0;
 #pragma unroll
@@ -264,6 +314,19 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
             const int gt_all = __reduce_add_sync(0xffffffffu, gt_w), eq_all = __reduce_add_sync(0xffffffffu, eq_w);
             gt_w = __reduce_add_sync(0xffffffffu, lane < warp ? gt_w : 0);
             eq_w = __reduce_add_sync(0xffffffffu, lane < warp ? eq_w : 0);
+            if constexpr (SPREAD) {
+                if (tid == 0) {
+                    block_counts[0] = gt_all;
+                    block_counts[1] = eq_all;
+                }
+                cluster_sync();
+                int2 c = make_int2(0, 0);
+                if (lane < rank) c = ld_cluster2(in_block(block_counts, lane));
+                gt_done = __reduce_add_sync(0xffffffffu, c.x);
+                eq_done = __reduce_add_sync(0xffffffffu, c.y);
+                // (nothing of another block is read after this: its end waits at the last line)
+                asm volatile("barrier.cluster.arrive.release;" ::: "memory");
+            }
             int seen = eq_done + eq_w;                               // rows with the last key before this warp's turn
             int pos = gt_done + gt_w + min(seen, ties);
             const float* from = total + base + first;
@@ -300,31 +363,47 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
             if (!ONE) __syncthreads();     // warp_gt, warp_eq are written again
         }
     }
-    for (int j = old + tid; j < n; j += threads) {
+    for (int j = old + rank * threads + tid; j < n; j += (SPREAD ? cluster : 1) * threads) {
         keep[want + j - old] = j;
         if (kept) kept[want + j - old] = total[j];
     }
+    if constexpr (SPREAD) {
+        __syncwarp();
+        if (want > 0) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
+    }
 }
 
-template <int IPT, bool ONE>
+template <int IPT, bool ONE, bool SPREAD>
 cudaError_t select_attr() {
-    return cudaFuncSetAttribute(select_rows_kernel<IPT, ONE>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    return cudaFuncSetAttribute(select_rows_kernel<IPT, ONE, SPREAD>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
-template <int IPT, bool ONE>
-cudaError_t launch_select_one(const SelectArgs& a, const SelectCounts& counts, int old, cudaStream_t stream) {
-    // no more warps than the longest unit has rows for
-    const long long warps = std::max(1, (old + 32 * IPT - 1) / (32 * IPT));
-    select_rows_kernel<IPT, ONE><<<(unsigned)a.units, (unsigned)std::min<long long>(kSelectThreads, 32 * warps), 0, stream>>>(a, counts);
-    return cudaGetLastError();
+// `old`: rows chosen from, of the longest unit.
+template <int IPT, bool ONE, bool SPREAD = false>
+cudaError_t launch_select_one(const SelectArgs& a, const SelectCounts& counts, int old, cudaStream_t stream, int cluster = 1) {
+    // no more warps than a block's share has rows for
+    const int share = (old + cluster - 1) / cluster, warps = std::max(1, (share + 32 * IPT - 1) / (32 * IPT));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.units * cluster));
+    cfg.blockDim = dim3((unsigned)std::min(kSelectThreads, 32 * warps));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = SPREAD ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, select_rows_kernel<IPT, ONE, SPREAD>, a, counts, cluster);
 }
 
 }  // namespace
 
 cudaError_t init_weights_kernels() {
-    cudaError_t e = select_attr<8, true>();
-    if (e == cudaSuccess) e = select_attr<32, true>();
-    return e == cudaSuccess ? select_attr<16, false>() : e;
+    cudaError_t e = select_attr<8, true, false>();
+    if (e == cudaSuccess) e = select_attr<8, true, true>();
+    if (e == cudaSuccess) e = select_attr<32, true, true>();
+    if (e == cudaSuccess) e = select_attr<32, true, false>();
+    return e == cudaSuccess ? select_attr<16, false, false>() : e;
 }
 
 cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, const float* total_in, float* total_out,
@@ -360,8 +439,18 @@ cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, c
 
 cudaError_t launch_select(const SelectArgs& a, const SelectCounts& counts, cudaStream_t stream) {
     const int old = std::max(0, a.n - a.n_recent);     // of the longest unit
-    // 256 threads up to 2048 rows (latency), then 32 rows per lane: blocks small enough that an SM holds several
-    if (old <= 2048) return launch_select_one<8, true>(a, counts, old, stream);
+    // Few units, up to 8192 rows: a block of 8 rows per lane; more units: 32 rows per lane, blocks small enough that an SM holds
+    // several (8192 rows, 128 units 10.3 us against 12.3, 640 units 30.8 against 26.7).
+    if (old <= 2048 || (old <= 8 * kSelectThreads && a.units <= 2 * a.sm_count)) return launch_select_one<8, true>(a, counts, old, stream);
+    // Longer ones: as many blocks per unit as there are SMs for, twice that if only then it stays in registers (a block alone
+    // / the cluster: 8 units of 16384 rows 14.4 / 12.4 us, of 32768 20.5 / 12.6, of 131072 74 / 19; 64 units of 32768
+    // 20.6 / 18.5, of 70000 49 / 37; beyond that it loses: 128 units of 32768 20.6 / 24.7, of 70000 49 / 70).
+    int cluster = 1;
+    while (old > 8 * kSelectThreads && cluster < kSelectCluster &&
+           2ll * cluster * a.units <= (old > cluster * 32 * kSelectThreads ? 2 : 1) * a.sm_count)
+        cluster *= 2;
+    if (cluster > 1 && old <= cluster * 8 * kSelectThreads) return launch_select_one<8, true, true>(a, counts, old, stream, cluster);
+    if (cluster > 1 && old <= cluster * 32 * kSelectThreads) return launch_select_one<32, true, true>(a, counts, old, stream, cluster);
     if (old <= 32 * kSelectThreads) return launch_select_one<32, true>(a, counts, old, stream);
     return launch_select_one<16, false>(a, counts, old, stream);
 }

@@ -677,6 +677,49 @@ def test_select_rows(n):
             _select_case(cache, total, counts, recent)
 
 
+@pytest.mark.parametrize("B,Hkv,n", [(1, 1, 8193), (1, 8, 16400), (1, 3, 40001), (4, 8, 20000), (8, 8, 9000), (16, 4, 33000), (1, 2, 70000),
+                                     (1, 1, 262144), (1, 1, 262200), (10, 14, 33000), (19, 8, 2500), (40, 8, 2500)])
+def test_select_long_units(B, Hkv, n):
+    """Units shared by a cluster's blocks, and the sizes around them; equal rows that end in another block than they begin."""
+    cache = SharedKVCache(1, Hkv, Hkv, 64, B, n, "bf16")
+    z = torch.zeros(B, n, Hkv, 64, dtype=torch.bfloat16, device="cuda")
+    cache.append(0, z, z)
+    rng = np.random.default_rng(n)
+    total = rng.random((B, Hkv, n), dtype=np.float32) ** 4
+    total[0, 0, n // 7: n - n // 9] = 0.5                                # one run of equal totals over most of the unit
+    total[-1, -1] = np.floor(total[-1, -1] * 3)
+    total[-1, -1, ::11] = np.nan
+    total = torch.from_numpy(total).cuda()
+    for recent, frac in ((0, 0.5), (n // 5, 0.3), (17, 0.97), (n - 1, 1.0)):
+        counts = [[max(1, recent, int(frac * n) - 13 * (b + i)) for i in range(Hkv)] for b in range(B)]
+        check_selection_all(cache, total, counts, recent)
+    # units of different lengths: some blocks of a cluster have no row
+    keep = torch.arange(n, dtype=torch.int32, device="cuda").expand(B, Hkv, n).contiguous()
+    lens = [[max(1, n - (b * Hkv + i) * n // (B * Hkv)) for i in range(Hkv)] for b in range(B)]
+    lens[-1][-1] = 1 if B * Hkv > 1 else n
+    cache.evict(0, keep, lens)
+    check_selection_all(cache, total, [[(x + 1) // 2 for x in r] for r in lens], 0)
+    check_selection_all(cache, total, lens, 1)
+
+
+def check_selection_all(cache, total, counts, recent):
+    """`_select_case` with the definition in numpy: a stable sort of the rows by falling total."""
+    B, Hkv = total.shape[:2]
+    stride = max(max(r) for r in counts) + 3
+    keep = torch.full((B, Hkv, stride), -7, dtype=torch.int32, device="cuda")
+    kept = torch.full((B, Hkv, stride), -7.0, device="cuda")
+    cache.select_rows(0, total, counts, recent, keep, kept)
+    got, got_kept, host = keep.cpu().numpy(), kept.cpu().numpy(), total.cpu().numpy()
+    for b in range(B):
+        for h in range(Hkv):
+            n, c = cache.unit_len(0, b, h), counts[b][h]
+            t = host[b, h, : n - recent]
+            order = np.lexsort((np.arange(len(t)), -np.where(np.isnan(t), -np.inf, t), np.isnan(t)))
+            rows = np.concatenate([np.sort(order[: c - recent]), np.arange(n - recent, n)])
+            assert np.array_equal(got[b, h, :c], rows) and (got[b, h, c:] == -7).all() and (got_kept[b, h, c:] == -7).all()
+            assert np.array_equal(got_kept[b, h, :c].view(np.int32), host[b, h, rows].view(np.int32))
+
+
 def test_select_odd_values():
     """Infinities, both zeros (equal), denormals and NaN (below everything)."""
     n = 64
