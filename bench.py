@@ -47,8 +47,8 @@ FALLBACK_HBM_GBS = 6650.0
 NCU_TRAFFIC = {
     1: {"files": ("kvs_kernels.cu", "kvs_device.cuh"), "dram_bytes": 1558.49e6, "kv_bytes": 1552.55e6,
         "sha256": "4e9e2db4a1d641464cd5a2542d77d47eccbeeee4092bf9641ecce864faec99d3"},
-    2: {"files": ("kvs_mma.cu", "kvs_device.cuh"), "dram_bytes": 541.89e6, "kv_bytes": 536.90e6,
-        "sha256": "949ae9641d02cdb5efbd95dd34539e87157c5e24b7ce905ee82dfac38fa6746a"},
+    2: {"files": ("kvs_mma.cu", "kvs_device.cuh"), "dram_bytes": 540.95e6, "kv_bytes": 536.90e6,
+        "sha256": "6fed13c321eea6e976fc7a48fe4433fed6be7ddf315434e382c3a061a8053a17"},
 }
 
 

@@ -602,6 +602,22 @@ def test_weights_under_graph_replay():
         assert (a - b).abs().max() < 1e-5
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,D", [("bf16", 32, 8, 128), ("bf16", 24, 8, 64), ("bf16", 4, 4, 128), ("f32", 8, 2, 64)])
+def test_weights_pass_does_not_drift_over_long_shares(dtype, Hq, Hkv, D):
+    """16000 rows of a sequence in three blocks: thousands of steps into one accumulator."""
+    n, B = 16000, 1
+    cache, k, v = filled(Hq, Hkv, D, B, n, dtype, cls=SharedKVCache)
+    cache.set_option(KVS_OPT_MAX_CTAS, 3)
+    q = normal(9, dtype, B, Hq, D)
+    total = torch.zeros(B, Hkv, n, device="cuda")
+    out = cache.decode_attention_weights(0, q, total).double()
+    s = torch.einsum("bhgd,bnhd->bhgn", q.double().view(B, Hkv, Hq // Hkv, D), k.double()) / D ** 0.5
+    want = torch.einsum("bhgn,bnhd->bhgd", torch.softmax(s, -1), v.double()).reshape(out.shape)
+    # A warp adds its quarter of the rows: N = 250 blocks of 16 (or 4000 rows one by one).  Rounded to nearest, independent, the
+    # sums walk sqrt(N) 2^-25 <= 1.9e-6 of the result; cut off towards zero they drift by N 2^-25.
+    assert (out - want).norm() <= 2e-6 * want.norm()
+
+
 def test_rotary_append_under_graph_replay():
     B, Hq, Hkv, D, n0, steps = 2, 4, 2, 64, 10, 5
     x = normal(1, "bf16", steps, B, 1, Hq + 2 * Hkv, D)
