@@ -736,6 +736,41 @@ def check_selection_all(cache, total, counts, recent):
             assert np.array_equal(got_kept[b, h, :c].view(np.int32), host[b, h, rows].view(np.int32))
 
 
+def test_long_units_and_long_prompts_captured_on_a_side_stream():
+    """The launches that long shapes take (clusters; a ring of tokens), recorded and replayed: the same bits as outside."""
+    n, n_new, Hq, Hkv, D = 20000, 900, 32, 8, 128
+    cache, _, _ = filled(Hq, Hkv, D, 1, n, "bf16", extra=n_new, cls=SharedKVCache)
+    total = torch.rand(1, Hkv, n + n_new, generator=torch.Generator().manual_seed(3)).cuda()
+    counts = [[700 * (h + 1) for h in range(Hkv)]]
+    keep = [torch.zeros(1, Hkv, 700 * Hkv, dtype=torch.int32, device="cuda") for _ in range(2)]
+    kept = [torch.zeros(1, Hkv, 700 * Hkv, device="cuda") for _ in range(2)]
+    q, k, v = (normal(i, "bf16", 1, n_new, h, D) for i, h in ((1, Hq), (2, Hkv), (3, Hkv)))
+    pos = torch.arange(n, n + n_new, dtype=torch.int32, device="cuda").view(1, n_new)
+    rot, w = Rotary.from_theta(D), normal(4, "bf16", D)
+    out = [torch.zeros_like(q) for _ in range(2)]
+
+    def step(i):
+        cache.select_rows(0, total, counts, 5, keep[i], kept[i])
+        cache.append_rotary(0, q, k, v, pos, rot, w, w, out=out[i])
+
+    step(0)
+    rows = [cache.plane(0, i)[0, :, n:n + n_new].clone() for i in range(2)]
+    cache.truncate(n)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(1)
+    for i in range(2):
+        cache.plane(0, i)[0, :, n:n + n_new] = 0
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(keep[0], keep[1]) and torch.equal(kept[0], kept[1]) and torch.equal(out[0], out[1])
+    for i in range(2):
+        assert torch.equal(rows[i], cache.plane(0, i)[0, :, n:n + n_new])
+    assert cache.device_status() == 0
+
+
 def test_select_odd_values():
     """Infinities, both zeros (equal), denormals and NaN (below everything)."""
     n = 64
