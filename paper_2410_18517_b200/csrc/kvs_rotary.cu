@@ -33,7 +33,7 @@ struct RotaryKernelArgs {
     const char* k;
     const char* v;
     long long q_stride, k_stride, v_stride;     // bytes between consecutive tokens
-    const int* positions;                       // [tokens]
+    const int* positions;                       // [tokens]; may be nullptr where half is 0
     const char* q_weight;                       // [D] or nullptr
     const char* k_weight;
     char* q_out;                                // [tokens][Hq][D]
@@ -262,7 +262,9 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamBlocks) append_rotary_s
         const uint32_t q_bytes = (uint32_t)a.Hq * RB, kv_bytes = (uint32_t)a.Hkv * RB;
         int it = 0;
         bool ok = true;
-        int position = blockIdx.x < a.tokens ? a.positions[blockIdx.x] : 0;
+        // (nothing is rotated: there may be no positions)
+        const bool turned = a.half > 0;
+        int position = turned && blockIdx.x < a.tokens ? a.positions[blockIdx.x] : 0;
         for (int tok = blockIdx.x; tok < a.tokens; tok += gridDim.x, ++it) {
             const int st = it % stages;
             if (it >= stages) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&empty[st], (uint32_t)(it / stages - 1) & 1u, abort_flag, a.status)) != 0;
@@ -281,7 +283,7 @@ __global__ void __launch_bounds__(kStreamThreads, kStreamBlocks) append_rotary_s
             }
             // the next token's position is on its way while this one's table is worked out
             const int now = position, next = tok + (int)gridDim.x;
-            if (next < a.tokens) position = a.positions[next];
+            if (turned && next < a.tokens) position = a.positions[next];
             float* cos_t = reinterpret_cast<float*>(base + heads * RB);
             for (int i = lane; i < a.half; i += 32) table_entry(now, a.turns[i], &cos_t[i], &cos_t[D / 2 + i]);
             __syncwarp();

@@ -1,0 +1,40 @@
+"""The serving operators in calls that the header allows and their main tests do not make."""
+import numpy as np
+import pytest
+import torch
+
+import operators_reference as ref
+import test_gpu_operators as t
+from paper_2410_18517_b200 import Rotary
+from paper_2410_18517_b200 import build as kbuild
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    kbuild.build()
+
+
+# ------------------------------------------------------------------------------------------ rotary append
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,B,n_new", [("bf16", 32, 8, 128, 1, 900), ("f32", 14, 7, 128, 3, 700), ("bf16", 32, 8, 128, 2, 3),
+                                                    ("f32", 4, 2, 64, 1, 1), ("bf16", 4, 2, 64, 2, 1000)])
+@pytest.mark.parametrize("norm", [True, False])
+def test_append_rotary_without_positions(dtype, Hq, Hkv, D, B, n_new, norm):
+    """Nothing is rotated (rotary_dim 0), so there are no positions: by both kernels, on a computing and a sharing layer."""
+    cache, _, _ = t.filled(Hq, Hkv, D, B, 4, dtype, extra=n_new, L=2, share_map=[0, 0])
+    q, k, v = (t.normal(3 + i, dtype, B, n_new, h, D) for i, h in enumerate((Hq, Hkv, Hkv)))
+    qw, kw = (t.normal(8, dtype, D), t.normal(9, dtype, D)) if norm else (None, None)
+    pos = torch.zeros(B, n_new, dtype=torch.int32, device="cuda")
+    got = cache.append_rotary(0, q, k, v, None, Rotary([]), qw, kw)
+    K, V = cache.plane(0, 0)[:B, :, 4:4 + n_new].transpose(1, 2), cache.plane(0, 1)[:B, :, 4:4 + n_new].transpose(1, 2)
+    assert torch.equal(cache.append_rotary(1, q, None, None, None, Rotary([]), qw), got)
+    if norm:
+        t.check_rotary(got, q, qw, pos, [], False, 1e-6)
+        t.check_rotary(K, k, kw, pos, [], False, 1e-6)
+    else:
+        assert torch.equal(got, q) and torch.equal(K, k)
+    assert torch.equal(V, v) and cache.seq_len(0) == 4 + n_new
+    assert cache.device_status() == 0
+    cache.check_canaries()
