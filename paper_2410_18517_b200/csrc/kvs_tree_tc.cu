@@ -7,7 +7,7 @@
 //                      lanes hold no query row stay out of it
 //   warp 4 (one lane)  TMA producer: the query tile per piece; K and V tiles through one ring (K0 V0 K1 V1 ...)
 //   warp 5             MMA issuer: S = Q K^T into one of two score buffers (S of tile t+1 runs during the softmax of
-//                      tile t), O += P V with P as bf16 read from tensor memory.  The whole warp walks the tiles and an
+//                      tile t), O += P V with P = hi + lo (two bf16 terms) read from tensor memory.  The whole warp walks the tiles and an
 //                      elected lane issues: operands are then in uniform registers (issued from a one-lane branch the
 //                      sixteen MMAs of a 128-key tile took 1700 cycles instead of 1200)
 // Bound: up to 128 query rows per kv-head HBM (32 heads, B = 8, n = 4096, 16 drafts: 537 MB in 85 us, 6.3 TB/s).  Above
@@ -20,9 +20,10 @@
 // that reads its weights, and S then waits for softmax, PV and S in a row); one block per SM with 128-key tiles, two
 // score buffers and two threads per row, 177; a quarter of the exp2 by a polynomial on the FMA pipe, 151; two stages per
 // operand instead of the ring of five, 147; K/V fetched before the wait for the previous kernel, 150.
-// P goes into the second contraction as one bf16 term (each weight off by at most 2^-8 of itself, the sum of the weights
-// kept in fp32 from the unrounded ones): the result is rounded to bf16 anyway, and a second term would add half again to the
-// tensor work of wide trees, which the tensor pipe bounds.
+// P goes into the second contraction as two bf16 terms, like the prefill kernel's: a weight is then off by 2^-16 of itself at
+// most.  With one term (2^-8) an element with large cancelling shares is off by several of its own rounding steps, which
+// shows at any length (70 keys: nine times the bound).  Per call, one term / two: 32 heads, B = 8, n = 4096, 16 drafts
+// 102 / 111 us; 32q/8kv, B = 4, n = 32768, 64 drafts 182 / 211; B = 4, n = 8192, 32 drafts 52.3 / 52.6.
 //
 // The last tiles of a unit hold drafts and rows past its end.  There the softmax warps also clean the V tile in
 // shared memory before the MMA may read it: rows past the end become zero, and so do non-finite elements of draft
@@ -93,12 +94,13 @@ struct Pieces {
 };
 
 // The weights p = 2^(x * scale - m_ref) of 32 scores, 0 where the key's bit in `vis` is not set (MASK), as they go to
-// tensor memory (two bf16 per column from `taddr` on); returns their sum.
+// tensor memory: p = hi + lo in bf16, two keys per column, hi from `taddr` and lo from `taddr + kTcKeys / 2` on.  Returns
+// their sum.
 template <bool MASK>
 __device__ __forceinline__ float weights32(const float (&x)[32], float scale_log2, float m_ref, uint32_t vis, uint32_t taddr) {
-    const float2 sc = make_float2(scale_log2, scale_log2), nm = make_float2(-m_ref, -m_ref);
+    const float2 sc = make_float2(scale_log2, scale_log2), nm = make_float2(-m_ref, -m_ref), minus1 = make_float2(-1.f, -1.f);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-    uint32_t w[16];
+    uint32_t hi[16], lo[16];
 #pragma unroll
     for (int i = 0; i < 32; i += 2) {
         const float2 t = __ffma2_rn(make_float2(x[i], x[i + 1]), sc, nm);
@@ -108,9 +110,13 @@ __device__ __forceinline__ float weights32(const float (&x)[32], float scale_log
             p.y = (vis >> (i + 1)) & 1u ? p.y : 0.f;
         }
         sum[(i >> 1) & 1] = __fadd2_rn(sum[(i >> 1) & 1], p);
-        w[i >> 1] = pack2_bf16(p.x, p.y);
+        const uint32_t h = pack2_bf16(p.x, p.y);
+        hi[i >> 1] = h;
+        const float2 r = __ffma2_rn(make_float2(__uint_as_float(h << 16), __uint_as_float(h & 0xffff0000u)), minus1, p);
+        lo[i >> 1] = pack2_bf16(r.x, r.y);
     }
-    tmem_st16(taddr, w);
+    tmem_st16(taddr, hi);
+    tmem_st16(taddr + kTcKeys / 2, lo);
     return (sum[0].x + sum[1].x) + (sum[0].y + sum[1].y);
 }
 
@@ -305,7 +311,10 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                 const uint32_t o = tmem + 128, w = tmem + (t & 1) * kTcKeys;
                 if (leader) {
 #pragma unroll
-                    for (int ks = 0; ks < kTcKeys / 16; ++ks) umma_bf16_ts(o, w + ks * 8, v + ks * 16 * 128 / 16, idesc_o, ks > 0 ? 1 : j > 0);
+                    for (int ks = 0; ks < kTcKeys / 16; ++ks) {
+                        umma_bf16_ts(o, w + ks * 8, v + ks * 16 * 128 / 16, idesc_o, ks > 0 ? 1 : j > 0);             // hi
+                        umma_bf16_ts(o, w + kTcKeys / 2 + ks * 8, v + ks * 16 * 128 / 16, idesc_o, 1);                // lo
+                    }
                     umma_commit(&o_full[t & 1]);
                     umma_commit(&empty[st]);
                 }

@@ -38,3 +38,28 @@ def test_append_rotary_without_positions(dtype, Hq, Hkv, D, B, n_new, norm):
     assert torch.equal(V, v) and cache.seq_len(0) == 4 + n_new
     assert cache.device_status() == 0
     cache.check_canaries()
+
+
+# ----------------------------------------------------------------------------------------- tree attention
+
+@pytest.mark.parametrize("Hq,Hkv,D,B,n,n_t", [(8, 2, 128, 2, 70, 7), (8, 8, 64, 2, 300, 30), (32, 8, 128, 1, 2100, 64), (5, 5, 128, 3, 9, 9),
+                                              (8, 1, 128, 1, 9000, 33)])
+def test_tree_weights_keep_sixteen_bits(Hq, Hkv, D, B, n, n_t):
+    """The softmax weights reach the second product with both bf16 terms: beside the rounding of the result to its own
+    type, an element is off by 2^-16 of the sum of |weight * value|, not by 2^-8 of it.  (hi = bf16(p) leaves a remainder of
+    2^-8 p at most, of which lo = bf16(p - hi) keeps all but 2^-8: 2^-16 p.)"""
+    cache, _, _ = t.filled(Hq, Hkv, D, B, n, "bf16")
+    rng = np.random.default_rng(n)
+    words = [ref.random_tree(rng, n_t) for _ in range(B)]
+    q = t.normal(7, "bf16", B, n_t, Hq, D)
+    out = cache.tree_attention(0, q, torch.tensor([ref.to_int64(w) for w in words]).cuda())
+    G = Hq // Hkv
+    for b in range(B):
+        for h in range(Hkv):
+            K, V = t.rows_of(cache, 0, b, h)
+            o, _, mass, d = ref.attend(q[b, :, h * G:(h + 1) * G], K, V, ref.tree_sees(words[b], n, n_t).cuda())
+            # (weight_error counts 2 n u for sums rounded to nearest; those of the tensor cores may be cut off: n 2^-23 more)
+            rest = (ref.weight_error(d, n) + 2.0 ** -16 + n * 2.0 ** -23) * mass
+            got = out[b, :, h * G:(h + 1) * G].double()
+            bound = ref.half_step(q.dtype) * (o.abs() + rest) + rest + 1e-30
+            assert ((got - o).abs() <= bound).all(), float(((got - o).abs() / bound).max())
