@@ -150,8 +150,8 @@ kvs_status kvs_required_bytes(const kvs_ctx* ctx, size_t* pool_bytes, size_t* wo
 
 /* Hand the context its device memory.  pool, workspace: device, 256-byte
  * aligned, at least the sizes kvs_required_bytes reported (else OOM).  The pool
- * is zero-filled on the default stream and the call waits for that, so that
- * rows past a slot's length never hold non-finite bit patterns.  Queries device
+ * is zero-filled on the default stream and the call waits for that.  What rows
+ * past a unit's end hold later (NaN included) reaches no result.  Queries device
  * properties; CUDA errors give KVS_ERR_CUDA.  Resets all slot lengths to 0.    */
 kvs_status kvs_bind_memory(kvs_ctx* ctx, void* pool, size_t pool_bytes,
                            void* workspace, size_t workspace_bytes);
@@ -303,7 +303,7 @@ kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* 
  * to the front of the drafts, bit for bit, and the unit ends behind them.
  *   path:     device, int32 [batch][path_stride], the same for all layers
  *   n_accept: host, int32 [batch], each 0 .. n_draft and at most path_stride
- * The rejected drafts' rows are cleared (kvs_truncate leaves rows as they are: fine for drafts whose rows are finite).
+ * The rejected drafts' rows are cleared (kvs_truncate leaves rows as they are; either way they reach no later result).
  * Where all sequences keep the same number a slot stays as it is; otherwise its units differ in length afterwards,
  * as after kvs_evict (kvs_prefill_attention and kvs_truncate then refuse it).  One launch per slot.  A path that is
  * not ascending or out of range cannot be seen by the host: the kernel leaves the row already there and sets the

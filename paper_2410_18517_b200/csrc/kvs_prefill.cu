@@ -396,6 +396,18 @@ __global__ void __launch_bounds__(kPfThreads, 2)
                 KVS_PF_CHUNK(16)
 #undef KVS_PF_CHUNK
                 l += lsum;
+                if ((j + 1) * kPfKeys > a.n) {
+                    // The unit ends in this tile.  Rows past the end may hold anything (0 * NaN is not 0): their values are
+                    // cleared in the staged tile before the MMA may read it.  (S of this tile was issued behind PV of
+                    // the tile two before it, so the barrier cannot be a phase behind the one waited for.)
+                    ok = mbar_wait_bounded(&v_full[st], (uint32_t)(tt >> 1) & 1u, abort_flag, a.status);
+                    if (!ok) break;
+                    const int first = a.n - j * kPfKeys, chunks = (kPfKeys - first) * 8;     // 16-byte chunks per column block
+                    for (int i = tid; i < S::HALVES * chunks; i += kSoftmaxThreads)
+                        *reinterpret_cast<uint4*>(sV + st * kKvBytes + (i / chunks) * kPfKvBlock + first * 128 + (i % chunks) * 16) = make_uint4(0u, 0u, 0u, 0u);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 mbar_arrive(&p_full[st]);

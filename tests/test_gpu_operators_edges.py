@@ -63,3 +63,43 @@ def test_tree_weights_keep_sixteen_bits(Hq, Hkv, D, B, n, n_t):
             got = out[b, :, h * G:(h + 1) * G].double()
             bound = ref.half_step(q.dtype) * (o.abs() + rest) + rest + 1e-30
             assert ((got - o).abs() <= bound).all(), float(((got - o).abs() / bound).max())
+
+
+# ------------------------------------------------------------------------------ rows left behind past the end
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,B,n,n_q", [("bf16", 8, 2, 128, 2, 73, 73), ("bf16", 2, 2, 64, 1, 1, 1), ("bf16", 4, 4, 128, 3, 130, 40),
+                                                    ("bf16", 8, 1, 64, 1, 383, 383), ("bf16", 2, 1, 128, 2, 64, 20), ("f32", 4, 2, 64, 2, 73, 73)])
+@pytest.mark.parametrize("how", ["truncate", "reset"])
+def test_prefill_over_rows_left_behind(dtype, Hq, Hkv, D, B, n, n_q, how):
+    """Rows of broken drafts (NaN) that were rolled back, or left by a sequence before, share the last tile with rows that
+    prefill attention reads."""
+    cache = t.GuardedCache(1, Hq, Hkv, D, B, n + 70, dtype)
+    cache.paint(n + 70, B)
+    k, v = t.normal(1, dtype, B, n, Hkv, D), t.normal(2, dtype, B, n, Hkv, D)
+    bad = torch.full((B, 70, Hkv, D), float("nan"), dtype=t.DT[dtype], device="cuda")
+    if how == "truncate":
+        cache.append(0, k, v)
+        cache.append(0, bad, bad)
+        cache.truncate(n)
+    else:
+        nan = torch.full((B, n + 70, Hkv, D), float("nan"), dtype=t.DT[dtype], device="cuda")
+        cache.append(0, nan, nan)
+        cache.reset()
+        cache.append(0, k, v)
+    q = t.normal(3, dtype, B, n_q, Hq, D)
+    out = cache.prefill_attention(0, q)
+    again = cache.prefill_attention(0, q)
+    assert torch.equal(out, again)
+    G = Hq // Hkv
+    causal = torch.arange(n)[None, :] <= (torch.arange(n_q) + n - n_q)[:, None]
+    for b in range(B):
+        for h in range(Hkv):
+            o, _, mass, d = ref.attend(q[b, :, h * G:(h + 1) * G], k[b, :, h], v[b, :, h], causal.cuda())
+            got = out[b, :, h * G:(h + 1) * G].double()
+            assert ((got - o).abs() <= (ref.weight_error(d, n) + 2.0 ** -16 + n * 2.0 ** -23) * mass + 1e-30).all()
+    # the other readers of the same rows
+    one = q[:, -1].contiguous()
+    want = out[:, -1]
+    assert (cache.decode_attention(0, one) - want).abs().max() < 1e-4
+    assert cache.device_status() == 0
+    cache.check_canaries()
