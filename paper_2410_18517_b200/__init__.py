@@ -59,7 +59,7 @@ class SharedKVCache:
         self.dtype = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
         self.shape = (n_layers, n_q_heads, n_kv_heads, head_dim)
         self.max_batch = max_batch
-        self._planes = {}           # views handed out by plane(): the pool stays where it is
+        self._planes = None         # the pool, and the planes seen in it so far (see plane())
         self.ctx = binding.kvs_create(n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq,
                                       KVS_BF16 if dtype == "bf16" else KVS_F32, softmax_scale, device)
         try:
@@ -83,8 +83,7 @@ class SharedKVCache:
             self._torch.cuda.synchronize(self.device)
             binding.kvs_destroy(self.ctx)
             self.ctx = None
-            self.pool = self.workspace = None
-            self._planes = {}
+            self.pool = self.workspace = self._planes = None
 
     def __del__(self):
         try:
@@ -295,15 +294,15 @@ class SharedKVCache:
 
     def plane(self, slot, kv):
         """View of plane (slot, kv) as ``[max_batch][n_kv_heads][row_stride][head_dim]``."""
-        view = self._planes.get((slot, kv))
-        if view is not None:
-            return view
-        off = binding.kvs_plane_offset(self.ctx, slot, kv)
-        nxt = binding.kvs_plane_offset(self.ctx, 0, 1)
-        rs = binding.kvs_row_stride(self.ctx)
-        view = self.pool[off:off + nxt].view(self.dtype).view(-1, self.shape[2], rs, self.shape[3])
-        self._planes[slot, kv] = view
-        return view
+        if self._planes is None or self._planes[0] is not self.pool:
+            self._planes = self.pool, {}
+        seen = self._planes[1].get((slot, kv))
+        if seen is None:
+            off, nbytes = binding.kvs_plane_offset(self.ctx, slot, kv), binding.kvs_plane_offset(self.ctx, 0, 1)
+            rs = binding.kvs_row_stride(self.ctx)
+            seen = self.pool[off:off + nbytes].view(self.dtype).view(-1, self.shape[2], rs, self.shape[3])
+            self._planes[1][slot, kv] = seen
+        return seen.detach()        # a tensor of its own for every caller
 
     # plain forwards
     def num_slots(self):

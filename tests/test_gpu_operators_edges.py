@@ -5,7 +5,7 @@ import torch
 
 import operators_reference as ref
 import test_gpu_operators as t
-from paper_2410_18517_b200 import Rotary
+from paper_2410_18517_b200 import KvsError, Rotary
 from paper_2410_18517_b200 import build as kbuild
 
 pytestmark = pytest.mark.gpu
@@ -103,3 +103,26 @@ def test_prefill_over_rows_left_behind(dtype, Hq, Hkv, D, B, n, n_q, how):
     assert (cache.decode_attention(0, one) - want).abs().max() < 1e-4
     assert cache.device_status() == 0
     cache.check_canaries()
+
+
+# ----------------------------------------------------------------------------------------- views of the pool
+
+def test_every_view_of_a_plane_is_its_callers_own():
+    cache, k, _ = t.filled(4, 2, 64, 3, 20, "bf16", L=2, max_batch=5)
+    shape = (5, 2, 128, 64)
+    first = cache.plane(1, 0)
+    first.transpose_(1, 2).unsqueeze_(0)
+    again = cache.plane(1, 0)
+    assert again.shape == shape and again.is_contiguous() and again is not first
+    for slot in (0, 1):
+        assert torch.equal(cache.plane(slot, 0)[:3, :, :20].transpose(1, 2), k)
+        for kv in (0, 1):
+            x = cache.plane(slot, kv)
+            assert x.shape == shape and x.data_ptr() == cache.pool.data_ptr() + (2 * slot + kv) * x.numel() * 2
+    for slot, kv in ((2, 0), (-1, 1), (0, 2)):
+        with pytest.raises(KvsError):
+            cache.plane(slot, kv)
+    old, cache.pool = cache.pool, torch.zeros_like(cache.pool)          # another pool: views of that one
+    assert not cache.plane(0, 0).any()
+    cache.pool = old
+    assert torch.equal(cache.plane(0, 0)[:3, :, :20].transpose(1, 2), k)
