@@ -322,7 +322,8 @@ kvs_status kvs_accept_draft(kvs_ctx* ctx, const int32_t* path, int32_t path_stri
  *   total_in:  device, float32 [batch][n_kv_heads][total_stride], or NULL: zeros
  *   total_out: the same layout; may be total_in itself, must not overlap it otherwise
  *   total_stride: at least the slot's rows (under KVS_OPT_REPLAY: max_seq)
- * The sums are made in a fixed order: the same call gives the same bits.  Two launches.
+ * The sums are made in a fixed order: the same call gives the same bits.  Two launches for every 64 MiB of scores, 4 bytes
+ * per q-head and row (under KVS_OPT_REPLAY: per q-head and row of the capacity).
  * Other arguments and errors: as kvs_decode_attention.                                                        */
 kvs_status kvs_decode_attention_weights(kvs_ctx* ctx, int32_t layer, const void* q, float* out, const float* total_in,
                                         float* total_out, int32_t total_stride, int32_t batch, void* stream);

@@ -15,6 +15,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int kRowStrideQuantum = 128;
+constexpr size_t kScoreBytes = 64u << 20;     // scores of one pass of kvs_decode_attention_weights
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace
@@ -85,7 +86,8 @@ struct kvs_ctx {
     // workspace carve-up (byte offsets)
     size_t off_status = 0, off_part_o = 0, off_part_ml = 0, off_stage_q = 0, off_stage_k = 0, off_stage_v = 0,
            off_stage_out = 0, off_unit_len = 0, off_counts = 0, off_search = 0, off_replay = 0, off_flags = 0, off_scores = 0,
-           off_tree_o = 0, off_tree_ml = 0, ws_bytes = 0, search_bytes = 0;
+           off_tree_o = 0, off_tree_ml = 0, ws_bytes = 0, search_bytes = 0,
+           score_bytes = 0;
 
     alignas(64) unsigned char tensor_map[128];  // TMA view of the pool (bf16 storage only), 64-row boxes
     alignas(64) unsigned char tensor_map_tail[128];   // the same view with 16-row boxes (partly filled tiles)
@@ -213,9 +215,12 @@ void layout_workspace(kvs_ctx* c) {
         c->search_bytes = need;
         // The same bytes serve the other calls whose scratch lives no longer than the call (every kernel writes it
         // only after its wait for the previous one):
-        // kvs_decode_attention_weights: one score per (sequence, q-head, row)
-        const size_t scores = (size_t)f.max_batch * f.n_q_heads * c->row_stride * sizeof(float);
+        // kvs_decode_attention_weights: one score per (unit, q-head of its group, row), for as many units at a time as
+        // kScoreBytes hold, so that contexts of long and wide caches do not pay for a call they may never make
+        const size_t unit_scores = (size_t)c->G * c->row_stride * sizeof(float);
+        const size_t scores = std::min(units, std::max<size_t>(1, kScoreBytes / unit_scores)) * unit_scores;
         c->off_scores = off;
+        c->score_bytes = scores;
         // kvs_tree_attention: two cut pieces per thread block at most
         const size_t tree_rows = (size_t)2 * kvs::kTreeMaxBlocks * kvs::tree_partial_rows(c->G);
         const size_t tree_o = align_up(tree_rows * f.head_dim * sizeof(float), kAlign);
@@ -346,38 +351,41 @@ struct WeightTotals {
     const float* in;     // nullptr: totals start at zero
     float* out;
     int stride;
+    int score_stride;    // floats between the scores of consecutive q-heads
 };
 
-// Split-K kernel + combine kernel of one layer, with the given plan and scratch.
+// Split-K kernel + combine kernel of one layer, with the given plan and scratch, over `units` (sequence, kv-head) units of
+// the slot from unit0 on.  q and out: of the whole batch.
 // With k_new / v_new the split-K kernel also appends that one row per unit (the slot's length must
 // already count it).
-kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int batch, const kvs::DecodePlan& plan,
+kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int unit0, int units, const kvs::DecodePlan& plan,
                          bool use_mma, const AttentionScratch& scratch, cudaStream_t st, const void* k_new = nullptr,
                          const void* v_new = nullptr, const WeightTotals* totals = nullptr) {
     kvs::DecodeArgs a;
-    a.q = q;
-    a.kplane = c->pool + (size_t)(2 * slot) * c->plane_bytes;
-    a.vplane = c->pool + (size_t)(2 * slot + 1) * c->plane_bytes;
+    const size_t skipped = (size_t)unit0 * c->row_stride * c->row_bytes, heads0 = (size_t)unit0 * c->G * c->cfg.head_dim;
+    a.q = static_cast<const char*>(q) + heads0 * c->elem;
+    a.kplane = c->pool + (size_t)(2 * slot) * c->plane_bytes + skipped;
+    a.vplane = c->pool + (size_t)(2 * slot + 1) * c->plane_bytes + skipped;
     a.part_o = scratch.part_o;
     a.part_ml = scratch.part_ml;
-    a.out = out;
+    a.out = out + heads0;
     a.status = scratch.status;
     a.n = c->slot_len[slot];
     a.row_stride = c->row_stride;
     a.capacity = c->cfg.max_seq;
-    a.units = batch * c->cfg.n_kv_heads;
+    a.units = units;
     a.G = c->G;
     a.D = c->cfg.head_dim;
     a.dtype = c->cfg.dtype;
     a.scale_log2 = c->scale * 1.4426950408889634f;
     a.programmatic = scratch.programmatic;
     a.safe_rows = scratch.programmatic ? safe_rows_of(c, slot) : 0;
-    a.unit_len = c->ragged[slot] ? unit_len_dev(c, slot) : nullptr;
+    a.unit_len = c->ragged[slot] ? unit_len_dev(c, slot) + unit0 : nullptr;
     a.n_extra = replay_counter(c);
     a.k_new = k_new;
     a.v_new = v_new;
     if (k_new) a.safe_rows = std::min(a.safe_rows, a.n - 1);   // the new row is fetched after the kernel has stored it
-    a.plane_bytes = (long long)c->plane_bytes;
+    a.plane_bytes = (long long)(c->plane_bytes - skipped);
     a.wait_ns = 1000ull * (unsigned long long)c->opt_wait_us;
     a.trace = nullptr;
     if (c->trace_buf && c->trace_launch < c->trace_capacity)
@@ -387,6 +395,7 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int ba
     // with totals the unit's (max, sum) are needed beyond its output: always the separate finishing kernel
     a.finish_in_kernel = c->opt_finish != 0 && kvs::can_finish_in_kernel(plan, a.units) && totals == nullptr;
     a.scores = totals ? reinterpret_cast<float*>(c->ws + c->off_scores) : nullptr;
+    a.score_stride = totals ? totals->score_stride : 0;
     a.flags = scratch.flags;
     if (scratch.tracked) {
         c->seq += a.finish_in_kernel ? 1 : 2;     // split-K kernel, then (unless it finishes the units itself) combine
@@ -394,14 +403,17 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int ba
     }
     if (use_mma) {
         const long long plane_rows = (long long)c->cfg.max_batch * c->cfg.n_kv_heads * c->row_stride;
-        if (kvs::launch_decode_mma(a, plan, c->tensor_map, c->tensor_map_tail, plane_rows * (2 * slot),
-                                   plane_rows * (2 * slot + 1), st) != cudaSuccess)
+        const long long row0 = (long long)unit0 * c->row_stride;
+        if (kvs::launch_decode_mma(a, plan, c->tensor_map, c->tensor_map_tail, plane_rows * (2 * slot) + row0,
+                                   plane_rows * (2 * slot + 1) + row0, st) != cudaSuccess)
             return KVS_ERR_CUDA;
     } else {
         if (kvs::launch_decode_scalar(a, plan, st) != cudaSuccess) return KVS_ERR_CUDA;
     }
     if (!a.finish_in_kernel) {
-        const cudaError_t e = totals ? kvs::launch_weights_finish(a, plan, totals->in, totals->out, totals->stride, st)
+        const size_t total0 = totals ? (size_t)unit0 * totals->stride : 0;
+        const cudaError_t e = totals ? kvs::launch_weights_finish(a, plan, totals->in ? totals->in + total0 : nullptr, totals->out + total0,
+                                                                  totals->stride, st)
                                      : kvs::launch_combine(a, plan, st);
         if (e != cudaSuccess) return KVS_ERR_CUDA;
         c->stats.combine_launches += 1;
@@ -410,7 +422,7 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int ba
     c->stats.attention_launches += 1;
     if (c->ragged[slot]) {
         unsigned long long rows = 0;
-        for (int u = 0; u < a.units; ++u) rows += c->unit_len_host[slot][u];
+        for (int u = unit0; u < unit0 + a.units; ++u) rows += c->unit_len_host[slot][u];
         c->stats.kv_bytes_read += 2ull * rows * c->row_bytes;
     } else {
         c->stats.kv_bytes_read += 2ull * a.units * a.n * c->row_bytes;
@@ -432,7 +444,7 @@ kvs_status do_fused_step(kvs_ctx* c, int layer, const void* q, const void* k, co
                                       reinterpret_cast<int*>(c->ws + c->off_status), take_early_start(c), true};
     // run_attention works out which rows are stable from the appends before this one
     c->slot_len[slot] = old_len + 1;
-    const kvs_status s = run_attention(c, slot, q, out, batch, plan, use_mma, scratch, st, k, v);
+    const kvs_status s = run_attention(c, slot, q, out, 0, batch * c->cfg.n_kv_heads, plan, use_mma, scratch, st, k, v);
     if (s != KVS_OK) {
         c->slot_len[slot] = old_len;
         return s;
@@ -447,15 +459,28 @@ kvs_status do_fused_step(kvs_ctx* c, int layer, const void* q, const void* k, co
 }
 
 kvs_status do_attention(kvs_ctx* c, int layer, const void* q, float* out, int batch, cudaStream_t st,
-                        const WeightTotals* totals = nullptr) {
-    const int slot = c->slot_of_layer[layer];
-    kvs::DecodePlan plan;
-    const bool use_mma = choose_plan(c, batch * c->cfg.n_kv_heads, c->slot_len[slot], &plan);
-    const AttentionScratch scratch = {reinterpret_cast<float*>(c->ws + c->off_part_o),
-                                      reinterpret_cast<float*>(c->ws + c->off_part_ml),
-                                      reinterpret_cast<int*>(c->ws + c->off_flags),
-                                      reinterpret_cast<int*>(c->ws + c->off_status), take_early_start(c), true};
-    return run_attention(c, slot, q, out, batch, plan, use_mma, scratch, st, nullptr, nullptr, totals);
+                        WeightTotals* totals = nullptr) {
+    const int slot = c->slot_of_layer[layer], units = batch * c->cfg.n_kv_heads;
+    int step = units;
+    if (totals) {
+        // as many units at a time as there is room for their scores; a recorded launch grows up to the capacity
+        totals->score_stride = c->opt_replay ? c->row_stride : (int)align_up(c->slot_len[slot], kRowStrideQuantum);
+        const int most = (int)std::min<size_t>(units, c->score_bytes / ((size_t)c->G * totals->score_stride * sizeof(float)));
+        const int passes = (units + most - 1) / most;
+        step = (units + passes - 1) / passes;
+    }
+    for (int u0 = 0; u0 < units; u0 += step) {
+        const int count = std::min(step, units - u0);
+        kvs::DecodePlan plan;
+        const bool use_mma = choose_plan(c, count, c->slot_len[slot], &plan);
+        const AttentionScratch scratch = {reinterpret_cast<float*>(c->ws + c->off_part_o),
+                                          reinterpret_cast<float*>(c->ws + c->off_part_ml),
+                                          reinterpret_cast<int*>(c->ws + c->off_flags),
+                                          reinterpret_cast<int*>(c->ws + c->off_status), take_early_start(c), true};
+        const kvs_status s = run_attention(c, slot, q, out, u0, count, plan, use_mma, scratch, st, nullptr, nullptr, totals);
+        if (s != KVS_OK) return s;
+    }
+    return KVS_OK;
 }
 
 // Rows of unit `u` of `slot` as the host knows them.
@@ -954,7 +979,7 @@ kvs_status kvs_decode_attention_weights(kvs_ctx* ctx, int32_t layer, const void*
     if (total_stride < (ctx->opt_replay ? ctx->cfg.max_seq : ctx->slot_len[ctx->slot_of_layer[layer]])) return KVS_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->cfg.device);
     if (!guard.ok) return KVS_ERR_CUDA;
-    const WeightTotals totals = {total_in, total_out, total_stride};
+    WeightTotals totals = {total_in, total_out, total_stride, 0};
     return do_attention(ctx, layer, q, out, batch, static_cast<cudaStream_t>(stream), &totals);
 }
 
@@ -1449,7 +1474,7 @@ kvs_status kvs_decode_attention_static(kvs_ctx* ctx, int32_t layer, const void* 
     const AttentionScratch scratch = {reinterpret_cast<float*>(base + kStaticStatusBytes + flag_bytes),
                                       reinterpret_cast<float*>(base + kStaticStatusBytes + flag_bytes + part_o_bytes),
                                       reinterpret_cast<int*>(base + kStaticStatusBytes), status_word, false, false};
-    return run_attention(c, slot, q, out, batch, plan, use_mma, scratch, st);
+    return run_attention(c, slot, q, out, 0, batch * c->cfg.n_kv_heads, plan, use_mma, scratch, st);
 }
 
 }  // extern "C"

@@ -294,7 +294,8 @@ struct ScalarKernelArgs {
     unsigned long long wait_ns;   // limit of every wait inside the kernel
     long long stall_tile;         // self-test only: the K/V copies of this tile are withheld (-1: none)
     unsigned long long* trace;    // tracing build: this launch's rows of time stamps, or nullptr
-    float* scores;                // W only: [units][G][row_stride] scores in the log2 domain
+    float* scores;                // W only: [units][G][score_stride] scores in the log2 domain
+    int score_stride;
 };
 
 // W: every row's score is stored beside the ordinary work (kvs_decode_attention_weights normalises them once the
@@ -567,7 +568,7 @@ __global__ void __launch_bounds__(ScalarShape<T, D, G>::THREADS, ScalarShape<T, 
                     if constexpr (W) {
                         // 2^SH neighbouring lanes hold the same row: the first of them stores it
                         if (mine_valid && (lig & ((1 << SH) - 1)) == 0)
-                            a.scores[(u * G + g0 + g) * a.row_stride + (long long)(ti0 + k) * TN + grp + NG * my_i] = sv;
+                            a.scores[(u * G + g0 + g) * a.score_stride + (long long)(ti0 + k) * TN + grp + NG * my_i] = sv;
                     }
                     sv = mine_valid ? sv : -INFINITY;
                     float tmax = sv;
@@ -983,6 +984,7 @@ cudaError_t launch_decode_scalar(const DecodeArgs& a, const DecodePlan& plan, cu
     ka.stall_tile = a.stall_tile;
     ka.trace = a.trace;
     ka.scores = a.scores;
+    ka.score_stride = a.score_stride;
     const bool pdl = a.programmatic;
     if (a.dtype == 0) {
         if (a.D == 128) return launch_scalar_groups<__nv_bfloat16, 128>(a.G, ka, plan.NC, pdl, stream);

@@ -51,8 +51,9 @@ struct DecodeArgs {
     long long stall_tile;    // self-test only: the K/V copies of this tile of the line are withheld (-1: none)
     unsigned long long* trace;    // tracing build only: this launch's [kTraceBlocks][kTraceSlots] words, or nullptr
     // kvs_decode_attention_weights: where the split-K kernel leaves every row's score (log2 domain),
-    // [units][G][row_stride], or nullptr
+    // [units][G][score_stride], or nullptr
     float* scores = nullptr;
+    int score_stride = 0;     // a multiple of 128, at least the rows of a unit
 };
 
 // Whether a launch of this plan over `units` units can finish inside the split-K kernel.

@@ -28,7 +28,7 @@ struct FinishArgs {
     float* total_out;
     float* out;
     long long T;
-    int total_stride, row_stride, G, tpu, NC, n, tile_rows, units, cap, chunks;
+    int total_stride, score_stride, G, tpu, NC, n, tile_rows, units, cap, chunks;
     int turns;                 // turns of a block: it takes turns * kFinishRows rows
     bool vec;                  // totals can be read and written four at a time
     const int* n_extra;
@@ -57,14 +57,14 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
     const int np = block_of_tile((u + 1) * a.tpu - 1, a.T, a.NC) - c0 + 1;
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + (u + c0) * a.G;    // piece c, head g: ml[c * G + g]
     const int n = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
-    const float* sc = a.scores + u * a.G * a.row_stride;
+    const float* sc = a.scores + u * a.G * a.score_stride;
     const long long tot = u * (long long)a.total_stride;
-    // (a score array's rows are padded to the planes' row stride, a multiple of 128: reading four at a time is safe)
+    // (a score array's rows are padded to a multiple of 128: reading four at a time is safe)
     float4 s[8];
     auto fetch = [&](int j) {
 #pragma unroll
         for (int g = 0; g < 8; ++g)
-            if (g < a.G && j < n) s[g] = *reinterpret_cast<const float4*>(sc + (long long)g * a.row_stride + j);
+            if (g < a.G && j < n) s[g] = *reinterpret_cast<const float4*>(sc + (long long)g * a.score_stride + j);
     };
     const int j_first = part * a.turns * kFinishRows + 4 * threadIdx.x;
     if (part < a.chunks) fetch(j_first);
@@ -417,7 +417,7 @@ cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, c
     f.out = a.out;
     f.T = plan.T;
     f.total_stride = total_stride;
-    f.row_stride = a.row_stride;
+    f.score_stride = a.score_stride;
     f.G = a.G;
     f.tpu = plan.tpu;
     f.NC = plan.NC;

@@ -5,7 +5,7 @@ import torch
 
 import operators_reference as ref
 import test_gpu_operators as t
-from paper_2410_18517_b200 import KvsError, Rotary
+from paper_2410_18517_b200 import KVS_OPT_REPLAY, KvsError, Rotary
 from paper_2410_18517_b200 import build as kbuild
 
 pytestmark = pytest.mark.gpu
@@ -126,3 +126,73 @@ def test_every_view_of_a_plane_is_its_callers_own():
     assert not cache.plane(0, 0).any()
     cache.pool = old
     assert torch.equal(cache.plane(0, 0)[:3, :, :20].transpose(1, 2), k)
+
+
+# ------------------------------------------------------------------------------- weighted decode in several passes
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,D,B,n,lens", [("bf16", 64, 8, 64, 5, 70001, None), ("f32", 32, 16, 64, 5, 120000, None), ("bf16", 40, 20, 64, 3, 150000, None),
+                                                     ("bf16", 64, 8, 64, 5, 70001, (70001, 1, 64, 33333, 69999, 5, 40960))])
+def test_weights_of_caches_whose_scores_take_several_passes(dtype, Hq, Hkv, D, B, n, lens):
+    cache = t.SharedKVCache(1, Hq, Hkv, D, B, n, dtype)
+    g = torch.Generator("cuda").manual_seed(n)
+    k, v = (torch.randn(B, n, Hkv, D, generator=g, device="cuda", dtype=t.DT[dtype]) for _ in range(2))
+    cache.append(0, k, v)
+    del k, v
+    if lens:
+        keep = torch.arange(n, dtype=torch.int32, device="cuda").expand(B, Hkv, n).contiguous()
+        cache.evict(0, keep, [[lens[(b * Hkv + h) % len(lens)] for h in range(Hkv)] for b in range(B)])
+    assert B * Hq * n * 4 > 64 << 20
+    before_launches = cache.stats()["attention_launches"]
+    q = t.normal(3, dtype, B, Hq, D)
+    total = torch.rand(B, Hkv, n + 3, device="cuda", generator=g)
+    new = torch.full_like(total, 9.0)
+    out = cache.decode_attention_weights(0, q, total, new)
+    assert cache.stats()["attention_launches"] - before_launches > 1
+    t.check_weights(cache, 0, q, total, new, out, n + 3)
+    assert (new[..., n:] == 9.0).all()
+    again = total.clone()
+    assert torch.equal(cache.decode_attention_weights(0, q, again), out)
+    for b in range(B):
+        for h in range(Hkv):
+            m = cache.unit_len(0, b, h)
+            assert torch.equal(again[b, h, :m], new[b, h, :m]) and torch.equal(again[b, h, m:], total[b, h, m:])
+    assert (out - cache.decode_attention(0, q)).abs().max() < 2e-5
+    assert cache.device_status() == 0
+
+
+def test_weights_in_several_passes_under_graph_replay():
+    """A recorded step reserves scores for the capacity: several passes although the rows are few."""
+    B, Hq, Hkv, D, n0, steps = 4, 64, 8, 64, 100, 4
+    results = []
+    ks, vs, qs = (t.normal(30 + i, "bf16", steps, B, 1, h, D) for i, h in enumerate((Hkv, Hkv, Hq)))
+    for graph in (False, True):
+        cache, _, _ = t.filled(Hq, Hkv, D, B, n0, "bf16", extra=80000, cls=t.SharedKVCache)
+        total = torch.zeros(B, Hkv, n0 + 80000, device="cuda")
+        k, v, q, out = ks[0].clone(), vs[0].clone(), qs[0, :, 0].clone(), torch.empty(B, Hq, D, device="cuda")
+
+        def step():
+            cache.append(0, k, v)
+            cache.decode_attention_weights(0, q, total, out=out)
+            if graph:
+                cache.replay_advance()
+
+        if graph:
+            cache.set_option(KVS_OPT_REPLAY, 1)
+            before = cache.stats()["attention_launches"]
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                step()
+            assert cache.stats()["attention_launches"] - before > 1
+        outs = []
+        for i in range(steps):
+            k.copy_(ks[i]); v.copy_(vs[i]); q.copy_(qs[i, :, 0])
+            g.replay() if graph else step()
+            outs.append(out.clone())
+        if graph:
+            cache.replay_commit(steps)
+        torch.cuda.synchronize()
+        assert cache.seq_len(0) == n0 + steps and cache.device_status() == 0
+        results.append((total, outs))
+    assert (results[0][0] - results[1][0]).abs().max() < 1e-5
+    for a, b in zip(results[0][1], results[1][1]):
+        assert (a - b).abs().max() < 1e-5

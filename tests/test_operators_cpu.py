@@ -100,3 +100,17 @@ def test_reference_selection_and_trees():
                 assert not (w >> j & 1) or words[j] & ~w == 0          # ancestors bring their own ancestors
         assert [x & (1 << 64) - 1 for x in ref.to_int64(words)] == words
     assert math.isclose(ref.weight_error(0.0, 1), 2 * 120 * ref.U + 2 * ref.EXP2 + 2 * ref.U)
+
+
+def test_workspace_does_not_grow_with_the_scores_of_the_whole_cache():
+    """The weighted decode works through a cache in passes of 64 MiB of scores: 32 sequences of 32768 rows and 32 q-heads would
+    fill 128 MiB.  Beyond that a context needs the partial results, and 48 MiB and the partial sums of the search reductions."""
+    def workspace(B, n, Hq=32, Hkv=8, D=128):
+        c = kb.kvs_create(1, Hq, Hkv, D, B, n, kb.KVS_BF16, 0.0, 0)
+        ws = kb.kvs_required_bytes(c)[1]
+        kb.kvs_destroy(c)
+        return ws
+
+    assert workspace(32, 32768) < 80 << 20
+    assert workspace(32, 32768) - workspace(32, 16384) < 1 << 20          # both at the limit
+    assert workspace(1, 1 << 20, Hq=64, Hkv=8) < 80 << 20                 # 8 units of 32 MiB of scores
