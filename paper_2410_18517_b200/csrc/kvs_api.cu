@@ -222,7 +222,7 @@ void layout_workspace(kvs_ctx* c) {
         c->off_scores = off;
         c->score_bytes = scores;
         // kvs_tree_attention: two cut pieces per thread block at most
-        const size_t tree_rows = (size_t)2 * kvs::kTreeMaxBlocks * kvs::tree_partial_rows(c->G);
+        const size_t tree_rows = (size_t)kvs::tree_piece_rows(c->G);
         const size_t tree_o = align_up(tree_rows * f.head_dim * sizeof(float), kAlign);
         c->off_tree_o = off;
         c->off_tree_ml = off + tree_o;
@@ -396,6 +396,7 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int un
     a.finish_in_kernel = c->opt_finish != 0 && kvs::can_finish_in_kernel(plan, a.units) && totals == nullptr;
     a.scores = totals ? reinterpret_cast<float*>(c->ws + c->off_scores) : nullptr;
     a.score_stride = totals ? totals->score_stride : 0;
+    a.score_count = (long long)(c->score_bytes / sizeof(float));
     a.flags = scratch.flags;
     if (scratch.tracked) {
         c->seq += a.finish_in_kernel ? 1 : 2;     // split-K kernel, then (unless it finishes the units itself) combine
@@ -1008,6 +1009,7 @@ kvs_status kvs_select_rows(kvs_ctx* ctx, int32_t layer, const float* total, int3
     a.unit_len = ctx->ragged[slot] ? unit_len_dev(ctx, slot) : nullptr;
     a.n_recent = n_recent;
     a.sm_count = ctx->sm_count;
+    a.status = reinterpret_cast<int*>(ctx->ws + ctx->off_status);
     for (int u0 = 0; u0 < units; u0 += kvs::SelectCounts::kMax) {
         a.unit0 = u0;
         a.units = std::min(units - u0, (int)kvs::SelectCounts::kMax);

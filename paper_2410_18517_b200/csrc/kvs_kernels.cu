@@ -296,6 +296,7 @@ struct ScalarKernelArgs {
     unsigned long long* trace;    // tracing build: this launch's rows of time stamps, or nullptr
     float* scores;                // W only: [units][G][score_stride] scores in the log2 domain
     int score_stride;
+    long long score_count;
 };
 
 // W: every row's score is stored beside the ordinary work (kvs_decode_attention_weights normalises them once the
@@ -567,8 +568,8 @@ __global__ void __launch_bounds__(ScalarShape<T, D, G>::THREADS, ScalarShape<T, 
                     float sv = reduce_transpose<R, LPR / 2>(s[g], lig);
                     if constexpr (W) {
                         // 2^SH neighbouring lanes hold the same row: the first of them stores it
-                        if (mine_valid && (lig & ((1 << SH) - 1)) == 0)
-                            a.scores[(u * G + g0 + g) * a.score_stride + (long long)(ti0 + k) * TN + grp + NG * my_i] = sv;
+                        const long long at = (u * G + g0 + g) * a.score_stride + (long long)(ti0 + k) * TN + grp + NG * my_i;
+                        if (mine_valid && (lig & ((1 << SH) - 1)) == 0 && KVS_BOUNDS_OK(at, 1, a.score_count, a.status)) a.scores[at] = sv;
                     }
                     sv = mine_valid ? sv : -INFINITY;
                     float tmax = sv;
@@ -985,6 +986,7 @@ cudaError_t launch_decode_scalar(const DecodeArgs& a, const DecodePlan& plan, cu
     ka.trace = a.trace;
     ka.scores = a.scores;
     ka.score_stride = a.score_stride;
+    ka.score_count = a.score_count;
     const bool pdl = a.programmatic;
     if (a.dtype == 0) {
         if (a.D == 128) return launch_scalar_groups<__nv_bfloat16, 128>(a.G, ka, plan.NC, pdl, stream);

@@ -54,6 +54,7 @@ struct DecodeArgs {
     // [units][G][score_stride], or nullptr
     float* scores = nullptr;
     int score_stride = 0;     // a multiple of 128, at least the rows of a unit
+    long long score_count = 0;   // floats there is room for (what a bounds-checking build checks against)
 };
 
 // Whether a launch of this plan over `units` units can finish inside the split-K kernel.
@@ -182,7 +183,9 @@ struct TreeArgs {
 constexpr int kTreeMaxTokens = 64;
 constexpr int kTreeMaxBlocks = 320;    // thread blocks of one call; bounds the partial results
 constexpr int kTreeTileRows = 128;     // query rows of the largest tile
-inline int tree_partial_rows(int G) { return G * kTreeMaxTokens < kTreeTileRows ? G * kTreeMaxTokens : kTreeTileRows; }
+__host__ __device__ inline int tree_partial_rows(int G) { return G * kTreeMaxTokens < kTreeTileRows ? G * kTreeMaxTokens : kTreeTileRows; }
+// rows of partial results there is room for: two cut pieces per thread block at most
+__host__ __device__ inline long long tree_piece_rows(int G) { return 2ll * kTreeMaxBlocks * tree_partial_rows(G); }
 cudaError_t init_tree_kernels();
 // the tensor-core kernel (bf16; see kvs_tree_tc.cu); launch_tree chooses and adds the combine step
 cudaError_t init_tree_tc_kernels();
@@ -209,6 +212,7 @@ struct SelectArgs {
     int n_recent;
     int unit0, units;         // units of this launch
     int sm_count;
+    int* status;
 };
 cudaError_t init_weights_kernels();
 cudaError_t launch_select(const SelectArgs& a, const SelectCounts& counts, cudaStream_t stream);

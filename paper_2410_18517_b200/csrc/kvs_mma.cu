@@ -145,6 +145,7 @@ struct MmaKernelArgs {
     unsigned long long* trace;    // tracing build: this launch's rows of time stamps, or nullptr
     float* scores;                // W only: [units][G][score_stride] scores in the log2 domain
     int score_stride;
+    long long score_count;
 };
 
 // G (q-heads per kv-head, 1..8) is a run-time argument: it only selects which rows of the padded
@@ -439,10 +440,11 @@ __global__ void __launch_bounds__(kMmaThreads, KVS_MMA_BLOCKS_PER_SM)
                     }
                 if constexpr (W) {
                     if (row < G) {
-                        float* dst = a.scores + (u * G + row) * a.score_stride + (long long)(ti0 + k) * TN + tok0 + quad * 2;
+                        const long long at = (u * G + row) * a.score_stride + (long long)(ti0 + k) * TN + tok0 + quad * 2;
 #pragma unroll
                         for (int nb = 0; nb < 2; ++nb)      // rows up to the stride, a multiple of 128, are scratch
-                            if (tok0 < valid) *reinterpret_cast<float2*>(dst + nb * 8) = make_float2(s[blk][nb][0], s[blk][nb][1]);
+                            if (tok0 < valid && KVS_BOUNDS_OK(at + nb * 8, 2, a.score_count, a.status))
+                                *reinterpret_cast<float2*>(a.scores + at + nb * 8) = make_float2(s[blk][nb][0], s[blk][nb][1]);
                     }
                 }
             }
@@ -728,6 +730,7 @@ cudaError_t launch_decode_mma(const DecodeArgs& a, const DecodePlan& plan, const
     ka.trace = a.trace;
     ka.scores = a.scores;
     ka.score_stride = a.score_stride;
+    ka.score_count = a.score_count;
     if (a.G < 1 || a.G > 8) return cudaErrorInvalidValue;
     const bool big = plan.tile_rows * a.D * 2 == kMmaBigTileBytes && kMmaBigTileBytes != kMmaTileBytes;
     if (a.D == 128)

@@ -160,7 +160,7 @@ __device__ __forceinline__ void finish_row(float (&x)[8], bool norm, const float
 // token's sequence and row in its units (of a ragged slot: behind the unit's length).
 template <int RB>
 __device__ __forceinline__ char* target(const RotaryKernelArgs& a, long long tok, int r, int h, bool is_q, bool is_v, int seq, int row, bool report) {
-    if (is_q) return a.q_out + (tok * a.Hq + r) * RB;
+    if (is_q) return KVS_BOUNDS_OK(tok, 1, a.tokens, a.status) ? a.q_out + (tok * a.Hq + r) * RB : nullptr;
     const int u = seq * a.Hkv + h;
     if (a.unit_len) row += a.unit_len[u];
     if (row >= a.capacity) {

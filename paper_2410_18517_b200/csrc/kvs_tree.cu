@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
             float f[EPL];
 #pragma unroll
             for (int e = 0; e < EPL; ++e) f[e] = 0.f;
-            if (r < rows) {
+            if (r < rows && KVS_BOUNDS_OK(tok0 + r / a.G, 1, a.n_t, a.status) && KVS_BOUNDS_OK(u, 1, a.units, a.status)) {
                 const long long off = (((long long)b * a.n_t + tok0 + r / a.G) * a.Hq + hk * a.G + r % a.G) * D + c * EPL;
                 Unpack<T>::run(*reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + off), f);
             }
@@ -212,6 +212,7 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
                     store4<T>(dst + 64 * c + 4 * tx, make_float4(o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv));
             } else {
                 const long long pr = (slot * p.m_tiles + mt) * p.tile_rows + row;
+                if (!KVS_BOUNDS_OK(pr, 1, tree_piece_rows(a.G), a.status)) continue;
 #pragma unroll
                 for (int c = 0; c < CB; ++c) *reinterpret_cast<float4*>(a.part_o + pr * D + 64 * c + 4 * tx) = o[r][c];
                 if (tx == 0) *reinterpret_cast<float2*>(a.part_ml + pr * 2) = make_float2(m[r], l[r]);
@@ -250,6 +251,7 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     const long long first = (long long)u * p.tpu;
     const int c0 = team_of_tile(first, p.T, p.teams), np = team_of_tile(first + nt - 1, p.T, p.teams) - c0 + 1;
     if (np == 1) return;                                         // finished by its one team
+    if (!KVS_BOUNDS_OK(((2ll * (c0 + np) - 1) * p.m_tiles + mt) * p.tile_rows + row, 1, tree_piece_rows(a.G), a.status)) return;
     // this warp's pieces, c = 0 .. mine-1; piece i of the unit: slot 2 (c0 + i), the first one 2 c0 + 1
     const int w0 = LONG ? warp : 0, mine = (np - w0 + STEP - 1) / STEP;
     auto where = [&](int c) {
@@ -340,7 +342,9 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* v
                 if (v == 0) atomicExch(status, 1);
                 src = j;
             }
-            if (!KVS_BOUNDS_OK((u * row_stride + base + src) * (long long)row_vecs, row_vecs, plane_vecs, status)) continue;
+            if (!KVS_BOUNDS_OK((u * row_stride + base + src) * (long long)row_vecs, row_vecs, plane_vecs, status) ||
+                !KVS_BOUNDS_OK(i, 1, kTreeMaxTokens * 32, status))
+                continue;
             buf[i] = rows[(long long)src * row_vecs + v];
         }
         __syncthreads();

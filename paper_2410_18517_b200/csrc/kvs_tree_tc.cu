@@ -424,6 +424,7 @@ __global__ void __launch_bounds__(kTcThreads, 2)
             const bool patch = broken[pc & 1] == pc + 1;
             const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;        // nothing visible: 0
             const long long orow = ((long long)b * a.n_t + tok) * a.Hq + hk * a.G + g;
+            const bool inside = KVS_BOUNDS_OK(orow, 1, (long long)a.B * a.n_t * a.Hq, a.status);
             const long long prow = ((2ll * team + (pi.ti0 == 0 ? 1 : 0)) * p.m_tiles + mt) * p.tile_rows + r;
 #pragma unroll 1
             for (int c = 0; c < D; c += 32) {
@@ -443,19 +444,19 @@ __global__ void __launch_bounds__(kTcThreads, 2)
                         }
                     }
                 }
-                if (real && pi.whole) {
+                if (real && pi.whole && inside) {
                     uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(a.out) + orow * D + c);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         dst[i] = make_uint4(pack2_bf16(o[8 * i] * inv, o[8 * i + 1] * inv), pack2_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv),
                                             pack2_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv), pack2_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv));
-                } else if (real) {
+                } else if (real && KVS_BOUNDS_OK(prow, 1, tree_piece_rows(a.G), a.status)) {
                     float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) dst[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
             }
-            if (!pi.whole && real) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(m_ref, l);
+            if (!pi.whole && real && KVS_BOUNDS_OK(prow, 1, tree_piece_rows(a.G), a.status)) *reinterpret_cast<float2*>(a.part_ml + prow * 2) = make_float2(m_ref, l);
             tc_fence_before();      // the next piece's first PV waits for this thread's arrival on p_full
         }
     }

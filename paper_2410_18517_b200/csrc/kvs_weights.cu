@@ -33,6 +33,8 @@ struct FinishArgs {
     bool vec;                  // totals can be read and written four at a time
     const int* n_extra;
     const int* unit_len;
+    long long score_count;
+    int* status;
 };
 
 __device__ __forceinline__ int block_of_tile(long long gt, long long T, int NC) { return (int)(((gt + 1) * NC + T - 1) / T - 1); }
@@ -54,7 +56,8 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
     const int part = blockIdx.x - (int)u * per_unit;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int c0 = block_of_tile(u * a.tpu, a.T, a.NC);
-    const int np = block_of_tile((u + 1) * a.tpu - 1, a.T, a.NC) - c0 + 1;
+    int np = block_of_tile((u + 1) * a.tpu - 1, a.T, a.NC) - c0 + 1;
+    if (!KVS_BOUNDS_OK(u, 1, a.units, a.status) || !KVS_BOUNDS_OK(u + c0, np, (long long)a.units + a.NC, a.status)) np = 0;
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + (u + c0) * a.G;    // piece c, head g: ml[c * G + g]
     const int n = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
     const float* sc = a.scores + u * a.G * a.score_stride;
@@ -64,7 +67,7 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
     auto fetch = [&](int j) {
 #pragma unroll
         for (int g = 0; g < 8; ++g)
-            if (g < a.G && j < n) s[g] = *reinterpret_cast<const float4*>(sc + (long long)g * a.score_stride + j);
+            if (g < a.G && j < n && KVS_BOUNDS_OK((u * a.G + g) * a.score_stride + j, 4, a.score_count, a.status)) s[g] = *reinterpret_cast<const float4*>(sc + (long long)g * a.score_stride + j);
     };
     const int j_first = part * a.turns * kFinishRows + 4 * threadIdx.x;
     if (part < a.chunks) fetch(j_first);
@@ -88,7 +91,7 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
     if (part < a.chunks) {
         for (int turn = 0; turn < a.turns; ++turn) {
             const int j = j_first + turn * kFinishRows;
-            if (j >= n) break;
+            if (j >= n || !KVS_BOUNDS_OK(j, min(4, n - j), a.total_stride, a.status)) break;
             if (turn > 0) fetch(j);
             float t[4] = {0.f, 0.f, 0.f, 0.f};
             const bool vec = a.vec && j + 4 <= n;
@@ -206,6 +209,8 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
     __shared__ int s_need;
     const int unit = SPREAD ? blockIdx.x / cluster : blockIdx.x, rank = SPREAD ? blockIdx.x - unit * cluster : 0;
     const long long u = a.unit0 + unit;
+    // (in a normal build the compiler drops the check)
+    auto fits = [&](int at) { return KVS_BOUNDS_OK(at, 1, a.keep_stride, a.status) && KVS_BOUNDS_OK(unit, 1, a.units, a.status); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, threads = blockDim.x, warps = threads >> 5;
     const int n = a.unit_len ? a.unit_len[u] : a.n;
     const int want = counts.n[unit] - a.n_recent;     // rows chosen by total
@@ -217,7 +222,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
 #pragma unroll
         for (int i = 0; i < IPT; ++i) {
             const int j = base + first + 32 * i;
-            key[i] = __float_as_uint(j < old ? total[j] : __uint_as_float(0x7fffffffu));
+            key[i] = __float_as_uint(j < old && KVS_BOUNDS_OK(j, 1, a.total_stride, a.status) ? total[j] : __uint_as_float(0x7fffffffu));
         }
 #pragma unroll
         for (int i = 0; i < IPT; ++i) key[i] = order_key(__uint_as_float(key[i]));
@@ -338,8 +343,10 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
                     const uint32_t taken = __ballot_sync(0xffffffffu, take);
                     if (take) {
                         const int at = pos + __popc(taken & below);
-                        keep[at] = base + first + 32 * i;
-                        if (kept) kept[at] = total_of(key[i], from + 32 * i);
+                        if (fits(at)) {
+                            keep[at] = base + first + 32 * i;
+                            if (kept) kept[at] = total_of(key[i], from + 32 * i);
+                        }
                     }
                     pos += __popc(taken);
                 }
@@ -351,8 +358,10 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
                     const uint32_t taken = __ballot_sync(0xffffffffu, take);
                     if (take) {
                         const int at = pos + __popc(taken & below);
-                        keep[at] = base + first + 32 * i;
-                        if (kept) kept[at] = total_of(key[i], from + 32 * i);
+                        if (fits(at)) {
+                            keep[at] = base + first + 32 * i;
+                            if (kept) kept[at] = total_of(key[i], from + 32 * i);
+                        }
                     }
                     pos += __popc(taken);
                     seen += __popc(same);
@@ -364,6 +373,7 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
         }
     }
     for (int j = old + rank * threads + tid; j < n; j += (SPREAD ? cluster : 1) * threads) {
+        if (!fits(want + j - old) || !KVS_BOUNDS_OK(j, 1, a.total_stride, a.status)) continue;
         keep[want + j - old] = j;
         if (kept) kept[want + j - old] = total[j];
     }
@@ -427,6 +437,8 @@ cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, c
     f.cap = a.capacity;
     f.n_extra = a.n_extra;
     f.unit_len = a.unit_len;
+    f.score_count = a.score_count;
+    f.status = a.status;
     const int turns = ((a.n_extra ? a.capacity : a.n) + kFinishRows - 1) / kFinishRows;      // of a unit's longest run of rows
     // several turns per block once eight blocks per SM are there without (640 units of 8192 rows: 2 blocks each)
     f.turns = (int)std::min<long long>(turns, std::max<long long>(1, (long long)a.units * turns / (8 * 148)));

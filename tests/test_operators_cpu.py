@@ -114,3 +114,20 @@ def test_workspace_does_not_grow_with_the_scores_of_the_whole_cache():
     assert workspace(32, 32768) < 80 << 20
     assert workspace(32, 32768) - workspace(32, 16384) < 1 << 20          # both at the limit
     assert workspace(1, 1 << 20, Hq=64, Hkv=8) < 80 << 20                 # 8 units of 32 MiB of scores
+
+
+@pytest.mark.parametrize("source,limits", [
+    ("kvs_kernels.cu", ["score_count"]), ("kvs_mma.cu", ["score_count"]), ("kvs_rotary.cu", ["plane_bytes", "a.tokens"]),
+    ("kvs_tree.cu", ["plane_bytes", "plane_vecs", "tree_piece_rows", "kTreeMaxTokens"]), ("kvs_tree_tc.cu", ["plane_rows", "tree_piece_rows", "a.n_t * a.Hq"]),
+    ("kvs_weights.cu", ["score_count", "a.units + a.NC", "total_stride", "keep_stride"]),
+])
+def test_bounds_build_checks_the_serving_kernels_buffers(source, limits):
+    """Every buffer the serving kernels index (scores, totals, partial results, keep lists, rows) is the limit of a check."""
+    import os
+    import re
+
+    with open(os.path.join(kbuild.CSRC, source)) as f:
+        text = re.sub(r"\s+", " ", f.read())
+    calls = [text[m.end(): m.end() + 220].split("status)")[0] for m in re.finditer(r"KVS_BOUNDS_OK\(", text)]
+    for limit in limits:
+        assert any(limit in c for c in calls), (source, limit)
