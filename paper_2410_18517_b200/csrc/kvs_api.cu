@@ -414,7 +414,7 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int un
     if (!a.finish_in_kernel) {
         const size_t total0 = totals ? (size_t)unit0 * totals->stride : 0;
         const cudaError_t e = totals ? kvs::launch_weights_finish(a, plan, totals->in ? totals->in + total0 : nullptr, totals->out + total0,
-                                                                  totals->stride, st)
+                                                                  totals->stride, c->sm_count, st)
                                      : kvs::launch_combine(a, plan, st);
         if (e != cudaSuccess) return KVS_ERR_CUDA;
         c->stats.combine_launches += 1;

@@ -197,7 +197,7 @@ cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* laun
 //   launch_weights_finish: merges the pieces of a split-K launch that stored its scores (out, as launch_combine)
 //   and adds every row's weight, summed over the group's heads, to its total
 cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, const float* total_in, float* total_out,
-                                  int total_stride, cudaStream_t stream);
+                                  int total_stride, int sm_count, cudaStream_t stream);
 struct SelectCounts {
     static constexpr int kMax = 900;   // units per launch
     int n[kMax];                       // rows to keep

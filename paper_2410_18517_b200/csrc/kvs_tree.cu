@@ -357,11 +357,11 @@ __global__ void __launch_bounds__(256) accept_draft_kernel(char* kplane, char* v
 }
 
 template <typename T, int D>
-cudaError_t launch_combine_one(const TreeKernelArgs& ka, cudaStream_t stream) {
+cudaError_t launch_combine_one(const TreeKernelArgs& ka, int sm_count, cudaStream_t stream) {
     const long long items = (long long)ka.a.units * ka.a.n_t * ka.a.G;
     // four warps per item where a unit may have more than 16 pieces and the items are few enough that their latency
     // counts (one unit of 8192 rows, 64 items: 22.5 us with one warp, 14.5 with four; 2048 items of 20 pieces: 25 and 29)
-    const bool many = ka.p.teams / ka.a.units + 2 > 16 && items <= 8 * 148;
+    const bool many = ka.p.teams / ka.a.units + 2 > 16 && items <= 8 * sm_count;
     const dim3 block(kTreeCombineWarps * 32), grid((unsigned)(many ? items : (items + kTreeCombineWarps - 1) / kTreeCombineWarps));
     return many ? launch_kernel(tree_combine_kernel<T, D, true>, grid, block, 0, stream, ka.a.programmatic, ka)
                 : launch_kernel(tree_combine_kernel<T, D, false>, grid, block, 0, stream, ka.a.programmatic, ka);
@@ -406,9 +406,9 @@ cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* laun
     *launches = cut ? 2 : 1;
     if (e != cudaSuccess || !cut) return e;
     if (a.dtype == 0)
-        return a.D == 128 ? launch_combine_one<__nv_bfloat16, 128>(ka, stream)
-                          : launch_combine_one<__nv_bfloat16, 64>(ka, stream);
-    return a.D == 128 ? launch_combine_one<float, 128>(ka, stream) : launch_combine_one<float, 64>(ka, stream);
+        return a.D == 128 ? launch_combine_one<__nv_bfloat16, 128>(ka, sm_count, stream)
+                          : launch_combine_one<__nv_bfloat16, 64>(ka, sm_count, stream);
+    return a.D == 128 ? launch_combine_one<float, 128>(ka, sm_count, stream) : launch_combine_one<float, 64>(ka, sm_count, stream);
 }
 
 cudaError_t launch_accept(void* kplane, void* vplane, const int* path, int path_stride, const AcceptCounts& counts,

@@ -417,7 +417,7 @@ cudaError_t init_weights_kernels() {
 }
 
 cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, const float* total_in, float* total_out,
-                                  int total_stride, cudaStream_t stream) {
+                                  int total_stride, int sm_count, cudaStream_t stream) {
     FinishArgs f;
     f.part_o = a.part_o;
     f.part_ml = a.part_ml;
@@ -441,7 +441,7 @@ cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, c
     f.status = a.status;
     const int turns = ((a.n_extra ? a.capacity : a.n) + kFinishRows - 1) / kFinishRows;      // of a unit's longest run of rows
     // several turns per block once eight blocks per SM are there without (640 units of 8192 rows: 2 blocks each)
-    f.turns = (int)std::min<long long>(turns, std::max<long long>(1, (long long)a.units * turns / (8 * 148)));
+    f.turns = (int)std::min<long long>(turns, std::max<long long>(1, (long long)a.units * turns / (8ll * sm_count)));
     f.chunks = (turns + f.turns - 1) / f.turns;
     f.vec = total_stride % 4 == 0 && (uintptr_t)total_in % 16 == 0 && (uintptr_t)total_out % 16 == 0;
     const dim3 grid((unsigned)(a.units * (f.chunks + a.G)));

@@ -131,3 +131,13 @@ def test_bounds_build_checks_the_serving_kernels_buffers(source, limits):
     calls = [text[m.end(): m.end() + 220].split("status)")[0] for m in re.finditer(r"KVS_BOUNDS_OK\(", text)]
     for limit in limits:
         assert any(limit in c for c in calls), (source, limit)
+
+
+@pytest.mark.parametrize("source", ["kvs_rotary.cu", "kvs_tree.cu", "kvs_tree_tc.cu", "kvs_weights.cu"])
+def test_launch_rules_ask_for_the_device_s_sm_count(source):
+    import os
+    import re
+
+    with open(os.path.join(kbuild.CSRC, source)) as f:
+        code = re.sub(r"//[^\n]*", "", f.read())
+    assert not re.search(r"\b148\b", code)
