@@ -148,7 +148,7 @@ cudaError_t launch_append_rotary(const RotaryArgs& r, cudaStream_t stream);
 // Attention of a tree of drafted tokens (see kvs_tree.cu).  The n_t queries of a sequence are the newest n_t rows
 // of its units; the G heads of a kv-head and the tokens form the rows of query tiles of `rows` rows.  A *team* of
 // thread blocks that covers the m_tiles query tiles walks a contiguous run of the line of key tiles (units * tiles per
-// unit), each block with its own query tile (tensor cores: two), so that the team reads every K/V tile at the same time.  A unit cut between teams
+// unit), each block with its own query tile, so that the team reads every K/V tile at the same time.  A unit cut between teams
 // leaves one piece per team: piece slot 2 * team + 1 if it begins the unit, 2 * team otherwise.
 struct TreePlan {
     int tokens;      // drafted tokens per query tile

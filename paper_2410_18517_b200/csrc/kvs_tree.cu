@@ -26,18 +26,13 @@ __host__ __device__ __forceinline__ int team_of_tile(long long gt, long long T, 
     return (int)(((gt + 1) * teams + T - 1) / T - 1);
 }
 
-template <typename T>
-__device__ __forceinline__ void store4(T* dst, const float4& v);
-template <>
-__device__ __forceinline__ void store4<float>(float* dst, const float4& v) { *reinterpret_cast<float4*>(dst) = v; }
-
 struct TreeKernelArgs {
     TreeArgs a;
     TreePlan p;
 };
 
 // --------------------------------------------------------------------------------------
-// fp32 FMA kernel.  32 query rows x 64 keys per step; thread (ty, tx) owns rows 2 ty, 2 ty + 1 and, of the
+// FMA kernel of fp32 storage.  32 query rows x 64 keys per step; thread (ty, tx) owns rows 2 ty, 2 ty + 1 and, of the
 // scores, keys tx + 16 i, of the output, columns 4 tx + 64 c: every operand comes from shared memory as float4 and
 // the 16 lanes of a row reduce its softmax with shuffles.
 // --------------------------------------------------------------------------------------
@@ -47,10 +42,10 @@ struct TreeShape {
     static constexpr int SMEM_BYTES = (kTreeRows * LD + kTreeKeys * LD + kTreeKeys * D + kTreeRows * kTreeKeys) * 4 + kTreeRows * 8;
 };
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __grid_constant__ TreeKernelArgs ka) {
     using S = TreeShape<D>;
-    constexpr int EPL = 16 / (int)sizeof(T), LPR = D / EPL, CB = D / 64;
+    constexpr int LPR = D / 4, CB = D / 64;       // 16-byte chunks of a row
     const TreeArgs& a = ka.a;
     const TreePlan& p = ka.p;
     extern __shared__ __align__(16) float smem_f[];
@@ -79,21 +74,17 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
         if (ti0 >= te) continue;                                 // the piece lies past a ragged unit's end
         const int b = (int)(u / a.Hkv), hk = (int)(u - (long long)b * a.Hkv);
         const int ctx = n - a.n_t;                               // rows every query sees
-        const T* K = reinterpret_cast<const T*>(a.kplane) + u * a.row_stride * (long long)D;
-        const T* V = reinterpret_cast<const T*>(a.vplane) + u * a.row_stride * (long long)D;
+        const float* K = static_cast<const float*>(a.kplane) + u * a.row_stride * (long long)D;
+        const float* V = static_cast<const float*>(a.vplane) + u * a.row_stride * (long long)D;
         __syncthreads();                                         // the previous piece's readers are done
         for (int i = tid; i < kTreeRows * LPR; i += kTreeThreads) {
             const int r = i / LPR, c = i - r * LPR;
-            float f[EPL];
-#pragma unroll
-            for (int e = 0; e < EPL; ++e) f[e] = 0.f;
+            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
             if (r < rows && KVS_BOUNDS_OK(tok0 + r / a.G, 1, a.n_t, a.status) && KVS_BOUNDS_OK(u, 1, a.units, a.status)) {
-                const long long off = (((long long)b * a.n_t + tok0 + r / a.G) * a.Hq + hk * a.G + r % a.G) * D + c * EPL;
-                Unpack<T>::run(*reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(a.q) + off), f);
+                const long long off = (((long long)b * a.n_t + tok0 + r / a.G) * a.Hq + hk * a.G + r % a.G) * D + c * 4;
+                f = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + off);
             }
-#pragma unroll
-            for (int e = 0; e < EPL; e += 4)
-                *reinterpret_cast<float4*>(Qs + r * S::LD + c * EPL + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+            *reinterpret_cast<float4*>(Qs + r * S::LD + c * 4) = f;
         }
         if (tid < kTreeRows) {
             const int t = tok0 + tid / a.G;
@@ -115,16 +106,11 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
                 const bool isv = i >= kTreeKeys * LPR;
                 const int ii = isv ? i - kTreeKeys * LPR : i;
                 const int r = ii / LPR, c = ii - r * LPR;
-                float f[EPL];
-#pragma unroll
-                for (int e = 0; e < EPL; ++e) f[e] = 0.f;
-                if (key0 + r < n && KVS_BOUNDS_OK(((u * a.row_stride + key0 + r) * (long long)D + c * EPL) * (int)sizeof(T), 16,
+                float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (key0 + r < n && KVS_BOUNDS_OK(((u * a.row_stride + key0 + r) * (long long)D + c * 4) * (int)sizeof(float), 16,
                                                   a.plane_bytes, a.status))
-                    Unpack<T>::run(*reinterpret_cast<const uint4*>((isv ? V : K) + (long long)(key0 + r) * D + c * EPL), f);
-                float* dst = isv ? Vs + r * D : Ks + r * S::LD;
-#pragma unroll
-                for (int e = 0; e < EPL; e += 4)
-                    *reinterpret_cast<float4*>(dst + c * EPL + e) = make_float4(f[e], f[e + 1], f[e + 2], f[e + 3]);
+                    f = *reinterpret_cast<const float4*>((isv ? V : K) + (long long)(key0 + r) * D + c * 4);
+                *reinterpret_cast<float4*>((isv ? Vs + r * D : Ks + r * S::LD) + c * 4) = f;
             }
             __syncthreads();
             float s[2][4];
@@ -206,10 +192,10 @@ __global__ void __launch_bounds__(kTreeThreads, 2) tree_attention_fma(const __gr
             if (row >= rows) continue;
             if (whole) {
                 const float inv = l[r] > 0.f || l[r] != l[r] ? 1.0f / l[r] : 0.f;    // nothing visible: 0
-                T* dst = reinterpret_cast<T*>(a.out) + (((long long)b * a.n_t + tok0 + row / a.G) * a.Hq + hk * a.G + row % a.G) * D;
+                float* dst = static_cast<float*>(a.out) + (((long long)b * a.n_t + tok0 + row / a.G) * a.Hq + hk * a.G + row % a.G) * D;
 #pragma unroll
                 for (int c = 0; c < CB; ++c)
-                    store4<T>(dst + 64 * c + 4 * tx, make_float4(o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv));
+                    *reinterpret_cast<float4*>(dst + 64 * c + 4 * tx) = make_float4(o[r][c].x * inv, o[r][c].y * inv, o[r][c].z * inv, o[r][c].w * inv);
             } else {
                 const long long pr = (slot * p.m_tiles + mt) * p.tile_rows + row;
                 if (!KVS_BOUNDS_OK(pr, 1, tree_piece_rows(a.G), a.status)) continue;
@@ -371,8 +357,8 @@ cudaError_t launch_combine_one(const TreeKernelArgs& ka, int sm_count, cudaStrea
 
 cudaError_t init_tree_kernels() {
     cudaError_t e;
-    if ((e = cudaFuncSetAttribute(tree_attention_fma<float, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<128>::SMEM_BYTES)) != cudaSuccess ||
-        (e = cudaFuncSetAttribute(tree_attention_fma<float, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<64>::SMEM_BYTES)) != cudaSuccess)
+    if ((e = cudaFuncSetAttribute(tree_attention_fma<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<128>::SMEM_BYTES)) != cudaSuccess ||
+        (e = cudaFuncSetAttribute(tree_attention_fma<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, TreeShape<64>::SMEM_BYTES)) != cudaSuccess)
         return e;
     return init_tree_tc_kernels();
 }
@@ -396,9 +382,9 @@ cudaError_t launch_tree(const TreeArgs& a, int sm_count, int max_ctas, int* laun
         p.T = (long long)a.units * p.tpu;
         p.teams = (int)std::min<long long>(p.T, std::max(1, blocks / p.m_tiles));
         const unsigned grid = (unsigned)(p.teams * p.m_tiles);
-        e = a.D == 128 ? launch_kernel(tree_attention_fma<float, 128>, dim3(grid), dim3(kTreeThreads), TreeShape<128>::SMEM_BYTES, stream,
+        e = a.D == 128 ? launch_kernel(tree_attention_fma<128>, dim3(grid), dim3(kTreeThreads), TreeShape<128>::SMEM_BYTES, stream,
                                        a.programmatic, ka)
-                       : launch_kernel(tree_attention_fma<float, 64>, dim3(grid), dim3(kTreeThreads), TreeShape<64>::SMEM_BYTES, stream,
+                       : launch_kernel(tree_attention_fma<64>, dim3(grid), dim3(kTreeThreads), TreeShape<64>::SMEM_BYTES, stream,
                                        a.programmatic, ka);
     }
     // some unit is cut unless every team boundary falls on a unit boundary
