@@ -34,7 +34,8 @@ struct TreeKernelArgs {
 // --------------------------------------------------------------------------------------
 // FMA kernel of fp32 storage.  32 query rows x 64 keys per step; thread (ty, tx) owns rows 2 ty, 2 ty + 1 and, of the
 // scores, keys tx + 16 i, of the output, columns 4 tx + 64 c: every operand comes from shared memory as float4 and
-// the 16 lanes of a row reduce its softmax with shuffles.
+// the 16 lanes of a row reduce its softmax with shuffles.  Bound: the FMA pipe and the shared-memory reads that feed it
+// (32q/8kv, D = 128, B = 4, n = 4096, 16 drafts: 189 us, 22.8 TFLOP/s; its 134 MB would take 21).
 // --------------------------------------------------------------------------------------
 template <int D>
 struct TreeShape {

@@ -7,17 +7,17 @@
 //                      lanes hold no query row stay out of it
 //   warp 4 (one lane)  TMA producer: the query tile per piece; K and V tiles through one ring (K0 V0 K1 V1 ...)
 //   warp 5             MMA issuer: S = Q K^T into one of two score buffers (S of tile t+1 runs during the softmax of
-//                      tile t), O += P V with P = hi + lo (two bf16 terms) read from tensor memory.  The whole warp walks the tiles and an
-//                      elected lane issues: operands are then in uniform registers (issued from a one-lane branch the
-//                      sixteen MMAs of a 128-key tile took 1700 cycles instead of 1200)
-// Bound: up to 128 query rows per kv-head HBM (32 heads, B = 8, n = 4096, 16 drafts: 537 MB in 85 us, 6.3 TB/s).  Above
-// that no single unit is full: at 256 rows (32q/8kv, B = 4, n = 32768, 64 drafts: 133 us, 1.03 PFLOP/s) the tensor pipe and
-// the special-function unit are busy 59 % of the time each, a softmax warp's 64 keys take 1700 cycles of which the
-// exponentials alone are 820 beside the other block's, and an S product of 64 keys reads 6 KiB of shared memory per
-// 32 tensor cycles, more than the 128 bytes a cycle there are (Q is read again for every tile).
-// Measured against this layout at 256 rows, where it takes 147 us with the combine step: one block per SM whose two softmax
-// groups take a query tile each and share K/V tiles of 128 keys, 156 us (a score buffer is free only after the product
-// that reads its weights, and S then waits for softmax, PV and S in a row); one block per SM with 128-key tiles, two
+//                      tile t), O += P V with P = hi + lo (two bf16 terms) read from tensor memory.  The whole warp walks
+//                      the tiles and an elected lane issues: operands are then in uniform registers (issued from a one-lane
+//                      branch the sixteen MMAs of a 128-key tile took 1700 cycles instead of 1200)
+// Bound: up to 128 query rows per kv-head HBM (32 heads, B = 8, n = 4096, 16 drafts: 537 MB in 87 us, 6.2 TB/s, tensor pipe
+// busy 64 % of the time).  Above that the tensor pipe more than anything: at 256 rows (32q/8kv, B = 4, n = 32768, 64
+// drafts: 160 us, 0.86 PFLOP/s and half again as much issued for the second term of P) it is busy 74 % of the time at the
+// 1.54 GHz the power cap leaves, issue slots 48, the special-function unit 50; an S product of 64 keys reads 6 KiB of shared
+// memory per 32 tensor cycles, more than the 128 bytes a cycle there are (Q is read again for every tile).
+// Measured against this layout at 256 rows while P had one term (147 us with the combine step, now 174): one block per SM whose
+// two softmax groups take a query tile each and share K/V tiles of 128 keys, 156 us (a score buffer is free only after the
+// product that reads its weights, and S then waits for softmax, PV and S in a row); one block per SM with 128-key tiles, two
 // score buffers and two threads per row, 177; a quarter of the exp2 by a polynomial on the FMA pipe, 151; two stages per
 // operand instead of the ring of five, 147; K/V fetched before the wait for the previous kernel, 150.
 // P goes into the second contraction as two bf16 terms, like the prefill kernel's: a weight is then off by 2^-16 of itself at
