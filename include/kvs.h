@@ -292,7 +292,8 @@ kvs_status kvs_append_rotary(kvs_ctx* ctx, int32_t layer, const kvs_rotary* rot,
  *   out:  device, same shape and type as q, 16-byte aligned, not overlapping it.  The storage type, not float32 as
  *         in kvs_decode_attention: 64 times the rows go on to the next matrix product in that type
  * A draft that sees nothing at all (an empty context and an empty mask) gets zeros.  What a masked draft's rows hold
- * (NaN of a padding token included) does not reach the result.  Works on ragged slots too: a unit's drafts are its
+ * (NaN of a padding token included) does not reach the result; an Inf or NaN in a value row that a draft does see makes
+ * that element of its result non-finite.  Works on ragged slots too: a unit's drafts are its
  * own newest n_t rows.
  * Errors: as kvs_decode_attention; INVALID_ARG if a unit holds fewer than n_t rows; STATE under KVS_OPT_REPLAY.  */
 kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* out, const uint64_t* mask, int32_t batch,

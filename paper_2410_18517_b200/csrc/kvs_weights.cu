@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kFinishThreads) weights_finish_kernel(const Fi
 // contiguous, and one vote orders 32 rows.  What pads a unit's end has the lowest key and the highest row numbers, so it
 // is never reached.  Bound: the chain of a block (three passes of histogram, barriers and search, then the positions), and
 // with many units how many blocks an SM holds: a block of 256 threads with 64 registers each, four of them, 592 in all.
-// Units of 8192 rows, cold: 304 in 20.5 us, 592 in 24.6, 600 to 720 in 30.7 (a second round on an almost empty GPU); issuing
+// Units of 8192 rows, cold: 304 in 20.5 us, 592 in 24.6, 600 to 720 in 30.7 (a second wave on an almost empty GPU); issuing
 // the 40 to 80 instructions for 32 rows would take 6 to 12.
 // (Keys in shared memory and a list of the first bin's keys for the later passes: 100 for 32 rows, 53 us for 640 units
 // of 8192 rows; neighbouring rows in one thread: the loads of a warp then touch 32 lines each, 47 us.)
