@@ -238,12 +238,13 @@ kvs_status kvs_prefill_attention(kvs_ctx* ctx, int32_t layer, const void* q, flo
  *           it sees the change, because they read the same slot
  *   keep:   device, int32 [batch][n_kv_heads][keep_stride]; the first n_keep[b*Hkv+h] entries of a
  *           unit are the row indices to keep, strictly ascending, each below the unit's length
- *   n_keep: host, int32 [batch * n_kv_heads], each in [1, current length of the unit]
+ *   n_keep: host, int32 [batch * n_kv_heads], each in [1, current length of the unit]; read during the call (a recorded
+ *           call keeps its counts)
  * The kept rows move to the front of the unit in order, bit for bit; afterwards the units of the
  * slot may differ in length ("ragged").  Appends then extend every unit at its own end,
  * kvs_decode_attention uses each unit's own length, kvs_seq_len reports the longest unit and
- * kvs_unit_len one unit; kvs_prefill_attention refuses a ragged slot (STATE).  One copy and two
- * kernels on `stream`.  A list that is not ascending or out of range cannot be seen by the host:
+ * kvs_unit_len one unit; kvs_prefill_attention refuses a ragged slot (STATE).  Two kernels on `stream`
+ * and one for every 900 counts.  A list that is not ascending or out of range cannot be seen by the host:
  * the kernel skips the offending entries and sets the device status word to KVS_ERR_INVALID_ARG.
  * Errors: STATE before bind or on an empty slot; INVALID_ARG for bad sizes or batch != cached batch. */
 kvs_status kvs_evict(kvs_ctx* ctx, int32_t layer, const int32_t* keep, const int32_t* n_keep,

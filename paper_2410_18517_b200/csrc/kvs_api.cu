@@ -760,8 +760,7 @@ kvs_status kvs_evict(kvs_ctx* ctx, int32_t layer, const int32_t* keep, const int
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int* counts = reinterpret_cast<int*>(ctx->ws + ctx->off_counts);
     int* lens = unit_len_dev(ctx, slot);
-    if (cudaMemcpyAsync(counts, n_keep, sizeof(int32_t) * units, cudaMemcpyHostToDevice, st) != cudaSuccess)
-        return KVS_ERR_CUDA;
+    if (kvs::launch_put_counts(counts, n_keep, units, st) != cudaSuccess) return KVS_ERR_CUDA;
     char* kp = ctx->pool + (size_t)(2 * slot) * ctx->plane_bytes;
     const bool pdl = ctx->opt_pdl != 0;
     if (kvs::launch_evict(kp, kp + ctx->plane_bytes, keep, counts, ctx->ragged[slot] ? lens : nullptr,

@@ -215,6 +215,8 @@ struct SelectArgs {
     int* status;
 };
 cudaError_t init_weights_kernels();
+// Host counts to device memory as launch arguments: the caller's array is not read after the call, by a recorded launch either.
+cudaError_t launch_put_counts(int* out, const int* n, int units, cudaStream_t stream);
 cudaError_t launch_select(const SelectArgs& a, const SelectCounts& counts, cudaStream_t stream);
 
 // Accepted drafts of one slot move to the front of its draft rows (see kvs_tree.cu).

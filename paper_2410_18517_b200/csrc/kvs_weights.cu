@@ -386,6 +386,10 @@ __global__ void __launch_bounds__(kSelectThreads) select_rows_kernel(const Selec
     }
 }
 
+__global__ void put_counts_kernel(int* out, const __grid_constant__ SelectCounts counts, int units) {
+    for (int u = threadIdx.x; u < units; u += blockDim.x) out[u] = counts.n[u];
+}
+
 template <int IPT, bool ONE, bool SPREAD>
 cudaError_t select_attr() {
     return cudaFuncSetAttribute(select_rows_kernel<IPT, ONE, SPREAD>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
@@ -417,6 +421,17 @@ cudaError_t init_weights_kernels() {
     if (e == cudaSuccess) e = select_attr<32, true, true>();
     if (e == cudaSuccess) e = select_attr<32, true, false>();
     return e == cudaSuccess ? select_attr<16, false, false>() : e;
+}
+
+cudaError_t launch_put_counts(int* out, const int* n, int units, cudaStream_t stream) {
+    for (int u0 = 0; u0 < units; u0 += SelectCounts::kMax) {
+        const int count = std::min(units - u0, (int)SelectCounts::kMax);
+        SelectCounts counts;
+        for (int i = 0; i < count; ++i) counts.n[i] = n[u0 + i];
+        const cudaError_t e = launch_kernel(put_counts_kernel, dim3(1), dim3(256), 0, stream, false, out + u0, counts, count);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 cudaError_t launch_weights_finish(const DecodeArgs& a, const DecodePlan& plan, const float* total_in, float* total_out,

@@ -196,3 +196,37 @@ def test_weights_in_several_passes_under_graph_replay():
     assert (results[0][0] - results[1][0]).abs().max() < 1e-5
     for a, b in zip(results[0][1], results[1][1]):
         assert (a - b).abs().max() < 1e-5
+
+
+# --------------------------------------------------------------------------------------- evictions recorded
+
+@pytest.mark.parametrize("B,Hkv", [(2, 2), (60, 16)])
+def test_a_recorded_eviction_keeps_its_counts(B, Hkv):
+    """The counts of a recorded eviction are those of the call, whatever the caller's array holds when the graph runs."""
+    Hq, D, n = Hkv, 64, 150
+    counts = [[1 + (37 * b + 11 * h) % n for h in range(Hkv)] for b in range(B)]
+    caches = [t.filled(Hq, Hkv, D, B, n, "bf16", extra=2)[0] for _ in range(2)]
+    total = torch.rand(B, Hkv, n, generator=torch.Generator().manual_seed(1)).cuda()
+    q = t.normal(5, "bf16", B, Hq, D)
+    want = caches[0].evict_by_weight(0, total, counts, 1)
+    outs = [torch.empty(B, Hq, D, device="cuda") for _ in range(2)]
+    caches[0].decode_attention(0, q, outs[0])
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = caches[1].evict_by_weight(0, total, counts, 1)
+        caches[1].decode_attention(0, q, outs[1])
+    junk = [(1 << 30 | i) for i in range(4096)]
+    arrays = [np.full(B * Hkv, 1 << 30, dtype=np.int32) for _ in range(64)]      # what was freed is used again
+    g.replay()
+    torch.cuda.synchronize()
+    assert len(junk) == 4096 and len(arrays) == 64
+    assert torch.equal(got, want) and torch.equal(outs[0], outs[1])
+    for b in range(B):
+        for h in range(Hkv):
+            assert caches[1].unit_len(0, b, h) == counts[b][h]
+    for i in range(2):
+        assert torch.equal(caches[0].plane(0, i)[:, :, :n].view(torch.int16), caches[1].plane(0, i)[:, :, :n].view(torch.int16))
+    for c in caches:
+        assert c.device_status() == 0
+        c.check_canaries()
