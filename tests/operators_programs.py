@@ -319,11 +319,19 @@ class Program:
             self.keep_rows(l, lists)
 
     # ------------------------------------------------------------------ run
-    def run(self, stream=None):
+    def run(self, stream=None, graph=False):
+        """`graph`: the calls are recorded, and run when the graph does."""
         torch.cuda.synchronize()
-        with torch.cuda.stream(stream or torch.cuda.current_stream()):
-            for call in self.calls:
-                call()
+        if graph:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                for call in self.calls:
+                    call()
+            g.replay()
+        else:
+            with torch.cuda.stream(stream or torch.cuda.current_stream()):
+                for call in self.calls:
+                    call()
         torch.cuda.synchronize()
         assert self.cache.device_status() == 0, (self.cache.device_status(), self.log)
         try:

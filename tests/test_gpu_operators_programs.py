@@ -45,3 +45,9 @@ def test_programs_over_long_caches(seed):
     """Kernels long enough that a call queued behind one really starts beside it."""
     *args, options = shape(seed, 12000)
     Program(seed, *args, 25, options, filled=9000 + 311 * (seed - 100)).run()
+
+
+@pytest.mark.parametrize("seed", range(200, 216))
+def test_recorded_programs(seed):
+    *args, options = shape(seed, (100, 700, 2500)[seed % 3])
+    Program(seed, *args, 30, options).run(graph=True)
