@@ -71,6 +71,12 @@ typedef enum {
 
 typedef enum { KVS_BF16 = 0, KVS_F32 = 1 } kvs_dtype;
 
+/* How the rows of a cache are held (kvs_set_cache_format). */
+typedef enum {
+    KVS_CACHE_PLAIN = 0,      /* the storage type, bit for bit                                  */
+    KVS_CACHE_4BIT = 1        /* four bits per element, a scale and an offset per quarter row    */
+} kvs_cache_format;
+
 typedef struct {
     int32_t n_layers;     /* L >= 1                                                 */
     int32_t n_q_heads;    /* Hq; a multiple of n_kv_heads; Hq/Hkv in 1..8 (3,5,6,7: bf16 only) */
@@ -143,6 +149,27 @@ kvs_status kvs_destroy(kvs_ctx* ctx);
  * Changes the required pool size: call before kvs_required_bytes/kvs_bind_memory;
  * a context that already has memory bound must be re-bound afterwards.          */
 kvs_status kvs_set_share_map(kvs_ctx* ctx, const int32_t* share_map);
+
+/* How this context's cache holds its rows: KVS_CACHE_PLAIN (default) or KVS_CACHE_4BIT.  STATE unless every slot is
+ * empty.  A change alters the required sizes: a context that already has memory bound must be re-bound afterwards.
+ *
+ * A 4-bit cache (nothing in the paper: it multiplies with the memory that sharing layers saves) cuts a row of D elements into
+ * four groups of D/4.  With lo, hi the group's smallest and largest element, in fp32:
+ *     s = (hi - lo) / 15 rounded up to bf16,   b = lo - 16 s rounded to bf16,
+ *     code c = clamp(rint((x - b) / s) - 16, 0, 15)  (ties to even; s = 0: c = 0),   value = s * (16 + c) + b
+ * and the value, rounded once to the storage type, is what the cache holds of x: it differs from x by at most s/2, the
+ * rounding of b (2^-8 |b|) and its own.  A group with an infinity or a NaN in it, or whose s or b overflows, has only NaN values
+ * (s = b = NaN, bits 0x7fc0, codes 0).
+ * A row takes 16 + D/2 bytes (80 or 48): the pairs (s, b) of the groups as bf16, then the codes, element 8 w + i in bits
+ * 4 i .. 4 i + 3 of word w; planes are [max_batch][n_kv_heads][row_stride] such rows.
+ *
+ * The calls keep their arguments and types: the append calls take the storage type and pack it (kvs_decode_step and
+ * kvs_step_host with a launch of its own for that, kvs_append_rotary through the workspace), attention (kvs_decode_attention,
+ * its _static form, kvs_decode_step, kvs_step_host, kvs_prefill_attention) is that over the values, kvs_evict,
+ * kvs_accept_draft, kvs_reorder, kvs_truncate and replays work as they do otherwise, kvs_read_rows gives the values.
+ * kvs_tree_attention, kvs_decode_attention_weights and kvs_layer_distances refuse such a context (STATE).
+ * The workspace gains room for rows in the storage type: 64 MiB, or one sequence of max_seq rows if that is more. */
+kvs_status kvs_set_cache_format(kvs_ctx* ctx, int32_t format);
 
 /* Bytes the caller must provide: pool = n_slots * 2 planes, workspace = split-K
  * partial results, a status word and staging for kvs_step_host.  Both host out. */
@@ -343,6 +370,51 @@ kvs_status kvs_decode_attention_weights(kvs_ctx* ctx, int32_t layer, const void*
 kvs_status kvs_select_rows(kvs_ctx* ctx, int32_t layer, const float* total, int32_t total_stride, const int32_t* n_keep,
                            int32_t n_recent, int32_t* keep, float* kept_total, int32_t keep_stride, int32_t batch, void* stream);
 
+/* Rows first .. first + n_rows - 1 of the slot `layer` reads, as kvs_append takes them: the storage type's bits, or the
+ * values of a 4-bit cache.
+ *   k_out, v_out: device, storage type [batch][n_rows][n_kv_heads][head_dim], 16-byte aligned, not overlapping
+ * A row that a unit of a ragged slot does not hold comes as zeros.  One launch.  (Under KVS_OPT_REPLAY the rows the host
+ * knows of; what replays have added since can be read after kvs_replay_commit.)
+ * Errors: STATE before bind or on an empty slot; INVALID_ARG for a bad layer, NULL or misaligned pointers, batch < 1 or above
+ * the cached one, first < 0, n_rows < 1, or rows the slot does not hold.                                          */
+kvs_status kvs_read_rows(kvs_ctx* ctx, int32_t layer, int32_t first, int32_t n_rows, void* k_out, void* v_out, int32_t batch,
+                         void* stream);
+
+/* ---- beam search ----------------------------------------------------------------------------------
+ * A request's n_beams beams are sequences r * n_beams .. of the batch.  A step: kvs_decode_step over the layers, the model's
+ * logits, kvs_beam_select, and kvs_reorder with the parents of the continuations that go on. */
+
+/* The best continuations of every request's beams:
+ *   score(b, v) = scores[b] + logits[b][v] - log(sum_w exp(logits[b][w]))
+ * and of a request's n_beams * vocab pairs the n_out with the highest score, best first; equal scores (in fp64, in which they
+ * are compared): the lowest (beam, token).  A pair of score minus infinity is no candidate, nor is any pair of a row whose own
+ * score or whose logits' sum is not finite (a NaN or +infinity among the logits, a row that is masked throughout).
+ *   logits:        device, logits_dtype (KVS_BF16 or KVS_F32) [n_requests * n_beams] rows of vocab, logits_stride elements
+ *                  apart; rows that start on 16 bytes are read fastest
+ *   scores:        device, float32 [n_requests * n_beams]: the beams' log-probabilities so far (minus infinity: not a beam,
+ *                  as all but the first of every request in the first step)
+ *   out_scores, out_tokens, out_parents: device, float32 / int32 [n_requests][n_out]; parents are sequence numbers of the batch,
+ *                  as kvs_reorder takes them.  Where a request has fewer candidates: minus infinity, -1, its first sequence.
+ *                  None may overlap an input.
+ * n_beams and n_out are at most 64; n_requests * n_beams at most max_batch; n_beams * vocab below 2^31.  The cache is neither
+ * read nor changed.  Two launches.  The same call gives the same bits, and rows with equal bits equal scores.
+ * Errors: STATE before bind; INVALID_ARG for the above. */
+kvs_status kvs_beam_select(kvs_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t logits_stride, int32_t vocab,
+                           const float* scores, int32_t n_requests, int32_t n_beams, int32_t n_out, float* out_scores,
+                           int32_t* out_tokens, int32_t* out_parents, void* stream);
+
+/* Every slot's sequences take the rows of others: sequence b becomes what sequence parent[b] was before the call, for
+ * b = 0 .. batch-1, rows first_row and on (rows before that are known to be the same, the prompt of a request's beams for
+ * instance, and stay).  The batch becomes `batch`: more sequences than before (a prompt forked to its beams; first_row must be
+ * 0) or fewer (finished requests dropped: the others close up).
+ *   parent: device, int32 [batch], each 0 .. cached batch - 1.  The host cannot see it: an entry out of range leaves its
+ *           sequence's rows as they are and sets the device status word to KVS_ERR_INVALID_ARG.
+ * Only rows that change are moved, a source is read once.  One launch for every 512 slots.  It may be recorded: under
+ * KVS_OPT_REPLAY the rows that replays added move too (the batch must stay the same).
+ * Errors: STATE before bind, with nothing cached, if a slot is ragged, or for another batch under KVS_OPT_REPLAY; INVALID_ARG for
+ * batch < 1, above max_batch or above 4096 (also the cached one), first_row < 0, NULL or misaligned parent.       */
+kvs_status kvs_reorder(kvs_ctx* ctx, const int32_t* parent, int32_t first_row, int32_t batch, void* stream);
+
 /* Rows cached for sequence b, kv-head h of the slot `layer` reads. */
 kvs_status kvs_unit_len(const kvs_ctx* ctx, int32_t layer, int32_t b, int32_t h, int32_t* len);
 
@@ -467,6 +539,8 @@ kvs_status kvs_num_slots(const kvs_ctx* ctx, int32_t* n_slots);
 kvs_status kvs_slot_of_layer(const kvs_ctx* ctx, int32_t layer, int32_t* slot);
 /* Tokens visible to `layer` now (the length of the slot it reads; of its longest unit if ragged). */
 kvs_status kvs_seq_len(const kvs_ctx* ctx, int32_t layer, int32_t* len);
+/* Sequences the cached rows belong to (0: nothing is cached). */
+kvs_status kvs_cached_batch(const kvs_ctx* ctx, int32_t* batch);
 /* Rows between consecutive (sequence, head) units of a plane. */
 kvs_status kvs_row_stride(const kvs_ctx* ctx, int32_t* rows);
 /* Byte offset into the pool of plane (slot, kv), kv = 0 for K, 1 for V. */
@@ -487,7 +561,8 @@ kvs_status kvs_clear_device_status(kvs_ctx* ctx, void* stream);
  * warps hand the give-up to one another, the producer waits for the copies it did issue, other blocks
  * that depend on this one give up in turn, and the launch ends normally with the device status word at
  * KVS_ERR_TIMEOUT and `out` undefined.  Nothing traps or faults, every wait on the way is bounded, and
- * kvs_clear_device_status brings the context back.  Same errors as kvs_decode_attention.               */
+ * kvs_clear_device_status brings the context back.  Same errors as kvs_decode_attention; STATE for a 4-bit cache of fp32
+ * storage, whose kernel has no such wait.                                                              */
 kvs_status kvs_selftest_stalled_copy(kvs_ctx* ctx, int32_t layer, const void* q, float* out, int32_t batch, void* stream);
 /* Failure-detection self-test (the paper has no counterpart; every wait inside the pipelined kernels
  * is bounded, and this call shows the give-up path working on the device at hand without disturbing
@@ -520,7 +595,7 @@ kvs_status kvs_trace_end(kvs_ctx* ctx, int32_t* launches_recorded);
 kvs_status kvs_selftest_bounds(kvs_ctx* ctx, void* stream);
 kvs_status kvs_set_option(kvs_ctx* ctx, int32_t option, int32_t value);
 /* How the last kvs_decode_attention call was decomposed: thread blocks launched,
- * rows per tile, and 1 or 2 for the scalar / tensor-core kernel.                */
+ * rows per tile, and 1 or 2 for the scalar / tensor-core kernel (3, 4: those over a 4-bit cache, of bf16 / fp32 storage). */
 kvs_status kvs_last_launch(const kvs_ctx* ctx, int32_t* ctas, int32_t* tile_rows, int32_t* kernel);
 const char* kvs_status_string(kvs_status s);
 

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 from . import binding
 from .binding import (  # noqa: F401
-    KVS_BF16, KVS_F32, KVS_OK, KVS_OPT_EARLY_START, KVS_OPT_FINISH_IN_KERNEL, KVS_OPT_HOST_CHUNKS, KVS_OPT_KERNEL, KVS_OPT_MAX_CTAS, KVS_OPT_REPLAY, KVS_OPT_WAIT_LIMIT_US, KvsError,
+    KVS_BF16, KVS_CACHE_4BIT, KVS_CACHE_PLAIN, KVS_F32, KVS_OK, KVS_OPT_EARLY_START, KVS_OPT_FINISH_IN_KERNEL, KVS_OPT_HOST_CHUNKS, KVS_OPT_KERNEL, KVS_OPT_MAX_CTAS, KVS_OPT_REPLAY, KVS_OPT_WAIT_LIMIT_US, KvsError,
 )
 
 __all__ = ["binding", "SharedKVCache", "Rotary", "KvsError"]
@@ -44,11 +44,12 @@ class SharedKVCache:
     """One context + the torch tensors backing it.
 
     ``share_map[l] == l``: layer l computes its own K/V; ``share_map[l] == s < l``:
-    layer l reads layer s's cache and appends nothing.
+    layer l reads layer s's cache and appends nothing.  ``cache_format``: ``"plain"`` (rows in the storage type) or
+    ``"4bit"`` (``kvs_set_cache_format`` says what a row holds and which calls take it).
     """
 
     def __init__(self, n_layers, n_q_heads, n_kv_heads, head_dim, max_batch, max_seq, dtype="bf16",
-                 share_map=None, softmax_scale=0.0, device=0):
+                 share_map=None, softmax_scale=0.0, device=0, cache_format="plain"):
         import torch
 
         self._torch = torch
@@ -65,6 +66,8 @@ class SharedKVCache:
         try:
             if share_map is not None:
                 binding.kvs_set_share_map(self.ctx, share_map)
+            self.cache_format = {"plain": KVS_CACHE_PLAIN, "4bit": KVS_CACHE_4BIT}[cache_format]
+            binding.kvs_set_cache_format(self.ctx, self.cache_format)
             self.pool_bytes, self.workspace_bytes = binding.kvs_required_bytes(self.ctx)
             self.pool = self._allocate(self.pool_bytes)
             self.workspace = self._allocate(self.workspace_bytes)
@@ -255,6 +258,43 @@ class SharedKVCache:
         self.evict(layer, keep, n_keep)
         return kept
 
+    def read_rows(self, layer, first=0, n_rows=None, batch=None):
+        """Rows of the slot the layer reads, as ``append`` takes them: k, v ``[batch][n_rows][n_kv_heads][head_dim]`` (of a
+        4-bit cache: the values its rows stand for).  None: all rows, all cached sequences."""
+        if n_rows is None:
+            n_rows = self.seq_len(layer) - first
+        if batch is None:
+            batch = binding.kvs_cached_batch(self.ctx)
+        shape = (batch, n_rows, self.shape[2], self.shape[3])
+        k, v = (self._torch.empty(shape, dtype=self.dtype, device=self.device) for _ in range(2))
+        binding.kvs_read_rows(self.ctx, layer, first, n_rows, k, v, batch, self._stream())
+        return k, v
+
+    def beam_select(self, logits, scores, n_beams, n_out, out=None):
+        """The n_out best continuations of every request's n_beams beams.  logits: bf16 or float32 ``[rows][vocab]`` (rows may be
+        strided), rows = requests * n_beams; scores: float32 of as many elements, the beams' log-probabilities so far.  Returns
+        (or fills ``out``) scores float32, tokens int32 and parents int32 (sequence numbers, as ``reorder`` takes them), each
+        ``[requests][n_out]``, best first."""
+        torch = self._torch
+        assert logits.ndim == 2 and logits.dtype in (torch.bfloat16, torch.float32)
+        rows, vocab = logits.shape
+        assert n_beams >= 1 and rows % n_beams == 0 and (vocab == 1 or logits.stride(1) == 1), "a row's logits must be contiguous"
+        assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows and self._here(logits, scores)
+        shape = (rows // n_beams, n_out)
+        if out is None:
+            out = tuple(torch.empty(shape, dtype=d, device=self.device) for d in (torch.float32, torch.int32, torch.int32))
+        for x, d in zip(out, (torch.float32, torch.int32, torch.int32)):
+            assert x.dtype == d and x.is_contiguous() and x.shape == shape and self._here(x)
+        binding.kvs_beam_select(self.ctx, logits, KVS_BF16 if logits.dtype == torch.bfloat16 else KVS_F32,
+                                logits.stride(0) if rows > 1 else vocab, vocab, scores, shape[0], n_beams, n_out, *out, self._stream())
+        return out
+
+    def reorder(self, parent, first_row=0):
+        """Every sequence b of every slot becomes what sequence ``parent[b]`` was, rows first_row and on.  parent: device int32
+        ``[batch]``; the batch may grow (fork) or shrink (compaction)."""
+        assert parent.dtype == self._torch.int32 and parent.is_contiguous() and parent.ndim == 1 and self._here(parent)
+        binding.kvs_reorder(self.ctx, parent, first_row, parent.shape[0], self._stream())
+
     def unit_len(self, layer, b, h):
         return binding.kvs_unit_len(self.ctx, layer, b, h)
 
@@ -293,14 +333,18 @@ class SharedKVCache:
         return binding.kvs_step_host(self.ctx, q_host, k_host, v_host, out_host, q_host.shape[1], self._stream())
 
     def plane(self, slot, kv):
-        """View of plane (slot, kv) as ``[max_batch][n_kv_heads][row_stride][head_dim]``."""
+        """View of plane (slot, kv) as ``[max_batch][n_kv_heads][row_stride][head_dim]`` (of a 4-bit cache: its bytes,
+        ``[max_batch][n_kv_heads][row_stride][16 + head_dim / 2]``)."""
         if self._planes is None or self._planes[0] is not self.pool:
             self._planes = self.pool, {}
         seen = self._planes[1].get((slot, kv))
         if seen is None:
             off, nbytes = binding.kvs_plane_offset(self.ctx, slot, kv), binding.kvs_plane_offset(self.ctx, 0, 1)
             rs = binding.kvs_row_stride(self.ctx)
-            seen = self.pool[off:off + nbytes].view(self.dtype).view(-1, self.shape[2], rs, self.shape[3])
+            plane = self.pool[off:off + nbytes]
+            if self.cache_format == KVS_CACHE_PLAIN:
+                plane = plane.view(self.dtype)
+            seen = plane.view(self.max_batch, self.shape[2], rs, -1)
             self._planes[1][slot, kv] = seen
         return seen.detach()        # a tensor of its own for every caller
 

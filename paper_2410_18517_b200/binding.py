@@ -28,6 +28,9 @@ KVS_ERR_BOUNDS = 9
 KVS_BF16 = 0
 KVS_F32 = 1
 
+KVS_CACHE_PLAIN = 0
+KVS_CACHE_4BIT = 1
+
 KVS_OPT_MAX_CTAS = 0
 KVS_OPT_KERNEL = 1
 KVS_OPT_EARLY_START = 2
@@ -48,6 +51,8 @@ EXPORTS = (
     "kvs_clear_device_status", "kvs_selftest_wait_timeout", "kvs_truncate",
     "kvs_selftest_bounds", "kvs_selftest_stalled_copy", "kvs_trace_begin", "kvs_trace_end",
     "kvs_append_rotary", "kvs_tree_attention", "kvs_accept_draft", "kvs_decode_attention_weights", "kvs_select_rows",
+    "kvs_set_cache_format", "kvs_read_rows", "kvs_beam_select", "kvs_reorder",
+    "kvs_cached_batch",
 )
 
 
@@ -112,6 +117,7 @@ def load() -> ctypes.CDLL:
         "kvs_num_slots": [vp, P(i32)],
         "kvs_slot_of_layer": [vp, i32, P(i32)],
         "kvs_seq_len": [vp, i32, P(i32)],
+        "kvs_cached_batch": [vp, P(i32)],
         "kvs_row_stride": [vp, P(i32)],
         "kvs_plane_offset": [vp, i32, i32, P(sz)],
         "kvs_stats": [vp, P(kvs_stats_t)],
@@ -130,6 +136,10 @@ def load() -> ctypes.CDLL:
         "kvs_accept_draft": [vp, vp, i32, P(i32), i32, i32, vp],
         "kvs_decode_attention_weights": [vp, i32, vp, vp, vp, vp, i32, i32, vp],
         "kvs_select_rows": [vp, i32, vp, i32, vp, i32, vp, vp, i32, i32, vp],
+        "kvs_set_cache_format": [vp, i32],
+        "kvs_read_rows": [vp, i32, i32, i32, vp, vp, i32, vp],
+        "kvs_beam_select": [vp, vp, i32, ctypes.c_int64, i32, vp, i32, i32, i32, vp, vp, vp, vp],
+        "kvs_reorder": [vp, vp, i32, i32, vp],
         "kvs_read_roof": [vp, sz, vp, i32, vp],
     }
     for name, argtypes in sig.items():
@@ -183,6 +193,10 @@ def kvs_destroy(ctx: int) -> None:
 def kvs_set_share_map(ctx: int, share_map) -> None:
     arr = (ctypes.c_int32 * len(share_map))(*[int(x) for x in share_map])
     _check(load().kvs_set_share_map(ctx, arr), "kvs_set_share_map")
+
+
+def kvs_set_cache_format(ctx: int, fmt: int) -> None:
+    _check(load().kvs_set_cache_format(ctx, fmt), "kvs_set_cache_format")
 
 
 def kvs_required_bytes(ctx: int) -> tuple[int, int]:
@@ -249,6 +263,21 @@ def kvs_decode_attention_weights(ctx: int, layer: int, q, out, total_in, total_o
                                                batch, stream), "kvs_decode_attention_weights")
 
 
+def kvs_read_rows(ctx: int, layer: int, first: int, n_rows: int, k_out, v_out, batch: int, stream: int = 0) -> None:
+    _check(load().kvs_read_rows(ctx, layer, first, n_rows, _ptr(k_out), _ptr(v_out), batch, stream), "kvs_read_rows")
+
+
+def kvs_beam_select(ctx: int, logits, logits_dtype: int, logits_stride: int, vocab: int, scores, n_requests: int, n_beams: int,
+                    n_out: int, out_scores, out_tokens, out_parents, stream: int = 0) -> None:
+    _check(load().kvs_beam_select(ctx, _ptr(logits), logits_dtype, logits_stride, vocab, _ptr(scores), n_requests, n_beams, n_out,
+                                  _ptr(out_scores), _ptr(out_tokens), _ptr(out_parents), stream), "kvs_beam_select")
+
+
+def kvs_reorder(ctx: int, parent, first_row: int, batch: int, stream: int = 0) -> None:
+    """parent: device int32 ``[batch]``."""
+    _check(load().kvs_reorder(ctx, _ptr(parent), first_row, batch, stream), "kvs_reorder")
+
+
 def kvs_select_rows(ctx: int, layer: int, total, total_stride: int, n_keep, n_recent: int, keep, kept_total, keep_stride: int,
                     batch: int, stream: int = 0) -> None:
     """n_keep: host sequence of batch*Hkv counts, or a contiguous int32 CPU tensor of them."""
@@ -308,6 +337,12 @@ def kvs_seq_len(ctx: int, layer: int) -> int:
     v = ctypes.c_int32()
     _check(load().kvs_seq_len(ctx, layer, ctypes.byref(v)), "kvs_seq_len")
     return v.value
+
+
+def kvs_cached_batch(ctx: int) -> int:
+    n = ctypes.c_int32()
+    _check(load().kvs_cached_batch(ctx, ctypes.byref(n)), "kvs_cached_batch")
+    return n.value
 
 
 def kvs_row_stride(ctx: int) -> int:

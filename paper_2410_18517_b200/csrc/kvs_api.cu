@@ -16,6 +16,7 @@ namespace {
 constexpr size_t kAlign = 256;
 constexpr int kRowStrideQuantum = 128;
 constexpr size_t kScoreBytes = 64u << 20;     // scores of one pass of kvs_decode_attention_weights
+constexpr size_t kPlainRowBytes = 64u << 20;  // 4-bit cache: rows in the storage type of one pass of the calls that need them so
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 }  // namespace
@@ -62,7 +63,8 @@ struct kvs_ctx {
     kvs_config cfg;
     int G = 1;
     int elem = 2;
-    int row_bytes = 0;
+    int format = KVS_CACHE_PLAIN;
+    int row_bytes = 0;         // of a cached row
     int row_stride = 0;        // rows between units of a plane
     size_t plane_bytes = 0;
     float scale = 0.f;
@@ -87,11 +89,12 @@ struct kvs_ctx {
     size_t off_status = 0, off_part_o = 0, off_part_ml = 0, off_stage_q = 0, off_stage_k = 0, off_stage_v = 0,
            off_stage_out = 0, off_unit_len = 0, off_counts = 0, off_search = 0, off_replay = 0, off_flags = 0, off_scores = 0,
            off_tree_o = 0, off_tree_ml = 0, ws_bytes = 0, search_bytes = 0,
-           score_bytes = 0;
+           score_bytes = 0, off_plain = 0, plain_bytes = 0;
 
     alignas(64) unsigned char tensor_map[128];  // TMA view of the pool (bf16 storage only), 64-row boxes
     alignas(64) unsigned char tensor_map_tail[128];   // the same view with 16-row boxes (partly filled tiles)
     bool have_tensor_map = false;
+    alignas(64) unsigned char plain_map[128];         // 4-bit cache: the scratch of storage-type rows
 
     // Launch bookkeeping for early-start (programmatic) launches.  Every kernel of this context
     // gets a sequence number.  A split-K kernel lets its successor start only after its own
@@ -180,6 +183,8 @@ int safe_rows_of(const kvs_ctx* c, int slot) {
 
 void layout_workspace(kvs_ctx* c) {
     const kvs_config& f = c->cfg;
+    c->row_bytes = c->format == KVS_CACHE_4BIT ? kvs::pack4_row_bytes(f.head_dim) : f.head_dim * c->elem;
+    c->plane_bytes = (size_t)f.max_batch * f.n_kv_heads * c->row_stride * c->row_bytes;
     const size_t units = (size_t)f.max_batch * f.n_kv_heads;
     const size_t pieces = units + kvs::kMaxCtas;
     size_t off = 0;
@@ -226,7 +231,16 @@ void layout_workspace(kvs_ctx* c) {
         const size_t tree_o = align_up(tree_rows * f.head_dim * sizeof(float), kAlign);
         c->off_tree_o = off;
         c->off_tree_ml = off + tree_o;
-        off = align_up(off + std::max(std::max(need, scores), tree_o + tree_rows * 2 * sizeof(float)), kAlign);
+        // kvs_beam_select: the segments' lists and sums
+        const size_t beam = kvs::beam_scratch_bytes(f.max_batch);
+        // 4-bit cache: K and V rows in the storage type, of at least one sequence as long as the cache
+        c->off_plain = off;
+        c->plain_bytes = 0;
+        if (c->format == KVS_CACHE_4BIT) {
+            const size_t seq = 2ull * f.n_kv_heads * c->row_stride * f.head_dim * c->elem;
+            c->plain_bytes = std::max(seq, std::min(f.max_batch * seq, kPlainRowBytes / kAlign * kAlign));
+        }
+        off = align_up(off + std::max({need, scores, tree_o + tree_rows * 2 * sizeof(float), beam, c->plain_bytes}), kAlign);
     }
     c->ws_bytes = off;
 }
@@ -243,6 +257,8 @@ cudaError_t init_device_once(int device) {
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_rotary_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_tree_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_weights_kernels();
+        if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_pack4_kernels();
+        if (g_init_err[device] == cudaSuccess) g_init_err[device] = kvs::init_beam_kernels();
         if (g_init_err[device] == cudaSuccess) g_init_err[device] = resolve_static_scratch(device);
     });
     return g_init_err[device];
@@ -292,8 +308,42 @@ kvs_status check_attention(kvs_ctx* c, int layer, const void* q, const void* out
 
 kvs_status appended(kvs_ctx* c, int slot, int batch, int n_new, cudaStream_t st);
 
+// Stores rows of sequences seq0 .. seq0+batch-1 behind the ones a 4-bit slot holds; strides of k and v in elements.
+cudaError_t store_packed(kvs_ctx* c, int slot, const void* k, const void* v, long long src_b, long long src_t, long long src_h,
+                         int seq0, int batch, int n_new, cudaStream_t st) {
+    const size_t skipped = (size_t)seq0 * c->cfg.n_kv_heads * c->row_stride * c->row_bytes;
+    kvs::PackArgs p = {};
+    p.k = k;
+    p.v = v;
+    p.src_b = src_b;
+    p.src_t = src_t;
+    p.src_h = src_h;
+    p.kplane = c->pool + (size_t)(2 * slot) * c->plane_bytes + skipped;
+    p.vplane = static_cast<char*>(p.kplane) + c->plane_bytes;
+    p.batch = batch;
+    p.n_new = n_new;
+    p.Hkv = c->cfg.n_kv_heads;
+    p.D = c->cfg.head_dim;
+    p.dtype = c->cfg.dtype;
+    p.row_stride = c->row_stride;
+    p.len0 = c->slot_len[slot];
+    p.capacity = c->cfg.max_seq;
+    p.unit_len = c->ragged[slot] ? unit_len_dev(c, slot) + (size_t)seq0 * p.Hkv : nullptr;
+    p.n_extra = replay_counter(c);
+    p.status = reinterpret_cast<int*>(c->ws + c->off_status);
+    p.plane_bytes = (long long)(c->plane_bytes - skipped);
+    p.sm_count = c->sm_count;
+    p.programmatic = take_early_start(c);
+    return kvs::launch_pack4(p, st);
+}
+
 kvs_status do_append(kvs_ctx* c, int layer, const void* k, const void* v, int batch, int n_new, cudaStream_t st) {
     const int slot = c->slot_of_layer[layer];
+    if (c->format == KVS_CACHE_4BIT) {
+        const long long D = c->cfg.head_dim, token = c->cfg.n_kv_heads * D;
+        if (store_packed(c, slot, k, v, n_new * token, token, D, 0, batch, n_new, st) != cudaSuccess) return KVS_ERR_CUDA;
+        return appended(c, slot, batch, n_new, st);
+    }
     char* kp = c->pool + (size_t)(2 * slot) * c->plane_bytes;
     char* vp = kp + c->plane_bytes;
     const bool rag = c->ragged[slot] != 0;
@@ -338,6 +388,13 @@ struct AttentionScratch {
 // Which kernel serves the context's shape and how the call is cut into work.  bf16 groups of three
 // or more q-heads per kv-head are a real (if thin) contraction and go to the tensor cores.
 bool choose_plan(const kvs_ctx* c, int units, int n, kvs::DecodePlan* plan) {
+    if (c->format == KVS_CACHE_4BIT) {
+        if (c->cfg.dtype == KVS_BF16)
+            kvs::plan_decode_pack4(units, n, c->cfg.head_dim, c->sm_count, c->opt_max_ctas, plan);
+        else
+            kvs::plan_decode_pack4_f32(units, n, c->sm_count, c->opt_max_ctas, plan);
+        return false;
+    }
     const bool use_mma = c->have_tensor_map && (c->opt_kernel == 2 || (c->opt_kernel == 0 && c->G >= 3));
     if (use_mma)
         kvs::plan_decode_mma(units, n, c->cfg.head_dim, c->sm_count, c->opt_max_ctas, plan);
@@ -402,7 +459,10 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int un
         c->seq += a.finish_in_kernel ? 1 : 2;     // split-K kernel, then (unless it finishes the units itself) combine
         c->last_splitk_seq = a.finish_in_kernel ? c->seq : c->seq - 1;
     }
-    if (use_mma) {
+    if (c->format == KVS_CACHE_4BIT) {
+        if ((plan.kernel == 3 ? kvs::launch_decode_pack4(a, plan, st) : kvs::launch_decode_pack4_f32(a, plan, st)) != cudaSuccess)
+            return KVS_ERR_CUDA;
+    } else if (use_mma) {
         const long long plane_rows = (long long)c->cfg.max_batch * c->cfg.n_kv_heads * c->row_stride;
         const long long row0 = (long long)unit0 * c->row_stride;
         if (kvs::launch_decode_mma(a, plan, c->tensor_map, c->tensor_map_tail, plane_rows * (2 * slot) + row0,
@@ -495,6 +555,40 @@ bool holds_rows(const kvs_ctx* c, int slot, int batch, int rows) {
     return true;
 }
 
+// Rows of a 4-bit slot in the storage type, into the scratch: sequences seq0 .. seq0+seqs-1, rows 0 .. n-1, laid out as planes
+// [seqs][Hkv][stride][D] of K, then of V.
+cudaError_t plain_rows(kvs_ctx* c, int slot, int seq0, int seqs, int n, int stride, cudaStream_t st) {
+    const size_t skipped = (size_t)seq0 * c->cfg.n_kv_heads * c->row_stride * c->row_bytes;
+    const long long D = c->cfg.head_dim, head = stride * D, seq = c->cfg.n_kv_heads * head;
+    kvs::ReadArgs r = {};
+    r.kplane = c->pool + (size_t)(2 * slot) * c->plane_bytes + skipped;
+    r.vplane = static_cast<const char*>(r.kplane) + c->plane_bytes;
+    r.packed = true;
+    r.row_stride = c->row_stride;
+    r.first = 0;
+    r.n = n;
+    r.k_out = c->ws + c->off_plain;
+    r.v_out = c->ws + c->off_plain + (size_t)seqs * seq * c->elem;
+    r.dst_b = seq;
+    r.dst_t = D;
+    r.dst_h = head;
+    r.batch = seqs;
+    r.Hkv = c->cfg.n_kv_heads;
+    r.D = c->cfg.head_dim;
+    r.dtype = c->cfg.dtype;
+    r.status = reinterpret_cast<int*>(c->ws + c->off_status);
+    r.plane_bytes = (long long)(c->plane_bytes - skipped);
+    r.sm_count = c->sm_count;
+    r.programmatic = take_early_start(c);
+    return kvs::launch_read_rows(r, st);
+}
+
+// Sequences whose rows, `stride` of them per head, the scratch holds at a time.
+int plain_seqs(const kvs_ctx* c, int batch, int stride) {
+    const size_t seq = 2ull * c->cfg.n_kv_heads * stride * c->cfg.head_dim * c->elem;
+    return (int)std::min<size_t>(batch, c->plain_bytes / seq);
+}
+
 // Every row of the slot may just have moved: nothing of it may be fetched early.
 void rows_moved(kvs_ctx* c, int slot) {
     c->app_seq_prev[slot] = c->seq;
@@ -527,9 +621,7 @@ kvs_status kvs_create(const kvs_config* cfg, kvs_ctx** out) {
     c->cfg = *cfg;
     c->G = G;
     c->elem = cfg->dtype == KVS_BF16 ? 2 : 4;
-    c->row_bytes = cfg->head_dim * c->elem;
     c->row_stride = (cfg->max_seq + kRowStrideQuantum - 1) / kRowStrideQuantum * kRowStrideQuantum;
-    c->plane_bytes = (size_t)cfg->max_batch * cfg->n_kv_heads * c->row_stride * c->row_bytes;
     c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / std::sqrt((float)cfg->head_dim);
     c->share_map.resize(cfg->n_layers);
     for (int l = 0; l < cfg->n_layers; ++l) c->share_map[l] = l;
@@ -576,6 +668,19 @@ kvs_status kvs_set_share_map(kvs_ctx* ctx, const int32_t* share_map) {
     return KVS_OK;
 }
 
+kvs_status kvs_set_cache_format(kvs_ctx* ctx, int32_t format) {
+    if (!ctx || (format != KVS_CACHE_PLAIN && format != KVS_CACHE_4BIT)) return KVS_ERR_INVALID_ARG;
+    for (int s = 0; s < ctx->n_slots; ++s)
+        if (ctx->slot_len[s] != 0) return KVS_ERR_STATE;
+    if (format == ctx->format) return KVS_OK;
+    ctx->format = format;
+    layout_workspace(ctx);
+    ctx->bound = false;        // pool and workspace have other sizes now
+    ctx->pool = nullptr;
+    ctx->ws = nullptr;
+    return KVS_OK;
+}
+
 kvs_status kvs_required_bytes(const kvs_ctx* ctx, size_t* pool_bytes, size_t* workspace_bytes) {
     if (!ctx || !pool_bytes || !workspace_bytes) return KVS_ERR_INVALID_ARG;
     *pool_bytes = (size_t)ctx->n_slots * 2 * ctx->plane_bytes;
@@ -597,7 +702,12 @@ kvs_status kvs_bind_memory(kvs_ctx* ctx, void* pool, size_t pool_bytes, void* wo
     if (cudaMemsetAsync(workspace, 0, ctx->ws_bytes, 0) != cudaSuccess) return KVS_ERR_CUDA;
     if (cudaStreamSynchronize(0) != cudaSuccess) return KVS_ERR_CUDA;
     ctx->have_tensor_map = false;
-    if (ctx->cfg.dtype == KVS_BF16) {
+    if (ctx->cfg.dtype == KVS_BF16 && ctx->format == KVS_CACHE_4BIT) {
+        const long long rows = (long long)(ctx->plain_bytes / ((size_t)ctx->cfg.head_dim * ctx->elem));
+        if (rows >= (1ll << 31)) return KVS_ERR_INVALID_ARG;
+        if (kvs::make_pool_tensor_map(ctx->plain_map, static_cast<char*>(workspace) + ctx->off_plain, rows, ctx->cfg.head_dim, false) != cudaSuccess)
+            return KVS_ERR_CUDA;
+    } else if (ctx->cfg.dtype == KVS_BF16) {
         const long long total_rows = (long long)(need_pool / ctx->row_bytes);
         if (total_rows >= (1ll << 31)) return KVS_ERR_INVALID_ARG;
         if (kvs::make_pool_tensor_map(ctx->tensor_map, pool, total_rows, ctx->cfg.head_dim, false) != cudaSuccess ||
@@ -689,7 +799,7 @@ kvs_status kvs_decode_step(kvs_ctx* ctx, int32_t layer, const void* q, const voi
     if (!guard.ok) return KVS_ERR_CUDA;
     const int slot = ctx->slot_of_layer[layer];
     if (((uintptr_t)q % 16) != 0 || ((uintptr_t)out % 4) != 0) return KVS_ERR_INVALID_ARG;
-    if (!ctx->ragged[slot]) return do_fused_step(ctx, layer, q, k, v, out, batch, st);
+    if (!ctx->ragged[slot] && ctx->format == KVS_CACHE_PLAIN) return do_fused_step(ctx, layer, q, k, v, out, batch, st);
     s = do_append(ctx, layer, k, v, batch, 1, st);
     if (s != KVS_OK) return s;
     return do_attention(ctx, layer, q, out, batch, st);
@@ -701,7 +811,8 @@ kvs_status kvs_prefill_attention(kvs_ctx* ctx, int32_t layer, const void* q, flo
     if (!ctx->bound) return KVS_ERR_STATE;
     if (layer < 0 || layer >= ctx->cfg.n_layers || !q || !out) return KVS_ERR_INVALID_ARG;
     if (batch < 1 || batch > ctx->cfg.max_batch || n_q < 1) return KVS_ERR_INVALID_ARG;
-    if (ctx->cfg.dtype == KVS_BF16 && !ctx->have_tensor_map) return KVS_ERR_STATE;
+    const bool packed = ctx->format == KVS_CACHE_4BIT;
+    if (ctx->cfg.dtype == KVS_BF16 && !packed && !ctx->have_tensor_map) return KVS_ERR_STATE;
     if (((uintptr_t)q % 16) != 0 || ((uintptr_t)out % 16) != 0) return KVS_ERR_INVALID_ARG;
     const int slot = ctx->slot_of_layer[layer];
     const int n = ctx->slot_len[slot];
@@ -709,6 +820,34 @@ kvs_status kvs_prefill_attention(kvs_ctx* ctx, int32_t layer, const void* q, flo
     if (batch > ctx->cur_batch || n_q > n) return KVS_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->cfg.device);
     if (!guard.ok) return KVS_ERR_CUDA;
+    if (packed) {
+        // Sequences at a time: their rows in the storage type into the scratch, then the kernel a plain cache gets.  The rows
+        // take 2 (D + 32 + 2 D e) bytes a token and head, the attention reads them n_q / 128 times.
+        const kvs_config& f = ctx->cfg;
+        cudaStream_t st = static_cast<cudaStream_t>(stream);
+        const int stride = (int)align_up(n, kRowStrideQuantum), step = plain_seqs(ctx, batch, stride);
+        for (int b0 = 0; b0 < batch; b0 += step) {
+            const int seqs = std::min(step, batch - b0);
+            if (plain_rows(ctx, slot, b0, seqs, n, stride, st) != cudaSuccess) return KVS_ERR_CUDA;
+            const size_t heads0 = (size_t)b0 * n_q * f.n_q_heads * f.head_dim;
+            const char* qb = static_cast<const char*>(q) + heads0 * ctx->elem;
+            const long long rows = (long long)seqs * f.n_kv_heads * stride;      // of one of the two planes
+            const char* kp = ctx->ws + ctx->off_plain;
+            const cudaError_t e =
+                f.dtype == KVS_F32
+                    ? kvs::launch_prefill_f32(qb, out + heads0, kp, kp + (size_t)rows * f.head_dim * ctx->elem, seqs, n_q, f.n_q_heads, ctx->G,
+                                              f.head_dim, n, stride, ctx->scale * 1.4426950408889634f, st)
+                    : kvs::launch_prefill(qb, out + heads0, reinterpret_cast<int*>(ctx->ws + ctx->off_status),
+                                          reinterpret_cast<int*>(ctx->ws + ctx->off_status + 64), ctx->plain_map, seqs, n_q, f.n_q_heads, ctx->G,
+                                          f.head_dim, n, stride, 0, rows, rows, ctx->scale * 1.4426950408889634f, ctx->sm_count, ctx->l2_bytes, st);
+            if (e != cudaSuccess) return KVS_ERR_CUDA;
+            ctx->seq += 2;
+            ctx->last_splitk_seq = ctx->seq;     // the attention is a plain launch
+            ctx->counter_written = false;
+        }
+        ctx->stats.prefill_launches += 1;
+        return KVS_OK;
+    }
     if (ctx->cfg.dtype == KVS_F32) {
         // fp32 storage: the plain fp32 kernel (a plain launch, like the tensor-core one)
         const char* kp = ctx->pool + (size_t)(2 * slot) * ctx->plane_bytes;
@@ -842,8 +981,35 @@ kvs_status kvs_append_rotary(kvs_ctx* ctx, int32_t layer, const kvs_rotary* rot,
         r.n_extra = replay_counter(ctx);
         r.plane_bytes = (long long)ctx->plane_bytes;
     }
-    r.programmatic = take_early_start(ctx);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (!sharing && ctx->format == KVS_CACHE_4BIT) {
+        // sequences at a time: finished keys and values into the scratch, from there into the 4-bit rows
+        const long long head = (long long)n_new * f.head_dim, seq = f.n_kv_heads * head;
+        const int step = plain_seqs(ctx, batch, n_new);
+        r.row_stride = r.capacity = n_new;
+        r.len0 = 0;
+        r.unit_len = nullptr;
+        r.n_extra = nullptr;
+        for (int b0 = 0; b0 < batch; b0 += step) {
+            const long long tok0 = (long long)b0 * n_new;
+            r.batch = std::min(step, batch - b0);
+            r.q = static_cast<const char*>(q) + tok0 * q_stride * ctx->elem;
+            r.k = static_cast<const char*>(k) + tok0 * k_stride * ctx->elem;
+            r.v = static_cast<const char*>(v) + tok0 * v_stride * ctx->elem;
+            r.positions = positions ? positions + tok0 : nullptr;
+            r.q_out = static_cast<char*>(q_out) + tok0 * q_row * ctx->elem;
+            r.kplane = ctx->ws + ctx->off_plain;
+            r.vplane = ctx->ws + ctx->off_plain + (size_t)r.batch * seq * ctx->elem;
+            r.plane_bytes = (long long)r.batch * seq * ctx->elem;
+            r.programmatic = take_early_start(ctx);
+            if (kvs::launch_append_rotary(r, st) != cudaSuccess ||
+                store_packed(ctx, slot, r.kplane, r.vplane, seq, f.head_dim, head, b0, r.batch, n_new, st) != cudaSuccess)
+                return KVS_ERR_CUDA;
+            ctx->seq += 2;
+        }
+        return appended(ctx, slot, batch, n_new, st);
+    }
+    r.programmatic = take_early_start(ctx);
     if (kvs::launch_append_rotary(r, st) != cudaSuccess) return KVS_ERR_CUDA;
     if (!sharing) return appended(ctx, slot, batch, n_new, st);
     ctx->seq += 1;
@@ -854,7 +1020,7 @@ kvs_status kvs_append_rotary(kvs_ctx* ctx, int32_t layer, const kvs_rotary* rot,
 kvs_status kvs_tree_attention(kvs_ctx* ctx, int32_t layer, const void* q, void* out, const uint64_t* mask, int32_t batch,
                               int32_t n_t, void* stream) {
     if (!ctx) return KVS_ERR_INVALID_ARG;
-    if (!ctx->bound || ctx->opt_replay) return KVS_ERR_STATE;
+    if (!ctx->bound || ctx->opt_replay || ctx->format == KVS_CACHE_4BIT) return KVS_ERR_STATE;
     if (ctx->cfg.dtype == KVS_BF16 && !ctx->have_tensor_map) return KVS_ERR_STATE;
     if (layer < 0 || layer >= ctx->cfg.n_layers || !q || !out) return KVS_ERR_INVALID_ARG;
     if (batch < 1 || batch > ctx->cfg.max_batch || n_t < 1 || n_t > kvs::kTreeMaxTokens) return KVS_ERR_INVALID_ARG;
@@ -974,6 +1140,7 @@ kvs_status kvs_decode_attention_weights(kvs_ctx* ctx, int32_t layer, const void*
                                         float* total_out, int32_t total_stride, int32_t batch, void* stream) {
     kvs_status s = check_attention(ctx, layer, q, out, batch);
     if (s != KVS_OK) return s;
+    if (ctx->format == KVS_CACHE_4BIT) return KVS_ERR_STATE;
     if (!total_out || ((uintptr_t)total_in % 4) != 0 || ((uintptr_t)total_out % 4) != 0) return KVS_ERR_INVALID_ARG;
     // a recorded launch grows on the device: its totals need room for every row the slot can hold
     if (total_stride < (ctx->opt_replay ? ctx->cfg.max_seq : ctx->slot_len[ctx->slot_of_layer[layer]])) return KVS_ERR_INVALID_ARG;
@@ -1022,6 +1189,122 @@ kvs_status kvs_select_rows(kvs_ctx* ctx, int32_t layer, const float* total, int3
     return KVS_OK;
 }
 
+kvs_status kvs_read_rows(kvs_ctx* ctx, int32_t layer, int32_t first, int32_t n_rows, void* k_out, void* v_out, int32_t batch, void* stream) {
+    if (!ctx) return KVS_ERR_INVALID_ARG;
+    if (!ctx->bound) return KVS_ERR_STATE;
+    if (layer < 0 || layer >= ctx->cfg.n_layers || !k_out || !v_out || first < 0 || n_rows < 1) return KVS_ERR_INVALID_ARG;
+    if (((uintptr_t)k_out % 16) != 0 || ((uintptr_t)v_out % 16) != 0) return KVS_ERR_INVALID_ARG;
+    const int slot = ctx->slot_of_layer[layer];
+    if (ctx->slot_len[slot] == 0) return KVS_ERR_STATE;
+    if (batch < 1 || batch > ctx->cur_batch || (long long)first + n_rows > ctx->slot_len[slot]) return KVS_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    const long long D = ctx->cfg.head_dim, token = ctx->cfg.n_kv_heads * D;
+    kvs::ReadArgs r = {};
+    r.kplane = ctx->pool + (size_t)(2 * slot) * ctx->plane_bytes;
+    r.vplane = static_cast<const char*>(r.kplane) + ctx->plane_bytes;
+    r.packed = ctx->format == KVS_CACHE_4BIT;
+    r.row_stride = ctx->row_stride;
+    r.first = first;
+    r.n = n_rows;
+    r.unit_len = ctx->ragged[slot] ? unit_len_dev(ctx, slot) : nullptr;
+    r.k_out = k_out;
+    r.v_out = v_out;
+    r.dst_b = n_rows * token;
+    r.dst_t = token;
+    r.dst_h = D;
+    r.batch = batch;
+    r.Hkv = ctx->cfg.n_kv_heads;
+    r.D = ctx->cfg.head_dim;
+    r.dtype = ctx->cfg.dtype;
+    r.status = reinterpret_cast<int*>(ctx->ws + ctx->off_status);
+    r.plane_bytes = (long long)ctx->plane_bytes;
+    r.sm_count = ctx->sm_count;
+    r.programmatic = take_early_start(ctx);
+    if (kvs::launch_read_rows(r, static_cast<cudaStream_t>(stream)) != cudaSuccess) return KVS_ERR_CUDA;
+    ctx->seq += 1;
+    return KVS_OK;
+}
+
+kvs_status kvs_beam_select(kvs_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t logits_stride, int32_t vocab, const float* scores,
+                           int32_t n_requests, int32_t n_beams, int32_t n_out, float* out_scores, int32_t* out_tokens,
+                           int32_t* out_parents, void* stream) {
+    if (!ctx || !logits || !scores || !out_scores || !out_tokens || !out_parents) return KVS_ERR_INVALID_ARG;
+    if (!ctx->bound) return KVS_ERR_STATE;
+    if (logits_dtype != KVS_BF16 && logits_dtype != KVS_F32) return KVS_ERR_INVALID_ARG;
+    if (vocab < 1 || logits_stride < vocab || n_requests < 1 || n_beams < 1 || n_beams > kvs::kBeamMaxBeams || n_out < 1 ||
+        n_out > kvs::kBeamMaxOut)
+        return KVS_ERR_INVALID_ARG;
+    if ((long long)n_requests * n_beams > ctx->cfg.max_batch || (long long)n_beams * vocab > 0x7fffffffll) return KVS_ERR_INVALID_ARG;
+    if (n_requests * n_beams > 65535) return KVS_ERR_INVALID_ARG;      // a grid dimension
+    if (((uintptr_t)logits % (logits_dtype == KVS_BF16 ? 2 : 4)) != 0 || ((uintptr_t)scores % 4) != 0 || ((uintptr_t)out_scores % 4) != 0 ||
+        ((uintptr_t)out_tokens % 4) != 0 || ((uintptr_t)out_parents % 4) != 0)
+        return KVS_ERR_INVALID_ARG;
+    if (scores == out_scores) return KVS_ERR_INVALID_ARG;      // one request's result would overwrite another's scores
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    kvs::BeamArgs b = {};
+    b.logits = logits;
+    b.stride = logits_stride;
+    b.vocab = vocab;
+    b.dtype = logits_dtype;
+    b.scores = scores;
+    b.requests = n_requests;
+    b.beams = n_beams;
+    b.n_out = n_out;
+    b.out_scores = out_scores;
+    b.out_tokens = out_tokens;
+    b.out_parents = out_parents;
+    b.scratch = ctx->ws + ctx->off_search;
+    b.status = reinterpret_cast<int*>(ctx->ws + ctx->off_status);
+    b.sm_count = ctx->sm_count;
+    b.programmatic = take_early_start(ctx);
+    if (kvs::launch_beam_select(b, static_cast<cudaStream_t>(stream)) != cudaSuccess) return KVS_ERR_CUDA;
+    ctx->seq += 2;
+    return KVS_OK;
+}
+
+kvs_status kvs_reorder(kvs_ctx* ctx, const int32_t* parent, int32_t first_row, int32_t batch, void* stream) {
+    if (!ctx || !parent) return KVS_ERR_INVALID_ARG;
+    if (!ctx->bound) return KVS_ERR_STATE;
+    if (batch < 1 || batch > ctx->cfg.max_batch || first_row < 0 || ((uintptr_t)parent % 4) != 0) return KVS_ERR_INVALID_ARG;
+    if (ctx->cur_batch == 0) return KVS_ERR_STATE;
+    // a recorded step keeps its batch; sequences the batch gains have no rows before first_row yet
+    if (batch != ctx->cur_batch && ctx->opt_replay) return KVS_ERR_STATE;
+    if (batch > ctx->cur_batch && first_row != 0) return KVS_ERR_INVALID_ARG;
+    if (batch > kvs::kReorderMaxBatch || ctx->cur_batch > kvs::kReorderMaxBatch) return KVS_ERR_INVALID_ARG;
+    for (int s = 0; s < ctx->n_slots; ++s)
+        if (ctx->ragged[s]) return KVS_ERR_STATE;      // whose lengths go with which sequence only the device knows
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return KVS_ERR_CUDA;
+    kvs::ReorderArgs r = {};
+    r.parent = parent;
+    r.plane_bytes = (long long)ctx->plane_bytes;
+    r.Hkv = ctx->cfg.n_kv_heads;
+    r.row_bytes = ctx->row_bytes;
+    r.row_stride = ctx->row_stride;
+    r.first = first_row;
+    r.capacity = ctx->cfg.max_seq;
+    r.old_batch = ctx->cur_batch;
+    r.new_batch = batch;
+    r.n_extra = replay_counter(ctx);
+    r.status = reinterpret_cast<int*>(ctx->ws + ctx->off_status);
+    r.wait_ns = 1000ull * (unsigned long long)ctx->opt_wait_us;
+    r.sm_count = ctx->sm_count;
+    for (int s0 = 0; s0 < ctx->n_slots; s0 += kvs::ReorderRows::kMax) {
+        r.pool = ctx->pool + (size_t)(2 * s0) * ctx->plane_bytes;
+        r.slots = std::min(ctx->n_slots - s0, (int)kvs::ReorderRows::kMax);
+        r.programmatic = take_early_start(ctx);
+        kvs::ReorderRows rows = {};
+        for (int s = 0; s < r.slots; ++s) rows.n[s] = ctx->slot_len[s0 + s];
+        if (kvs::launch_reorder(r, rows, static_cast<cudaStream_t>(stream)) != cudaSuccess) return KVS_ERR_CUDA;
+        ctx->seq += 1;
+    }
+    for (int s = 0; s < ctx->n_slots; ++s) rows_moved(ctx, s);
+    ctx->cur_batch = batch;
+    return KVS_OK;
+}
+
 kvs_status kvs_unit_len(const kvs_ctx* ctx, int32_t layer, int32_t b, int32_t h, int32_t* len) {
     if (!ctx || !len || layer < 0 || layer >= ctx->cfg.n_layers) return KVS_ERR_INVALID_ARG;
     if (b < 0 || b >= ctx->cfg.max_batch || h < 0 || h >= ctx->cfg.n_kv_heads) return KVS_ERR_INVALID_ARG;
@@ -1033,7 +1316,7 @@ kvs_status kvs_unit_len(const kvs_ctx* ctx, int32_t layer, int32_t b, int32_t h,
 
 kvs_status kvs_layer_distances(kvs_ctx* ctx, int32_t batch, float* dist, void* stream) {
     if (!ctx || !dist) return KVS_ERR_INVALID_ARG;
-    if (!ctx->bound) return KVS_ERR_STATE;
+    if (!ctx->bound || ctx->format == KVS_CACHE_4BIT) return KVS_ERR_STATE;
     if (ctx->cfg.n_layers > kvs::kMaxLayersSearch) return KVS_ERR_INVALID_ARG;
     if (batch < 1 || batch > ctx->cur_batch) return ctx->cur_batch == 0 ? KVS_ERR_STATE : KVS_ERR_INVALID_ARG;
     const int n = ctx->slot_len[0];
@@ -1199,7 +1482,7 @@ kvs_status kvs_step_host(kvs_ctx* ctx, const void* q_host, const void* k_host, c
         for (int l = l0; l < l1; ++l) {
             float* o = reinterpret_cast<float*>(dout + out_layer * l);
             kvs_status s;
-            if (ctx->share_map[l] == l && !ctx->ragged[ctx->slot_of_layer[l]]) {
+            if (ctx->share_map[l] == l && !ctx->ragged[ctx->slot_of_layer[l]] && ctx->format == KVS_CACHE_PLAIN) {
                 // the append rides in the split-K kernel (the staging rows are 16-byte aligned)
                 s = do_fused_step(ctx, l, dq + q_layer * l, dk + kv_layer * l, dv + kv_layer * l, o, batch, st);
             } else {
@@ -1242,6 +1525,12 @@ kvs_status kvs_slot_of_layer(const kvs_ctx* ctx, int32_t layer, int32_t* slot) {
 kvs_status kvs_seq_len(const kvs_ctx* ctx, int32_t layer, int32_t* len) {
     if (!ctx || !len || layer < 0 || layer >= ctx->cfg.n_layers) return KVS_ERR_INVALID_ARG;
     *len = ctx->slot_len[ctx->slot_of_layer[layer]];
+    return KVS_OK;
+}
+
+kvs_status kvs_cached_batch(const kvs_ctx* ctx, int32_t* batch) {
+    if (!ctx || !batch) return KVS_ERR_INVALID_ARG;
+    *batch = ctx->cur_batch;
     return KVS_OK;
 }
 
@@ -1293,6 +1582,7 @@ kvs_status kvs_clear_device_status(kvs_ctx* ctx, void* stream) {
 kvs_status kvs_selftest_stalled_copy(kvs_ctx* ctx, int32_t layer, const void* q, float* out, int32_t batch, void* stream) {
     kvs_status s = check_attention(ctx, layer, q, out, batch);
     if (s != KVS_OK) return s;
+    if (ctx->format == KVS_CACHE_4BIT && ctx->cfg.dtype == KVS_F32) return KVS_ERR_STATE;
     DeviceGuard guard(ctx->cfg.device);
     if (!guard.ok) return KVS_ERR_CUDA;
     const int slot = ctx->slot_of_layer[layer];

@@ -1,0 +1,506 @@
+// Beam search around the cache: the best continuations of every request's beams, and the sequences of every slot taking the
+// rows of the beams they continue.
+#include <algorithm>
+
+#include "kvs_device.cuh"
+#include "kvs_kernels.h"
+
+namespace kvs {
+
+namespace {
+
+// --------------------------------------------------------------------------------------
+// Selection.  score(b, v) = scores[b] - lse_b + x_bv,  lse_b = log sum_v exp x_bv;  of a request's W beams x V tokens the K
+// best, equal scores by the lowest (beam, token).
+//
+// First kernel: every logits row is cut into segments, a block each (one pass over the logits): running maximum and sum of
+// its exponentials per thread, and the segment's K best, by a threshold.  Logits become 64-bit keys (order of the value, then
+// the lower index), all different.  The K-th largest of the threads' own maxima bounds the K-th best from below, and exactly
+// K threads reach it: at most K times a thread's share passes, however the logits are ordered and however many are equal.
+// Second kernel, a block per request: lse in fp64 (a rounding of 1e-7 would decide between beams whose scores nearly tie), the
+// segments' lists by the same threshold, and the K best in order.
+// Bound: HBM for the logits, once; small calls: two launches.
+// --------------------------------------------------------------------------------------
+constexpr int kBeamThreads = 256;
+constexpr int kBeamPer = 16;                              // logits per thread and turn
+constexpr int kBeamTurn = kBeamThreads * kBeamPer;
+constexpr int kBeamRoom = kBeamMaxOut * kBeamPer * 2;     // candidates: what is kept, and what one turn adds
+
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t u = __float_as_uint(x + 0.f);          // -0 and 0 are equal
+    return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xffffffffu)); }
+
+// exp(t), t <= 0 or NaN, to fp32 accuracy: the rounding of t * log2(e) goes back in as a factor
+__device__ __forceinline__ float exp_of(float t) {
+    constexpr float L = 1.44269504f, L2 = 1.92596303e-8f;     // log2(e) in two parts
+    const float y = t * L;
+    const float r = fmaf(t, L2, fmaf(t, L, -y));
+    const float e = fast_exp2(y);
+    return t < -200.f ? 0.f : fmaf(e, r * 0.693147181f, e);     // (far below, t * log2(e) overflows)
+}
+
+// 64-bit keys by value, then by the lower index: the second kernel's key needs more bits than one word
+struct Wide {
+    uint64_t v;      // order of the fp64 score
+    uint32_t i;      // ~(flat index)
+};
+__device__ __forceinline__ bool above(uint64_t a, uint64_t b) { return a > b; }
+__device__ __forceinline__ bool above(const Wide& a, const Wide& b) { return a.v > b.v || (a.v == b.v && a.i > b.i); }
+
+// The K-th largest of all threads' keys into *cut, for every thread (keys that differ, except `lowest`, which nothing is
+// below).  `keys`: a shared array of a key per thread.
+template <typename Key>
+__device__ __forceinline__ void kth_of_threads(const Key& mine, int K, const Key& lowest, Key* keys, Key* cut) {
+    keys[threadIdx.x] = mine;
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 16
+    for (int j = 0; j < kBeamThreads; ++j) rank += above(keys[j], mine) ? 1 : 0;
+    if (rank == K - 1 || (rank < K - 1 && !above(mine, lowest))) *cut = mine;        // (several lowest keys: the same value)
+    __syncthreads();
+}
+
+// Of the `count` keys in `list` the K best, in order, to put(rank, key); `lowest` is a key nothing is below.
+template <typename Key, typename Put>
+__device__ __forceinline__ void best_in_order(Key* list, int* count, int K, const Key& lowest, Key* keys, Key* cut, Put put) {
+    while (*count > kBeamThreads) {
+        const int n = *count;
+        constexpr int MOST = (kBeamRoom + kBeamThreads - 1) / kBeamThreads;
+        Key mine[MOST], top = lowest;
+        int have = 0;
+#pragma unroll
+        for (int j = 0; j < MOST; ++j) {
+            const int at = threadIdx.x + j * kBeamThreads;
+            if (at < n) {
+                mine[j] = list[at];
+                if (above(mine[j], top)) top = mine[j];
+                have = j + 1;
+            }
+        }
+        kth_of_threads(top, K, lowest, keys, cut);
+        const Key c = *cut;
+        if (threadIdx.x == 0) *count = 0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < MOST; ++j)
+            if (j < have && !above(c, mine[j])) list[atomicAdd(count, 1)] = mine[j];
+        __syncthreads();
+    }
+    const int n = *count;
+    if ((int)threadIdx.x < n) {
+        const Key mine = list[threadIdx.x];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += above(list[j], mine) ? 1 : 0;
+        if (rank < K) put(rank, mine);
+    }
+}
+
+struct BeamKernelArgs {
+    const void* logits;
+    long long stride;        // elements between rows
+    int vocab, rows, segs, seg_len;
+    bool vec;                // rows start on 16 bytes
+    const float* scores;
+    int W, K;
+    float* out_scores;
+    int* out_tokens;
+    int* out_parents;
+    uint64_t* lists;         // [rows][segs][K] keys, best first, 0 where there are fewer
+    float2* sums;            // [rows][segs] maximum, sum of exponentials below it
+    int* status;
+    long long list_count, sum_count;
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kBeamThreads) beam_segments_kernel(const BeamKernelArgs a) {
+    __shared__ uint64_t s_list[kBeamRoom];
+    __shared__ uint64_t s_keys[kBeamThreads];
+    __shared__ uint64_t s_cut;
+    __shared__ int s_count, s_more[2];       // kept; candidates of a turn, of even and odd turns
+    __shared__ float2 s_sum[kBeamThreads / 32];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int seg = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+    const int v0 = seg * a.seg_len, v1 = min(a.vocab, v0 + a.seg_len);
+    const T* x_row = static_cast<const T*>(a.logits) + row * a.stride;
+    const uint64_t none = (uint64_t)order_of(-INFINITY) << 32 | 0xffffffffu;     // minus infinity is no candidate
+    constexpr int PER16 = 16 / (int)sizeof(T);       // logits per 16-byte load
+    uint64_t cut = none;
+    float m = -INFINITY, sum = 0.f;
+    if (tid == 0) s_count = s_more[0] = s_more[1] = 0;
+    __syncthreads();
+    int turn = 0;
+    for (int base = v0; base < v1; base += kBeamTurn, turn ^= 1) {
+        const int count = s_count;       // (nobody adds before the next barrier)
+        // thread t takes runs of 16 bytes, t, t + 256, ...: the same elements whether they can be loaded as vectors or not
+        float x[kBeamPer];
+        int idx[kBeamPer / PER16];
+#pragma unroll
+        for (int j = 0; j < kBeamPer / PER16; ++j) {
+            const int v = base + (j * kBeamThreads + tid) * PER16;
+            idx[j] = v;
+            if (a.vec && v + PER16 <= v1) {
+                const uint4 r = __ldcs(reinterpret_cast<const uint4*>(x_row + v));
+                float f[PER16];
+                Unpack<T>::run(r, f);
+#pragma unroll
+                for (int i = 0; i < PER16; ++i) x[j * PER16 + i] = f[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER16; ++i) x[j * PER16 + i] = v + i < v1 ? (float)x_row[v + i] : -INFINITY;
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < kBeamPer; ++i) top = fmaxf(top, x[i]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        sum *= exp_of(m - ref);          // a NaN stays one, and makes the row's sum NaN
+#pragma unroll
+        for (int i = 0; i < kBeamPer; ++i) sum += exp_of(x[i] - ref);
+        m = top;
+        // candidates: keys above the threshold
+        auto key = [&](int i) { return (uint64_t)order_of(x[i]) << 32 | (uint32_t)~(idx[i / PER16] + i % PER16); };
+        if (base == v0) {
+            uint64_t best = none;
+#pragma unroll
+            for (int i = 0; i < kBeamPer; ++i) best = max(best, key(i));
+            kth_of_threads(best, a.K, none, s_keys, &s_cut);
+            cut = s_cut;
+        }
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < kBeamPer; ++i) mine += key(i) >= cut && key(i) > none ? 1 : 0;
+        if (mine) atomicAdd(&s_more[turn], mine);
+        __syncthreads();
+        const int more = s_more[turn];
+        if (tid == 0) s_more[turn ^ 1] = 0;
+        if (more) {
+            if (count + more > kBeamRoom) {
+                // too many: this turn's own threshold, and that of what has been kept
+                uint64_t best = none;
+#pragma unroll
+                for (int i = 0; i < kBeamPer; ++i) best = max(best, key(i));
+                kth_of_threads(best, a.K, none, s_keys, &s_cut);
+                cut = max(cut, s_cut);
+                __syncthreads();
+                uint64_t kept[kBeamRoom / kBeamThreads];
+                best = none;
+#pragma unroll
+                for (int j = 0; j < kBeamRoom / kBeamThreads; ++j) {
+                    const int at = tid + j * kBeamThreads;
+                    kept[j] = at < count ? s_list[at] : none;
+                    best = max(best, kept[j]);
+                }
+                kth_of_threads(best, a.K, none, s_keys, &s_cut);
+                cut = max(cut, s_cut);
+                if (tid == 0) s_count = 0;
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < kBeamRoom / kBeamThreads; ++j)
+                    if (kept[j] >= cut && kept[j] > none) s_list[atomicAdd(&s_count, 1)] = kept[j];
+                __syncthreads();
+            }
+#pragma unroll
+            for (int i = 0; i < kBeamPer; ++i)
+                if (key(i) >= cut && key(i) > none) {
+                    const int at = atomicAdd(&s_count, 1);
+                    if (at < kBeamRoom) s_list[at] = key(i);
+                }
+        }
+        __syncthreads();
+    }
+    // the segment's maximum and sum, in a fixed order
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, d), sum2 = __shfl_xor_sync(0xffffffffu, sum, d);
+        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
+        const float lo = m <= m2 ? sum * exp_of(m - ref) : sum2 * exp_of(m2 - ref), hi = m <= m2 ? sum2 : sum;
+        sum = m == m2 ? sum + sum2 : hi + lo;
+        m = top;
+    }
+    if ((tid & 31) == 0) s_sum[tid >> 5] = make_float2(m, sum);
+    __syncthreads();
+    const long long at = (long long)row * a.segs + seg;
+    if (tid == 0 && KVS_BOUNDS_OK(at, 1, a.sum_count, a.status)) {
+        float top = -INFINITY, total = 0.f;
+        for (int w = 0; w < kBeamThreads / 32; ++w) top = fmaxf(top, s_sum[w].x);
+        for (int w = 0; w < kBeamThreads / 32; ++w)
+            total += s_sum[w].x == top ? s_sum[w].y : s_sum[w].y * exp_of(s_sum[w].x - top);
+        a.sums[at] = make_float2(top, total);
+    }
+    uint64_t* out = a.lists + at * a.K;
+    const bool room = KVS_BOUNDS_OK(at * a.K, a.K, a.list_count, a.status);
+    best_in_order(s_list, &s_count, a.K, none, s_keys, &s_cut, [&](int rank, uint64_t k) {
+        if (room) out[rank] = k;
+    });
+    if (room && tid < a.K && tid >= s_count) out[tid] = 0;
+}
+
+__device__ __forceinline__ uint64_t order_of(double x) {
+    const uint64_t u = __double_as_longlong(x + 0.0);
+    return u ^ (u >> 63 ? 0xffffffffffffffffull : 0x8000000000000000ull);
+}
+__device__ __forceinline__ double value_of(uint64_t o) { return __longlong_as_double(o ^ (o >> 63 ? 0x8000000000000000ull : 0xffffffffffffffffull)); }
+
+__global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKernelArgs a) {
+    __shared__ Wide s_list[kBeamRoom];
+    __shared__ Wide s_keys[kBeamThreads];
+    __shared__ Wide s_cut;
+    __shared__ double s_base[kBeamMaxBeams];      // scores[b] - log of the sum below the row's maximum
+    __shared__ float s_top[kBeamMaxBeams];
+    __shared__ int s_count;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int req = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const long long row0 = (long long)req * a.W;
+    for (int b = warp; b < a.W; b += kBeamThreads / 32) {
+        const float2* sums = a.sums + (row0 + b) * a.segs;
+        float top = -INFINITY;
+        for (int i = lane; i < a.segs; i += 32) top = fmaxf(top, __ldcg(&sums[i].x));
+#pragma unroll
+        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        double total = 0;
+        for (int i = lane; i < a.segs; i += 32) {
+            const float2 s = __ldcg(sums + i);
+            total += (double)s.y * (s.x == top ? 1.0 : exp((double)s.x - (double)top));
+        }
+#pragma unroll
+        for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+        if (lane == 0) {
+            const double base = (double)a.scores[row0 + b] - log(total);
+            s_base[b] = isfinite(base) ? base : -(double)INFINITY;      // such a row has no candidates
+            s_top[b] = top;
+        }
+    }
+    if (tid == 0) s_count = 0;
+    __syncthreads();
+    // a thread per list (best first): its head bounds it
+    const Wide lowest = {order_of(-(double)INFINITY), 0u};      // scores of minus infinity and NaN are no candidates
+    const int lists = a.W * a.segs, beam = tid / a.segs;
+    const uint64_t* list = a.lists + (row0 * a.segs + tid) * a.K;
+    auto candidate = [&](uint64_t k) {
+        Wide w = lowest;
+        if (k) {
+            const double score = s_base[beam] + ((double)value_of((uint32_t)(k >> 32)) - (double)s_top[beam]);
+            const uint32_t flat = (uint32_t)beam * (uint32_t)a.vocab + ~(uint32_t)k;
+            if (score > -(double)INFINITY) w = {order_of(score), ~flat};
+        }
+        return w;
+    };
+    const Wide head = tid < lists ? candidate(__ldcg(list)) : lowest;
+    kth_of_threads(head, a.K, lowest, s_keys, &s_cut);
+    Wide cut = s_cut;
+    int held = 0;       // what the list holds, the same in every thread
+    for (int j = 0; j < a.K; ++j) {
+        const Wide w = j == 0 ? head : tid < lists ? candidate(__ldcg(list + j)) : lowest;
+        const bool in = above(w, lowest) && !above(cut, w);
+        if (in) s_list[atomicAdd(&s_count, 1)] = w;
+        // after every step of all lists: room for another, or a new threshold first
+        const int added = __syncthreads_count(in);
+        if (added == 0) break;
+        held += added;
+        if (held > kBeamRoom - kBeamThreads) {
+            constexpr int MOST = kBeamRoom / kBeamThreads;
+            Wide mine[MOST], top = lowest;
+#pragma unroll
+            for (int i = 0; i < MOST; ++i) {
+                mine[i] = tid + i * kBeamThreads < held ? s_list[tid + i * kBeamThreads] : lowest;
+                if (above(mine[i], top)) top = mine[i];
+            }
+            kth_of_threads(top, a.K, lowest, s_keys, &s_cut);
+            if (above(s_cut, cut)) cut = s_cut;
+            if (tid == 0) s_count = 0;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < MOST; ++i)
+                if (above(mine[i], lowest) && !above(cut, mine[i])) s_list[atomicAdd(&s_count, 1)] = mine[i];
+            __syncthreads();
+            held = s_count;
+            __syncthreads();
+        }
+    }
+    __syncthreads();
+    const long long o = (long long)req * a.K;
+    best_in_order(s_list, &s_count, a.K, lowest, s_keys, &s_cut, [&](int rank, const Wide& w) {
+        const uint32_t flat = ~w.i;
+        a.out_scores[o + rank] = (float)value_of(w.v);
+        a.out_tokens[o + rank] = (int)(flat % (uint32_t)a.vocab);
+        a.out_parents[o + rank] = (int)(row0 + flat / (uint32_t)a.vocab);
+    });
+    if (tid < a.K && tid >= s_count) {     // fewer candidates than places
+        a.out_scores[o + tid] = -INFINITY;
+        a.out_tokens[o + tid] = -1;
+        a.out_parents[o + tid] = (int)row0;
+    }
+}
+
+// --------------------------------------------------------------------------------------
+// Reordering.  Sequence b of every plane takes rows first .. n-1 of sequence parent[b].  In place: a block takes one run of
+// bytes of one head's rows, the same run of every sequence; it brings the runs of all sequences that another one takes
+// into shared memory (bulk copies), waits, and sends them to their takers (bulk copies).  A source is read once however many
+// take it, a sequence that stays as it is costs nothing.  Bound: HBM, bytes read and written once.
+// --------------------------------------------------------------------------------------
+constexpr int kReorderThreads = 128;
+constexpr int kReorderBytes = 64 * 1024;       // shared memory for the runs; three blocks per SM
+
+struct ReorderKernelArgs {
+    char* pool;
+    const int* parent;
+    long long plane_bytes;
+    int planes, Hkv, row_bytes, row_stride, first, cap, old_batch, new_batch;
+    const int* n_extra;
+    int* status;
+    unsigned long long wait_ns;
+};
+
+__global__ void __launch_bounds__(kReorderThreads) reorder_kernel(const ReorderKernelArgs a, const ReorderRows rows) {
+    extern __shared__ __align__(128) unsigned char run[];
+    int* from = reinterpret_cast<int*>(run + kReorderBytes);       // [sources]: the sequences to read
+    int* place = from + a.old_batch;                              // [old_batch]: where a sequence's run lies, or -1
+    int* to = place + a.old_batch;                                // [takers]: sequence
+    int* what = to + a.new_batch;                                 // [takers]: its source, then where that lies
+    __shared__ uint64_t bar;
+    __shared__ int s_sources, s_takers, s_abort, s_gave_up;
+    const int tid = threadIdx.x;
+    if (tid == 0) {
+        mbar_init(&bar, 1);
+        fence_mbar_init();
+        s_sources = s_takers = s_abort = s_gave_up = 0;
+    }
+    for (int b = tid; b < a.old_batch; b += kReorderThreads) place[b] = -1;
+    pdl_launch_dependents();
+    pdl_wait();
+    __syncthreads();
+    // who takes from whom; a parent out of range leaves its sequence as it is
+    for (int b = tid; b < a.new_batch; b += kReorderThreads) {
+        const int p = a.parent[b];
+        if (p < 0 || p >= a.old_batch) {
+            if (blockIdx.x == 0) atomicExch(a.status, 1);
+            continue;
+        }
+        if (p == b) continue;
+        const int i = atomicAdd(&s_takers, 1);
+        to[i] = b;
+        what[i] = p;
+        if (atomicExch(&place[p], -2) == -1) from[atomicAdd(&s_sources, 1)] = p;
+    }
+    __syncthreads();
+    const int sources = s_sources, takers = s_takers;
+    if (takers == 0) return;
+    for (int i = tid; i < sources; i += kReorderThreads) place[from[i]] = i;
+    __syncthreads();
+    for (int i = tid; i < takers; i += kReorderThreads) what[i] = place[what[i]];      // (read again by the same thread)
+    const int chunk = kReorderBytes / sources / 16 * 16;
+    const int extra = a.n_extra ? *a.n_extra : 0;
+    int longest = 0;
+    for (int s = 0; s < a.planes / 2; ++s) longest = max(longest, min(rows.n[s] + extra, a.cap));
+    const long long most = (long long)max(0, longest - a.first) * a.row_bytes;      // bytes of a unit's rows that move
+    const long long chunks = (most + chunk - 1) / chunk, items = chunks * a.planes * a.Hkv;
+    int turn = 0;
+    for (long long it = blockIdx.x; it < items; it += gridDim.x) {
+        const long long head = it / chunks, c = it - head * chunks;
+        const int plane = (int)(head / a.Hkv), h = (int)(head - (long long)plane * a.Hkv);
+        const int n = min(rows.n[plane / 2] + extra, a.cap);
+        const long long len = (long long)max(0, n - a.first) * a.row_bytes, at = c * chunk;
+        if (at >= len) continue;            // a slot with fewer rows than others
+        const uint32_t bytes = (uint32_t)min((long long)chunk, len - at);
+        const long long off0 = ((long long)h * a.row_stride + a.first) * a.row_bytes + at;
+        const long long seq = (long long)a.Hkv * a.row_stride * a.row_bytes;
+        char* base = a.pool + plane * a.plane_bytes;
+        // the previous item's runs have left shared memory before they are overwritten
+        if (turn) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncthreads();
+        if (tid == 0) mbar_arrive_expect_tx(&bar, bytes * (uint32_t)sources);
+        __syncthreads();
+        for (int i = tid; i < sources; i += kReorderThreads) {
+            long long off = from[i] * seq + off0;
+            if (!KVS_BOUNDS_OK(off, bytes, a.plane_bytes, a.status)) off = 0;
+            bulk_g2s(run + (size_t)i * chunk, base + off, bytes, &bar);
+        }
+        const bool ok = mbar_wait_bounded(&bar, turn & 1, &s_abort, a.status, a.wait_ns);
+        ++turn;
+        if (__syncthreads_or(!ok)) {     // give up, with nothing of this item written, once the copies have landed
+            mbar_wait_bounded(&bar, (turn + 1) & 1, &s_gave_up, a.status, a.wait_ns);
+            break;
+        }
+        for (int i = tid; i < takers; i += kReorderThreads) {
+            const long long off = to[i] * seq + off0;
+            if (KVS_BOUNDS_OK(off, bytes, a.plane_bytes, a.status))
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(base + off),
+                             "r"(smem_u32(run + (size_t)what[i] * chunk)), "r"(bytes)
+                             : "memory");
+        }
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+}
+
+size_t reorder_smem(int old_batch, int new_batch) { return kReorderBytes + 2ull * (old_batch + new_batch) * sizeof(int); }
+
+}  // namespace
+
+cudaError_t init_beam_kernels() {
+    return cudaFuncSetAttribute(reorder_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)reorder_smem(kReorderMaxBatch, kReorderMaxBatch));
+}
+
+cudaError_t launch_beam_select(const BeamArgs& p, cudaStream_t stream) {
+    BeamKernelArgs a;
+    a.logits = p.logits;
+    a.stride = p.stride;
+    a.vocab = p.vocab;
+    a.rows = p.requests * p.beams;
+    // Segments: enough blocks for eight on every SM, but none shorter than a turn of a block and at most 256 lists (a thread
+    // each in the second kernel) per request, and room for the lists.
+    const long long want = ((long long)p.sm_count * 8 + a.rows - 1) / a.rows;
+    const long long most = std::min<long long>({(p.vocab + kBeamTurn - 1) / kBeamTurn, kBeamThreads / p.beams, std::max(1, kBeamMaxLists / a.rows)});
+    a.segs = (int)std::max(1ll, std::min(want, most));
+    a.seg_len = ((p.vocab + a.segs - 1) / a.segs + 15) / 16 * 16;
+    a.segs = (p.vocab + a.seg_len - 1) / a.seg_len;
+    const int e = p.dtype == 0 ? 2 : 4;
+    a.vec = (uintptr_t)p.logits % 16 == 0 && p.stride * e % 16 == 0;
+    a.scores = p.scores;
+    a.W = p.beams;
+    a.K = p.n_out;
+    a.out_scores = p.out_scores;
+    a.out_tokens = p.out_tokens;
+    a.out_parents = p.out_parents;
+    a.lists = static_cast<uint64_t*>(p.scratch);
+    a.list_count = beam_lists(a.rows) * kBeamMaxOut;
+    a.sums = reinterpret_cast<float2*>(a.lists + a.list_count);
+    a.sum_count = beam_lists(a.rows);
+    a.status = p.status;
+    const dim3 grid(a.segs, a.rows);
+    const cudaError_t err = p.dtype == 0 ? launch_kernel(beam_segments_kernel<__nv_bfloat16>, grid, dim3(kBeamThreads), 0, stream, p.programmatic, a)
+                                         : launch_kernel(beam_segments_kernel<float>, grid, dim3(kBeamThreads), 0, stream, p.programmatic, a);
+    if (err != cudaSuccess) return err;
+    return launch_kernel(beam_finish_kernel, dim3(p.requests), dim3(kBeamThreads), 0, stream, p.programmatic, a);
+}
+
+cudaError_t launch_reorder(const ReorderArgs& p, const ReorderRows& rows, cudaStream_t stream) {
+    ReorderKernelArgs a;
+    a.pool = static_cast<char*>(p.pool);
+    a.parent = p.parent;
+    a.plane_bytes = p.plane_bytes;
+    a.planes = 2 * p.slots;
+    a.Hkv = p.Hkv;
+    a.row_bytes = p.row_bytes;
+    a.row_stride = p.row_stride;
+    a.first = p.first;
+    a.cap = p.capacity;
+    a.old_batch = p.old_batch;
+    a.new_batch = p.new_batch;
+    a.n_extra = p.n_extra;
+    a.status = p.status;
+    a.wait_ns = p.wait_ns;
+    // no more blocks than there can be items: every run at least a sixteen-byte piece per sequence
+    long long bytes = 0;
+    for (int s = 0; s < p.slots; ++s) bytes = std::max(bytes, (long long)(p.n_extra ? p.capacity : rows.n[s]) * p.row_bytes);
+    const long long smallest = std::max(16, kReorderBytes / std::min(p.old_batch, p.new_batch) / 16 * 16);
+    const long long items = (bytes + smallest - 1) / smallest * a.planes * p.Hkv;
+    const unsigned blocks = (unsigned)std::max(1ll, std::min<long long>(items, p.sm_count * 3));
+    return launch_kernel(reorder_kernel, dim3(blocks), dim3(kReorderThreads), reorder_smem(p.old_batch, p.new_batch), stream, p.programmatic, a, rows);
+}
+
+}  // namespace kvs

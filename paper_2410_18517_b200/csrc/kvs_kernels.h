@@ -17,7 +17,7 @@ struct DecodePlan {
     int tpu;         // tiles per unit = ceil(n / tile_rows)
     long long T;     // total tiles = units * tpu
     int NC;          // thread blocks launched
-    int kernel;      // 1 = scalar, 2 = tensor-core
+    int kernel;      // 1 = scalar, 2 = tensor-core, 3 = tensor-core over a 4-bit cache, 4 = the same for fp32 storage (scalar)
 };
 
 struct DecodeArgs {
@@ -58,7 +58,7 @@ struct DecodeArgs {
 };
 
 // Whether a launch of this plan over `units` units can finish inside the split-K kernel.
-inline bool can_finish_in_kernel(const DecodePlan& plan, int units) { return units >= plan.NC; }
+inline bool can_finish_in_kernel(const DecodePlan& plan, int units) { return units >= plan.NC && plan.kernel != 4; }
 
 // Largest number of thread blocks any plan may use (sizes the partial buffers).
 constexpr int kMaxCtas = 1024;
@@ -82,6 +82,49 @@ cudaError_t make_pool_tensor_map(void* storage, void* pool, long long total_rows
 // krow0 / vrow0: first row of the K / V plane in the pool-wide row numbering.
 cudaError_t launch_decode_mma(const DecodeArgs& a, const DecodePlan& plan, const void* tensor_map,
                               const void* tensor_map_tail, long long krow0, long long vrow0, cudaStream_t stream);
+
+// 4-bit caches (see kvs_pack4.cuh for the row).
+inline int pack4_row_bytes(int D) { return 16 + D / 2; }
+struct PackArgs {
+    const void* k;                     // storage type; strides in elements between sequences, tokens, heads (multiples of 16 bytes)
+    const void* v;
+    long long src_b, src_t, src_h;
+    void* kplane;                      // [batch][Hkv][row_stride] rows
+    void* vplane;
+    int batch, n_new, Hkv, D, dtype;
+    int row_stride, len0, capacity;
+    const int* unit_len;
+    const int* n_extra;
+    int* status;
+    long long plane_bytes;
+    int sm_count;
+    bool programmatic;
+};
+cudaError_t launch_pack4(const PackArgs& p, cudaStream_t stream);
+
+// Rows first .. first+n-1 of every unit to k_out / v_out, storage type, at any strides (elements).
+struct ReadArgs {
+    const void* kplane;
+    const void* vplane;
+    bool packed;                       // 4-bit rows
+    int row_stride, first, n;
+    const int* unit_len;
+    void* k_out;
+    void* v_out;
+    long long dst_b, dst_t, dst_h;
+    int batch, Hkv, D, dtype;
+    int* status;
+    long long plane_bytes;
+    int sm_count;
+    bool programmatic;
+};
+cudaError_t launch_read_rows(const ReadArgs& p, cudaStream_t stream);
+
+cudaError_t init_pack4_kernels();
+void plan_decode_pack4(int units, int n, int D, int sm_count, int max_ctas, DecodePlan* plan);
+cudaError_t launch_decode_pack4(const DecodeArgs& a, const DecodePlan& plan, cudaStream_t stream);
+void plan_decode_pack4_f32(int units, int n, int sm_count, int max_ctas, DecodePlan* plan);
+cudaError_t launch_decode_pack4_f32(const DecodeArgs& a, const DecodePlan& plan, cudaStream_t stream);
 
 // Tensor-core prefill attention (bf16, head size D = 64 or 128): q [B][T][Hq][D], out fp32 of the same shape.
 cudaError_t init_prefill_kernels();
@@ -218,6 +261,47 @@ cudaError_t init_weights_kernels();
 // Host counts to device memory as launch arguments: the caller's array is not read after the call, by a recorded launch either.
 cudaError_t launch_put_counts(int* out, const int* n, int units, cudaStream_t stream);
 cudaError_t launch_select(const SelectArgs& a, const SelectCounts& counts, cudaStream_t stream);
+
+// Beam search (see kvs_beam.cu).
+constexpr int kBeamMaxOut = 64;        // continuations per request
+constexpr int kBeamMaxBeams = 64;      // beams per request
+constexpr int kBeamMaxLists = 2048;    // segments of all rows together (more only where there are more rows)
+inline long long beam_lists(long long rows) { return rows > kBeamMaxLists ? rows : kBeamMaxLists; }
+inline size_t beam_scratch_bytes(long long rows) { return (size_t)beam_lists(rows) * (kBeamMaxOut * sizeof(uint64_t) + 2 * sizeof(float)); }
+struct BeamArgs {
+    const void* logits;       // [requests * beams] rows of `vocab`, `stride` elements apart
+    long long stride;
+    int vocab, dtype;
+    const float* scores;      // [requests * beams]
+    int requests, beams, n_out;
+    float* out_scores;        // [requests][n_out]
+    int* out_tokens;
+    int* out_parents;
+    void* scratch;            // beam_scratch_bytes(requests * beams)
+    int* status;
+    int sm_count;
+    bool programmatic;
+};
+cudaError_t init_beam_kernels();
+cudaError_t launch_beam_select(const BeamArgs& p, cudaStream_t stream);   // two launches
+
+constexpr int kReorderMaxBatch = 4096;
+struct ReorderRows {
+    static constexpr int kMax = 512;   // slots per launch
+    int n[kMax];                       // rows of every unit of the slot
+};
+struct ReorderArgs {
+    void* pool;               // first plane of the launch's slots
+    const int* parent;        // device, [new_batch]
+    long long plane_bytes;
+    int slots, Hkv, row_bytes, row_stride, first, capacity, old_batch, new_batch;
+    const int* n_extra;
+    int* status;
+    unsigned long long wait_ns;
+    int sm_count;
+    bool programmatic;
+};
+cudaError_t launch_reorder(const ReorderArgs& p, const ReorderRows& rows, cudaStream_t stream);
 
 // Accepted drafts of one slot move to the front of its draft rows (see kvs_tree.cu).
 struct AcceptCounts {

@@ -1,0 +1,520 @@
+// Split-K decode attention over a 4-bit cache, bf16 storage: the codes become bf16 tensor-core operands in registers.
+//
+// Mathematics: S = q K^T, P = 2^(S - max), O = sum P V over the values of the rows (kvs_pack4.cuh), one pass with a running
+// maximum and sum.  mma.sync.m16n8k16 with the q-heads of a kv-head as rows: a product of 16 rows costs what one of 8 does, so
+// the rows the heads leave free carry the softmax weights' further terms.  P = hi + mid + lo, three bf16 terms:
+//   up to four heads:  rows 0..3 hi, 8..11 mid, 4..7 lo, in ONE product (row r holds head r mod 4 in S, so the lanes of rows
+//                      4..7 have the weights too);
+//   five to eight:     rows 0..7 hi and 8..15 mid in one product, lo in a second.
+// Two terms would leave 1.5e-6 of the result, three the fp32 rounding.  The products of a tile start from zero and are added to
+// the running state rounded to nearest: an MMA cuts its sum off, and over thousands of rows that would drift.
+//
+// Fragments: the contraction may take the elements in any order, so lane t of a quad takes group t of its key's row - D/8 bytes in
+// a run and one (s, b) pair - and the queries' fragments follow that order.  For P V the columns may be numbered at will:
+// column n stands for D/8 neighbouring elements of a row, again of one group; the codes of two keys are interleaved by byte
+// permutes.  A code costs 1/2 (shift + and-or + multiply-add); everything else per row is small beside that.
+//
+// What bounds it: HBM (D + 32 bytes per row of K and V together) until the conversion does: at 6.5 TB/s an SM has 7 cycles per
+// row of 128, in which it issues at most 28 warp instructions, 14 of them integer; the conversion takes 12.5 and 8.5.
+//
+// Work decomposition, pieces, the hand-over between blocks and the combine kernel are those of the other split-K kernels.  Rows of
+// a tile are contiguous and come by two 1-D bulk copies, exactly as many as the unit holds.
+#include <algorithm>
+
+#include "kvs_kernels.h"
+#include "kvs_pack4.cuh"
+
+namespace kvs {
+
+namespace {
+
+// Geometries.  Large: 8 warps x 32 rows a tile; small, where that would leave blocks idle: 4 warps x 16 rows.
+template <int D, int BIG>
+struct Pack4Shape {
+    static constexpr int WARPS = BIG ? 8 : 4;
+    static constexpr int BPW = BIG ? 2 : 1;                // 16-row blocks per warp and tile
+    static constexpr int TN = WARPS * BPW * 16;            // rows per tile
+    static constexpr int STAGES = BIG ? 4 : 6;
+    static constexpr int RB = Pack4Row<D>::RB;
+    static constexpr int TILE = TN * RB;                   // bytes of a K tile and of a V tile
+    static constexpr int QBYTES = 8 * D * 2;               // room for the queries of eight heads
+    static constexpr int STAGE_BYTES = 2 * TILE + QBYTES;
+    static constexpr int CONSUMERS = WARPS * 32;
+    static constexpr int THREADS = CONSUMERS + 64;         // + the producer warp and the hand-over warp
+    static constexpr int SCRATCH_FLOATS = WARPS * 8 * (D + 2);
+    static constexpr int HANDOVER_FLOATS = 8 * (D + 2);
+    static constexpr int SMEM_BYTES = 16 + STAGES * STAGE_BYTES + (SCRATCH_FLOATS + HANDOVER_FLOATS) * 4 + (2 * STAGES + 2) * 8 + 16;
+};
+
+struct Pack4KernelArgs {
+    const char* q;
+    const char* kplane;
+    const char* vplane;
+    float* part_o;
+    float* part_ml;
+    float* out;             // [units][G][D], or nullptr: every piece goes to part_o / part_ml
+    int* flags;             // [units], zero between launches: 1 = the unit's second piece is written
+    int* status;
+    int n, row_stride, tpu, G, units, cap, safe_rows;
+    long long T;
+    float scale_log2;
+    const int* unit_len;
+    const int* n_extra;
+    long long plane_bytes;
+    unsigned long long wait_ns;
+    long long stall_tile;
+    unsigned long long* trace;
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// the next bf16 term of a pair: its value, and what remains of the pair
+__device__ __forceinline__ uint32_t take_term(float& x, float& y) {
+    const uint32_t t = pack2(x, y);
+    x -= bf16_lo(t);
+    y -= bf16_hi(t);
+    return t;
+}
+
+template <int D, int BIG, bool WIDE>      // WIDE: five to eight q-heads per kv-head
+__global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_mma(const Pack4KernelArgs a_in) {
+    using S = Pack4Shape<D, BIG>;
+    constexpr int TN = S::TN, BPW = S::BPW, RB = S::RB, kStages = S::STAGES, kTile = S::TILE, WARPS = S::WARPS;
+    constexpr int KSTEPS = D / 16;        // products of a score block
+    constexpr int NB = D / 8;             // column blocks of the output: D/8 elements per column
+    constexpr int XW = D / 32;            // words of a row's group (K)
+    constexpr int VW = D / 64;            // words of a column's elements (V)
+    Pack4KernelArgs a = a_in;
+    unsigned long long* tr = a.trace ? a.trace + (size_t)blockIdx.x * kTraceSlots : nullptr;
+    if (threadIdx.x == 0) {
+        KVS_TRACE_STAMP(tr, kTrEntry);
+        KVS_TRACE_VALUE(tr, kTrSm, sm_id());
+    }
+    if (a.n_extra != nullptr) {
+        // a replayed launch: the counter is stable here without a wait (see decode_splitk_mma)
+        a.n = min(a.n + *a.n_extra, a.cap);
+        a.tpu = (a.n + TN - 1) / TN;
+        a.T = (long long)a.units * a.tpu;
+    }
+    const int G = a.G;
+    const int qbytes = G * D * 2;
+
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = smem_raw + ((16u - (smem_u32(smem_raw) & 15u)) & 15u);
+    float* scratch = reinterpret_cast<float*>(smem + kStages * S::STAGE_BYTES);
+    uint64_t* full_bar = reinterpret_cast<uint64_t*>(scratch + S::SCRATCH_FLOATS);
+    uint64_t* empty_bar = full_bar + kStages;
+    uint64_t* tail_bar = empty_bar + kStages;
+    uint64_t* head_bar = tail_bar + 1;
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(head_bar + 1);
+    float* handover = const_cast<float*>(reinterpret_cast<volatile float*>(abort_flag + 4));
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int NC = gridDim.x;
+    const long long t0 = ((long long)blockIdx.x * a.T) / NC;
+    const long long t1 = ((long long)(blockIdx.x + 1) * a.T) / NC;
+
+    if (tid == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&full_bar[s], 1);
+            mbar_init(&empty_bar[s], WARPS);
+        }
+        mbar_init(tail_bar, S::CONSUMERS);
+        mbar_init(head_bar, 1);
+        abort_flag[0] = 0;
+        abort_flag[1] = 0;
+        fence_mbar_init();
+    }
+    __syncthreads();
+
+    if (warp == WARPS) {
+        // ------------------------------ producer (one lane) ------------------------------
+        if (lane != 0) return;
+        // The barrier of a stage is armed once with its full byte count; K/V and q may be issued apart.
+        auto issue = [&](long long gt, int st, bool arm, bool kv, bool qpart) {
+            const long long u = gt / a.tpu;
+            const int ti = (int)(gt - u * a.tpu);
+            const bool with_q = (gt == t0) || (ti == 0);
+            const int n_u = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
+            const int rows = min(TN, n_u - ti * TN);          // <= 0: a ragged unit ended before this tile
+            const uint32_t bytes = rows > 0 ? (uint32_t)rows * RB : 0u;
+            unsigned char* sb = smem + st * S::STAGE_BYTES;
+            if (arm) {
+                const uint32_t total = 2 * bytes + (with_q ? qbytes : 0);
+                if (total) mbar_arrive_expect_tx(&full_bar[st], total);
+                else mbar_arrive(&full_bar[st]);
+            }
+            if (kv && bytes && gt != a.stall_tile) {
+                long long off = (u * a.row_stride + (long long)ti * TN) * RB;
+                if (!KVS_BOUNDS_OK(off, bytes, a.plane_bytes, a.status) || !KVS_BOUNDS_OK(u, 1, a.units, a.status)) off = 0;
+                bulk_g2s(sb, a.kplane + off, bytes, &full_bar[st]);
+                bulk_g2s(sb + kTile, a.vplane + off, bytes, &full_bar[st]);
+            }
+            if (qpart && with_q)
+                bulk_g2s(sb + 2 * kTile, a.q + (KVS_BOUNDS_OK(u, 1, a.units, a.status) ? u : 0) * (long long)qbytes, qbytes, &full_bar[st]);
+        };
+        // until the preceding kernel is known to have finished: only tiles made of rows that nothing in flight writes
+        int npre = 0;
+        for (; npre < kStages && t0 + npre < t1; ++npre) {
+            const int ti = (int)((t0 + npre) % a.tpu);
+            if ((long long)(ti + 1) * TN > a.safe_rows) break;
+            issue(t0 + npre, npre, true, true, false);
+        }
+        KVS_TRACE_STAMP(tr, kTrProducerPre);
+        pdl_wait();
+        KVS_TRACE_STAMP(tr, kTrProducerGo);
+        pdl_launch_dependents();
+        for (int j = 0; j < npre; ++j) issue(t0 + j, j, false, false, true);
+        int it = npre;
+        bool ok = true;
+        for (long long gt = t0 + npre; gt < t1; ++gt, ++it) {
+            const int st = it % kStages;
+            if (it >= kStages) ok = mbar_wait_bounded(&empty_bar[st], ((it / kStages) - 1) & 1, abort_flag, a.status, a.wait_ns);
+            if (!ok) break;
+            issue(gt, st, true, true, true);
+        }
+        if (!ok)
+            for (int j = max(0, it - kStages); j < it; ++j)
+                mbar_wait_bounded(&full_bar[j % kStages], (j / kStages) & 1, abort_flag + 1, a.status, a.wait_ns);
+        return;
+    }
+
+    if (warp == WARPS + 1) {
+        // ------------------ hand-over of units that are cut between two blocks (see decode_splitk_mma) ------------------
+        if (a.out == nullptr || t0 >= t1) return;
+        const bool has_tail = (t0 % a.tpu) != 0, has_head = (t1 % a.tpu) != 0;
+        if (!has_tail && !has_head) return;
+        pdl_wait();   // the flags are back to zero only once the previous launch has completed
+        if (has_tail) {
+            if (!mbar_wait_bounded(tail_bar, 0, abort_flag, a.status, a.wait_ns)) return;
+            if (lane == 0) st_release_gpu(a.flags + t0 / a.tpu, 1);
+        }
+        if (has_head) {
+            const long long u = (t1 - 1) / a.tpu;
+            int ok = 1;
+            if (lane == 0) ok = flag_wait_bounded(a.flags + u, 1, abort_flag, a.status, a.wait_ns) ? 1 : 0;
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            __syncwarp();
+            if (!ok) return;
+            const long long pt = u + blockIdx.x + 1;
+            for (int i = lane; i < G * D; i += 32) handover[(i / D) * (D + 2) + (i % D)] = __ldcg(a.part_o + pt * G * D + i);
+            for (int i = lane; i < G * 2; i += 32) handover[(i >> 1) * (D + 2) + D + (i & 1)] = __ldcg(a.part_ml + pt * G * 2 + i);
+            __syncwarp();
+            if (lane == 0) {
+                a.flags[u] = 0;          // this block is the flag's only reader
+                mbar_arrive(head_bar);
+            }
+        }
+        return;
+    }
+
+    // ---------------------------------- consumers ----------------------------------
+    pdl_wait();               // partial results of the previous call may still be read until here
+    if (tid == 0) KVS_TRACE_STAMP(tr, kTrConsumerGo);
+    pdl_launch_dependents();
+    int trace_piece = 0;
+    const int row = lane >> 2, quad = lane & 3;
+    const int head = WIDE ? row : (row & 3);       // the q-head whose scores this lane holds
+    const bool third = !WIDE && row >= 4;          // this lane's rows carry the third term
+
+    int it = 0;
+    long long gt = t0;
+    while (gt < t1) {
+        const long long u = gt / a.tpu;
+        const int ti0 = (int)(gt - u * a.tpu);
+        const int piece_tiles = (int)min((long long)(a.tpu - ti0), t1 - gt);
+        const int n_u = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
+
+        uint32_t qa[KSTEPS][2];
+        float o[NB][2];
+        float m = -1.0e30f, lsum = 0.f;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) o[nb][0] = o[nb][1] = 0.f;
+
+        for (int k = 0; k < piece_tiles; ++k, ++it) {
+            const int st = it % kStages;
+            if (!mbar_wait_bounded(&full_bar[st], (it / kStages) & 1, abort_flag, a.status, a.wait_ns)) return;
+            if (tid == 0 && it == 0) KVS_TRACE_STAMP(tr, kTrFirstTile);
+            unsigned char* ks = smem + st * S::STAGE_BYTES;
+            unsigned char* vs = ks + kTile;
+            if (k == 0) {
+                // step j of lane t: elements e, e + 4 and e + 1, e + 5 of its group, e = 8 (j / 2) + 2 (j % 2)
+                const __nv_bfloat16* qs = reinterpret_cast<const __nv_bfloat16*>(vs + kTile) + head * D + quad * (D / 4);
+#pragma unroll
+                for (int j = 0; j < KSTEPS; ++j)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int e = 8 * (j / 2) + 2 * (j % 2) + x;
+                        uint32_t v = 0;
+                        if (head < G)
+                            v = (uint32_t)__bfloat16_as_ushort(qs[e]) | (uint32_t)__bfloat16_as_ushort(qs[e + 4]) << 16;
+                        qa[j][x] = v;
+                    }
+            }
+            const int valid = n_u - (ti0 + k) * TN;     // rows of this tile that exist (may exceed TN or be <= 0)
+            if (warp * BPW * 16 >= valid) {             // none of this warp's
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty_bar[st]);
+                continue;
+            }
+            // ---- scores ----
+            float s[BPW][2][2];
+            float tmax = -INFINITY;
+#pragma unroll
+            for (int blk = 0; blk < BPW; ++blk) {
+                const int tok0 = (warp * BPW + blk) * 16;
+#pragma unroll
+                for (int nb = 0; nb < 2; ++nb) {
+                    // rows past the end hold whatever the stage held before: their columns are replaced below
+                    const unsigned char* kr = ks + (tok0 + nb * 8 + row) * RB;
+                    const uint32_t pair = *reinterpret_cast<const uint32_t*>(kr + 4 * quad);
+                    const uint32_t s2 = __byte_perm(pair, pair, 0x1010), b2 = __byte_perm(pair, pair, 0x3232);
+                    uint32_t w[XW];
+                    if constexpr (D == 128) {
+                        const uint4 x = *reinterpret_cast<const uint4*>(kr + 16 + 16 * quad);
+                        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+                    } else {
+                        const uint2 x = *reinterpret_cast<const uint2*>(kr + 16 + 8 * quad);
+                        w[0] = x.x, w[1] = x.y;
+                    }
+                    float c[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};     // even and odd steps apart
+#pragma unroll
+                    for (int x = 0; x < XW; ++x) {
+                        mma_bf16(c[0], qa[2 * x][0], 0u, qa[2 * x][1], 0u, fma_bf16x2(pack4_pair<0>(w[x]), s2, b2), fma_bf16x2(pack4_pair<1>(w[x]), s2, b2));
+                        mma_bf16(c[1], qa[2 * x + 1][0], 0u, qa[2 * x + 1][1], 0u, fma_bf16x2(pack4_pair<2>(w[x]), s2, b2), fma_bf16x2(pack4_pair<3>(w[x]), s2, b2));
+                    }
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int tok = tok0 + nb * 8 + quad * 2 + j;
+                        s[blk][nb][j] = tok < valid ? (c[0][j] + c[1][j]) * a.scale_log2 : -INFINITY;
+                        tmax = fmaxf(tmax, s[blk][nb][j]);
+                    }
+                }
+            }
+            // ---- one online-softmax update of the row over the warp's rows of this tile ----
+            tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 1));
+            tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 2));
+            const float m_new = fmaxf(m, tmax);
+            const float alpha = fast_exp2(m - m_new);
+            m = m_new;
+            float psum = 0.f;
+            // A fragments of P: [block][keys 0..7 or 8..15]: rows 0..7 / rows 8..15 (/ the second product's rows 0..7)
+            uint32_t pa[BPW][2], pb[BPW][2], pc[BPW][2];
+#pragma unroll
+            for (int blk = 0; blk < BPW; ++blk)
+#pragma unroll
+                for (int nb = 0; nb < 2; ++nb) {
+                    float p0 = fast_exp2(s[blk][nb][0] - m_new), p1 = fast_exp2(s[blk][nb][1] - m_new);
+                    psum += p0 + p1;
+                    const uint32_t hi = take_term(p0, p1), mid = take_term(p0, p1), lo = pack2(p0, p1);
+                    pa[blk][nb] = third ? lo : hi;
+                    pb[blk][nb] = third ? 0u : mid;
+                    pc[blk][nb] = lo;
+                }
+            lsum = fmaf(lsum, alpha, psum);
+            // ---- O = alpha O + P V ----
+            if (warp * BPW * 16 + BPW * 16 > valid) {
+                // The end of a unit: rows past it may hold anything (0 * NaN is not 0).  With s = b = 0 their values are zero; only
+                // this warp reads them, and the fence orders the stores before the copy that refills the stage.
+                for (int r = warp * BPW * 16 + lane; r < (warp + 1) * BPW * 16; r += 32)
+                    if (r >= valid) *reinterpret_cast<uint4*>(vs + r * RB) = make_uint4(0u, 0u, 0u, 0u);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            uint32_t s2[BPW][2], b2[BPW][2];       // (s, b) of the keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
+#pragma unroll
+            for (int blk = 0; blk < BPW; ++blk)
+#pragma unroll
+                for (int nb = 0; nb < 2; ++nb) {
+                    const unsigned char* vr = vs + ((warp * BPW + blk) * 16 + nb * 8 + quad * 2) * RB + 4 * (row >> 1);
+                    const uint32_t h0 = *reinterpret_cast<const uint32_t*>(vr), h1 = *reinterpret_cast<const uint32_t*>(vr + RB);
+                    s2[blk][nb] = __byte_perm(h0, h1, 0x5410);
+                    b2[blk][nb] = __byte_perm(h0, h1, 0x7632);
+                }
+#pragma unroll
+            for (int x = 0; x < VW; ++x) {
+                uint32_t w[BPW][2][2];             // codes of the two keys, interleaved: [block][key pair][half of the word]
+#pragma unroll
+                for (int blk = 0; blk < BPW; ++blk)
+#pragma unroll
+                    for (int nb = 0; nb < 2; ++nb) {
+                        const unsigned char* vr = vs + ((warp * BPW + blk) * 16 + nb * 8 + quad * 2) * RB + 16 + row * (D / 16) + 4 * x;
+                        const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vr), w1 = *reinterpret_cast<const uint32_t*>(vr + RB);
+                        w[blk][nb][0] = __byte_perm(w0, w1, 0x5410);
+                        w[blk][nb][1] = __byte_perm(w0, w1, 0x7632);
+                    }
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int blk = 0; blk < BPW; ++blk) {
+                            auto pair_of = [&](uint32_t v) { return i == 0 ? pack4_pair<0>(v) : i == 1 ? pack4_pair<1>(v) : i == 2 ? pack4_pair<2>(v) : pack4_pair<3>(v); };
+                            const uint32_t v0 = fma_bf16x2(pair_of(w[blk][0][half]), s2[blk][0], b2[blk][0]);
+                            const uint32_t v1 = fma_bf16x2(pair_of(w[blk][1][half]), s2[blk][1], b2[blk][1]);
+                            mma_bf16(c, pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v0, v1);
+                            if constexpr (WIDE) mma_bf16(c, pc[blk][0], 0u, pc[blk][1], 0u, v0, v1);
+                        }
+                        const int nb = 8 * x + 4 * half + i;
+                        o[nb][0] = fmaf(o[nb][0], alpha, c[0] + c[2]);
+                        o[nb][1] = fmaf(o[nb][1], alpha, c[1] + c[3]);
+                    }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&empty_bar[st]);
+        }
+
+        // ---- end of piece: merge the consumer warps (see decode_splitk_mma for the cases) ----
+        const long long pid = u + blockIdx.x;
+        if (tid == 0 && trace_piece < 8) KVS_TRACE_STAMP(tr, kTrPiece + 2 * trace_piece);
+        const bool finish = a.out != nullptr;
+        const bool whole = finish && ti0 == 0 && piece_tiles == a.tpu;
+        const bool head_piece = finish && ti0 == 0 && piece_tiles < a.tpu;
+        const bool tail = finish && ti0 > 0;
+        float l = lsum;
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        if constexpr (!WIDE)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {       // the third term's share, from rows 4..7
+                o[nb][0] += __shfl_down_sync(0xffffffffu, o[nb][0], 16);
+                o[nb][1] += __shfl_down_sync(0xffffffffu, o[nb][1], 16);
+            }
+        named_bar_sync(1, S::CONSUMERS);
+        if (row < G) {
+            float* dst = scratch + (warp * 8 + row) * (D + 2);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                dst[quad * 2 * NB + nb] = o[nb][0];
+                dst[(quad * 2 + 1) * NB + nb] = o[nb][1];
+            }
+            if (quad == 0) {
+                dst[D] = m;
+                dst[D + 1] = l;
+            }
+        }
+        if (head_piece && !mbar_wait_bounded(head_bar, 0, abort_flag, a.status, a.wait_ns)) return;
+        named_bar_sync(1, S::CONSUMERS);
+        for (int idx = tid; idx < G * D; idx += S::CONSUMERS) {
+            const int g = idx / D, d = idx - g * D;
+            const float* src = scratch + g * (D + 2);
+            constexpr int WS = 8 * (D + 2);
+            float M = -1.0e30f;
+#pragma unroll
+            for (int j = 0; j < WARPS; ++j) M = fmaxf(M, src[j * WS + D]);
+            float acc = 0.f, den = 0.f;
+#pragma unroll
+            for (int j = 0; j < WARPS; ++j) {
+                const float w = fast_exp2(src[j * WS + D] - M);
+                acc = fmaf(w, src[j * WS + d], acc);
+                den = fmaf(w, src[j * WS + D + 1], den);
+            }
+            if (whole) {
+                a.out[(u * G + g) * D + d] = acc / den;
+            } else if (head_piece) {
+                const float* hv = handover + g * (D + 2);      // the unit's second piece
+                const float Mx = fmaxf(M, hv[D]);
+                const float w0 = fast_exp2(M - Mx), w1 = fast_exp2(hv[D] - Mx);
+                a.out[(u * G + g) * D + d] = fmaf(w1, hv[d], w0 * acc) / fmaf(w1, hv[D + 1], w0 * den);
+            } else if (KVS_BOUNDS_OK(pid, 1, a.units + (long long)gridDim.x, a.status)) {
+                a.part_o[(pid * G + g) * D + d] = acc;
+                if (d == 0) {
+                    a.part_ml[(pid * G + g) * 2] = M;
+                    a.part_ml[(pid * G + g) * 2 + 1] = den;
+                }
+            }
+        }
+        if (tail) mbar_arrive(tail_bar);   // this thread's part of the piece is written
+        if (tid == 0 && trace_piece < 8) KVS_TRACE_STAMP(tr, kTrPiece + 2 * trace_piece + 1);
+        ++trace_piece;
+        gt += piece_tiles;
+    }
+    if (tid == 0) {
+        KVS_TRACE_STAMP(tr, kTrEnd);
+        KVS_TRACE_VALUE(tr, kTrPieces, trace_piece);
+    }
+}
+
+template <int D, int BIG, bool WIDE>
+cudaError_t set_attr() {
+    cudaError_t e = cudaFuncSetAttribute(decode_pack4_mma<D, BIG, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pack4Shape<D, BIG>::SMEM_BYTES);
+    if (e != cudaSuccess) return e;
+    // room for the combine kernel's blocks beside this kernel's (see decode_splitk_mma)
+    return cudaFuncSetAttribute(decode_pack4_mma<D, BIG, WIDE>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+}
+
+template <int D, int BIG>
+cudaError_t launch_one(const Pack4KernelArgs& ka, int NC, bool pdl, cudaStream_t stream) {
+    using S = Pack4Shape<D, BIG>;
+    return ka.G > 4 ? launch_kernel(decode_pack4_mma<D, BIG, true>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, pdl, ka)
+                    : launch_kernel(decode_pack4_mma<D, BIG, false>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, pdl, ka);
+}
+
+}  // namespace
+
+cudaError_t init_pack4_kernels() {
+    cudaError_t e;
+    if ((e = set_attr<128, 0, false>()) != cudaSuccess || (e = set_attr<128, 0, true>()) != cudaSuccess ||
+        (e = set_attr<128, 1, false>()) != cudaSuccess || (e = set_attr<128, 1, true>()) != cudaSuccess ||
+        (e = set_attr<64, 0, false>()) != cudaSuccess || (e = set_attr<64, 0, true>()) != cudaSuccess ||
+        (e = set_attr<64, 1, false>()) != cudaSuccess)
+        return e;
+    return set_attr<64, 1, true>();
+}
+
+void plan_decode_pack4(int units, int n, int D, int sm_count, int max_ctas, DecodePlan* plan) {
+    int cap = sm_count;
+    if (max_ctas > 0) cap = std::min(cap, max_ctas);
+    cap = std::min(cap, kMaxCtas);
+    // the large tiles when every block gets at least four of them
+    const int big_rows = Pack4Shape<128, 1>::TN;
+    const long long big_T = (long long)units * ((n + big_rows - 1) / big_rows);
+    plan->tile_rows = big_T >= 4ll * cap ? big_rows : Pack4Shape<128, 0>::TN;
+    plan->tpu = (n + plan->tile_rows - 1) / plan->tile_rows;
+    plan->T = (long long)units * plan->tpu;
+    plan->NC = (int)std::min<long long>(plan->T, cap);
+    plan->kernel = 3;
+}
+
+cudaError_t launch_decode_pack4(const DecodeArgs& a, const DecodePlan& plan, cudaStream_t stream) {
+    if (a.G < 1 || a.G > 8 || (a.D != 64 && a.D != 128)) return cudaErrorInvalidValue;
+    Pack4KernelArgs ka;
+    ka.q = static_cast<const char*>(a.q);
+    ka.kplane = static_cast<const char*>(a.kplane);
+    ka.vplane = static_cast<const char*>(a.vplane);
+    ka.part_o = a.part_o;
+    ka.part_ml = a.part_ml;
+    ka.out = a.finish_in_kernel ? a.out : nullptr;
+    ka.flags = a.flags;
+    ka.status = a.status;
+    ka.n = a.n;
+    ka.row_stride = a.row_stride;
+    ka.tpu = plan.tpu;
+    ka.G = a.G;
+    ka.units = a.units;
+    ka.cap = a.capacity;
+    ka.safe_rows = (a.programmatic && !a.unit_len) ? a.safe_rows : 0;
+    ka.T = plan.T;
+    ka.scale_log2 = a.scale_log2;
+    ka.unit_len = a.unit_len;
+    ka.n_extra = a.n_extra;
+    ka.plane_bytes = a.plane_bytes;
+    ka.wait_ns = a.wait_ns;
+    ka.stall_tile = a.stall_tile;
+    ka.trace = a.trace;
+    const bool big = plan.tile_rows == Pack4Shape<128, 1>::TN;
+    if (a.D == 128) return big ? launch_one<128, 1>(ka, plan.NC, a.programmatic, stream) : launch_one<128, 0>(ka, plan.NC, a.programmatic, stream);
+    return big ? launch_one<64, 1>(ka, plan.NC, a.programmatic, stream) : launch_one<64, 0>(ka, plan.NC, a.programmatic, stream);
+}
+
+}  // namespace kvs
