@@ -155,7 +155,7 @@ kvs_status kvs_set_share_map(kvs_ctx* ctx, const int32_t* share_map);
  *
  * A 4-bit cache (nothing in the paper: it multiplies with the memory that sharing layers saves) cuts a row of D elements into
  * four groups of D/4.  With lo, hi the group's smallest and largest element, in fp32:
- *     s = (hi - lo) / 15 rounded up to bf16,   b = lo - 16 s rounded to bf16,
+ *     s = (hi - lo) * (1/15) rounded up to bf16 (1/15: the nearest fp32),   b = lo - 16 s rounded to bf16,
  *     code c = clamp(rint((x - b) / s) - 16, 0, 15)  (ties to even; s = 0: c = 0),   value = s * (16 + c) + b
  * and the value, rounded once to the storage type, is what the cache holds of x: it differs from x by at most s/2, the
  * rounding of b (2^-8 |b|) and its own.  A group with an infinity or a NaN in it, or whose s or b overflows, has only NaN values

@@ -14,6 +14,9 @@ from .binding import (  # noqa: F401
 __all__ = ["binding", "SharedKVCache", "Rotary", "KvsError"]
 
 
+_unfinished = []        # caches closed while a graph was being recorded: (context, device, memory)
+
+
 class Rotary:
     """Rotary positions for ``append_rotary``: radians per position of every pair (``rotary_dim / 2`` numbers).
 
@@ -82,9 +85,18 @@ class SharedKVCache:
         return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
 
     def close(self):
+        while _unfinished and not self._torch.cuda.is_current_stream_capturing():
+            ctx, device, _ = _unfinished.pop()
+            self._torch.cuda.synchronize(device)
+            binding.kvs_destroy(ctx)
         if getattr(self, "ctx", None):
-            self._torch.cuda.synchronize(self.device)
-            binding.kvs_destroy(self.ctx)
+            if self._torch.cuda.is_current_stream_capturing():
+                # Python may collect a cache at any time, so also while a graph is being recorded, which waiting for the
+                # device would end: its memory is kept until the next cache is closed
+                _unfinished.append((self.ctx, self.device, (self.pool, self.workspace)))
+            else:
+                self._torch.cuda.synchronize(self.device)
+                binding.kvs_destroy(self.ctx)
             self.ctx = None
             self.pool = self.workspace = self._planes = None
 

@@ -59,7 +59,7 @@ __device__ __forceinline__ void pack_eight(const float (&x)[8], uint32_t* pair, 
         lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
         hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, d));
     }
-    const float step = __fdiv_rn(__fsub_rn(hi, lo), 15.f);
+    const float step = __fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f);
     const float s = __uint_as_float((__float_as_uint(step) + 0xffffu) & 0xffff0000u);
     const float b = __bfloat162float(__float2bfloat16_rn(__fsub_rn(lo, 16.f * s)));
     if (!(finite(step) && finite(s) && finite(b))) {

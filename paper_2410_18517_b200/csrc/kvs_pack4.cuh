@@ -1,7 +1,7 @@
 // The row of a 4-bit cache, shared by the kernels that write, read and attend over it.
 //
 // A row of D elements is cut into four groups of D/4.  With lo and hi the group's smallest and largest element (fp32):
-//   s = (hi - lo) / 15 rounded up to bf16,  b = lo - 16 s rounded to bf16
+//   s = (hi - lo) * (1/15) rounded up to bf16,  b = lo - 16 s rounded to bf16
 //   code c = clamp(rint((x - b) / s) - 16, 0, 15),  value = s * (16 + c) + b rounded once to the storage type
 // Why 16 + c and not c: four bits laid at bits 3..6 of a bf16 whose upper bits are those of 16.0 ARE the number 16 + c, so
 // one OR makes a factor of the code and one fused multiply-add the value.  Why s is rounded up: the largest element then has

@@ -20,7 +20,7 @@ def pack(x):
     broken = ~torch.isfinite(g).all(-1, keepdim=True)
     clean = torch.where(broken, 0.0, g)
     lo, hi = clean.amin(-1, keepdim=True), clean.amax(-1, keepdim=True)
-    step = (hi - lo) / 15
+    step = (hi - lo) * torch.tensor(1 / 15)          # both fp32
     s = up_to_bf16(step)
     b = (lo - 16 * s).bfloat16().float()
     broken |= ~(torch.isfinite(step) & torch.isfinite(s) & torch.isfinite(b))
