@@ -10,15 +10,16 @@ namespace kvs {
 namespace {
 
 // --------------------------------------------------------------------------------------
-// Selection.  score(b, v) = scores[b] - lse_b + x_bv,  lse_b = log sum_v exp x_bv;  of a request's W beams x V tokens the K
+// Selection.  score(b, v) = scores[b] + x_bv - lse_b,  lse_b = log sum_v exp x_bv;  of a request's W beams x V tokens the K
 // best, equal scores by the lowest (beam, token).
 //
 // First kernel: every logits row is cut into segments, a block each (one pass over the logits): running maximum and sum of
-// its exponentials per thread, and the segment's K best, by a threshold.  Logits become 64-bit keys (order of the value, then
-// the lower index), all different.  The K-th largest of the threads' own maxima bounds the K-th best from below, and exactly
-// K threads reach it: at most K times a thread's share passes, however the logits are ordered and however many are equal.
+// exponentials per thread, and the segment's K best, by a threshold: the K-th largest of the threads' own maxima in the first
+// turn.  K elements at least reach it and hardly more do, so that a logit costs a maximum, an exponential, a sum and a
+// comparison.  Where too many reach it (equal logits, rising ones) the candidates become 64-bit keys - order of the value, then
+// the lower index, all different - and the threads' maxima of those bound them: exactly K threads reach the K-th largest.
 // Second kernel, a block per request: lse in fp64 (a rounding of 1e-7 would decide between beams whose scores nearly tie), the
-// segments' lists by the same threshold, and the K best in order.
+// lists by the K-th largest of their heads, and the K best in order.
 // Bound: HBM for the logits, once; small calls: two launches.
 // --------------------------------------------------------------------------------------
 constexpr int kBeamThreads = 256;
@@ -31,17 +32,16 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xffffffffu)); }
-
-// exp(t), t <= 0 or NaN, to fp32 accuracy: the rounding of t * log2(e) goes back in as a factor
-__device__ __forceinline__ float exp_of(float t) {
-    constexpr float L = 1.44269504f, L2 = 1.92596303e-8f;     // log2(e) in two parts
-    const float y = t * L;
-    const float r = fmaf(t, L2, fmaf(t, L, -y));
-    const float e = fast_exp2(y);
-    return t < -200.f ? 0.f : fmaf(e, r * 0.693147181f, e);     // (far below, t * log2(e) overflows)
+__device__ __forceinline__ uint64_t order_of(double x) {
+    const uint64_t u = __double_as_longlong(x + 0.0);
+    return u ^ (u >> 63 ? 0xffffffffffffffffull : 0x8000000000000000ull);
 }
+__device__ __forceinline__ double value_of(uint64_t o) { return __longlong_as_double(o ^ (o >> 63 ? 0x8000000000000000ull : 0xffffffffffffffffull)); }
 
-// 64-bit keys by value, then by the lower index: the second kernel's key needs more bits than one word
+// exp(t), t <= 0 (or NaN): the product's rounding costs 2^-24 |t| of it, next to nothing where a term counts
+__device__ __forceinline__ float exp_below(float t) { return fast_exp2(t * 1.44269504f); }
+
+// The second kernel's keys need more bits than one word: by score, then by the lower index
 struct Wide {
     uint64_t v;      // order of the fp64 score
     uint32_t i;      // ~(flat index)
@@ -49,46 +49,66 @@ struct Wide {
 __device__ __forceinline__ bool above(uint64_t a, uint64_t b) { return a > b; }
 __device__ __forceinline__ bool above(const Wide& a, const Wide& b) { return a.v > b.v || (a.v == b.v && a.i > b.i); }
 
+// The K-th largest of `n` numbers s_x[0 .. n-1] (n a multiple of four, at least 4), of which thread t < n holds `mine`, as
+// order_of: into *cut, which is to hold the highest order before.  n < K: minus infinity.  Ends with a barrier.
+__device__ __forceinline__ void kth_of(const float* s_x, int n, float mine, int K, uint32_t* cut) {
+    if ((int)threadIdx.x < n) {
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; j += 4) {
+            const float4 x = *reinterpret_cast<const float4*>(s_x + j);
+            rank += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
+        }
+        if (rank < K) atomicMin(cut, order_of(n < K ? -INFINITY : mine));
+    }
+    __syncthreads();
+}
+
 // The K-th largest of all threads' keys into *cut, for every thread (keys that differ, except `lowest`, which nothing is
 // below).  `keys`: a shared array of a key per thread.
 template <typename Key>
-__device__ __forceinline__ void kth_of_threads(const Key& mine, int K, const Key& lowest, Key* keys, Key* cut) {
+__device__ __noinline__ void kth_of_threads(Key mine, int K, Key lowest, Key* keys, Key* cut) {
     keys[threadIdx.x] = mine;
     __syncthreads();
     int rank = 0;
-#pragma unroll 16
+#pragma unroll 4
     for (int j = 0; j < kBeamThreads; ++j) rank += above(keys[j], mine) ? 1 : 0;
     if (rank == K - 1 || (rank < K - 1 && !above(mine, lowest))) *cut = mine;        // (several lowest keys: the same value)
     __syncthreads();
 }
 
-// Of the `count` keys in `list` the K best, in order, to put(rank, key); `lowest` is a key nothing is below.
+// Keeps of the `n` keys in `list` (at most kBeamRoom) those that reach the K-th largest of the threads' best: at most
+// K * kBeamRoom / 256, the K best among them.  *count receives how many; returns the threshold.
+template <typename Key>
+__device__ __noinline__ Key prune(Key* list, int n, int* count, int K, Key lowest, Key* keys, Key* cut) {
+    constexpr int MOST = kBeamRoom / kBeamThreads;
+    Key mine[MOST], top = lowest;
+#pragma unroll
+    for (int j = 0; j < MOST; ++j) {
+        const int at = threadIdx.x + j * kBeamThreads;
+        mine[j] = at < n ? list[at] : lowest;
+        if (above(mine[j], top)) top = mine[j];
+    }
+    kth_of_threads(top, K, lowest, keys, cut);
+    const Key c = *cut;
+    if (threadIdx.x == 0) *count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < MOST; ++j)
+        if (above(mine[j], lowest) && !above(c, mine[j])) list[atomicAdd(count, 1)] = mine[j];
+    __syncthreads();
+    return c;
+}
+
+// Of the *count keys in `list` the K best, in order, to put(rank, key).
 template <typename Key, typename Put>
-__device__ __forceinline__ void best_in_order(Key* list, int* count, int K, const Key& lowest, Key* keys, Key* cut, Put put) {
-    while (*count > kBeamThreads) {
-        const int n = *count;
-        constexpr int MOST = (kBeamRoom + kBeamThreads - 1) / kBeamThreads;
-        Key mine[MOST], top = lowest;
-        int have = 0;
-#pragma unroll
-        for (int j = 0; j < MOST; ++j) {
-            const int at = threadIdx.x + j * kBeamThreads;
-            if (at < n) {
-                mine[j] = list[at];
-                if (above(mine[j], top)) top = mine[j];
-                have = j + 1;
-            }
-        }
-        kth_of_threads(top, K, lowest, keys, cut);
-        const Key c = *cut;
-        if (threadIdx.x == 0) *count = 0;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < MOST; ++j)
-            if (j < have && !above(c, mine[j])) list[atomicAdd(count, 1)] = mine[j];
+__device__ __forceinline__ void best_in_order(Key* list, int* count, int K, Key lowest, Key* keys, Key* cut, Put put) {
+    int n = *count;
+    while (n > kBeamThreads) {
+        prune(list, n, count, K, lowest, keys, cut);
+        n = *count;
         __syncthreads();
     }
-    const int n = *count;
     if ((int)threadIdx.x < n) {
         const Key mine = list[threadIdx.x];
         int rank = 0;
@@ -117,34 +137,38 @@ template <typename T>
 __global__ void __launch_bounds__(kBeamThreads) beam_segments_kernel(const BeamKernelArgs a) {
     __shared__ uint64_t s_list[kBeamRoom];
     __shared__ uint64_t s_keys[kBeamThreads];
-    __shared__ uint64_t s_cut;
+    __shared__ __align__(16) float s_max[kBeamThreads];
+    __shared__ uint64_t s_kth;
+    __shared__ uint32_t s_cut;
     __shared__ int s_count, s_more[2];       // kept; candidates of a turn, of even and odd turns
     __shared__ float2 s_sum[kBeamThreads / 32];
+    const int seg = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+    if (tid == 0) {
+        s_count = s_more[0] = s_more[1] = 0;
+        s_cut = 0xffffffffu;
+    }
     pdl_launch_dependents();
     pdl_wait();
-    const int seg = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
     const int v0 = seg * a.seg_len, v1 = min(a.vocab, v0 + a.seg_len);
     const T* x_row = static_cast<const T*>(a.logits) + row * a.stride;
     const uint64_t none = (uint64_t)order_of(-INFINITY) << 32 | 0xffffffffu;     // minus infinity is no candidate
     constexpr int PER16 = 16 / (int)sizeof(T);       // logits per 16-byte load
-    uint64_t cut = none;
+    float cut = -INFINITY;
     float m = -INFINITY, sum = 0.f;
-    if (tid == 0) s_count = s_more[0] = s_more[1] = 0;
+    // thread t takes runs of 16 bytes, t, t + 256, ...: the same elements whether they can be loaded as vectors or not
+    auto index = [&](int base, int i) { return base + (i / PER16 * kBeamThreads + tid) * PER16 + i % PER16; };
+    auto key = [&](float x, int v) { return (uint64_t)order_of(x) << 32 | (uint32_t)~v; };
     __syncthreads();
     int turn = 0;
     for (int base = v0; base < v1; base += kBeamTurn, turn ^= 1) {
         const int count = s_count;       // (nobody adds before the next barrier)
-        // thread t takes runs of 16 bytes, t, t + 256, ...: the same elements whether they can be loaded as vectors or not
         float x[kBeamPer];
-        int idx[kBeamPer / PER16];
 #pragma unroll
         for (int j = 0; j < kBeamPer / PER16; ++j) {
-            const int v = base + (j * kBeamThreads + tid) * PER16;
-            idx[j] = v;
+            const int v = index(base, j * PER16);
             if (a.vec && v + PER16 <= v1) {
-                const uint4 r = __ldcs(reinterpret_cast<const uint4*>(x_row + v));
                 float f[PER16];
-                Unpack<T>::run(r, f);
+                Unpack<T>::run(__ldcs(reinterpret_cast<const uint4*>(x_row + v)), f);
 #pragma unroll
                 for (int i = 0; i < PER16; ++i) x[j * PER16 + i] = f[i];
             } else {
@@ -152,62 +176,58 @@ __global__ void __launch_bounds__(kBeamThreads) beam_segments_kernel(const BeamK
                 for (int i = 0; i < PER16; ++i) x[j * PER16 + i] = v + i < v1 ? (float)x_row[v + i] : -INFINITY;
             }
         }
-        float top = m;
+        float best = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < kBeamPer; ++i) top = fmaxf(top, x[i]);
-        const float ref = top == -INFINITY ? 0.f : top;
-        sum *= exp_of(m - ref);          // a NaN stays one, and makes the row's sum NaN
+        for (int i = 0; i < kBeamPer; ++i) best = fmaxf(best, x[i]);
+        const float top = fmaxf(m, best), ref = top == -INFINITY ? 0.f : top;
+        sum *= exp_below(m - ref);       // a NaN stays one, and makes the row's sum NaN
 #pragma unroll
-        for (int i = 0; i < kBeamPer; ++i) sum += exp_of(x[i] - ref);
+        for (int i = 0; i < kBeamPer; ++i) sum += exp_below(x[i] - ref);
         m = top;
-        // candidates: keys above the threshold
-        auto key = [&](int i) { return (uint64_t)order_of(x[i]) << 32 | (uint32_t)~(idx[i / PER16] + i % PER16); };
-        if (base == v0) {
-            uint64_t best = none;
-#pragma unroll
-            for (int i = 0; i < kBeamPer; ++i) best = max(best, key(i));
-            kth_of_threads(best, a.K, none, s_keys, &s_cut);
-            cut = s_cut;
-        }
         int mine = 0;
+        if (base == v0) {
+            // for few continuations the maxima of four threads each are enough of them
+            const bool quads = a.K <= 16;
+            float most = best;
+            if (quads) {
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            }
+            if (!quads || tid % 4 == 0) s_max[quads ? tid / 4 : tid] = most;
+            __syncthreads();
+            kth_of(s_max, quads ? kBeamThreads / 4 : kBeamThreads, s_max[quads ? tid % (kBeamThreads / 4) : tid], a.K, &s_cut);
+            cut = value_of(s_cut);
+            if (best >= cut)
 #pragma unroll
-        for (int i = 0; i < kBeamPer; ++i) mine += key(i) >= cut && key(i) > none ? 1 : 0;
+                for (int i = 0; i < kBeamPer; ++i) mine += x[i] >= cut && x[i] > -INFINITY ? 1 : 0;
+        } else if (best > cut) {         // (an equal one comes after K others)
+#pragma unroll
+            for (int i = 0; i < kBeamPer; ++i) mine += x[i] > cut ? 1 : 0;
+        }
         if (mine) atomicAdd(&s_more[turn], mine);
         __syncthreads();
         const int more = s_more[turn];
         if (tid == 0) s_more[turn ^ 1] = 0;
-        if (more) {
-            if (count + more > kBeamRoom) {
-                // too many: this turn's own threshold, and that of what has been kept
-                uint64_t best = none;
+        if (count + more <= kBeamRoom) {
+            if (mine)
 #pragma unroll
-                for (int i = 0; i < kBeamPer; ++i) best = max(best, key(i));
-                kth_of_threads(best, a.K, none, s_keys, &s_cut);
-                cut = max(cut, s_cut);
-                __syncthreads();
-                uint64_t kept[kBeamRoom / kBeamThreads];
-                best = none;
+                for (int i = 0; i < kBeamPer; ++i)
+                    if ((base == v0 ? x[i] >= cut : x[i] > cut) && x[i] > -INFINITY) s_list[atomicAdd(&s_count, 1)] = key(x[i], index(base, i));
+        } else {
+            // too many: the threads' best keys of this turn, and those of what has been kept, as thresholds
+            uint64_t first = none;
 #pragma unroll
-                for (int j = 0; j < kBeamRoom / kBeamThreads; ++j) {
-                    const int at = tid + j * kBeamThreads;
-                    kept[j] = at < count ? s_list[at] : none;
-                    best = max(best, kept[j]);
-                }
-                kth_of_threads(best, a.K, none, s_keys, &s_cut);
-                cut = max(cut, s_cut);
-                if (tid == 0) s_count = 0;
-                __syncthreads();
+            for (int i = 0; i < kBeamPer; ++i) first = max(first, key(x[i], index(base, i)));
+            kth_of_threads(first, a.K, none, s_keys, &s_kth);
+            uint64_t least = s_kth;
+            __syncthreads();
+            least = max(least, prune(s_list, count, &s_count, a.K, none, s_keys, &s_kth));
 #pragma unroll
-                for (int j = 0; j < kBeamRoom / kBeamThreads; ++j)
-                    if (kept[j] >= cut && kept[j] > none) s_list[atomicAdd(&s_count, 1)] = kept[j];
-                __syncthreads();
+            for (int i = 0; i < kBeamPer; ++i) {
+                const uint64_t k = key(x[i], index(base, i));
+                if (k >= least && k > none) s_list[atomicAdd(&s_count, 1)] = k;
             }
-#pragma unroll
-            for (int i = 0; i < kBeamPer; ++i)
-                if (key(i) >= cut && key(i) > none) {
-                    const int at = atomicAdd(&s_count, 1);
-                    if (at < kBeamRoom) s_list[at] = key(i);
-                }
+            cut = fmaxf(cut, value_of((uint32_t)(least >> 32)));
         }
         __syncthreads();
     }
@@ -216,7 +236,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_segments_kernel(const BeamK
     for (int d = 16; d; d >>= 1) {
         const float m2 = __shfl_xor_sync(0xffffffffu, m, d), sum2 = __shfl_xor_sync(0xffffffffu, sum, d);
         const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-        const float lo = m <= m2 ? sum * exp_of(m - ref) : sum2 * exp_of(m2 - ref), hi = m <= m2 ? sum2 : sum;
+        const float lo = m <= m2 ? sum * exp_below(m - ref) : sum2 * exp_below(m2 - ref), hi = m <= m2 ? sum2 : sum;
         sum = m == m2 ? sum + sum2 : hi + lo;
         m = top;
     }
@@ -226,35 +246,41 @@ __global__ void __launch_bounds__(kBeamThreads) beam_segments_kernel(const BeamK
     if (tid == 0 && KVS_BOUNDS_OK(at, 1, a.sum_count, a.status)) {
         float top = -INFINITY, total = 0.f;
         for (int w = 0; w < kBeamThreads / 32; ++w) top = fmaxf(top, s_sum[w].x);
-        for (int w = 0; w < kBeamThreads / 32; ++w)
-            total += s_sum[w].x == top ? s_sum[w].y : s_sum[w].y * exp_of(s_sum[w].x - top);
+        for (int w = 0; w < kBeamThreads / 32; ++w) total += s_sum[w].x == top ? s_sum[w].y : s_sum[w].y * exp_below(s_sum[w].x - top);
         a.sums[at] = make_float2(top, total);
     }
     uint64_t* out = a.lists + at * a.K;
     const bool room = KVS_BOUNDS_OK(at * a.K, a.K, a.list_count, a.status);
-    best_in_order(s_list, &s_count, a.K, none, s_keys, &s_cut, [&](int rank, uint64_t k) {
+    best_in_order(s_list, &s_count, a.K, none, s_keys, &s_kth, [&](int rank, uint64_t k) {
         if (room) out[rank] = k;
     });
     if (room && tid < a.K && tid >= s_count) out[tid] = 0;
 }
 
-__device__ __forceinline__ uint64_t order_of(double x) {
-    const uint64_t u = __double_as_longlong(x + 0.0);
-    return u ^ (u >> 63 ? 0xffffffffffffffffull : 0x8000000000000000ull);
-}
-__device__ __forceinline__ double value_of(uint64_t o) { return __longlong_as_double(o ^ (o >> 63 ? 0x8000000000000000ull : 0xffffffffffffffffull)); }
-
 __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKernelArgs a) {
     __shared__ Wide s_list[kBeamRoom];
     __shared__ Wide s_keys[kBeamThreads];
-    __shared__ Wide s_cut;
+    __shared__ __align__(16) float s_head[kBeamThreads];
+    __shared__ Wide s_kth;
     __shared__ double s_base[kBeamMaxBeams];      // scores[b] - log of the sum below the row's maximum
     __shared__ float s_top[kBeamMaxBeams];
+    __shared__ uint32_t s_cut;
     __shared__ int s_count;
-    pdl_launch_dependents();
-    pdl_wait();
     const int req = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long row0 = (long long)req * a.W;
+    const int lists = a.W * a.segs, entries = lists * a.K;
+    if (tid == 0) {
+        s_cut = 0xffffffffu;
+        s_count = 0;
+    }
+    pdl_launch_dependents();
+    pdl_wait();
+    const uint64_t* list = a.lists + row0 * a.segs * a.K;
+    constexpr int AHEAD = 8;                      // entries a thread has in flight
+    uint64_t ahead[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) ahead[j] = tid + j * kBeamThreads < entries ? __ldcg(list + tid + j * kBeamThreads) : 0;
+    const uint64_t head = tid < lists ? __ldcg(list + tid * a.K) : 0;
     for (int b = warp; b < a.W; b += kBeamThreads / 32) {
         const float2* sums = a.sums + (row0 + b) * a.segs;
         float top = -INFINITY;
@@ -274,56 +300,62 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
             s_top[b] = top;
         }
     }
-    if (tid == 0) s_count = 0;
     __syncthreads();
-    // a thread per list (best first): its head bounds it
     const Wide lowest = {order_of(-(double)INFINITY), 0u};      // scores of minus infinity and NaN are no candidates
-    const int lists = a.W * a.segs, beam = tid / a.segs;
-    const uint64_t* list = a.lists + (row0 * a.segs + tid) * a.K;
-    auto candidate = [&](uint64_t k) {
+    auto candidate = [&](uint64_t k, int beam) {
         Wide w = lowest;
         if (k) {
             const double score = s_base[beam] + ((double)value_of((uint32_t)(k >> 32)) - (double)s_top[beam]);
-            const uint32_t flat = (uint32_t)beam * (uint32_t)a.vocab + ~(uint32_t)k;
-            if (score > -(double)INFINITY) w = {order_of(score), ~flat};
+            if (score > -(double)INFINITY) w = {order_of(score), ~((uint32_t)beam * (uint32_t)a.vocab + ~(uint32_t)k)};
         }
         return w;
     };
-    const Wide head = tid < lists ? candidate(__ldcg(list)) : lowest;
-    kth_of_threads(head, a.K, lowest, s_keys, &s_cut);
-    Wide cut = s_cut;
-    int held = 0;       // what the list holds, the same in every thread
-    for (int j = 0; j < a.K; ++j) {
-        const Wide w = j == 0 ? head : tid < lists ? candidate(__ldcg(list + j)) : lowest;
-        const bool in = above(w, lowest) && !above(cut, w);
-        if (in) s_list[atomicAdd(&s_count, 1)] = w;
-        // after every step of all lists: room for another, or a new threshold first
-        const int added = __syncthreads_count(in);
-        if (added == 0) break;
-        held += added;
-        if (held > kBeamRoom - kBeamThreads) {
-            constexpr int MOST = kBeamRoom / kBeamThreads;
-            Wide mine[MOST], top = lowest;
+    // the K-th largest head, in fp32 (whose rounding keeps the order): what is below it is not among the K best
+    const int heads = (lists + 3) / 4 * 4;
+    const float mine = tid < lists ? (float)value_of(candidate(head, tid / a.segs).v) : -INFINITY;
+    if (tid < heads) s_head[tid] = mine;
+    __syncthreads();
+    kth_of(s_head, heads, mine, a.K, &s_cut);
+    const float cut = value_of(s_cut);
+    const int per = a.segs * a.K;                 // entries of a beam
+    auto reaches = [&](const Wide& w) { return above(w, lowest) && (float)value_of(w.v) >= cut; };
+    for (int j = 0, e = tid; e < entries; ++j, e += kBeamThreads) {
+        uint64_t k = 0;
+        if (j < AHEAD) {
 #pragma unroll
-            for (int i = 0; i < MOST; ++i) {
-                mine[i] = tid + i * kBeamThreads < held ? s_list[tid + i * kBeamThreads] : lowest;
-                if (above(mine[i], top)) top = mine[i];
-            }
-            kth_of_threads(top, a.K, lowest, s_keys, &s_cut);
-            if (above(s_cut, cut)) cut = s_cut;
-            if (tid == 0) s_count = 0;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < MOST; ++i)
-                if (above(mine[i], lowest) && !above(cut, mine[i])) s_list[atomicAdd(&s_count, 1)] = mine[i];
-            __syncthreads();
-            held = s_count;
-            __syncthreads();
+            for (int i = 0; i < AHEAD; ++i)
+                if (i == j) k = ahead[i];
+        } else {
+            k = __ldcg(list + e);
+        }
+        const Wide w = candidate(k, e / per);
+        if (reaches(w)) {
+            const int at = atomicAdd(&s_count, 1);
+            if (at < kBeamRoom) s_list[at] = w;
         }
     }
     __syncthreads();
+    if (s_count > kBeamRoom) {
+        // more than there is room for (many equal scores): a row of entries of all threads at a time, keeping the best so far
+        __syncthreads();
+        if (tid == 0) s_count = 0;
+        __syncthreads();
+        int held = 0;
+        Wide least = lowest;
+        for (int e0 = 0; e0 < entries; e0 += kBeamThreads) {
+            const Wide w = e0 + tid < entries ? candidate(__ldcg(list + e0 + tid), (e0 + tid) / per) : lowest;
+            const bool in = reaches(w) && !above(least, w);
+            if (in) s_list[atomicAdd(&s_count, 1)] = w;
+            held += __syncthreads_count(in);
+            if (held > kBeamRoom - kBeamThreads) {
+                least = prune(s_list, held, &s_count, a.K, lowest, s_keys, &s_kth);
+                held = s_count;
+                __syncthreads();
+            }
+        }
+    }
     const long long o = (long long)req * a.K;
-    best_in_order(s_list, &s_count, a.K, lowest, s_keys, &s_cut, [&](int rank, const Wide& w) {
+    best_in_order(s_list, &s_count, a.K, lowest, s_keys, &s_kth, [&](int rank, const Wide& w) {
         const uint32_t flat = ~w.i;
         a.out_scores[o + rank] = (float)value_of(w.v);
         a.out_tokens[o + rank] = (int)(flat % (uint32_t)a.vocab);
@@ -451,10 +483,10 @@ cudaError_t launch_beam_select(const BeamArgs& p, cudaStream_t stream) {
     a.stride = p.stride;
     a.vocab = p.vocab;
     a.rows = p.requests * p.beams;
-    // Segments: enough blocks for eight on every SM, but none shorter than a turn of a block and at most 256 lists (a thread
-    // each in the second kernel) per request, and room for the lists.
-    const long long want = ((long long)p.sm_count * 8 + a.rows - 1) / a.rows;
-    const long long most = std::min<long long>({(p.vocab + kBeamTurn - 1) / kBeamTurn, kBeamThreads / p.beams, std::max(1, kBeamMaxLists / a.rows)});
+    // Segments: enough blocks for four on every SM, but none shorter than a quarter turn of a block and at most 256 lists (a
+    // thread each in the second kernel) per request, and room for the lists.
+    const long long want = ((long long)p.sm_count * 4 + a.rows - 1) / a.rows;
+    const long long most = std::min<long long>({(p.vocab + kBeamTurn / 4 - 1) / (kBeamTurn / 4), kBeamThreads / p.beams, std::max(1, kBeamMaxLists / a.rows)});
     a.segs = (int)std::max(1ll, std::min(want, most));
     a.seg_len = ((p.vocab + a.segs - 1) / a.segs + 15) / 16 * 16;
     a.segs = (p.vocab + a.seg_len - 1) / a.seg_len;

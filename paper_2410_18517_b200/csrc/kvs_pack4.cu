@@ -11,8 +11,9 @@ namespace {
 // --------------------------------------------------------------------------------------
 // Storing.  A lane takes eight neighbouring elements of a row: their smallest and largest go around the D/32 lanes of the
 // group by shuffles, the eight codes make one word of the row.  Rows are dealt out with the tokens of a head in a run, so
-// that what a warp writes is contiguous.  A code next to the border between two is settled in fp64 (in fp32 the quotient,
-// at most 32, is off by less than 1e-5; ties are real: bf16 elements lie on few values).
+// that what a warp writes is contiguous.  In fp32 the quotient, at most 32, is off by less than 1e-5: a code next to the
+// border between two is settled by the sign of x - b - (k + 1/2) s, which two fp32 operations and their remainders give exactly.
+// (Ties are real, bf16 elements lie on few values: of normal draws 1 in 300, so that two warps in five have one.)
 // Bound: HBM, 2 D e bytes in and D + 32 out per token and head.
 // --------------------------------------------------------------------------------------
 constexpr int kPackThreads = 256;
@@ -24,8 +25,9 @@ struct PackKernelArgs {
     char* kplane;
     char* vplane;
     long long src_b, src_t, src_h;      // bytes between sequences, tokens, heads of the source
-    long long rows;                     // batch * n_new * Hkv
-    int n_new, Hkv, row_stride, len0, cap;
+    uint32_t rows;                      // batch * n_new * Hkv
+    FastDiv by_token, by_head;          // n_new, Hkv
+    int n_new, row_stride, len0, cap;
     const int* unit_len;
     const int* n_extra;
     int* status;
@@ -82,11 +84,26 @@ __device__ __forceinline__ void pack_eight(const float (&x)[8], uint32_t* pair, 
     }
     if (s == 0.f) {
         word = 0;
-    } else if (worst > 0.4999f || s < 1e-30f) {     // (the reciprocal of a tiny s overflows)
+    } else if (s < 1e-30f) {                // its reciprocal may overflow, products may lose bits
         word = 0;
         for (int i = 7; i >= 0; --i) {
             const double q = rint(((double)x[i] - (double)b) / (double)s);
             word = word * 16 + (uint32_t)(fmin(fmax(q, 16.0), 31.0) - 16.0);
+        }
+    } else if (worst > 0.4999f) {
+        word = 0;
+#pragma unroll
+        for (int i = 7; i >= 0; --i) {
+            const float d = __fsub_rn(x[i], b), f = fminf(fmaxf(__fmul_rn(d, inv), 16.f), 31.f);
+            float r = __fsub_rn(__fadd_rn(f, kRint), kRint);
+            const float below = f - r >= 0.f ? r : r - 1.f;             // the border next to f is below + 1/2
+            if (fabsf(__fsub_rn(f, r)) > 0.4999f) {
+                const float back = __fsub_rn(x[i], d);                  // x - b = d + lost exactly
+                const float lost = __fadd_rn(__fsub_rn(x[i], __fadd_rn(d, back)), __fsub_rn(back, b));
+                const float side = __fadd_rn(__fmaf_rn(-(below + 0.5f), s, d), lost);
+                r = side > 0.f ? below + 1.f : side < 0.f ? below : below + ((int)below & 1);
+            }
+            word = word * 16 + ((uint32_t)r & 15u);
         }
     }
     *codes = word;
@@ -107,42 +124,44 @@ __global__ void __launch_bounds__(kPackThreads) pack4_kernel(const PackKernelArg
     }
     const char* src = blockIdx.y == 0 ? a.k : a.v;
     char* dst = blockIdx.y == 0 ? a.kplane : a.vplane;
-    const int lane = threadIdx.x % LPR;
-    const long long step = (long long)gridDim.x * RPB;
-    for (long long r0 = (long long)blockIdx.x * RPB + threadIdx.x / LPR; r0 - threadIdx.x / LPR < a.rows; r0 += kPackRows * step) {
-        float x[kPackRows][8];
+    const uint32_t lane = threadIdx.x % LPR, step = gridDim.x * RPB;
+    for (uint32_t base = blockIdx.x * RPB; base < a.rows; base += kPackRows * step) {
+        constexpr int V = sizeof(T) / 2;        // 16-byte pieces of eight elements
+        uint4 in[kPackRows][V];
         long long to[kPackRows];
 #pragma unroll
         for (int j = 0; j < kPackRows; ++j) {
-            const long long r = r0 + j * step;
+            const uint32_t r = base + threadIdx.x / LPR + j * step;
             to[j] = -1;
             if (r < a.rows) {
-                const long long u = r / a.n_new;            // (sequence, head)
-                const int t = (int)(r - u * a.n_new), h = (int)(u % a.Hkv);
-                const uint4* p = reinterpret_cast<const uint4*>(src + u / a.Hkv * a.src_b + t * a.src_t + h * a.src_h) + lane * (sizeof(T) / 2);
-                if constexpr (sizeof(T) == 2) {
-                    Unpack<T>::run(__ldcs(p), x[j]);
-                } else {
-                    const uint4 p0 = __ldcs(p), p1 = __ldcs(p + 1);
-                    x[j][0] = __uint_as_float(p0.x), x[j][1] = __uint_as_float(p0.y), x[j][2] = __uint_as_float(p0.z), x[j][3] = __uint_as_float(p0.w);
-                    x[j][4] = __uint_as_float(p1.x), x[j][5] = __uint_as_float(p1.y), x[j][6] = __uint_as_float(p1.z), x[j][7] = __uint_as_float(p1.w);
-                }
+                const uint32_t u = a.by_token.div(r), t = r - u * a.n_new;          // (sequence, head), token
+                const uint32_t seq = a.by_head.div(u), h = u - seq * a.by_head.d;
+                const uint4* p = reinterpret_cast<const uint4*>(src + seq * a.src_b + t * a.src_t + h * a.src_h) + lane * V;
+#pragma unroll
+                for (int i = 0; i < V; ++i) in[j][i] = __ldcs(p + i);
                 const int first = a.unit_len ? a.unit_len[u] : a.len0;      // ragged slots append per unit
-                if (first + t < a.cap) {
-                    to[j] = (u * a.row_stride + first + t) * (long long)R::RB;
+                if (first + (int)t < a.cap) {
+                    to[j] = ((long long)u * a.row_stride + first + t) * R::RB;
                     if (!KVS_BOUNDS_OK(to[j], R::RB, a.plane_bytes, a.status)) to[j] = -1;
                 } else if (lane == 0) {     // only a replay that outran the capacity gets here
                     atomicExch(a.status, 4);
                 }
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
+                for (int i = 0; i < V; ++i) in[j][i] = make_uint4(0u, 0u, 0u, 0u);
             }
         }
 #pragma unroll
         for (int j = 0; j < kPackRows; ++j) {
+            float x[8];
+            if constexpr (V == 1) {
+                Unpack<T>::run(in[j][0], x);
+            } else {
+                Unpack<T>::run(in[j][0], *reinterpret_cast<float(*)[4]>(x));
+                Unpack<T>::run(in[j][1], *reinterpret_cast<float(*)[4]>(x + 4));
+            }
             uint32_t pair, codes;
-            pack_eight<R::GROUP / 8>(x[j], &pair, &codes);
+            pack_eight<R::GROUP / 8>(x, &pair, &codes);
             if (to[j] >= 0) {
                 uint32_t* row = reinterpret_cast<uint32_t*>(dst + to[j]);
                 row[4 + lane] = codes;
@@ -156,14 +175,17 @@ __global__ void __launch_bounds__(kPackThreads) pack4_kernel(const PackKernelArg
 // Reading rows back, to [b][t][h] places of any strides.  packed: the values of a 4-bit row, eight per lane; otherwise a
 // copy of the storage type's row.  Rows a unit does not hold become zeros.  Bound: HBM.
 // --------------------------------------------------------------------------------------
+constexpr int kReadRows = 4;        // rows a lane has in flight
+
 struct ReadKernelArgs {
     const char* kplane;
     const char* vplane;
     char* k_out;
     char* v_out;
     long long dst_b, dst_t, dst_h;      // bytes
-    long long rows;                     // batch * n * Hkv
-    int n, Hkv, row_stride, first;
+    uint32_t rows;                      // batch * n * Hkv
+    FastDiv by_token, by_head;          // n, Hkv
+    int n, row_stride, first;
     const int* unit_len;
     int* status;
     long long plane_bytes, out_bytes;
@@ -187,38 +209,58 @@ __global__ void __launch_bounds__(256) read_rows_kernel(const ReadKernelArgs a) 
     pdl_wait();
     const char* src = blockIdx.y == 0 ? a.kplane : a.vplane;
     char* dst = blockIdx.y == 0 ? a.k_out : a.v_out;
-    const int lane = threadIdx.x % LPR;
-    for (long long r = (long long)blockIdx.x * RPB + threadIdx.x / LPR; r < a.rows; r += (long long)gridDim.x * RPB) {
-        const long long u = r / a.n;
-        const int t = (int)(r - u * a.n), h = (int)(u % a.Hkv);
-        const long long at = (u * a.row_stride + a.first + t) * (long long)RB;
-        uint4 x[V];
-        bool have = !a.unit_len || a.first + t < a.unit_len[u];
-        if (!KVS_BOUNDS_OK(at, RB, a.plane_bytes, a.status)) have = false;
-        if (!have) {
+    const uint32_t lane = threadIdx.x % LPR, step = gridDim.x * RPB;
+    for (uint32_t base = blockIdx.x * RPB + threadIdx.x / LPR; base < a.rows; base += kReadRows * step) {
+        uint4 x[kReadRows][PACKED ? 1 : V];         // packed: the codes and the pair
+        long long to[kReadRows];
+        bool have[kReadRows];
 #pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = make_uint4(0u, 0u, 0u, 0u);
-        } else if constexpr (!PACKED) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = reinterpret_cast<const uint4*>(src + at)[lane * V + i];
-        } else {
-            const uint32_t* row = reinterpret_cast<const uint32_t*>(src + at);
-            const uint32_t pair = row[lane / (LPR / 4)], w = row[4 + lane];
-            if constexpr (sizeof(T) == 2) {
-                x[0] = pack4_expand(w, pair);
+        for (int j = 0; j < kReadRows; ++j) {
+            const uint32_t r = base + j * step;
+            to[j] = -1;
+            have[j] = false;
+            if (r >= a.rows) continue;
+            const uint32_t u = a.by_token.div(r), t = r - u * a.n;
+            const uint32_t seq = a.by_head.div(u), h = u - seq * a.by_head.d;
+            const long long at = ((long long)u * a.row_stride + a.first + t) * RB;
+            to[j] = seq * a.dst_b + t * a.dst_t + h * a.dst_h;
+            have[j] = !a.unit_len || a.first + (int)t < a.unit_len[u];
+            if (!KVS_BOUNDS_OK(at, RB, a.plane_bytes, a.status)) have[j] = false;
+            if (!have[j]) continue;
+            if constexpr (PACKED) {
+                const uint32_t* row = reinterpret_cast<const uint32_t*>(src + at);
+                x[j][0].x = row[4 + lane];
+                x[j][0].y = row[lane / (LPR / 4)];
             } else {
-                const float s = bf16_lo(pair), b = bf16_hi(pair);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[j][i] = reinterpret_cast<const uint4*>(src + at)[lane * V + i];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kReadRows; ++j) {
+            if (to[j] < 0) break;
+            uint4 y[V];
+            if (!have[j]) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = make_uint4(0u, 0u, 0u, 0u);
+            } else if constexpr (!PACKED) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = x[j][i];
+            } else if constexpr (V == 1) {
+                y[0] = pack4_expand(x[j][0].x, x[j][0].y);
+            } else {
+                const uint32_t w = x[j][0].x;
+                const float s = bf16_lo(x[j][0].y), b = bf16_hi(x[j][0].y);
                 float f[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) f[i] = pack4_value(w >> (4 * i) & 15u, s, b);
-                x[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-                x[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
+                y[0] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+                y[1] = make_uint4(__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7]));
             }
-        }
-        const long long to = u / a.Hkv * a.dst_b + t * a.dst_t + h * a.dst_h;
-        if (KVS_BOUNDS_OK(to, D * (int)sizeof(T), a.out_bytes, a.status))
+            if (KVS_BOUNDS_OK(to[j], D * (int)sizeof(T), a.out_bytes, a.status))
 #pragma unroll
-            for (int i = 0; i < V; ++i) reinterpret_cast<uint4*>(dst + to)[lane * V + i] = x[i];
+                for (int i = 0; i < V; ++i) reinterpret_cast<uint4*>(dst + to[j])[lane * V + i] = y[i];
+        }
     }
 }
 
@@ -386,9 +428,10 @@ cudaError_t launch_pack4(const PackArgs& p, cudaStream_t stream) {
     a.src_b = p.src_b * e;
     a.src_t = p.src_t * e;
     a.src_h = p.src_h * e;
-    a.rows = (long long)p.batch * p.n_new * p.Hkv;
+    a.rows = (uint32_t)p.batch * p.n_new * p.Hkv;
     a.n_new = p.n_new;
-    a.Hkv = p.Hkv;
+    a.by_token = FastDiv(p.n_new);
+    a.by_head = FastDiv(p.Hkv);
     a.row_stride = p.row_stride;
     a.len0 = p.len0;
     a.cap = p.capacity;
@@ -397,6 +440,7 @@ cudaError_t launch_pack4(const PackArgs& p, cudaStream_t stream) {
     a.status = p.status;
     a.plane_bytes = p.plane_bytes;
     const int rpb = kPackThreads / (p.D / 8);
+    if ((long long)p.batch * p.n_new * p.Hkv > 0x7fffffffll) return cudaErrorInvalidValue;
     const dim3 grid((unsigned)std::min<long long>((a.rows + rpb - 1) / rpb, p.sm_count * 16), 2), block(kPackThreads);
     if (p.dtype == 0)
         return p.D == 128 ? launch_kernel(pack4_kernel<__nv_bfloat16, 128>, grid, block, 0, stream, p.programmatic, a)
@@ -415,9 +459,10 @@ cudaError_t launch_read_rows(const ReadArgs& p, cudaStream_t stream) {
     a.dst_b = p.dst_b * e;
     a.dst_t = p.dst_t * e;
     a.dst_h = p.dst_h * e;
-    a.rows = (long long)p.batch * p.n * p.Hkv;
+    a.rows = (uint32_t)p.batch * p.n * p.Hkv;
     a.n = p.n;
-    a.Hkv = p.Hkv;
+    a.by_token = FastDiv(p.n);
+    a.by_head = FastDiv(p.Hkv);
     a.row_stride = p.row_stride;
     a.first = p.first;
     a.unit_len = p.unit_len;
@@ -425,6 +470,7 @@ cudaError_t launch_read_rows(const ReadArgs& p, cudaStream_t stream) {
     a.plane_bytes = p.plane_bytes;
     a.out_bytes = ((p.batch - 1) * p.dst_b + (p.n - 1) * p.dst_t + (p.Hkv - 1) * p.dst_h + p.D) * e;
     const int rpb = 256 / (p.D / 8);
+    if ((long long)p.batch * p.n * p.Hkv > 0x7fffffffll) return cudaErrorInvalidValue;
     const dim3 grid((unsigned)std::min<long long>((a.rows + rpb - 1) / rpb, p.sm_count * 16), 2), block(256);
 #define KVS_READ(T, D) (p.packed ? launch_kernel(read_rows_kernel<T, D, true>, grid, block, 0, stream, p.programmatic, a) \
                                  : launch_kernel(read_rows_kernel<T, D, false>, grid, block, 0, stream, p.programmatic, a))
