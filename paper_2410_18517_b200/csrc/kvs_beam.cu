@@ -13,19 +13,20 @@ namespace {
 // Selection.  score(b, v) = scores[b] + x_bv - lse_b,  lse_b = log sum_v exp x_bv;  of a request's W beams x V tokens the K
 // best, equal scores by the lowest (beam, token).
 //
-// First kernel: every logits row is cut into segments, a block each (one pass over the logits): running maximum and sum of
-// exponentials per thread, and the segment's K best, by a threshold: the K-th largest of the threads' own maxima in the first
-// turn.  K elements at least reach it and hardly more do, so that a logit costs a maximum, an exponential, a sum and a
-// comparison.  Where too many reach it (equal logits, rising ones) the candidates become 64-bit keys - order of the value, then
-// the lower index, all different - and the threads' maxima of those bound them: exactly K threads reach the K-th largest.
+// First kernel: every logits row is cut into segments, a block each: running maximum and sum of exponentials per thread, then
+// the segment's K best by a threshold: the K-th largest of the threads' own maxima.  K elements at least reach it and hardly
+// more do, and only the logits of threads whose maximum does are read again (from L2, a warp for a thread's pieces).  Where
+// too many reach it (equal logits, sorted ones) the candidates become 64-bit keys - order of the value, then the lower index, all different - and the
+// threads' best of those bound them, a run of logits at a time: exactly K threads reach the K-th largest.
 // Second kernel, a block per request: lse in fp64 (a rounding of 1e-7 would decide between beams whose scores nearly tie), the
-// lists by the K-th largest of their heads, and the K best in order.
+// lists' entries by the same kind of threshold, and the K best in order.
 // Bound: HBM for the logits, once; small calls: two launches.
 // --------------------------------------------------------------------------------------
 constexpr int kBeamThreads = 256;
-constexpr int kBeamPer = 16;                              // logits per thread and turn
-constexpr int kBeamTurn = kBeamThreads * kBeamPer;
-constexpr int kBeamRoom = kBeamMaxOut * kBeamPer * 2;     // candidates: what is kept, and what one turn adds
+constexpr int kBeamAhead = 4;                             // 16-byte pieces of logits a thread has in flight
+constexpr int kBeamRoom = 2048;                           // candidates a block has room for
+constexpr int kBeamRun = 8;                               // logits of a thread at a time where there are too many
+static_assert(kBeamMaxOut * (kBeamRun + 1) * 2 <= kBeamRoom, "what is kept, and what a run adds");
 
 __device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);          // -0 and 0 are equal
@@ -38,7 +39,7 @@ __device__ __forceinline__ uint64_t order_of(double x) {
 }
 __device__ __forceinline__ double value_of(uint64_t o) { return __longlong_as_double(o ^ (o >> 63 ? 0x8000000000000000ull : 0xffffffffffffffffull)); }
 
-// exp(t), t <= 0 (or NaN): the product's rounding costs 2^-24 |t| of it, next to nothing where a term counts
+// exp(t), t <= 0 (or NaN)
 __device__ __forceinline__ float exp_below(float t) { return fast_exp2(t * 1.44269504f); }
 
 // The second kernel's keys need more bits than one word: by score, then by the lower index
@@ -81,7 +82,7 @@ __device__ __noinline__ void kth_of_threads(Key mine, int K, Key lowest, Key* ke
 // K * kBeamRoom / 256, the K best among them.  *count receives how many; returns the threshold.
 template <typename Key>
 __device__ __noinline__ Key prune(Key* list, int n, int* count, int K, Key lowest, Key* keys, Key* cut) {
-    constexpr int MOST = kBeamRoom / kBeamThreads;
+    constexpr int MOST = (kBeamRoom + kBeamThreads - 1) / kBeamThreads;
     Key mine[MOST], top = lowest;
 #pragma unroll
     for (int j = 0; j < MOST; ++j) {
@@ -133,18 +134,53 @@ struct BeamKernelArgs {
     long long list_count, sum_count;
 };
 
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {      // two fp32 sums
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_of(float lo, float hi) { return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo); }
+__device__ __forceinline__ float low_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float high_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+
+// The values are made from the pieces anew wherever they are needed: eight floats a piece would not fit beside them.
+template <int NV>
+__device__ __forceinline__ void only_pieces(uint4 (&x)[NV]) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) asm volatile("" : "+r"(x[j].x), "+r"(x[j].y), "+r"(x[j].z), "+r"(x[j].w));
+}
+
+// 16 bytes of logits that are all minus infinity, and 16 bytes that lie anywhere
 template <typename T>
-__global__ void __launch_bounds__(kBeamThreads) beam_segments_kernel(const BeamKernelArgs a) {
+__device__ __forceinline__ uint4 masked_piece() {
+    constexpr uint32_t w = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    return make_uint4(w, w, w, w);
+}
+__device__ __forceinline__ uint4 gather_piece(const __nv_bfloat16* p) {
+    auto bits = [&](int i) { return (uint32_t)__bfloat16_as_ushort(p[i]); };
+    return make_uint4(bits(0) | bits(1) << 16, bits(2) | bits(3) << 16, bits(4) | bits(5) << 16, bits(6) | bits(7) << 16);
+}
+__device__ __forceinline__ uint4 gather_piece(const float* p) {
+    return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]));
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kBeamThreads, 5) beam_segments_kernel(const BeamKernelArgs a) {
     __shared__ uint64_t s_list[kBeamRoom];
     __shared__ uint64_t s_keys[kBeamThreads];
     __shared__ __align__(16) float s_max[kBeamThreads];
     __shared__ uint64_t s_kth;
     __shared__ uint32_t s_cut;
-    __shared__ int s_count, s_more[2];       // kept; candidates of a turn, of even and odd turns
+    __shared__ int s_count, s_found, s_who[kBeamThreads];
     __shared__ float2 s_sum[kBeamThreads / 32];
     const int seg = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
     if (tid == 0) {
-        s_count = s_more[0] = s_more[1] = 0;
+        s_count = s_found = 0;
         s_cut = 0xffffffffu;
     }
     pdl_launch_dependents();
@@ -152,91 +188,123 @@ __global__ void __launch_bounds__(kBeamThreads) beam_segments_kernel(const BeamK
     const int v0 = seg * a.seg_len, v1 = min(a.vocab, v0 + a.seg_len);
     const T* x_row = static_cast<const T*>(a.logits) + row * a.stride;
     const uint64_t none = (uint64_t)order_of(-INFINITY) << 32 | 0xffffffffu;     // minus infinity is no candidate
-    constexpr int PER16 = 16 / (int)sizeof(T);       // logits per 16-byte load
-    float cut = -INFINITY;
-    float m = -INFINITY, sum = 0.f;
-    // thread t takes runs of 16 bytes, t, t + 256, ...: the same elements whether they can be loaded as vectors or not
-    auto index = [&](int base, int i) { return base + (i / PER16 * kBeamThreads + tid) * PER16 + i % PER16; };
+    constexpr int PER16 = 16 / (int)sizeof(T);       // logits per piece
+    constexpr int AHEAD = kBeamAhead, TURN = AHEAD * kBeamThreads;
     auto key = [&](float x, int v) { return (uint64_t)order_of(x) << 32 | (uint32_t)~v; };
-    __syncthreads();
-    int turn = 0;
-    for (int base = v0; base < v1; base += kBeamTurn, turn ^= 1) {
-        const int count = s_count;       // (nobody adds before the next barrier)
-        float x[kBeamPer];
+    // thread t takes pieces t, t + 256, ...: the same logits whether they can be loaded as vectors or not; what is left of the
+    // row behind the last whole piece goes to the first threads, a logit each
+    const int pieces = (v1 - v0) / PER16, at_rest = v0 + pieces * PER16 + tid;
+    const float extra = at_rest < v1 ? (float)x_row[at_rest] : -INFINITY;
+    auto piece = [&](int p) {
+        if (p >= pieces) return masked_piece<T>();
+        const T* at = x_row + v0 + p * PER16;
+        return a.vec ? *reinterpret_cast<const uint4*>(at) : gather_piece(at);
+    };
+    float m = extra, sum = extra > -INFINITY ? 1.f : extra != extra ? extra : 0.f;
+    for (int p0 = tid; p0 < pieces; p0 += TURN) {
+        uint4 x[AHEAD];
 #pragma unroll
-        for (int j = 0; j < kBeamPer / PER16; ++j) {
-            const int v = index(base, j * PER16);
-            if (a.vec && v + PER16 <= v1) {
-                float f[PER16];
-                Unpack<T>::run(__ldcs(reinterpret_cast<const uint4*>(x_row + v)), f);
+        for (int j = 0; j < AHEAD; ++j) x[j] = piece(p0 + j * kBeamThreads);
+        float top = m;
 #pragma unroll
-                for (int i = 0; i < PER16; ++i) x[j * PER16 + i] = f[i];
-            } else {
+        for (int j = 0; j < AHEAD; ++j) {
+            float f[PER16];
+            Unpack<T>::run(x[j], f);
 #pragma unroll
-                for (int i = 0; i < PER16; ++i) x[j * PER16 + i] = v + i < v1 ? (float)x_row[v + i] : -INFINITY;
+            for (int i = 0; i < PER16; ++i) top = fmaxf(top, f[i]);
+        }
+        // exp(x - top), two at a time (a product's rounding costs 2^-24 |x - top| of it: next to nothing where a term counts)
+        const float ref = top == -INFINITY ? 0.f : top;
+        const uint64_t minus = pair_of(-ref, -ref), scale = pair_of(1.44269504f, 1.44269504f);
+        uint64_t sums[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            float f[PER16];
+            Unpack<T>::run(x[j], f);
+#pragma unroll
+            for (int i = 0; i < PER16; i += 2) {
+                const uint64_t y = mul2(add2(pair_of(f[i], f[i + 1]), minus), scale);
+                sums[i / 2 % 2] = add2(sums[i / 2 % 2], pair_of(fast_exp2(low_of(y)), fast_exp2(high_of(y))));
             }
         }
-        float best = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < kBeamPer; ++i) best = fmaxf(best, x[i]);
-        const float top = fmaxf(m, best), ref = top == -INFINITY ? 0.f : top;
-        sum *= exp_below(m - ref);       // a NaN stays one, and makes the row's sum NaN
-#pragma unroll
-        for (int i = 0; i < kBeamPer; ++i) sum += exp_below(x[i] - ref);
+        const uint64_t both = add2(sums[0], sums[1]);
+        sum = sum * exp_below(m - ref) + (low_of(both) + high_of(both));    // a NaN among the logits makes it, and the row's sum, NaN
         m = top;
-        int mine = 0;
-        if (base == v0) {
-            // for few continuations the maxima of four threads each are enough of them
-            const bool quads = a.K <= 16;
-            float most = best;
-            if (quads) {
-                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-                most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            }
-            if (!quads || tid % 4 == 0) s_max[quads ? tid / 4 : tid] = most;
-            __syncthreads();
-            kth_of(s_max, quads ? kBeamThreads / 4 : kBeamThreads, s_max[quads ? tid % (kBeamThreads / 4) : tid], a.K, &s_cut);
-            cut = value_of(s_cut);
-            if (best >= cut)
-#pragma unroll
-                for (int i = 0; i < kBeamPer; ++i) mine += x[i] >= cut && x[i] > -INFINITY ? 1 : 0;
-        } else if (best > cut) {         // (an equal one comes after K others)
-#pragma unroll
-            for (int i = 0; i < kBeamPer; ++i) mine += x[i] > cut ? 1 : 0;
+    }
+    // the threshold; for few continuations the maxima of four threads each are enough of them
+    const bool quads = a.K <= 16;
+    float most = m;
+    if (quads) {
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    }
+    if (!quads || tid % 4 == 0) s_max[quads ? tid / 4 : tid] = most;
+    __syncthreads();
+    kth_of(s_max, quads ? kBeamThreads / 4 : kBeamThreads, s_max[quads ? tid % (kBeamThreads / 4) : tid], a.K, &s_cut);
+    const float cut = value_of(s_cut);
+    auto offer = [&](float x, int v) {
+        if (x >= cut && x > -INFINITY) {
+            const int at = atomicAdd(&s_count, 1);
+            if (at < kBeamRoom) s_list[at] = key(x, v);
         }
-        if (mine) atomicAdd(&s_more[turn], mine);
-        __syncthreads();
-        const int more = s_more[turn];
-        if (tid == 0) s_more[turn ^ 1] = 0;
-        if (count + more <= kBeamRoom) {
-            if (mine)
+    };
+    if (m >= cut && m > -INFINITY) {
+        s_who[atomicAdd(&s_found, 1)] = tid;
+        offer(extra, at_rest);
+    }
+    __syncthreads();
+    const int found = s_found;
+    for (int i = tid / 32; i < found; i += kBeamThreads / 32)
+        for (int p = s_who[i] + tid % 32 * kBeamThreads; p < pieces; p += 32 * kBeamThreads) {
+            float f[PER16];
+            Unpack<T>::run(piece(p), f);
+            float high = f[0];
 #pragma unroll
-                for (int i = 0; i < kBeamPer; ++i)
-                    if ((base == v0 ? x[i] >= cut : x[i] > cut) && x[i] > -INFINITY) s_list[atomicAdd(&s_count, 1)] = key(x[i], index(base, i));
-        } else {
-            // too many: the threads' best keys of this turn, and those of what has been kept, as thresholds
+            for (int j = 1; j < PER16; ++j) high = fmaxf(high, f[j]);
+            if (high >= cut)
+#pragma unroll
+                for (int j = 0; j < PER16; ++j) offer(f[j], v0 + p * PER16 + j);
+        }
+    __syncthreads();
+    if (s_count > kBeamRoom) {
+        // too many: with keys, a few logits of a thread and the extra one at a time
+        __syncthreads();
+        if (tid == 0) s_count = 0;
+        int held = 0;
+        constexpr int RUN = kBeamRun / PER16;
+#pragma unroll 1
+        for (int p0 = 0; p0 < max(pieces, 1); p0 += RUN * kBeamThreads) {
+            uint64_t k[kBeamRun + 1];
+            k[kBeamRun] = p0 == 0 ? key(extra, at_rest) : none;
+#pragma unroll
+            for (int j = 0; j < RUN; ++j) {
+                float f[PER16];
+                const int p = p0 + j * kBeamThreads + tid;
+                Unpack<T>::run(piece(p), f);
+#pragma unroll
+                for (int i = 0; i < PER16; ++i) k[j * PER16 + i] = key(f[i], v0 + p * PER16 + i);
+            }
             uint64_t first = none;
 #pragma unroll
-            for (int i = 0; i < kBeamPer; ++i) first = max(first, key(x[i], index(base, i)));
+            for (int i = 0; i <= kBeamRun; ++i) first = max(first, k[i]);
             kth_of_threads(first, a.K, none, s_keys, &s_kth);
             uint64_t least = s_kth;
             __syncthreads();
-            least = max(least, prune(s_list, count, &s_count, a.K, none, s_keys, &s_kth));
+            if (held > kBeamRoom / 2) least = max(least, prune(s_list, held, &s_count, a.K, none, s_keys, &s_kth));
 #pragma unroll
-            for (int i = 0; i < kBeamPer; ++i) {
-                const uint64_t k = key(x[i], index(base, i));
-                if (k >= least && k > none) s_list[atomicAdd(&s_count, 1)] = k;
-            }
-            cut = fmaxf(cut, value_of((uint32_t)(least >> 32)));
+            for (int i = 0; i <= kBeamRun; ++i)
+                if (k[i] >= least && k[i] > none) s_list[atomicAdd(&s_count, 1)] = k[i];
+            __syncthreads();
+            held = s_count;
+            __syncthreads();
         }
-        __syncthreads();
     }
     // the segment's maximum and sum, in a fixed order
 #pragma unroll
     for (int d = 16; d; d >>= 1) {
         const float m2 = __shfl_xor_sync(0xffffffffu, m, d), sum2 = __shfl_xor_sync(0xffffffffu, sum, d);
-        const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.f : top;
-        const float lo = m <= m2 ? sum * exp_below(m - ref) : sum2 * exp_below(m2 - ref), hi = m <= m2 ? sum2 : sum;
+        const float top = fmaxf(m, m2), ref2 = top == -INFINITY ? 0.f : top;
+        const float lo = m <= m2 ? sum * exp_below(m - ref2) : sum2 * exp_below(m2 - ref2), hi = m <= m2 ? sum2 : sum;
         sum = m == m2 ? sum + sum2 : hi + lo;
         m = top;
     }
@@ -265,7 +333,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
     __shared__ double s_base[kBeamMaxBeams];      // scores[b] - log of the sum below the row's maximum
     __shared__ float s_top[kBeamMaxBeams];
     __shared__ uint32_t s_cut;
-    __shared__ int s_count;
+    __shared__ int s_count, s_equal[kBeamMaxOut];
     const int req = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const long long row0 = (long long)req * a.W;
     const int lists = a.W * a.segs, entries = lists * a.K;
@@ -276,11 +344,10 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
     pdl_launch_dependents();
     pdl_wait();
     const uint64_t* list = a.lists + row0 * a.segs * a.K;
-    constexpr int AHEAD = 8;                      // entries a thread has in flight
+    constexpr int AHEAD = 4;                      // entries a thread has in flight
     uint64_t ahead[AHEAD];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) ahead[j] = tid + j * kBeamThreads < entries ? __ldcg(list + tid + j * kBeamThreads) : 0;
-    const uint64_t head = tid < lists ? __ldcg(list + tid * a.K) : 0;
     for (int b = warp; b < a.W; b += kBeamThreads / 32) {
         const float2* sums = a.sums + (row0 + b) * a.segs;
         float top = -INFINITY;
@@ -310,30 +377,35 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
         }
         return w;
     };
-    // the K-th largest head, in fp32 (whose rounding keeps the order): what is below it is not among the K best
-    const int heads = (lists + 3) / 4 * 4;
-    const float mine = tid < lists ? (float)value_of(candidate(head, tid / a.segs).v) : -INFINITY;
-    if (tid < heads) s_head[tid] = mine;
-    __syncthreads();
-    kth_of(s_head, heads, mine, a.K, &s_cut);
-    const float cut = value_of(s_cut);
+    // The threads' best entries, in fp32 (whose rounding keeps the order), or the best of four threads each: what is below the
+    // K-th largest of those is not among the K best.
     const int per = a.segs * a.K;                 // entries of a beam
-    auto reaches = [&](const Wide& w) { return above(w, lowest) && (float)value_of(w.v) >= cut; };
-    for (int j = 0, e = tid; e < entries; ++j, e += kBeamThreads) {
-        uint64_t k = 0;
-        if (j < AHEAD) {
+    auto entry = [&](int j, int e) { return candidate(j < AHEAD ? ahead[j] : __ldcg(list + e), e / per); };
+    float most = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < AHEAD; ++i)
-                if (i == j) k = ahead[i];
-        } else {
-            k = __ldcg(list + e);
-        }
-        const Wide w = candidate(k, e / per);
+    for (int j = 0; j < AHEAD; ++j)
+        if (tid + j * kBeamThreads < entries) most = fmaxf(most, (float)value_of(entry(j, tid + j * kBeamThreads).v));
+    for (int e = tid + AHEAD * kBeamThreads; e < entries; e += kBeamThreads) most = fmaxf(most, (float)value_of(entry(AHEAD, e).v));
+    const bool quads = a.K <= 16;
+    if (quads) {
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    }
+    if (!quads || tid % 4 == 0) s_head[quads ? tid / 4 : tid] = most;
+    __syncthreads();
+    kth_of(s_head, quads ? kBeamThreads / 4 : kBeamThreads, s_head[quads ? tid % (kBeamThreads / 4) : tid], a.K, &s_cut);
+    const float cut = value_of(s_cut);
+    auto reaches = [&](const Wide& w) { return above(w, lowest) && (float)value_of(w.v) >= cut; };
+    auto offer = [&](const Wide& w) {
         if (reaches(w)) {
             const int at = atomicAdd(&s_count, 1);
             if (at < kBeamRoom) s_list[at] = w;
         }
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+        if (tid + j * kBeamThreads < entries) offer(entry(j, tid + j * kBeamThreads));
+    for (int e = tid + AHEAD * kBeamThreads; e < entries; e += kBeamThreads) offer(entry(AHEAD, e));
     __syncthreads();
     if (s_count > kBeamRoom) {
         // more than there is room for (many equal scores): a row of entries of all threads at a time, keeping the best so far
@@ -354,13 +426,41 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
             }
         }
     }
+    // in order: by the fp32 scores, in which a hundred candidates compare quickly, equal ones by their keys
     const long long o = (long long)req * a.K;
-    best_in_order(s_list, &s_count, a.K, lowest, s_keys, &s_kth, [&](int rank, const Wide& w) {
-        const uint32_t flat = ~w.i;
-        a.out_scores[o + rank] = (float)value_of(w.v);
-        a.out_tokens[o + rank] = (int)(flat % (uint32_t)a.vocab);
-        a.out_parents[o + rank] = (int)(row0 + flat / (uint32_t)a.vocab);
-    });
+    int n = s_count;
+    while (n > kBeamThreads) {
+        __syncthreads();
+        prune(s_list, n, &s_count, a.K, lowest, s_keys, &s_kth);
+        n = s_count;
+    }
+    Wide w = lowest;
+    if (tid < n) w = s_list[tid];
+    s_head[tid] = tid < n ? (float)value_of(w.v) : -INFINITY;
+    if (tid < a.K) s_equal[tid] = 0;
+    __syncthreads();
+    int rank = a.K;
+    const float x = s_head[tid];
+    if (tid < n) {
+        rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; j += 4) {
+            const float4 y = *reinterpret_cast<const float4*>(s_head + j);
+            rank += (y.x > x) + (y.y > x) + (y.z > x) + (y.w > x);
+        }
+        if (rank < a.K) atomicAdd(&s_equal[rank], 1);
+    }
+    __syncthreads();
+    if (rank < a.K) {
+        if (s_equal[rank] > 1)
+            for (int j = 0; j < n; ++j) rank += s_head[j] == x && above(s_list[j], w) ? 1 : 0;
+        if (rank < a.K) {
+            const uint32_t flat = ~w.i;
+            a.out_scores[o + rank] = x;
+            a.out_tokens[o + rank] = (int)(flat % (uint32_t)a.vocab);
+            a.out_parents[o + rank] = (int)(row0 + flat / (uint32_t)a.vocab);
+        }
+    }
     if (tid < a.K && tid >= s_count) {     // fewer candidates than places
         a.out_scores[o + tid] = -INFINITY;
         a.out_tokens[o + tid] = -1;
@@ -483,14 +583,13 @@ cudaError_t launch_beam_select(const BeamArgs& p, cudaStream_t stream) {
     a.stride = p.stride;
     a.vocab = p.vocab;
     a.rows = p.requests * p.beams;
-    // Segments: enough blocks for four on every SM, but none shorter than a quarter turn of a block and at most 256 lists (a
-    // thread each in the second kernel) per request, and room for the lists.
-    const long long want = ((long long)p.sm_count * 4 + a.rows - 1) / a.rows;
-    const long long most = std::min<long long>({(p.vocab + kBeamTurn / 4 - 1) / (kBeamTurn / 4), kBeamThreads / p.beams, std::max(1, kBeamMaxLists / a.rows)});
-    a.segs = (int)std::max(1ll, std::min(want, most));
-    a.seg_len = ((p.vocab + a.segs - 1) / a.segs + 15) / 16 * 16;
-    a.segs = (p.vocab + a.seg_len - 1) / a.seg_len;
-    const int e = p.dtype == 0 ? 2 : 4;
+    // Segments: as many as make the blocks fill the SMs once, five on each, but none shorter than a piece per thread; at most 256
+    // lists (a thread each in the second kernel) per request, and no more than there is room for.
+    const int e = p.dtype == 0 ? 2 : 4, piece = kBeamThreads * (16 / e);
+    const int most = std::min({(p.vocab - 1) / piece + 1, kBeamThreads / p.beams, std::max(1, kBeamMaxLists / a.rows)});
+    a.segs = std::min(std::max(1, p.sm_count * 5 / a.rows), most);
+    a.seg_len = ((p.vocab - 1) / a.segs + 1 + 15) / 16 * 16;
+    a.segs = (p.vocab - 1) / a.seg_len + 1;
     a.vec = (uintptr_t)p.logits % 16 == 0 && p.stride * e % 16 == 0;
     a.scores = p.scores;
     a.W = p.beams;
