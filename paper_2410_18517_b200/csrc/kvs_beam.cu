@@ -134,27 +134,6 @@ struct BeamKernelArgs {
     long long list_count, sum_count;
 };
 
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {      // two fp32 sums
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t pair_of(float lo, float hi) { return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo); }
-__device__ __forceinline__ float low_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
-__device__ __forceinline__ float high_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
-
-// The values are made from the pieces anew wherever they are needed: eight floats a piece would not fit beside them.
-template <int NV>
-__device__ __forceinline__ void only_pieces(uint4 (&x)[NV]) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) asm volatile("" : "+r"(x[j].x), "+r"(x[j].y), "+r"(x[j].z), "+r"(x[j].w));
-}
-
 // 16 bytes of logits that are all minus infinity, and 16 bytes that lie anywhere
 template <typename T>
 __device__ __forceinline__ uint4 masked_piece() {

@@ -1,10 +1,12 @@
 // Split-K decode attention over a 4-bit cache, bf16 storage: the codes become bf16 tensor-core operands in registers.
 //
-// Mathematics: S = q K^T, P = 2^(S - max), O = sum P V over the values of the rows (kvs_pack4.cuh), one pass with a running
-// maximum and sum.  mma.sync.m16n8k16 with the q-heads of a kv-head as rows: a product of 16 rows costs what one of 8 does, so
-// the rows the heads leave free carry the softmax weights' further terms.  P = hi + mid + lo, three bf16 terms:
-//   up to four heads:  rows 0..3 hi, 8..11 mid, 4..7 lo, in ONE product (row r holds head r mod 4 in S, so the lanes of rows
-//                      4..7 have the weights too);
+// Mathematics: S = K q^T, P = 2^(S - max), O = P^T V over the values of the rows (kvs_pack4.cuh), one pass with a running
+// maximum and sum, by mma.sync.m16n8k16.  S has 16 keys as rows and the q-heads of a kv-head as columns (no row is padding, no
+// operand register holds constant zeros: those cost a move each per product); P's 8 x 8 blocks are transposed on the way to
+// the second product, which has the heads as rows.  A product of 16 rows costs what one of 8 does, so the rows the heads leave
+// free carry the weights' further terms.  P = hi + mid + lo, three bf16 terms:
+//   up to four heads:  rows 0..3 hi, 8..11 mid, 4..7 lo, in ONE product (column c of S is head c mod 4, so the lanes of
+//                      columns 4..7 have the weights too);
 //   five to eight:     rows 0..7 hi and 8..15 mid in one product, lo in a second.
 // Two terms would leave 1.5e-6 of the result, three the fp32 rounding.  The products of a tile start from zero and are added to
 // the running state rounded to nearest: an MMA cuts its sum off, and over thousands of rows that would drift.
@@ -28,13 +30,23 @@ namespace kvs {
 
 namespace {
 
-// Geometries.  Large: 8 warps x 32 rows a tile; small, where that would leave blocks idle: 4 warps x 16 rows.
+// Geometries (compile-time; the defaults are the measured best).  Large: warps x blocks of 16 rows a tile; small, where that would
+// leave thread blocks idle: 4 warps x 16 rows.
+#ifndef KVS_PACK4_WARPS
+#define KVS_PACK4_WARPS 8
+#endif
+#ifndef KVS_PACK4_BLOCKS
+#define KVS_PACK4_BLOCKS 4
+#endif
+#ifndef KVS_PACK4_STAGES
+#define KVS_PACK4_STAGES 2
+#endif
 template <int D, int BIG>
 struct Pack4Shape {
-    static constexpr int WARPS = BIG ? 8 : 4;
-    static constexpr int BPW = BIG ? 2 : 1;                // 16-row blocks per warp and tile
+    static constexpr int WARPS = BIG ? KVS_PACK4_WARPS : 4;
+    static constexpr int BPW = BIG ? KVS_PACK4_BLOCKS : 1;                // 16-row blocks per warp and tile: WARPS blocks apart
     static constexpr int TN = WARPS * BPW * 16;            // rows per tile
-    static constexpr int STAGES = BIG ? 4 : 6;
+    static constexpr int STAGES = BIG ? KVS_PACK4_STAGES : 6;
     static constexpr int RB = Pack4Row<D>::RB;
     static constexpr int TILE = TN * RB;                   // bytes of a K tile and of a V tile
     static constexpr int QBYTES = 8 * D * 2;               // room for the queries of eight heads
@@ -70,6 +82,18 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void mma_bf16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {      // of an 8 x 8 matrix of 16-bit elements
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
 }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -222,9 +246,10 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
     if (tid == 0) KVS_TRACE_STAMP(tr, kTrConsumerGo);
     pdl_launch_dependents();
     int trace_piece = 0;
+    // S: keys row and row + 8, heads 2 quad and 2 quad + 1; O: head row, columns 2 quad and 2 quad + 1
     const int row = lane >> 2, quad = lane & 3;
-    const int head = WIDE ? row : (row & 3);       // the q-head whose scores this lane holds
-    const bool third = !WIDE && row >= 4;          // this lane's rows carry the third term
+    const int head = WIDE ? row : (row & 3);       // whose queries this lane brings in
+    const bool third = !WIDE && quad >= 2;         // this lane's columns of S carry the third term
 
     int it = 0;
     long long gt = t0;
@@ -235,10 +260,10 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
         const int n_u = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
 
         uint32_t qa[KSTEPS][2];
-        float o[NB][2];
-        float m = -1.0e30f, lsum = 0.f;
+        uint64_t o[NB];                   // pairs: elements nb of the lane's two columns
+        float m[2] = {-1.0e30f, -1.0e30f}, lsum[2] = {0.f, 0.f};   // maximum (log2 domain) of a head, sum over the lane's keys
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) o[nb][0] = o[nb][1] = 0.f;
+        for (int nb = 0; nb < NB; ++nb) o[nb] = 0;
 
         for (int k = 0; k < piece_tiles; ++k, ++it) {
             const int st = it % kStages;
@@ -261,81 +286,103 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
                     }
             }
             const int valid = n_u - (ti0 + k) * TN;     // rows of this tile that exist (may exceed TN or be <= 0)
-            if (warp * BPW * 16 >= valid) {             // none of this warp's
+            if (warp * 16 >= valid) {                   // none of this warp's
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&empty_bar[st]);
                 continue;
             }
             // ---- scores ----
-            float s[BPW][2][2];
-            float tmax = -INFINITY;
+            float s[BPW][4];                            // [block]: (key row, two heads), (key row + 8, two heads)
 #pragma unroll
             for (int blk = 0; blk < BPW; ++blk) {
-                const int tok0 = (warp * BPW + blk) * 16;
+                // rows past the end hold whatever the stage held before: their scores are replaced below
+                uint32_t w[2][XW], s2[2], b2[2];
 #pragma unroll
-                for (int nb = 0; nb < 2; ++nb) {
-                    // rows past the end hold whatever the stage held before: their columns are replaced below
-                    const unsigned char* kr = ks + (tok0 + nb * 8 + row) * RB;
+                for (int y = 0; y < 2; ++y) {
+                    const unsigned char* kr = ks + ((blk * WARPS + warp) * 16 + y * 8 + row) * RB;
                     const uint32_t pair = *reinterpret_cast<const uint32_t*>(kr + 4 * quad);
-                    const uint32_t s2 = __byte_perm(pair, pair, 0x1010), b2 = __byte_perm(pair, pair, 0x3232);
-                    uint32_t w[XW];
+                    s2[y] = __byte_perm(pair, pair, 0x1010);
+                    b2[y] = __byte_perm(pair, pair, 0x3232);
                     if constexpr (D == 128) {
                         const uint4 x = *reinterpret_cast<const uint4*>(kr + 16 + 16 * quad);
-                        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+                        w[y][0] = x.x, w[y][1] = x.y, w[y][2] = x.z, w[y][3] = x.w;
                     } else {
                         const uint2 x = *reinterpret_cast<const uint2*>(kr + 16 + 8 * quad);
-                        w[0] = x.x, w[1] = x.y;
-                    }
-                    float c[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};     // even and odd steps apart
-#pragma unroll
-                    for (int x = 0; x < XW; ++x) {
-                        mma_bf16(c[0], qa[2 * x][0], 0u, qa[2 * x][1], 0u, fma_bf16x2(pack4_pair<0>(w[x]), s2, b2), fma_bf16x2(pack4_pair<1>(w[x]), s2, b2));
-                        mma_bf16(c[1], qa[2 * x + 1][0], 0u, qa[2 * x + 1][1], 0u, fma_bf16x2(pack4_pair<2>(w[x]), s2, b2), fma_bf16x2(pack4_pair<3>(w[x]), s2, b2));
-                    }
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const int tok = tok0 + nb * 8 + quad * 2 + j;
-                        s[blk][nb][j] = tok < valid ? (c[0][j] + c[1][j]) * a.scale_log2 : -INFINITY;
-                        tmax = fmaxf(tmax, s[blk][nb][j]);
+                        w[y][0] = x.x, w[y][1] = x.y;
                     }
                 }
+                float c[2][4];                          // even and odd steps apart
+#pragma unroll
+                for (int x = 0; x < XW; ++x) {
+                    const uint32_t v0 = fma_bf16x2(pack4_pair<0>(w[0][x]), s2[0], b2[0]), u0 = fma_bf16x2(pack4_pair<0>(w[1][x]), s2[1], b2[1]);
+                    const uint32_t v1 = fma_bf16x2(pack4_pair<1>(w[0][x]), s2[0], b2[0]), u1 = fma_bf16x2(pack4_pair<1>(w[1][x]), s2[1], b2[1]);
+                    const uint32_t v2 = fma_bf16x2(pack4_pair<2>(w[0][x]), s2[0], b2[0]), u2 = fma_bf16x2(pack4_pair<2>(w[1][x]), s2[1], b2[1]);
+                    const uint32_t v3 = fma_bf16x2(pack4_pair<3>(w[0][x]), s2[0], b2[0]), u3 = fma_bf16x2(pack4_pair<3>(w[1][x]), s2[1], b2[1]);
+                    if (x == 0) {
+                        mma_bf16_first(c[0], v0, u0, v1, u1, qa[0][0], qa[0][1]);
+                        mma_bf16_first(c[1], v2, u2, v3, u3, qa[1][0], qa[1][1]);
+                    } else {
+                        mma_bf16(c[0], v0, u0, v1, u1, qa[2 * x][0], qa[2 * x][1]);
+                        mma_bf16(c[1], v2, u2, v3, u3, qa[2 * x + 1][0], qa[2 * x + 1][1]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[blk][i] = c[0][i] + c[1][i];
             }
-            // ---- one online-softmax update of the row over the warp's rows of this tile ----
-            tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 1));
-            tmax = fmaxf(tmax, __shfl_xor_sync(0xffffffffu, tmax, 2));
-            const float m_new = fmaxf(m, tmax);
-            const float alpha = fast_exp2(m - m_new);
-            m = m_new;
-            float psum = 0.f;
+            const bool part = valid < TN;       // the end of a unit
+            if (part) {
+#pragma unroll
+                for (int i = 0; i < BPW * 4; ++i)
+                    if ((i / 4 * WARPS + warp) * 16 + i / 2 % 2 * 8 + row >= valid) s[i / 4][i % 4] = -INFINITY;
+                // Value rows past the end may hold anything (0 * NaN is not 0).  With s = b = 0 their values are zero; only this
+                // warp reads them, and the fence orders the stores before the copy that refills the stage.
+                for (int i = lane; i < BPW * 16; i += 32) {
+                    const int r = (i / 16 * WARPS + warp) * 16 + i % 16;
+                    if (r >= valid) *reinterpret_cast<uint4*>(vs + r * RB) = make_uint4(0u, 0u, 0u, 0u);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            // ---- one online-softmax update of the heads over the warp's rows of this tile (the scale is positive) ----
+            float alpha[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float top = fmaxf(s[0][j], s[0][2 + j]);
+#pragma unroll
+                for (int blk = 1; blk < BPW; ++blk) top = fmaxf(top, fmaxf(s[blk][j], s[blk][2 + j]));
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                const float m_new = fmaxf(m[j], top * a.scale_log2);
+                alpha[j] = fast_exp2(m[j] - m_new);
+                m[j] = m_new;
+                lsum[j] *= alpha[j];
+            }
             // A fragments of P: [block][keys 0..7 or 8..15]: rows 0..7 / rows 8..15 (/ the second product's rows 0..7)
             uint32_t pa[BPW][2], pb[BPW][2], pc[BPW][2];
 #pragma unroll
             for (int blk = 0; blk < BPW; ++blk)
 #pragma unroll
                 for (int nb = 0; nb < 2; ++nb) {
-                    float p0 = fast_exp2(s[blk][nb][0] - m_new), p1 = fast_exp2(s[blk][nb][1] - m_new);
-                    psum += p0 + p1;
+                    float p0 = fast_exp2(fmaf(s[blk][2 * nb], a.scale_log2, -m[0])), p1 = fast_exp2(fmaf(s[blk][2 * nb + 1], a.scale_log2, -m[1]));
+                    lsum[0] += p0;
+                    lsum[1] += p1;
                     const uint32_t hi = take_term(p0, p1), mid = take_term(p0, p1), lo = pack2(p0, p1);
-                    pa[blk][nb] = third ? lo : hi;
-                    pb[blk][nb] = third ? 0u : mid;
-                    pc[blk][nb] = lo;
+                    pa[blk][nb] = transposed(third ? lo : hi);
+                    pb[blk][nb] = transposed(third ? 0u : mid);
+                    if constexpr (WIDE) pc[blk][nb] = transposed(lo);
                 }
-            lsum = fmaf(lsum, alpha, psum);
+            // the head of this lane's row of O: its alpha is with lane row / 2
+            const float alpha0 = __shfl_sync(0xffffffffu, alpha[0], row >> 1), alpha1 = __shfl_sync(0xffffffffu, alpha[1], row >> 1);
+            const float alpha_row = row & 1 ? alpha1 : alpha0;
             // ---- O = alpha O + P V ----
-            if (warp * BPW * 16 + BPW * 16 > valid) {
-                // The end of a unit: rows past it may hold anything (0 * NaN is not 0).  With s = b = 0 their values are zero; only
-                // this warp reads them, and the fence orders the stores before the copy that refills the stage.
-                for (int r = warp * BPW * 16 + lane; r < (warp + 1) * BPW * 16; r += 32)
-                    if (r >= valid) *reinterpret_cast<uint4*>(vs + r * RB) = make_uint4(0u, 0u, 0u, 0u);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-            }
+            const uint64_t alpha2 = pair_of(alpha_row, alpha_row);
+            const unsigned char* vq = vs + (warp * 16 + quad * 2) * RB;       // the first of this lane's rows
             uint32_t s2[BPW][2], b2[BPW][2];       // (s, b) of the keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
             for (int blk = 0; blk < BPW; ++blk)
 #pragma unroll
                 for (int nb = 0; nb < 2; ++nb) {
-                    const unsigned char* vr = vs + ((warp * BPW + blk) * 16 + nb * 8 + quad * 2) * RB + 4 * (row >> 1);
+                    const unsigned char* vr = vq + (blk * WARPS * 16 + nb * 8) * RB + 4 * (row >> 1);
                     const uint32_t h0 = *reinterpret_cast<const uint32_t*>(vr), h1 = *reinterpret_cast<const uint32_t*>(vr + RB);
                     s2[blk][nb] = __byte_perm(h0, h1, 0x5410);
                     b2[blk][nb] = __byte_perm(h0, h1, 0x7632);
@@ -347,7 +394,7 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
                 for (int blk = 0; blk < BPW; ++blk)
 #pragma unroll
                     for (int nb = 0; nb < 2; ++nb) {
-                        const unsigned char* vr = vs + ((warp * BPW + blk) * 16 + nb * 8 + quad * 2) * RB + 16 + row * (D / 16) + 4 * x;
+                        const unsigned char* vr = vq + (blk * WARPS * 16 + nb * 8) * RB + 16 + row * (D / 16) + 4 * x;
                         const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vr), w1 = *reinterpret_cast<const uint32_t*>(vr + RB);
                         w[blk][nb][0] = __byte_perm(w0, w1, 0x5410);
                         w[blk][nb][1] = __byte_perm(w0, w1, 0x7632);
@@ -356,18 +403,18 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
                 for (int half = 0; half < 2; ++half)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float c[4] = {0.f, 0.f, 0.f, 0.f};
+                        float c[4];
 #pragma unroll
                         for (int blk = 0; blk < BPW; ++blk) {
-                            auto pair_of = [&](uint32_t v) { return i == 0 ? pack4_pair<0>(v) : i == 1 ? pack4_pair<1>(v) : i == 2 ? pack4_pair<2>(v) : pack4_pair<3>(v); };
-                            const uint32_t v0 = fma_bf16x2(pair_of(w[blk][0][half]), s2[blk][0], b2[blk][0]);
-                            const uint32_t v1 = fma_bf16x2(pair_of(w[blk][1][half]), s2[blk][1], b2[blk][1]);
-                            mma_bf16(c, pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v0, v1);
+                            auto pair_at = [&](uint32_t v) { return i == 0 ? pack4_pair<0>(v) : i == 1 ? pack4_pair<1>(v) : i == 2 ? pack4_pair<2>(v) : pack4_pair<3>(v); };
+                            const uint32_t v0 = fma_bf16x2(pair_at(w[blk][0][half]), s2[blk][0], b2[blk][0]);
+                            const uint32_t v1 = fma_bf16x2(pair_at(w[blk][1][half]), s2[blk][1], b2[blk][1]);
+                            if (blk == 0) mma_bf16_first(c, pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v0, v1);
+                            else mma_bf16(c, pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v0, v1);
                             if constexpr (WIDE) mma_bf16(c, pc[blk][0], 0u, pc[blk][1], 0u, v0, v1);
                         }
-                        const int nb = 8 * x + 4 * half + i;
-                        o[nb][0] = fmaf(o[nb][0], alpha, c[0] + c[2]);
-                        o[nb][1] = fmaf(o[nb][1], alpha, c[1] + c[3]);
+                        uint64_t& acc = o[8 * x + 4 * half + i];
+                        acc = fma2(acc, alpha2, add2(pair_of(c[0], c[1]), pair_of(c[2], c[3])));
                     }
             }
             __syncwarp();
@@ -381,26 +428,27 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
         const bool whole = finish && ti0 == 0 && piece_tiles == a.tpu;
         const bool head_piece = finish && ti0 == 0 && piece_tiles < a.tpu;
         const bool tail = finish && ti0 > 0;
-        float l = lsum;
-        l += __shfl_xor_sync(0xffffffffu, l, 1);
-        l += __shfl_xor_sync(0xffffffffu, l, 2);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int d = 4; d < 32; d *= 2) lsum[j] += __shfl_xor_sync(0xffffffffu, lsum[j], d);
+        const float m0 = __shfl_sync(0xffffffffu, m[0], row >> 1), m1 = __shfl_sync(0xffffffffu, m[1], row >> 1);
+        const float l0 = __shfl_sync(0xffffffffu, lsum[0], row >> 1), l1 = __shfl_sync(0xffffffffu, lsum[1], row >> 1);
         if constexpr (!WIDE)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) {       // the third term's share, from rows 4..7
-                o[nb][0] += __shfl_down_sync(0xffffffffu, o[nb][0], 16);
-                o[nb][1] += __shfl_down_sync(0xffffffffu, o[nb][1], 16);
-            }
+            for (int nb = 0; nb < NB; ++nb)         // the third term's share, from rows 4..7
+                o[nb] = add2(o[nb], __shfl_down_sync(0xffffffffu, o[nb], 16));
         named_bar_sync(1, S::CONSUMERS);
         if (row < G) {
             float* dst = scratch + (warp * 8 + row) * (D + 2);
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                dst[quad * 2 * NB + nb] = o[nb][0];
-                dst[(quad * 2 + 1) * NB + nb] = o[nb][1];
+                dst[quad * 2 * NB + nb] = low_of(o[nb]);
+                dst[(quad * 2 + 1) * NB + nb] = high_of(o[nb]);
             }
             if (quad == 0) {
-                dst[D] = m;
-                dst[D + 1] = l;
+                dst[D] = row & 1 ? m1 : m0;
+                dst[D + 1] = row & 1 ? l1 : l0;
             }
         }
         if (head_piece && !mbar_wait_bounded(head_bar, 0, abort_flag, a.status, a.wait_ns)) return;

@@ -239,7 +239,7 @@ def test_large_tiles_and_the_hand_over():
         cache.append(0, k, v)
         q = torch.randn(units_b, Hkv * G, D, device="cuda", generator=g).bfloat16()
         out = cache.decode_attention(0, q)
-        assert cache.last_launch()["tile_rows"] == 256 and cache.last_launch()["kernel"] == 3
+        assert cache.last_launch()["tile_rows"] > 64 and cache.last_launch()["kernel"] == 3
         cache.set_option(KVS_OPT_FINISH_IN_KERNEL, 0)
         again = cache.decode_attention(0, q)
         some = [0, units_b // 2, units_b - 1]
