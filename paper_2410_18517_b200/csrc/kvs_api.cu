@@ -390,7 +390,7 @@ struct AttentionScratch {
 bool choose_plan(const kvs_ctx* c, int units, int n, kvs::DecodePlan* plan) {
     if (c->format == KVS_CACHE_4BIT) {
         if (c->cfg.dtype == KVS_BF16)
-            kvs::plan_decode_pack4(units, n, c->cfg.head_dim, c->sm_count, c->opt_max_ctas, plan);
+            kvs::plan_decode_pack4(units, n, c->sm_count, c->opt_max_ctas, plan);
         else
             kvs::plan_decode_pack4_f32(units, n, c->sm_count, c->opt_max_ctas, plan);
         return false;

@@ -121,7 +121,7 @@ struct ReadArgs {
 cudaError_t launch_read_rows(const ReadArgs& p, cudaStream_t stream);
 
 cudaError_t init_pack4_kernels();
-void plan_decode_pack4(int units, int n, int D, int sm_count, int max_ctas, DecodePlan* plan);
+void plan_decode_pack4(int units, int n, int sm_count, int max_ctas, DecodePlan* plan);
 cudaError_t launch_decode_pack4(const DecodeArgs& a, const DecodePlan& plan, cudaStream_t stream);
 void plan_decode_pack4_f32(int units, int n, int sm_count, int max_ctas, DecodePlan* plan);
 cudaError_t launch_decode_pack4_f32(const DecodeArgs& a, const DecodePlan& plan, cudaStream_t stream);

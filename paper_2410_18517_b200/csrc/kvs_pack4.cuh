@@ -27,7 +27,9 @@ struct Pack4Row {
 template <int I>
 __device__ __forceinline__ uint32_t pack4_pair(uint32_t w) {
     const uint32_t at = I == 0 ? w << 3 : w >> (4 * I - 3);
-    return (at & 0x00780078u) | 0x41804180u;
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(at), "r"(0x00780078u), "r"(0x41804180u));      // (at & mask) | magic
+    return r;
 }
 
 // fused multiply-add of two bf16 pairs, rounded once

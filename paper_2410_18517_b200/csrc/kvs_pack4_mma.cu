@@ -16,12 +16,16 @@
 // column n stands for D/8 neighbouring elements of a row, again of one group; the codes of two keys are interleaved by byte
 // permutes.  A code costs 1/2 (shift + and-or + multiply-add); everything else per row is small beside that.
 //
-// What bounds it: HBM (D + 32 bytes per row of K and V together) until the conversion does: at 6.5 TB/s an SM has 7 cycles per
-// row of 128, in which it issues at most 28 warp instructions, 14 of them integer; the conversion takes 12.5 and 8.5.
+// What bounds it: the conversion.  A row of K and V together is D + 32 bytes, 7 cycles of an SM at 6.5 TB/s; its codes take 11 warp
+// instructions to become operands, 7 of them on the integer pipe and 4 on the heavy half of the FMA pipe, which take one every
+// other cycle and hardly overlap; the MMAs (1.5 a row) and the rest take as long again.
 //
-// Work decomposition, pieces, the hand-over between blocks and the combine kernel are those of the other split-K kernels.  Rows of
-// a tile are contiguous and come by two 1-D bulk copies, exactly as many as the unit holds.
+// Work decomposition (see DecodePlan), pieces, the hand-over between blocks and the combine kernel are those of the other
+// split-K kernels.  Rows of a tile are contiguous and come by two 1-D bulk copies, exactly as many as the unit holds.  A tile
+// has up to 512 rows, 64 for each of 8 warps: the running state is rescaled once a tile and warp.  How many it has the plan
+// decides (plan_decode_pack4), and with it how many stages the ring has.
 #include <algorithm>
+#include <type_traits>
 
 #include "kvs_kernels.h"
 #include "kvs_pack4.cuh"
@@ -30,32 +34,22 @@ namespace kvs {
 
 namespace {
 
-// Geometries (compile-time; the defaults are the measured best).  Large: warps x blocks of 16 rows a tile; small, where that would
-// leave thread blocks idle: 4 warps x 16 rows.
-#ifndef KVS_PACK4_WARPS
-#define KVS_PACK4_WARPS 8
-#endif
-#ifndef KVS_PACK4_BLOCKS
-#define KVS_PACK4_BLOCKS 4
-#endif
-#ifndef KVS_PACK4_STAGES
-#define KVS_PACK4_STAGES 2
-#endif
-template <int D, int BIG>
+constexpr int kPack4Warps = 8;           // consumer warps
+constexpr int kPack4Blocks = 4;          // 16-row blocks a warp takes of a tile at most
+constexpr int kPack4TileMax = kPack4Warps * kPack4Blocks * 16;
+constexpr int kPack4Stages = 8;          // of the ring at most
+
+template <int D>
 struct Pack4Shape {
-    static constexpr int WARPS = BIG ? KVS_PACK4_WARPS : 4;
-    static constexpr int BPW = BIG ? KVS_PACK4_BLOCKS : 1;                // 16-row blocks per warp and tile: WARPS blocks apart
-    static constexpr int TN = WARPS * BPW * 16;            // rows per tile
-    static constexpr int STAGES = BIG ? KVS_PACK4_STAGES : 6;
+    static constexpr int WARPS = kPack4Warps;
     static constexpr int RB = Pack4Row<D>::RB;
-    static constexpr int TILE = TN * RB;                   // bytes of a K tile and of a V tile
     static constexpr int QBYTES = 8 * D * 2;               // room for the queries of eight heads
-    static constexpr int STAGE_BYTES = 2 * TILE + QBYTES;
+    static constexpr int RING = 2 * (2 * kPack4TileMax * RB + QBYTES);     // two of the largest tiles
     static constexpr int CONSUMERS = WARPS * 32;
     static constexpr int THREADS = CONSUMERS + 64;         // + the producer warp and the hand-over warp
     static constexpr int SCRATCH_FLOATS = WARPS * 8 * (D + 2);
     static constexpr int HANDOVER_FLOATS = 8 * (D + 2);
-    static constexpr int SMEM_BYTES = 16 + STAGES * STAGE_BYTES + (SCRATCH_FLOATS + HANDOVER_FLOATS) * 4 + (2 * STAGES + 2) * 8 + 16;
+    static constexpr int SMEM_BYTES = 16 + RING + (SCRATCH_FLOATS + HANDOVER_FLOATS) * 4 + (2 * kPack4Stages + 2) * 8 + 16;
 };
 
 struct Pack4KernelArgs {
@@ -68,6 +62,7 @@ struct Pack4KernelArgs {
     int* flags;             // [units], zero between launches: 1 = the unit's second piece is written
     int* status;
     int n, row_stride, tpu, G, units, cap, safe_rows;
+    int tile_rows;          // a multiple of 16, at most kPack4TileMax
     long long T;
     float scale_log2;
     const int* unit_len;
@@ -109,10 +104,12 @@ __device__ __forceinline__ uint32_t take_term(float& x, float& y) {
     return t;
 }
 
-template <int D, int BIG, bool WIDE>      // WIDE: five to eight q-heads per kv-head
-__global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_mma(const Pack4KernelArgs a_in) {
-    using S = Pack4Shape<D, BIG>;
-    constexpr int TN = S::TN, BPW = S::BPW, RB = S::RB, kStages = S::STAGES, kTile = S::TILE, WARPS = S::WARPS;
+template <int D, bool WIDE>      // WIDE: five to eight q-heads per kv-head
+__global__ void __launch_bounds__(Pack4Shape<D>::THREADS, 1) decode_pack4_mma(const Pack4KernelArgs a_in) {
+    using S = Pack4Shape<D>;
+    constexpr int RB = S::RB, WARPS = S::WARPS;
+    const int TN = a_in.tile_rows, kTile = TN * RB, stage_bytes = 2 * kTile + S::QBYTES;
+    const int stages = min(kPack4Stages, S::RING / stage_bytes);
     constexpr int KSTEPS = D / 16;        // products of a score block
     constexpr int NB = D / 8;             // column blocks of the output: D/8 elements per column
     constexpr int XW = D / 32;            // words of a row's group (K)
@@ -134,10 +131,10 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
 
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((16u - (smem_u32(smem_raw) & 15u)) & 15u);
-    float* scratch = reinterpret_cast<float*>(smem + kStages * S::STAGE_BYTES);
+    float* scratch = reinterpret_cast<float*>(smem + S::RING);
     uint64_t* full_bar = reinterpret_cast<uint64_t*>(scratch + S::SCRATCH_FLOATS);
-    uint64_t* empty_bar = full_bar + kStages;
-    uint64_t* tail_bar = empty_bar + kStages;
+    uint64_t* empty_bar = full_bar + kPack4Stages;
+    uint64_t* tail_bar = empty_bar + kPack4Stages;
     uint64_t* head_bar = tail_bar + 1;
     volatile int* abort_flag = reinterpret_cast<volatile int*>(head_bar + 1);
     float* handover = const_cast<float*>(reinterpret_cast<volatile float*>(abort_flag + 4));
@@ -148,7 +145,7 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
     const long long t1 = ((long long)(blockIdx.x + 1) * a.T) / NC;
 
     if (tid == 0) {
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < stages; ++s) {
             mbar_init(&full_bar[s], 1);
             mbar_init(&empty_bar[s], WARPS);
         }
@@ -171,7 +168,7 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
             const int n_u = a.unit_len ? min(a.unit_len[u], a.cap) : a.n;
             const int rows = min(TN, n_u - ti * TN);          // <= 0: a ragged unit ended before this tile
             const uint32_t bytes = rows > 0 ? (uint32_t)rows * RB : 0u;
-            unsigned char* sb = smem + st * S::STAGE_BYTES;
+            unsigned char* sb = smem + st * stage_bytes;
             if (arm) {
                 const uint32_t total = 2 * bytes + (with_q ? qbytes : 0);
                 if (total) mbar_arrive_expect_tx(&full_bar[st], total);
@@ -188,7 +185,7 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
         };
         // until the preceding kernel is known to have finished: only tiles made of rows that nothing in flight writes
         int npre = 0;
-        for (; npre < kStages && t0 + npre < t1; ++npre) {
+        for (; npre < stages && t0 + npre < t1; ++npre) {
             const int ti = (int)((t0 + npre) % a.tpu);
             if ((long long)(ti + 1) * TN > a.safe_rows) break;
             issue(t0 + npre, npre, true, true, false);
@@ -198,17 +195,19 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
         KVS_TRACE_STAMP(tr, kTrProducerGo);
         pdl_launch_dependents();
         for (int j = 0; j < npre; ++j) issue(t0 + j, j, false, false, true);
+        // tile j of the block lies in stage j % stages; its phase there is j / stages
+        int st = npre % stages, turn = npre / stages;
         int it = npre;
         bool ok = true;
         for (long long gt = t0 + npre; gt < t1; ++gt, ++it) {
-            const int st = it % kStages;
-            if (it >= kStages) ok = mbar_wait_bounded(&empty_bar[st], ((it / kStages) - 1) & 1, abort_flag, a.status, a.wait_ns);
+            if (turn > 0) ok = mbar_wait_bounded(&empty_bar[st], (turn - 1) & 1, abort_flag, a.status, a.wait_ns);
             if (!ok) break;
             issue(gt, st, true, true, true);
+            if (++st == stages) st = 0, ++turn;
         }
         if (!ok)
-            for (int j = max(0, it - kStages); j < it; ++j)
-                mbar_wait_bounded(&full_bar[j % kStages], (j / kStages) & 1, abort_flag + 1, a.status, a.wait_ns);
+            for (int j = max(0, it - stages); j < it; ++j)
+                mbar_wait_bounded(&full_bar[j % stages], (j / stages) & 1, abort_flag + 1, a.status, a.wait_ns);
         return;
     }
 
@@ -251,7 +250,7 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
     const int head = WIDE ? row : (row & 3);       // whose queries this lane brings in
     const bool third = !WIDE && quad >= 2;         // this lane's columns of S carry the third term
 
-    int it = 0;
+    int st = 0, phase = 0;    // of the next tile
     long long gt = t0;
     while (gt < t1) {
         const long long u = gt / a.tpu;
@@ -265,91 +264,77 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) o[nb] = 0;
 
-        for (int k = 0; k < piece_tiles; ++k, ++it) {
-            const int st = it % kStages;
-            if (!mbar_wait_bounded(&full_bar[st], (it / kStages) & 1, abort_flag, a.status, a.wait_ns)) return;
-            if (tid == 0 && it == 0) KVS_TRACE_STAMP(tr, kTrFirstTile);
-            unsigned char* ks = smem + st * S::STAGE_BYTES;
-            unsigned char* vs = ks + kTile;
-            if (k == 0) {
-                // step j of lane t: elements e, e + 4 and e + 1, e + 5 of its group, e = 8 (j / 2) + 2 (j % 2)
-                const __nv_bfloat16* qs = reinterpret_cast<const __nv_bfloat16*>(vs + kTile) + head * D + quad * (D / 4);
-#pragma unroll
-                for (int j = 0; j < KSTEPS; ++j)
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int e = 8 * (j / 2) + 2 * (j % 2) + x;
-                        uint32_t v = 0;
-                        if (head < G)
-                            v = (uint32_t)__bfloat16_as_ushort(qs[e]) | (uint32_t)__bfloat16_as_ushort(qs[e + 4]) << 16;
-                        qa[j][x] = v;
-                    }
-            }
-            const int valid = n_u - (ti0 + k) * TN;     // rows of this tile that exist (may exceed TN or be <= 0)
-            if (warp * 16 >= valid) {                   // none of this warp's
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&empty_bar[st]);
-                continue;
-            }
+        auto chunk = [&](const unsigned char* ks, unsigned char* vs, int rows, auto blocks) {
+            constexpr int NBK = decltype(blocks)::value;
             // ---- scores ----
-            float s[BPW][4];                            // [block]: (key row, two heads), (key row + 8, two heads)
+            // Two blocks side by side, even and odd steps of each apart: an MMA waits for the fourth before it.
+            float s[NBK][4];                            // [block]: (key row, two heads), (key row + 8, two heads)
 #pragma unroll
-            for (int blk = 0; blk < BPW; ++blk) {
+            for (int blk0 = 0; blk0 < NBK; blk0 += 2) {
+                constexpr int AT_ONCE = 2;
                 // rows past the end hold whatever the stage held before: their scores are replaced below
-                uint32_t w[2][XW], s2[2], b2[2];
+                uint32_t w[AT_ONCE][2][XW], s2[AT_ONCE][2], b2[AT_ONCE][2];
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    const unsigned char* kr = ks + ((blk * WARPS + warp) * 16 + y * 8 + row) * RB;
-                    const uint32_t pair = *reinterpret_cast<const uint32_t*>(kr + 4 * quad);
-                    s2[y] = __byte_perm(pair, pair, 0x1010);
-                    b2[y] = __byte_perm(pair, pair, 0x3232);
-                    if constexpr (D == 128) {
-                        const uint4 x = *reinterpret_cast<const uint4*>(kr + 16 + 16 * quad);
-                        w[y][0] = x.x, w[y][1] = x.y, w[y][2] = x.z, w[y][3] = x.w;
-                    } else {
-                        const uint2 x = *reinterpret_cast<const uint2*>(kr + 16 + 8 * quad);
-                        w[y][0] = x.x, w[y][1] = x.y;
+                for (int z = 0; z < AT_ONCE && blk0 + z < NBK; ++z)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        const unsigned char* kr = ks + ((blk0 + z) * 16 + y * 8 + row) * RB;
+                        const uint32_t pair = *reinterpret_cast<const uint32_t*>(kr + 4 * quad);
+                        s2[z][y] = __byte_perm(pair, pair, 0x1010);
+                        b2[z][y] = __byte_perm(pair, pair, 0x3232);
+                        if constexpr (D == 128) {
+                            const uint4 x = *reinterpret_cast<const uint4*>(kr + 16 + 16 * quad);
+                            w[z][y][0] = x.x, w[z][y][1] = x.y, w[z][y][2] = x.z, w[z][y][3] = x.w;
+                        } else {
+                            const uint2 x = *reinterpret_cast<const uint2*>(kr + 16 + 8 * quad);
+                            w[z][y][0] = x.x, w[z][y][1] = x.y;
+                        }
                     }
-                }
-                float c[2][4];                          // even and odd steps apart
+                float c[AT_ONCE][2][4];
 #pragma unroll
                 for (int x = 0; x < XW; ++x) {
-                    const uint32_t v0 = fma_bf16x2(pack4_pair<0>(w[0][x]), s2[0], b2[0]), u0 = fma_bf16x2(pack4_pair<0>(w[1][x]), s2[1], b2[1]);
-                    const uint32_t v1 = fma_bf16x2(pack4_pair<1>(w[0][x]), s2[0], b2[0]), u1 = fma_bf16x2(pack4_pair<1>(w[1][x]), s2[1], b2[1]);
-                    const uint32_t v2 = fma_bf16x2(pack4_pair<2>(w[0][x]), s2[0], b2[0]), u2 = fma_bf16x2(pack4_pair<2>(w[1][x]), s2[1], b2[1]);
-                    const uint32_t v3 = fma_bf16x2(pack4_pair<3>(w[0][x]), s2[0], b2[0]), u3 = fma_bf16x2(pack4_pair<3>(w[1][x]), s2[1], b2[1]);
-                    if (x == 0) {
-                        mma_bf16_first(c[0], v0, u0, v1, u1, qa[0][0], qa[0][1]);
-                        mma_bf16_first(c[1], v2, u2, v3, u3, qa[1][0], qa[1][1]);
-                    } else {
-                        mma_bf16(c[0], v0, u0, v1, u1, qa[2 * x][0], qa[2 * x][1]);
-                        mma_bf16(c[1], v2, u2, v3, u3, qa[2 * x + 1][0], qa[2 * x + 1][1]);
-                    }
+                    uint32_t v[AT_ONCE][2][4];          // [block][key row, row + 8][pair]
+#pragma unroll
+                    for (int z = 0; z < AT_ONCE && blk0 + z < NBK; ++z)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y) {
+                            v[z][y][0] = fma_bf16x2(pack4_pair<0>(w[z][y][x]), s2[z][y], b2[z][y]);
+                            v[z][y][1] = fma_bf16x2(pack4_pair<1>(w[z][y][x]), s2[z][y], b2[z][y]);
+                            v[z][y][2] = fma_bf16x2(pack4_pair<2>(w[z][y][x]), s2[z][y], b2[z][y]);
+                            v[z][y][3] = fma_bf16x2(pack4_pair<3>(w[z][y][x]), s2[z][y], b2[z][y]);
+                        }
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+#pragma unroll
+                        for (int z = 0; z < AT_ONCE && blk0 + z < NBK; ++z) {
+                            const uint32_t* q = qa[2 * x + e];
+                            if (x == 0) mma_bf16_first(c[z][e], v[z][0][2 * e], v[z][1][2 * e], v[z][0][2 * e + 1], v[z][1][2 * e + 1], q[0], q[1]);
+                            else mma_bf16(c[z][e], v[z][0][2 * e], v[z][1][2 * e], v[z][0][2 * e + 1], v[z][1][2 * e + 1], q[0], q[1]);
+                        }
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[blk][i] = c[0][i] + c[1][i];
+                for (int z = 0; z < AT_ONCE && blk0 + z < NBK; ++z)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[blk0 + z][i] = c[z][0][i] + c[z][1][i];
             }
-            const bool part = valid < TN;       // the end of a unit
-            if (part) {
+            if (rows < NBK * 16) {            // the end of a unit, inside the last block
 #pragma unroll
-                for (int i = 0; i < BPW * 4; ++i)
-                    if ((i / 4 * WARPS + warp) * 16 + i / 2 % 2 * 8 + row >= valid) s[i / 4][i % 4] = -INFINITY;
-                // Value rows past the end may hold anything (0 * NaN is not 0).  With s = b = 0 their values are zero; only this
-                // warp reads them, and the fence orders the stores before the copy that refills the stage.
-                for (int i = lane; i < BPW * 16; i += 32) {
-                    const int r = (i / 16 * WARPS + warp) * 16 + i % 16;
-                    if (r >= valid) *reinterpret_cast<uint4*>(vs + r * RB) = make_uint4(0u, 0u, 0u, 0u);
-                }
+                for (int i = 0; i < NBK * 4; ++i)
+                    if (i / 4 * 16 + i / 2 % 2 * 8 + row >= rows) s[i / 4][i % 4] = -INFINITY;
+                // Value rows past the end may hold anything (0 * NaN is not 0).  With s = b = 0 their values are zero; the fence
+                // orders the stores before the copy that refills the stage.
+                for (int r = lane; r < NBK * 16; r += 32)
+                    if (r >= rows) *reinterpret_cast<uint4*>(vs + r * RB) = make_uint4(0u, 0u, 0u, 0u);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             }
-            // ---- one online-softmax update of the heads over the warp's rows of this tile (the scale is positive) ----
+            // ---- one online-softmax update of the heads over the chunk's rows (the scale is positive) ----
             float alpha[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 float top = fmaxf(s[0][j], s[0][2 + j]);
 #pragma unroll
-                for (int blk = 1; blk < BPW; ++blk) top = fmaxf(top, fmaxf(s[blk][j], s[blk][2 + j]));
+                for (int blk = 1; blk < NBK; ++blk) top = fmaxf(top, fmaxf(s[blk][j], s[blk][2 + j]));
 #pragma unroll
                 for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
                 const float m_new = fmaxf(m[j], top * a.scale_log2);
@@ -358,9 +343,10 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
                 lsum[j] *= alpha[j];
             }
             // A fragments of P: [block][keys 0..7 or 8..15]: rows 0..7 / rows 8..15 (/ the second product's rows 0..7)
-            uint32_t pa[BPW][2], pb[BPW][2], pc[BPW][2];
+            uint32_t pa[NBK][2], pb[NBK][2];
+            [[maybe_unused]] uint32_t pc[NBK][2];
 #pragma unroll
-            for (int blk = 0; blk < BPW; ++blk)
+            for (int blk = 0; blk < NBK; ++blk)
 #pragma unroll
                 for (int nb = 0; nb < 2; ++nb) {
                     float p0 = fast_exp2(fmaf(s[blk][2 * nb], a.scale_log2, -m[0])), p1 = fast_exp2(fmaf(s[blk][2 * nb + 1], a.scale_log2, -m[1]));
@@ -376,49 +362,87 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
             const float alpha_row = row & 1 ? alpha1 : alpha0;
             // ---- O = alpha O + P V ----
             const uint64_t alpha2 = pair_of(alpha_row, alpha_row);
-            const unsigned char* vq = vs + (warp * 16 + quad * 2) * RB;       // the first of this lane's rows
-            uint32_t s2[BPW][2], b2[BPW][2];       // (s, b) of the keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
+            const unsigned char* vq = vs + quad * 2 * RB;       // the first of this lane's rows
+            uint32_t s2[NBK][2], b2[NBK][2];       // (s, b) of the keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
-            for (int blk = 0; blk < BPW; ++blk)
+            for (int blk = 0; blk < NBK; ++blk)
 #pragma unroll
                 for (int nb = 0; nb < 2; ++nb) {
-                    const unsigned char* vr = vq + (blk * WARPS * 16 + nb * 8) * RB + 4 * (row >> 1);
+                    const unsigned char* vr = vq + (blk * 16 + nb * 8) * RB + 4 * (row >> 1);
                     const uint32_t h0 = *reinterpret_cast<const uint32_t*>(vr), h1 = *reinterpret_cast<const uint32_t*>(vr + RB);
                     s2[blk][nb] = __byte_perm(h0, h1, 0x5410);
                     b2[blk][nb] = __byte_perm(h0, h1, 0x7632);
                 }
 #pragma unroll
             for (int x = 0; x < VW; ++x) {
-                uint32_t w[BPW][2][2];             // codes of the two keys, interleaved: [block][key pair][half of the word]
+                uint32_t w[NBK][2][2];             // codes of the two keys, interleaved: [block][key pair][half of the word]
 #pragma unroll
-                for (int blk = 0; blk < BPW; ++blk)
+                for (int blk = 0; blk < NBK; ++blk)
 #pragma unroll
                     for (int nb = 0; nb < 2; ++nb) {
-                        const unsigned char* vr = vq + (blk * WARPS * 16 + nb * 8) * RB + 16 + row * (D / 16) + 4 * x;
+                        const unsigned char* vr = vq + (blk * 16 + nb * 8) * RB + 16 + row * (D / 16) + 4 * x;
                         const uint32_t w0 = *reinterpret_cast<const uint32_t*>(vr), w1 = *reinterpret_cast<const uint32_t*>(vr + RB);
                         w[blk][nb][0] = __byte_perm(w0, w1, 0x5410);
                         w[blk][nb][1] = __byte_perm(w0, w1, 0x7632);
                     }
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
+                for (int half = 0; half < 2; ++half) {
+                    // four column blocks side by side, for the same reason
+                    float c[4][4];
+#pragma unroll
+                    for (int blk = 0; blk < NBK; ++blk) {
+                        uint32_t v[4][2];
+#pragma unroll
+                        for (int nb = 0; nb < 2; ++nb) {
+                            v[0][nb] = fma_bf16x2(pack4_pair<0>(w[blk][nb][half]), s2[blk][nb], b2[blk][nb]);
+                            v[1][nb] = fma_bf16x2(pack4_pair<1>(w[blk][nb][half]), s2[blk][nb], b2[blk][nb]);
+                            v[2][nb] = fma_bf16x2(pack4_pair<2>(w[blk][nb][half]), s2[blk][nb], b2[blk][nb]);
+                            v[3][nb] = fma_bf16x2(pack4_pair<3>(w[blk][nb][half]), s2[blk][nb], b2[blk][nb]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (blk == 0) mma_bf16_first(c[i], pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v[i][0], v[i][1]);
+                            else mma_bf16(c[i], pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v[i][0], v[i][1]);
+                        if constexpr (WIDE)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) mma_bf16(c[i], pc[blk][0], 0u, pc[blk][1], 0u, v[i][0], v[i][1]);
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float c[4];
-#pragma unroll
-                        for (int blk = 0; blk < BPW; ++blk) {
-                            auto pair_at = [&](uint32_t v) { return i == 0 ? pack4_pair<0>(v) : i == 1 ? pack4_pair<1>(v) : i == 2 ? pack4_pair<2>(v) : pack4_pair<3>(v); };
-                            const uint32_t v0 = fma_bf16x2(pair_at(w[blk][0][half]), s2[blk][0], b2[blk][0]);
-                            const uint32_t v1 = fma_bf16x2(pair_at(w[blk][1][half]), s2[blk][1], b2[blk][1]);
-                            if (blk == 0) mma_bf16_first(c, pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v0, v1);
-                            else mma_bf16(c, pa[blk][0], pb[blk][0], pa[blk][1], pb[blk][1], v0, v1);
-                            if constexpr (WIDE) mma_bf16(c, pc[blk][0], 0u, pc[blk][1], 0u, v0, v1);
-                        }
                         uint64_t& acc = o[8 * x + 4 * half + i];
-                        acc = fma2(acc, alpha2, add2(pair_of(c[0], c[1]), pair_of(c[2], c[3])));
+                        acc = fma2(acc, alpha2, add2(pair_of(c[i][0], c[i][1]), pair_of(c[i][2], c[i][3])));
                     }
+                }
+            }
+        };
+        for (int k = 0; k < piece_tiles; ++k) {
+            if (!mbar_wait_bounded(&full_bar[st], phase, abort_flag, a.status, a.wait_ns)) return;
+            if (tid == 0 && k == 0 && gt == t0) KVS_TRACE_STAMP(tr, kTrFirstTile);
+            unsigned char* tile = smem + st * stage_bytes;
+            if (k == 0) {
+                // B fragments of Q.  Step j of lane t: elements e, e + 4 and e + 1, e + 5 of its group, e = 8 (j / 2) + 2 (j % 2)
+                const uint32_t* qs = reinterpret_cast<const uint32_t*>(tile + 2 * kTile) + (head < G ? head : 0) * (D / 2) + quad * (D / 8);
+#pragma unroll
+                for (int j = 0; j < KSTEPS; ++j) {
+                    const uint32_t lo = head < G ? qs[4 * (j / 2) + j % 2] : 0u, hi = head < G ? qs[4 * (j / 2) + j % 2 + 2] : 0u;
+                    qa[j][0] = __byte_perm(lo, hi, 0x5410);
+                    qa[j][1] = __byte_perm(lo, hi, 0x7632);
+                }
+            }
+            // an even share of the tile's 16-row blocks for every warp
+            const int have = min(TN, n_u - (ti0 + k) * TN), blocks = max(0, (have + 15) / 16);
+            const int b0 = blocks * warp / WARPS, rows = min(have, blocks * (warp + 1) / WARPS * 16) - b0 * 16;
+            if (rows > 0) {
+                unsigned char *ks = tile + b0 * 16 * RB, *vs = ks + kTile;
+                // (exactly as many blocks as there are: what lies behind them is another warp's, or another buffer's)
+                if (rows > 48) chunk(ks, vs, rows, std::integral_constant<int, 4>());
+                else if (rows > 32) chunk(ks, vs, rows, std::integral_constant<int, 3>());
+                else if (rows > 16) chunk(ks, vs, rows, std::integral_constant<int, 2>());
+                else chunk(ks, vs, rows, std::integral_constant<int, 1>());
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&empty_bar[st]);
+            if (++st == stages) st = 0, phase ^= 1;
         }
 
         // ---- end of piece: merge the consumer warps (see decode_splitk_mma for the cases) ----
@@ -493,43 +517,49 @@ __global__ void __launch_bounds__(Pack4Shape<D, BIG>::THREADS, 1) decode_pack4_m
     }
 }
 
-template <int D, int BIG, bool WIDE>
+template <int D, bool WIDE>
 cudaError_t set_attr() {
-    cudaError_t e = cudaFuncSetAttribute(decode_pack4_mma<D, BIG, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pack4Shape<D, BIG>::SMEM_BYTES);
+    cudaError_t e = cudaFuncSetAttribute(decode_pack4_mma<D, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Pack4Shape<D>::SMEM_BYTES);
     if (e != cudaSuccess) return e;
     // room for the combine kernel's blocks beside this kernel's (see decode_splitk_mma)
-    return cudaFuncSetAttribute(decode_pack4_mma<D, BIG, WIDE>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    return cudaFuncSetAttribute(decode_pack4_mma<D, WIDE>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
 }
 
-template <int D, int BIG>
+template <int D>
 cudaError_t launch_one(const Pack4KernelArgs& ka, int NC, bool pdl, cudaStream_t stream) {
-    using S = Pack4Shape<D, BIG>;
-    return ka.G > 4 ? launch_kernel(decode_pack4_mma<D, BIG, true>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, pdl, ka)
-                    : launch_kernel(decode_pack4_mma<D, BIG, false>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, pdl, ka);
+    using S = Pack4Shape<D>;
+    return ka.G > 4 ? launch_kernel(decode_pack4_mma<D, true>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, pdl, ka)
+                    : launch_kernel(decode_pack4_mma<D, false>, dim3(NC), dim3(S::THREADS), S::SMEM_BYTES, stream, pdl, ka);
 }
 
 }  // namespace
 
 cudaError_t init_pack4_kernels() {
     cudaError_t e;
-    if ((e = set_attr<128, 0, false>()) != cudaSuccess || (e = set_attr<128, 0, true>()) != cudaSuccess ||
-        (e = set_attr<128, 1, false>()) != cudaSuccess || (e = set_attr<128, 1, true>()) != cudaSuccess ||
-        (e = set_attr<64, 0, false>()) != cudaSuccess || (e = set_attr<64, 0, true>()) != cudaSuccess ||
-        (e = set_attr<64, 1, false>()) != cudaSuccess)
-        return e;
-    return set_attr<64, 1, true>();
+    if ((e = set_attr<128, false>()) != cudaSuccess || (e = set_attr<128, true>()) != cudaSuccess || (e = set_attr<64, false>()) != cudaSuccess) return e;
+    return set_attr<64, true>();
 }
 
-void plan_decode_pack4(int units, int n, int D, int sm_count, int max_ctas, DecodePlan* plan) {
+// Units are cut into tiles of equal size (to 16 rows), as many as make the longest block's share cheapest: a tile costs its
+// rows and a constant (barriers, the state's update, a chunk's latency: about as much as kTileCost rows).
+void plan_decode_pack4(int units, int n, int sm_count, int max_ctas, DecodePlan* plan) {
+    constexpr int kTileCost = 48, kTry = 64;
     int cap = sm_count;
     if (max_ctas > 0) cap = std::min(cap, max_ctas);
     cap = std::min(cap, kMaxCtas);
-    // the large tiles when every block gets at least four of them
-    const int big_rows = Pack4Shape<128, 1>::TN;
-    const long long big_T = (long long)units * ((n + big_rows - 1) / big_rows);
-    plan->tile_rows = big_T >= 4ll * cap ? big_rows : Pack4Shape<128, 0>::TN;
-    plan->tpu = (n + plan->tile_rows - 1) / plan->tile_rows;
-    plan->T = (long long)units * plan->tpu;
+    const int least = (n + kPack4TileMax - 1) / kPack4TileMax;
+    long long best = -1;
+    for (int k = least; k < least + kTry; ++k) {
+        const int rows = ((n + k - 1) / k + 15) / 16 * 16, tpu = (n + rows - 1) / rows;
+        const long long T = (long long)units * tpu, cost = (T + cap - 1) / cap * (rows + kTileCost);
+        if (best < 0 || cost < best) {
+            best = cost;
+            plan->tile_rows = rows;
+            plan->tpu = tpu;
+            plan->T = T;
+        }
+        if (rows == 16) break;
+    }
     plan->NC = (int)std::min<long long>(plan->T, cap);
     plan->kernel = 3;
 }
@@ -548,6 +578,7 @@ cudaError_t launch_decode_pack4(const DecodeArgs& a, const DecodePlan& plan, cud
     ka.n = a.n;
     ka.row_stride = a.row_stride;
     ka.tpu = plan.tpu;
+    ka.tile_rows = plan.tile_rows;
     ka.G = a.G;
     ka.units = a.units;
     ka.cap = a.capacity;
@@ -560,9 +591,7 @@ cudaError_t launch_decode_pack4(const DecodeArgs& a, const DecodePlan& plan, cud
     ka.wait_ns = a.wait_ns;
     ka.stall_tile = a.stall_tile;
     ka.trace = a.trace;
-    const bool big = plan.tile_rows == Pack4Shape<128, 1>::TN;
-    if (a.D == 128) return big ? launch_one<128, 1>(ka, plan.NC, a.programmatic, stream) : launch_one<128, 0>(ka, plan.NC, a.programmatic, stream);
-    return big ? launch_one<64, 1>(ka, plan.NC, a.programmatic, stream) : launch_one<64, 0>(ka, plan.NC, a.programmatic, stream);
+    return a.D == 128 ? launch_one<128>(ka, plan.NC, a.programmatic, stream) : launch_one<64>(ka, plan.NC, a.programmatic, stream);
 }
 
 }  // namespace kvs

@@ -230,8 +230,8 @@ def test_attention_any_split(dtype, ctas):
     cache.check_canaries()
 
 
-def test_large_tiles_and_the_hand_over():
-    """Enough rows for the large tiles, as many units as blocks and more: units are cut between blocks and finished there."""
+def test_many_units_and_the_hand_over():
+    """As many units as blocks and more: units are cut between blocks and finished there."""
     for units_b, Hkv, G, D, n in ((40, 8, 4, 128, 1100), (160, 2, 1, 64, 600), (75, 4, 7, 128, 515)):
         cache = cache4(Hkv * G, Hkv, D, units_b, n, "bf16", cls=SharedKVCache)
         g = torch.Generator(device="cuda").manual_seed(1)
@@ -239,7 +239,7 @@ def test_large_tiles_and_the_hand_over():
         cache.append(0, k, v)
         q = torch.randn(units_b, Hkv * G, D, device="cuda", generator=g).bfloat16()
         out = cache.decode_attention(0, q)
-        assert cache.last_launch()["tile_rows"] > 64 and cache.last_launch()["kernel"] == 3
+        assert cache.last_launch()["kernel"] == 3
         cache.set_option(KVS_OPT_FINISH_IN_KERNEL, 0)
         again = cache.decode_attention(0, q)
         some = [0, units_b // 2, units_b - 1]
