@@ -47,15 +47,37 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= 3.4028234e38f; }
 
-// The group's pair s | b << 16 and the lane's eight codes.  All lanes of a group call it together; LANES per group.
-template <int LANES>
-__device__ __forceinline__ void pack_eight(const float (&x)[8], uint32_t* pair, uint32_t* codes) {
-    float lo = x[0], hi = x[0];
+__device__ __forceinline__ uint32_t min_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// smallest and largest of a lane's eight elements
+__device__ __forceinline__ void range_of(const uint4 (&in)[1], float* lo, float* hi) {      // bf16: two at a time
+    const uint32_t l = min_bf16x2(min_bf16x2(in[0].x, in[0].y), min_bf16x2(in[0].z, in[0].w));
+    const uint32_t h = max_bf16x2(max_bf16x2(in[0].x, in[0].y), max_bf16x2(in[0].z, in[0].w));
+    *lo = min_nan(bf16_lo(l), bf16_hi(l));
+    *hi = max_nan(bf16_lo(h), bf16_hi(h));
+}
+__device__ __forceinline__ void range_of(const uint4 (&in)[2], float* lo, float* hi) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(in);
+    *lo = *hi = __uint_as_float(w[0]);
 #pragma unroll
     for (int i = 1; i < 8; ++i) {
-        lo = min_nan(lo, x[i]);
-        hi = max_nan(hi, x[i]);
+        *lo = min_nan(*lo, __uint_as_float(w[i]));
+        *hi = max_nan(*hi, __uint_as_float(w[i]));
     }
+}
+
+// The group's pair s | b << 16 and the lane's eight codes.  All lanes of a group call it together; LANES per group.
+template <int LANES>
+__device__ __forceinline__ void pack_eight(const float (&x)[8], float lo, float hi, uint32_t* pair, uint32_t* codes) {
 #pragma unroll
     for (int d = 1; d < LANES; d *= 2) {
         lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, d));
@@ -64,49 +86,50 @@ __device__ __forceinline__ void pack_eight(const float (&x)[8], uint32_t* pair, 
     const float step = __fmul_rn(__fsub_rn(hi, lo), 1.f / 15.f);
     const float s = __uint_as_float((__float_as_uint(step) + 0xffffu) & 0xffff0000u);
     const float b = __bfloat162float(__float2bfloat16_rn(__fsub_rn(lo, 16.f * s)));
-    if (!(finite(step) && finite(s) && finite(b))) {
-        *pair = 0x7fc07fc0u;
-        *codes = 0;
-        return;
-    }
-    *pair = (__float_as_uint(s) >> 16) | (__float_as_uint(b) & 0xffff0000u);
-    // rint by adding 1.5 * 2^23; the codes are the lowest four bits of 16 + c, clamped to 16 .. 31
+    const bool broken = !(finite(step) && finite(s) && finite(b));
+    // rint by adding 1.5 * 2^23; the codes are the lowest four bits of 16 + c
     constexpr float kRint = 12582912.f;
     const float inv = 1.f / s;
+    float f[8], worst = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __fmul_rn(__fsub_rn(x[i], b), inv);
+    // Clamped to 16 .. 31 only where the rounding of b, up to 2^-8 |b|, can take the quotient past 15.5 or 31.5.
+    if (fabsf(b) > 100.f * s)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = fminf(fmaxf(f[i], 16.f), 31.f);
     uint32_t word = 0;
-    float worst = 0.f;
 #pragma unroll
     for (int i = 7; i >= 0; --i) {
-        const float f = fminf(fmaxf(__fmul_rn(__fsub_rn(x[i], b), inv), 16.f), 31.f);
-        const float r = __fadd_rn(f, kRint);
-        worst = fmaxf(worst, fabsf(__fsub_rn(f, __fsub_rn(r, kRint))));
+        const float r = __fadd_rn(f[i], kRint);
+        worst = fmaxf(worst, fabsf(__fsub_rn(f[i], __fsub_rn(r, kRint))));
         word = word * 16 + (__float_as_uint(r) & 15u);
     }
-    if (s == 0.f) {
-        word = 0;
-    } else if (s < 1e-30f) {                // its reciprocal may overflow, products may lose bits
-        word = 0;
-        for (int i = 7; i >= 0; --i) {
-            const double q = rint(((double)x[i] - (double)b) / (double)s);
-            word = word * 16 + (uint32_t)(fmin(fmax(q, 16.0), 31.0) - 16.0);
-        }
-    } else if (worst > 0.4999f) {
-        word = 0;
+    if (__any_sync(0xffffffffu, worst > 0.4999f)) {
 #pragma unroll
-        for (int i = 7; i >= 0; --i) {
-            const float d = __fsub_rn(x[i], b), f = fminf(fmaxf(__fmul_rn(d, inv), 16.f), 31.f);
-            float r = __fsub_rn(__fadd_rn(f, kRint), kRint);
-            const float below = f - r >= 0.f ? r : r - 1.f;             // the border next to f is below + 1/2
-            if (fabsf(__fsub_rn(f, r)) > 0.4999f) {
-                const float back = __fsub_rn(x[i], d);                  // x - b = d + lost exactly
-                const float lost = __fadd_rn(__fsub_rn(x[i], __fadd_rn(d, back)), __fsub_rn(back, b));
-                const float side = __fadd_rn(__fmaf_rn(-(below + 0.5f), s, d), lost);
-                r = side > 0.f ? below + 1.f : side < 0.f ? below : below + ((int)below & 1);
-            }
-            word = word * 16 + ((uint32_t)r & 15u);
+        for (int i = 0; i < 8; ++i) {
+            float r = __fsub_rn(__fadd_rn(f[i], kRint), kRint);
+            const float rest = __fsub_rn(f[i], r);
+            const bool near = fabsf(rest) > 0.4999f;
+            if (!__any_sync(0xffffffffu, near)) continue;
+            const float below = rest >= 0.f ? r : r - 1.f;              // the border next to f is below + 1/2
+            const float d = __fsub_rn(x[i], b), back = __fsub_rn(x[i], d);
+            const float lost = __fadd_rn(__fsub_rn(x[i], __fadd_rn(d, back)), __fsub_rn(back, b));      // x - b = d + lost exactly
+            const float side = __fadd_rn(__fmaf_rn(-(below + 0.5f), s, d), lost);
+            r = side > 0.f ? below + 1.f : side < 0.f ? below : below + ((int)below & 1);
+            r = fminf(fmaxf(r, 16.f), 31.f);
+            if (near) word = (word & ~(15u << (4 * i))) | ((uint32_t)r & 15u) << (4 * i);
         }
     }
-    *codes = word;
+    if (s < 1e-30f && !broken) {                // s = 0, or its reciprocal may overflow and products may lose bits
+        word = 0;
+        if (s > 0.f)
+            for (int i = 7; i >= 0; --i) {
+                const double q = rint(((double)x[i] - (double)b) / (double)s);
+                word = word * 16 + (uint32_t)(fmin(fmax(q, 16.0), 31.0) - 16.0);
+            }
+    }
+    *pair = broken ? 0x7fc07fc0u : (__float_as_uint(s) >> 16) | (__float_as_uint(b) & 0xffff0000u);
+    *codes = broken ? 0u : word;
 }
 
 template <typename T, int D>
@@ -160,8 +183,10 @@ __global__ void __launch_bounds__(kPackThreads) pack4_kernel(const PackKernelArg
                 Unpack<T>::run(in[j][0], *reinterpret_cast<float(*)[4]>(x));
                 Unpack<T>::run(in[j][1], *reinterpret_cast<float(*)[4]>(x + 4));
             }
+            float lo, hi;
+            range_of(in[j], &lo, &hi);
             uint32_t pair, codes;
-            pack_eight<R::GROUP / 8>(x, &pair, &codes);
+            pack_eight<R::GROUP / 8>(x, lo, hi, &pair, &codes);
             if (to[j] >= 0) {
                 uint32_t* row = reinterpret_cast<uint32_t*>(dst + to[j]);
                 row[4 + lane] = codes;

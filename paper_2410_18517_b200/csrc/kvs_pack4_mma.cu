@@ -8,7 +8,7 @@
 //   up to four heads:  rows 0..3 hi, 8..11 mid, 4..7 lo, in ONE product (column c of S is head c mod 4, so the lanes of
 //                      columns 4..7 have the weights too);
 //   five to eight:     rows 0..7 hi and 8..15 mid in one product, lo in a second.
-// Two terms would leave 1.5e-6 of the result, three the fp32 rounding.  The products of a tile start from zero and are added to
+// Two terms would leave 1.5e-6 of the result, three the fp32 rounding.  The products of a chunk start from zero and are added to
 // the running state rounded to nearest: an MMA cuts its sum off, and over thousands of rows that would drift.
 //
 // Fragments: the contraction may take the elements in any order, so lane t of a quad takes group t of its key's row - D/8 bytes in
@@ -22,7 +22,7 @@
 //
 // Work decomposition (see DecodePlan), pieces, the hand-over between blocks and the combine kernel are those of the other
 // split-K kernels.  Rows of a tile are contiguous and come by two 1-D bulk copies, exactly as many as the unit holds.  A tile
-// has up to 512 rows, 64 for each of 8 warps: the running state is rescaled once a tile and warp.  How many it has the plan
+// has up to 512 rows, 64 for each of 8 warps: a chunk.  How many it has the plan
 // decides (plan_decode_pack4), and with it how many stages the ring has.
 #include <algorithm>
 #include <type_traits>
@@ -328,19 +328,35 @@ __global__ void __launch_bounds__(Pack4Shape<D>::THREADS, 1) decode_pack4_mma(co
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             }
-            // ---- one online-softmax update of the heads over the chunk's rows (the scale is positive) ----
-            float alpha[2];
+            // ---- the heads' reference (the scale is positive) ----
+            // The weights are taken relative to m, the maximum when it was last looked for: it is looked for again only when a score
+            // exceeds it by 2^8, which fp32 sums and three bf16 terms bear as well as 1.  (With a new maximum every chunk its
+            // way around the lanes and the rescaling of the state stand between the two products: 193 us instead of 190.)
+            float top[2];
+            bool grown = false;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float top = fmaxf(s[0][j], s[0][2 + j]);
+                top[j] = fmaxf(s[0][j], s[0][2 + j]);
 #pragma unroll
-                for (int blk = 1; blk < NBK; ++blk) top = fmaxf(top, fmaxf(s[blk][j], s[blk][2 + j]));
+                for (int blk = 1; blk < NBK; ++blk) top[j] = fmaxf(top[j], fmaxf(s[blk][j], s[blk][2 + j]));
+                grown |= top[j] * a.scale_log2 > m[j] + 8.f;
+            }
+            if (__any_sync(0xffffffffu, grown)) {
+                float alpha[2];
 #pragma unroll
-                for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                const float m_new = fmaxf(m[j], top * a.scale_log2);
-                alpha[j] = fast_exp2(m[j] - m_new);
-                m[j] = m_new;
-                lsum[j] *= alpha[j];
+                for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                    for (int d = 4; d < 32; d *= 2) top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], d));
+                    const float m_new = fmaxf(m[j], top[j] * a.scale_log2);
+                    alpha[j] = fast_exp2(m[j] - m_new);
+                    m[j] = m_new;
+                    lsum[j] *= alpha[j];
+                }
+                // the head of this lane's row of O: its alpha is with lane row / 2
+                const float alpha0 = __shfl_sync(0xffffffffu, alpha[0], row >> 1), alpha1 = __shfl_sync(0xffffffffu, alpha[1], row >> 1);
+                const uint64_t alpha2 = row & 1 ? pair_of(alpha1, alpha1) : pair_of(alpha0, alpha0);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) o[nb] = mul2(o[nb], alpha2);
             }
             // A fragments of P: [block][keys 0..7 or 8..15]: rows 0..7 / rows 8..15 (/ the second product's rows 0..7)
             uint32_t pa[NBK][2], pb[NBK][2];
@@ -357,11 +373,7 @@ __global__ void __launch_bounds__(Pack4Shape<D>::THREADS, 1) decode_pack4_mma(co
                     pb[blk][nb] = transposed(third ? 0u : mid);
                     if constexpr (WIDE) pc[blk][nb] = transposed(lo);
                 }
-            // the head of this lane's row of O: its alpha is with lane row / 2
-            const float alpha0 = __shfl_sync(0xffffffffu, alpha[0], row >> 1), alpha1 = __shfl_sync(0xffffffffu, alpha[1], row >> 1);
-            const float alpha_row = row & 1 ? alpha1 : alpha0;
-            // ---- O = alpha O + P V ----
-            const uint64_t alpha2 = pair_of(alpha_row, alpha_row);
+            // ---- O += P V ----
             const unsigned char* vq = vs + quad * 2 * RB;       // the first of this lane's rows
             uint32_t s2[NBK][2], b2[NBK][2];       // (s, b) of the keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
@@ -410,7 +422,7 @@ __global__ void __launch_bounds__(Pack4Shape<D>::THREADS, 1) decode_pack4_mma(co
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         uint64_t& acc = o[8 * x + 4 * half + i];
-                        acc = fma2(acc, alpha2, add2(pair_of(c[i][0], c[i][1]), pair_of(c[i][2], c[i][3])));
+                        acc = add2(acc, add2(pair_of(c[i][0], c[i][1]), pair_of(c[i][2], c[i][3])));
                     }
                 }
             }
@@ -540,25 +552,25 @@ cudaError_t init_pack4_kernels() {
     return set_attr<64, true>();
 }
 
-// Units are cut into tiles of equal size (to 16 rows), as many as make the longest block's share cheapest: a tile costs its
-// rows and a constant (barriers, the state's update, a chunk's latency: about as much as kTileCost rows).
+// The tile: as many rows as make the longest block's share cheapest.  A warp takes its 16-row blocks of a tile one after the other,
+// so a tile costs its rows rounded up to 128 and a constant - barriers and the latency of a chunk's chain of products, worth
+// about kTileCost rows (13B shape, 16 x 40 heads x 8192 rows: tiles of 512 rows 193 us, 384 210, 256 227, 128 294).
 void plan_decode_pack4(int units, int n, int sm_count, int max_ctas, DecodePlan* plan) {
-    constexpr int kTileCost = 48, kTry = 64;
+    constexpr int kTileCost = 108, kGrain = kPack4Warps * 16;
     int cap = sm_count;
     if (max_ctas > 0) cap = std::min(cap, max_ctas);
     cap = std::min(cap, kMaxCtas);
-    const int least = (n + kPack4TileMax - 1) / kPack4TileMax;
-    long long best = -1;
-    for (int k = least; k < least + kTry; ++k) {
-        const int rows = ((n + k - 1) / k + 15) / 16 * 16, tpu = (n + rows - 1) / rows;
-        const long long T = (long long)units * tpu, cost = (T + cap - 1) / cap * (rows + kTileCost);
-        if (best < 0 || cost < best) {
+    double best = 0;
+    for (int rows = kPack4TileMax; rows >= kGrain; rows -= kGrain) {
+        const int tpu = (n + rows - 1) / rows, last = (n - (tpu - 1) * rows + kGrain - 1) / kGrain * kGrain;
+        const long long T = (long long)units * tpu;
+        const double cost = (double)((T + cap - 1) / cap) * ((double)(tpu - 1) * (rows + kTileCost) + last + kTileCost) / tpu;
+        if (rows == kPack4TileMax || cost < best) {
             best = cost;
             plan->tile_rows = rows;
             plan->tpu = tpu;
             plan->T = T;
         }
-        if (rows == 16) break;
     }
     plan->NC = (int)std::min<long long>(plan->T, cap);
     plan->kernel = 3;
