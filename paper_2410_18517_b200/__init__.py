@@ -294,9 +294,10 @@ class SharedKVCache:
         assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows and self._here(logits, scores)
         shape = (rows // n_beams, n_out)
         if out is None:
-            out = tuple(torch.empty(shape, dtype=d, device=self.device) for d in (torch.float32, torch.int32, torch.int32))
-        for x, d in zip(out, (torch.float32, torch.int32, torch.int32)):
-            assert x.dtype == d and x.is_contiguous() and x.shape == shape and self._here(x)
+            out = scores.new_empty(shape), scores.new_empty(shape, dtype=torch.int32), scores.new_empty(shape, dtype=torch.int32)
+        else:
+            for x, d in zip(out, (torch.float32, torch.int32, torch.int32)):
+                assert x.dtype == d and x.is_contiguous() and x.shape == shape and self._here(x)
         binding.kvs_beam_select(self.ctx, logits, KVS_BF16 if logits.dtype == torch.bfloat16 else KVS_F32,
                                 logits.stride(0) if rows > 1 else vocab, vocab, scores, shape[0], n_beams, n_out, *out, self._stream())
         return out
