@@ -38,6 +38,7 @@
  *   [max_batch][n_kv_heads][row_stride][head_dim] elements of the storage
  *   type, row_stride = max_seq rounded up to a multiple of 128 rows;
  *   plane(slot, kv) starts (2 * slot + kv) * plane_bytes into the pool.
+ *   (A 4-bit cache has rows of its own, see kvs_set_cache_format.)
  *   One token row of one head is head_dim contiguous elements; the rows of one
  *   (sequence, head) are contiguous, so a tile of consecutive tokens is one
  *   contiguous run of bytes.
@@ -94,8 +95,8 @@ typedef struct {
     uint64_t append_skipped;      /* the same on sharing layers (nothing appended)           */
     uint64_t attention_launches;  /* split-K kernels launched                                */
     uint64_t combine_launches;    /* combine kernels launched                                */
-    uint64_t kv_bytes_read;       /* 2*B*Hkv*n*D*elem summed over attention calls            */
-    uint64_t kv_bytes_appended;   /* 2*B*Hkv*n_new*D*elem summed over launched appends       */
+    uint64_t kv_bytes_read;       /* 2*B*Hkv*n*(bytes of a cached row) summed over attention calls */
+    uint64_t kv_bytes_appended;   /* 2*B*Hkv*n_new*(bytes of a cached row) over launched appends   */
     uint64_t prefill_launches;    /* kvs_prefill_attention and kvs_tree_attention calls      */
     uint64_t evict_launches;      /* kvs_evict and kvs_accept_draft calls that launched      */
     uint64_t search_launches;     /* kernels launched by kvs_layer_distances / kvs_mean_cosine */
