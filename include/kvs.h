@@ -164,8 +164,8 @@ kvs_status kvs_set_share_map(kvs_ctx* ctx, const int32_t* share_map);
  * A row takes 16 + D/2 bytes (80 or 48): the pairs (s, b) of the groups as bf16, then the codes, element 8 w + i in bits
  * 4 i .. 4 i + 3 of word w; planes are [max_batch][n_kv_heads][row_stride] such rows.
  *
- * The calls keep their arguments and types: the append calls take the storage type and pack it (kvs_decode_step and
- * kvs_step_host with a launch of its own for that, kvs_append_rotary through the workspace), attention (kvs_decode_attention,
+ * The calls keep their arguments and types: the append calls take the storage type and pack it (fp32 storage: kvs_decode_step
+ * and kvs_step_host with a launch of its own for that; kvs_append_rotary through the workspace), attention (kvs_decode_attention,
  * its _static form, kvs_decode_step, kvs_step_host, kvs_prefill_attention) is that over the values, kvs_evict,
  * kvs_accept_draft, kvs_reorder, kvs_truncate and replays work as they do otherwise, kvs_read_rows gives the values.
  * kvs_tree_attention, kvs_decode_attention_weights and kvs_layer_distances refuse such a context (STATE).

@@ -491,6 +491,11 @@ kvs_status run_attention(kvs_ctx* c, int slot, const void* q, float* out, int un
     return KVS_OK;
 }
 
+// Whether the attention kernel of the slot can store the step's new rows itself (all but the one over 4-bit rows for fp32).
+bool can_fuse_append(const kvs_ctx* c, int slot) {
+    return !c->ragged[slot] && (c->format == KVS_CACHE_PLAIN || c->cfg.dtype == KVS_BF16);
+}
+
 // One decode step of a computing layer with the append riding in the split-K kernel (the caller
 // has checked the arguments; the slot is not ragged).
 kvs_status do_fused_step(kvs_ctx* c, int layer, const void* q, const void* k, const void* v, float* out, int batch,
@@ -799,7 +804,7 @@ kvs_status kvs_decode_step(kvs_ctx* ctx, int32_t layer, const void* q, const voi
     if (!guard.ok) return KVS_ERR_CUDA;
     const int slot = ctx->slot_of_layer[layer];
     if (((uintptr_t)q % 16) != 0 || ((uintptr_t)out % 4) != 0) return KVS_ERR_INVALID_ARG;
-    if (!ctx->ragged[slot] && ctx->format == KVS_CACHE_PLAIN) return do_fused_step(ctx, layer, q, k, v, out, batch, st);
+    if (can_fuse_append(ctx, slot)) return do_fused_step(ctx, layer, q, k, v, out, batch, st);
     s = do_append(ctx, layer, k, v, batch, 1, st);
     if (s != KVS_OK) return s;
     return do_attention(ctx, layer, q, out, batch, st);
@@ -1482,7 +1487,7 @@ kvs_status kvs_step_host(kvs_ctx* ctx, const void* q_host, const void* k_host, c
         for (int l = l0; l < l1; ++l) {
             float* o = reinterpret_cast<float*>(dout + out_layer * l);
             kvs_status s;
-            if (ctx->share_map[l] == l && !ctx->ragged[ctx->slot_of_layer[l]] && ctx->format == KVS_CACHE_PLAIN) {
+            if (ctx->share_map[l] == l && can_fuse_append(ctx, ctx->slot_of_layer[l])) {
                 // the append rides in the split-K kernel (the staging rows are 16-byte aligned)
                 s = do_fused_step(ctx, l, dq + q_layer * l, dk + kv_layer * l, dv + kv_layer * l, o, batch, st);
             } else {

@@ -71,6 +71,8 @@ struct Pack4KernelArgs {
     unsigned long long wait_ns;
     long long stall_tile;
     unsigned long long* trace;
+    const char* k_new;      // the step's new rows (bf16, [units][D]), appended by this kernel (n counts them), or nullptr
+    const char* v_new;
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -120,8 +122,10 @@ __global__ void __launch_bounds__(Pack4Shape<D>::THREADS, 1) decode_pack4_mma(co
         KVS_TRACE_STAMP(tr, kTrEntry);
         KVS_TRACE_VALUE(tr, kTrSm, sm_id());
     }
+    bool over = false;    // a replayed launch with an append that would pass the capacity
     if (a.n_extra != nullptr) {
         // a replayed launch: the counter is stable here without a wait (see decode_splitk_mma)
+        over = a.n + *a.n_extra > a.cap;
         a.n = min(a.n + *a.n_extra, a.cap);
         a.tpu = (a.n + TN - 1) / TN;
         a.T = (long long)a.units * a.tpu;
@@ -158,8 +162,8 @@ __global__ void __launch_bounds__(Pack4Shape<D>::THREADS, 1) decode_pack4_mma(co
     __syncthreads();
 
     if (warp == WARPS) {
-        // ------------------------------ producer (one lane) ------------------------------
-        if (lane != 0) return;
+        // ------------------------------ producer ------------------------------
+        // Lane 0 issues the copies; the whole warp packs the step's new rows when the launch carries an append.
         // The barrier of a stage is armed once with its full byte count; K/V and q may be issued apart.
         auto issue = [&](long long gt, int st, bool arm, bool kv, bool qpart) {
             const long long u = gt / a.tpu;
@@ -185,16 +189,44 @@ __global__ void __launch_bounds__(Pack4Shape<D>::THREADS, 1) decode_pack4_mma(co
         };
         // until the preceding kernel is known to have finished: only tiles made of rows that nothing in flight writes
         int npre = 0;
-        for (; npre < stages && t0 + npre < t1; ++npre) {
-            const int ti = (int)((t0 + npre) % a.tpu);
-            if ((long long)(ti + 1) * TN > a.safe_rows) break;
-            issue(t0 + npre, npre, true, true, false);
-        }
-        KVS_TRACE_STAMP(tr, kTrProducerPre);
+        if (lane == 0)
+            for (; npre < stages && t0 + npre < t1; ++npre) {
+                const int ti = (int)((t0 + npre) % a.tpu);
+                if ((long long)(ti + 1) * TN > a.safe_rows) break;
+                issue(t0 + npre, npre, true, true, false);
+            }
+        if (lane == 0) KVS_TRACE_STAMP(tr, kTrProducerPre);
         pdl_wait();
-        KVS_TRACE_STAMP(tr, kTrProducerGo);
+        if (lane == 0) KVS_TRACE_STAMP(tr, kTrProducerGo);
         pdl_launch_dependents();
-        for (int j = 0; j < npre; ++j) issue(t0 + j, j, false, false, true);
+        if (lane == 0)
+            for (int j = 0; j < npre; ++j) issue(t0 + j, j, false, false, true);
+        if (a.k_new != nullptr && t0 < t1) {
+            // Of every unit whose last tile lies in this block's share the new row, a group per lane, four units at a time.  Only
+            // this block fetches that tile, after this: the fence orders the stores before the copies lane 0 issues next.
+            if (over) {
+                if (lane == 0 && blockIdx.x == 0) atomicExch(a.status, 4);
+            } else {
+                constexpr int PIECES = Pack4Row<D>::GROUP / 8;
+                const bool isv = lane & 4;
+                const uint32_t group = lane & 3;
+                for (long long u = t0 / a.tpu + lane / 8; u <= (t1 - 1) / a.tpu; u += 4) {
+                    const long long last = u * a.tpu + a.tpu - 1, to = (u * a.row_stride + a.n - 1) * RB;
+                    if (last < t0 || last >= t1) continue;
+                    if (!KVS_BOUNDS_OK(to, RB, a.plane_bytes, a.status) || !KVS_BOUNDS_OK(u, 1, a.units, a.status)) continue;
+                    const uint4* p = reinterpret_cast<const uint4*>((isv ? a.v_new : a.k_new) + u * (D * 2)) + group * PIECES;
+                    uint4 in[PIECES];
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) in[i] = p[i];
+                    uint32_t pair, words[PIECES];
+                    pack_group<__nv_bfloat16, D>(in, &pair, words);
+                    store_group<D>(reinterpret_cast<uint32_t*>(const_cast<char*>(isv ? a.vplane : a.kplane) + to), group, pair, words);
+                }
+            }
+            asm volatile("fence.proxy.async.global;" ::: "memory");
+            __syncwarp();
+        }
+        if (lane != 0) return;
         // tile j of the block lies in stage j % stages; its phase there is j / stages
         int st = npre % stages, turn = npre / stages;
         int it = npre;
@@ -603,6 +635,8 @@ cudaError_t launch_decode_pack4(const DecodeArgs& a, const DecodePlan& plan, cud
     ka.wait_ns = a.wait_ns;
     ka.stall_tile = a.stall_tile;
     ka.trace = a.trace;
+    ka.k_new = static_cast<const char*>(a.k_new);
+    ka.v_new = static_cast<const char*>(a.v_new);
     return a.D == 128 ? launch_one<128>(ka, plan.NC, a.programmatic, stream) : launch_one<64>(ka, plan.NC, a.programmatic, stream);
 }
 

@@ -330,6 +330,7 @@ def test_steps_shared_layers_and_host_buffers(dtype):
         for l in range(L):
             assert torch.equal(outs[0][l], outs[1][l]) and torch.equal(outs[0][l], outs[3][l])
             assert torch.equal(outs[0][l].cpu(), out_host[l])
+    assert caches[0].stats()["fused_appends"] == (8 if dtype == "bf16" else 0)      # two own layers, four steps
     for c in caches:
         assert c.device_status() == 0 and c.seq_len(2) == n + 4
         c.check_canaries()
