@@ -7,6 +7,7 @@ import torch
 
 import operators_reference as oref
 import pack4_reference as ref
+import synth_inputs as si
 from helpers import GuardedCache
 from paper_2410_18517_b200 import (KVS_OPT_EARLY_START, KVS_OPT_FINISH_IN_KERNEL, KVS_OPT_MAX_CTAS, KVS_OPT_REPLAY,
                                    KVS_OPT_WAIT_LIMIT_US, KvsError, Rotary, SharedKVCache)
@@ -446,3 +447,32 @@ def test_a_stalled_copy_ends_with_an_error_status():
     x = normal(1, "f32", 1, 10, 4, 64).cuda()
     f.append(0, x, x)
     refused(kb.KVS_ERR_STATE, kb.kvs_selftest_stalled_copy, f.ctx, 0, x[:, 0].contiguous(), torch.empty(1, 4, 64, device="cuda"), 1)
+
+
+@pytest.mark.parametrize("Hq,Hkv,dtype", [(8, 8, "bf16"), (8, 2, "bf16"), (4, 4, "f32")])
+def test_static_calls_twice_in_a_row(Hq, Hkv, dtype):
+    """The form without a workspace: nothing the call before left in the built-in scratch is used, results as the other form's.
+
+    It also loads kernels before tests/test_zz_no_alloc.py compares the device's free memory around the same calls: the
+    driver loads a kernel's code at its first launch and takes 2 MiB when a chunk fills up, which that comparison cannot
+    tell from an allocation.  With CUDA_MODULE_LOADING=EAGER that file passes without this test.
+    """
+    w = si.Workload(f"pack4_static_{Hq}_{Hkv}_{dtype}", L=3, Hq=Hq, Hkv=Hkv, D=128, B=4, context=2500, dtype=dtype, n_shared=1,
+                    map_seed=0, steps=1, fixed_map=(0, 1, 0))
+    cache = SharedKVCache(w.L, Hq, Hkv, w.D, w.B, w.context, dtype, share_map=w.share_map(), cache_format="4bit")
+    for l in (0, 1):
+        cache.append(l, *si.context_kv(w, l, device="cuda"))
+    stream = torch.cuda.current_stream().cuda_stream
+    status = torch.full((1,), -1, dtype=torch.int32, device="cuda")
+    for call, layer in enumerate((2, 1)):
+        q = si.step_qkv(w, call, layer, device="cuda")[0]
+        ref_out = cache.decode_attention(layer, q)
+        out = torch.full_like(ref_out, float("nan"))
+        kb.kvs_decode_attention_static(cache.ctx, layer, q, out, w.B, stream, status)
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0 and torch.equal(out, ref_out)
+        assert (out - ref_out).abs().max().item() == 0 and ((out - ref_out).norm() / ref_out.norm()).item() == 0
+        check_attention(cache, layer, q, out)
+    out2 = torch.empty_like(ref_out)
+    kb.kvs_decode_attention_static(cache.ctx, 1, q, out2, w.B, stream, None)
+    assert torch.equal(out2, ref_out)
