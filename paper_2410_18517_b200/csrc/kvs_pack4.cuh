@@ -140,8 +140,9 @@ __device__ __forceinline__ void pack_group(const uint4 (&in)[Pack4Row<D>::GROUP 
     const bool broken = !(finite(step) && finite(s) && finite(b));
     const float inv = 1.f / s;
     // What the two words say is not taken where the rounding of b (up to 2^-8 |b|) can bring a quotient past 15.5 or 31.5,
-    // and where s is tiny: its reciprocal may overflow, products may lose bits.
-    const bool plain = fabsf(b) <= 100.f * s && s >= 1e-30f;
+    // and where fp32 steps do not carry: where s is tiny its reciprocal may overflow and products may lose bits, where it is
+    // huge x - b, up to 31 s, may overflow.
+    const bool carries = s >= 1e-30f && s <= 1e36f, plain = fabsf(b) <= 100.f * s && carries;
     const uint64_t minus = pair_of(-b, -b), above = pair_of(inv * 1.000001f, inv * 1.000001f), under = pair_of(inv * 0.999999f, inv * 0.999999f);
     const uint64_t magic = pair_of(kRint, kRint);
 #pragma unroll
@@ -161,7 +162,7 @@ __device__ __forceinline__ void pack_group(const uint4 (&in)[Pack4Row<D>::GROUP 
         if (unsure && !broken) {
             if (s == 0.f) {
                 one = 0;
-            } else if (s < 1e-30f) {
+            } else if (!carries) {
                 one = 0;
 #pragma unroll
                 for (int i = 7; i >= 0; --i) {

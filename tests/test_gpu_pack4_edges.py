@@ -1,0 +1,47 @@
+"""The 4-bit cache where its numbers are extreme."""
+import pytest
+import torch
+
+import pack4_reference as ref
+from paper_2410_18517_b200 import SharedKVCache
+from paper_2410_18517_b200 import build as kbuild
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _built():
+    kbuild.build()
+
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def stored(x, dtype):
+    """The bytes of a 4-bit cache's K rows of x [tokens][D], and what reading them gives."""
+    cache = SharedKVCache(1, 1, 1, x.shape[1], 1, x.shape[0], dtype, cache_format="4bit")
+    rows = x.to(DT[dtype])[None, :, None].contiguous().cuda()
+    cache.append(0, rows, rows)
+    raw, (k, v) = cache.plane(0, 0)[0, 0, :x.shape[0]].cpu(), cache.read_rows(0)
+    assert torch.equal(cache.plane(0, 1)[0, 0, :x.shape[0]].cpu(), raw) and torch.equal(v.view(torch.uint8), k.view(torch.uint8))
+    assert cache.device_status() == 0
+    return raw, k[0, :, 0].cpu()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_groups_whose_range_is_near_the_largest_number(dtype, D):
+    """x - b, up to 31 steps, passes the fp32 range long before s and b do (a range of 1.7e38): codes and bytes are the
+    definition's up to where b overflows, and NaN from there on."""
+    g = torch.Generator().manual_seed(D)
+    scale = torch.logspace(36, 38.5, 200, dtype=torch.float64)[:, None]
+    x = ((torch.rand(200, D, generator=g, dtype=torch.float64) * 2 - 1) * scale)
+    x[100:] += scale[100:] * 0.5 * (torch.rand(100, 1, generator=g, dtype=torch.float64) - 0.5)
+    x = x.clamp(-3.3e38, 3.3e38).to(DT[dtype])
+    raw, values = stored(x, dtype)
+    assert torch.equal(raw, ref.row_bytes(x))
+    want = ref.values(x)
+    assert bool(want.isnan().any()) and bool(((values == want) | (values.isnan() & want.isnan())).all())
+    wide = x.float().unflatten(1, (4, -1))
+    wide = (wide.amax(-1) - wide.amin(-1) > 1.7e38) & ~want.unflatten(1, (4, -1)).isnan().any(-1)
+    assert int(wide.sum()) > 20                  # groups with values whose differences overflow
