@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kBeamThreads, 5) beam_segments_kernel(const Be
     }
     pdl_launch_dependents();
     pdl_wait();
-    const int v0 = seg * a.seg_len, v1 = min(a.vocab, v0 + a.seg_len);
+    const int v0 = seg * a.seg_len, len = min(a.seg_len, a.vocab - v0);      // (v0 + seg_len may pass 31 bits)
     const T* x_row = static_cast<const T*>(a.logits) + row * a.stride;
     const uint64_t none = (uint64_t)order_of(-INFINITY) << 32 | 0xffffffffu;     // minus infinity is no candidate
     constexpr int PER16 = 16 / (int)sizeof(T);       // logits per piece
@@ -172,8 +172,8 @@ __global__ void __launch_bounds__(kBeamThreads, 5) beam_segments_kernel(const Be
     auto key = [&](float x, int v) { return (uint64_t)order_of(x) << 32 | (uint32_t)~v; };
     // thread t takes pieces t, t + 256, ...: the same logits whether they can be loaded as vectors or not; what is left of the
     // row behind the last whole piece goes to the first threads, a logit each
-    const int pieces = (v1 - v0) / PER16, at_rest = v0 + pieces * PER16 + tid;
-    const float extra = at_rest < v1 ? (float)x_row[at_rest] : -INFINITY;
+    const int pieces = len / PER16, rest = len - pieces * PER16, at_rest = v0 + pieces * PER16 + min(tid, rest);
+    const float extra = tid < rest ? (float)x_row[at_rest] : -INFINITY;
     auto piece = [&](int p) {
         if (p >= pieces) return masked_piece<T>();
         const T* at = x_row + v0 + p * PER16;
