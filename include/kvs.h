@@ -388,7 +388,8 @@ kvs_status kvs_read_rows(kvs_ctx* ctx, int32_t layer, int32_t first, int32_t n_r
 /* The best continuations of every request's beams:
  *   score(b, v) = scores[b] + logits[b][v] - log(sum_w exp(logits[b][w]))
  * and of a request's n_beams * vocab pairs the n_out with the highest score, best first; equal scores (in fp64, in which they
- * are compared): the lowest (beam, token).  A pair of score minus infinity is no candidate, nor is any pair of a row whose own
+ * are compared): the lowest beam, of one beam's the higher logit (fp64 scores of different logits may be equal), then the lowest
+ * token.  A pair of score minus infinity is no candidate, nor is any pair of a row whose own
  * score or whose logits' sum is not finite (a NaN or +infinity among the logits, a row that is masked throughout).
  *   logits:        device, logits_dtype (KVS_BF16 or KVS_F32) [n_requests * n_beams] rows of vocab, logits_stride elements
  *                  apart; rows that start on 16 bytes are read fastest

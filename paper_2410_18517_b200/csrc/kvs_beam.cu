@@ -11,7 +11,7 @@ namespace {
 
 // --------------------------------------------------------------------------------------
 // Selection.  score(b, v) = scores[b] + x_bv - lse_b,  lse_b = log sum_v exp x_bv;  of a request's W beams x V tokens the K
-// best, equal scores by the lowest (beam, token).
+// best, equal scores by the lowest beam, within it the higher logit, then the lower token.
 //
 // First kernel: every logits row is cut into segments, a block each: running maximum and sum of exponentials per thread, then
 // the segment's K best by a threshold: the K-th largest of the threads' own maxima.  K elements at least reach it and hardly
@@ -42,13 +42,14 @@ __device__ __forceinline__ double value_of(uint64_t o) { return __longlong_as_do
 // exp(t), t <= 0 (or NaN)
 __device__ __forceinline__ float exp_below(float t) { return fast_exp2(t * 1.44269504f); }
 
-// The second kernel's keys need more bits than one word: by score, then by the lower index
+// The second kernel's keys need more bits than one word.  By score, then by the lower beam, the higher logit and the lower
+// token: within a beam that is the order by which the segments' lists are cut, also where fp64 scores are equal and logits are not.
 struct Wide {
     uint64_t v;      // order of the fp64 score
-    uint32_t i;      // ~(flat index)
+    uint64_t t;      // from the top: beams after this one, order of the logit (32 bits), tokens after this one (token_bits)
 };
 __device__ __forceinline__ bool above(uint64_t a, uint64_t b) { return a > b; }
-__device__ __forceinline__ bool above(const Wide& a, const Wide& b) { return a.v > b.v || (a.v == b.v && a.i > b.i); }
+__device__ __forceinline__ bool above(const Wide& a, const Wide& b) { return a.v > b.v || (a.v == b.v && a.t > b.t); }
 
 // The K-th largest of `n` numbers s_x[0 .. n-1] (n a multiple of four, at least 4), of which thread t < n holds `mine`, as
 // order_of: into *cut, which is to hold the highest order before.  n < K: minus infinity.  Ends with a barrier.
@@ -125,6 +126,7 @@ struct BeamKernelArgs {
     bool vec;                // rows start on 16 bytes
     const float* scores;
     int W, K;
+    int token_bits;          // of vocab - 1; with a beam's they are 32 at most (beams * vocab is below 2^31)
     float* out_scores;
     int* out_tokens;
     int* out_parents;
@@ -347,12 +349,13 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
         }
     }
     __syncthreads();
-    const Wide lowest = {order_of(-(double)INFINITY), 0u};      // scores of minus infinity and NaN are no candidates
+    const Wide lowest = {order_of(-(double)INFINITY), 0ull};      // scores of minus infinity and NaN are no candidates
     auto candidate = [&](uint64_t k, int beam) {
         Wide w = lowest;
         if (k) {
             const double score = s_base[beam] + ((double)value_of((uint32_t)(k >> 32)) - (double)s_top[beam]);
-            if (score > -(double)INFINITY) w = {order_of(score), ~((uint32_t)beam * (uint32_t)a.vocab + ~(uint32_t)k)};
+            if (score > -(double)INFINITY)
+                w = {order_of(score), (uint64_t)(a.W - 1 - beam) << (32 + a.token_bits) | (k >> 32) << a.token_bits | ((uint32_t)a.vocab - 1 - ~(uint32_t)k)};
         }
         return w;
     };
@@ -434,10 +437,9 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
         if (s_equal[rank] > 1)
             for (int j = 0; j < n; ++j) rank += s_head[j] == x && above(s_list[j], w) ? 1 : 0;
         if (rank < a.K) {
-            const uint32_t flat = ~w.i;
             a.out_scores[o + rank] = x;
-            a.out_tokens[o + rank] = (int)(flat % (uint32_t)a.vocab);
-            a.out_parents[o + rank] = (int)(row0 + flat / (uint32_t)a.vocab);
+            a.out_tokens[o + rank] = a.vocab - 1 - (int)(w.t & ((1ull << a.token_bits) - 1));
+            a.out_parents[o + rank] = (int)(row0 + a.W - 1 - (int)(w.t >> (32 + a.token_bits)));
         }
     }
     if (tid < a.K && tid >= s_count) {     // fewer candidates than places
@@ -573,6 +575,8 @@ cudaError_t launch_beam_select(const BeamArgs& p, cudaStream_t stream) {
     a.scores = p.scores;
     a.W = p.beams;
     a.K = p.n_out;
+    a.token_bits = 0;
+    while ((long long)p.vocab > 1ll << a.token_bits) ++a.token_bits;
     a.out_scores = p.out_scores;
     a.out_tokens = p.out_tokens;
     a.out_parents = p.out_parents;

@@ -36,3 +36,39 @@ def test_select_over_the_largest_vocabulary(dtype):
     # score's own rounding (2^-24 of 21.5)
     assert float((s[0].cpu().double() - want).abs().max()) < 16 * 2.0 ** -22
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [50, 6000, 70000])
+def test_select_logits_that_differ_by_less_than_scores_show(dtype, V):
+    """Logits of a few 1e-20 apart: their fp64 scores are equal.  A beam's go by the logit, beams by their number, whatever
+    n_out is: fewer continuations are the first of more."""
+    W = 3
+    cache = SharedKVCache(1, 1, 1, 64, 2 * W, 1, "bf16")
+    x = torch.zeros(2 * W, V)
+    for b in range(2 * W):
+        for i, at in enumerate((V - 1, V // 2, 7 + b, V // 3)):
+            x[b, at] = (i % 3 + 1 + b) * 1e-20 * (-1 if i == 2 else 1)
+    x[1, 3], x[4] = 2.0, -math.inf               # a beam with a score that shows, a beam without candidates
+    x = x.to(DT[dtype])
+    scores = torch.tensor([-1.0, -8.0, -1.0, -0.5, 0.0, -0.5])
+    scores[1] = -1.0 + float(torch.logsumexp(x[1].double(), 0) - math.log(V)) - 2.0
+    want = []
+    for r in range(2):
+        every = []
+        for w in range(W):
+            row = x[r * W + w].double()
+            top = row.max()
+            base = float(scores[r * W + w]) - float((row - top).exp().sum().log())
+            total = base + (row - top)
+            every += [(-float(total[v]), w, -float(row[v]), v) for v in range(V) if math.isfinite(float(total[v]))]
+        want.append([(v, r * W + w) for _, w, _, v in sorted(every)[:64]])
+    got = {}
+    for K in (64, 40, 17, 16, 5, 2, 1):
+        _, t, p = cache.beam_select(x.cuda(), scores.cuda(), W, K)
+        got[K] = [list(zip(t[r].tolist(), p[r].tolist())) for r in range(2)]
+        if K == 64:
+            assert got[K][1] == want[1]
+        for r in range(2):
+            assert got[K][r] == got[64][r][:K], (K, r)
+    assert cache.device_status() == 0
