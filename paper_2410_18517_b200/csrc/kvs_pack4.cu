@@ -220,8 +220,8 @@ __global__ void __launch_bounds__(256) decode_pack4_f32(const Pack4F32Args a_in)
     __shared__ float s_p[G][kF32Tile];
     __shared__ float s_alpha[G];
     __shared__ float s_o[PARTS][G][D];
-    pdl_launch_dependents();
     pdl_wait();
+    pdl_launch_dependents();      // in this order, as in every split-K kernel (see safe_rows_of)
     if (a.n_extra) {    // replayed launch: the lengths have grown on the device
         a.n = min(a.n + *a.n_extra, a.cap);
         a.tpu = (a.n + kF32Tile - 1) / kF32Tile;

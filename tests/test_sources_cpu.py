@@ -1,0 +1,31 @@
+"""Rules that the library's sources keep and no result shows."""
+import os
+import re
+
+import pytest
+
+from paper_2410_18517_b200 import build as kbuild
+
+
+def kernel(source, name):
+    """The text of a kernel, up to the next one."""
+    with open(os.path.join(kbuild.CSRC, source)) as f:
+        parts = f.read().split("__global__")
+    found = [p for p in parts[1:] if re.match(r"[^{;]*\b%s\(" % name, p)]
+    assert len(found) == 1, (source, name)
+    return found[0]
+
+
+@pytest.mark.parametrize("source,name", [
+    ("kvs_kernels.cu", "decode_splitk_scalar"), ("kvs_mma.cu", "decode_splitk_mma"), ("kvs_pack4_mma.cu", "decode_pack4_mma"),
+    ("kvs_pack4.cu", "decode_pack4_f32"), ("kvs_tree.cu", "tree_attention_fma"), ("kvs_tree_tc.cu", "tree_attention_tc"),
+])
+def test_attention_kernels_wait_before_they_let_the_next_launch_start(source, name):
+    """What a later launch may fetch early (safe_rows_of) rests on it: once such a kernel has let its successor start,
+    everything before the kernel is complete."""
+    text = kernel(source, name)
+    releases = [m.start() for m in re.finditer(r"pdl_launch_dependents\(\);", text)]
+    waits = [m.start() for m in re.finditer(r"pdl_wait\(\);", text)]
+    assert releases and len(waits) >= len(releases)
+    for n, at in enumerate(releases):        # every role of the kernel waits, then releases
+        assert sum(w < at for w in waits) > n, (source, text[at - 200:at])
