@@ -524,8 +524,8 @@ kvs_status kvs_step_host(kvs_ctx* ctx, const void* q_host, const void* k_host, c
  *     bookkeeping, so it may be issued on another stream than the context's other calls, provided
  *     that stream waits (event) for the kernels that append the rows the call is to see; the other
  *     calls need not wait for it, except those that move or overwrite rows it reads: kvs_evict,
- *     kvs_accept_draft, and appends behind kvs_truncate or kvs_reset.  It reads the slot lengths as
- *     they stand on the host at the call.
+ *     kvs_accept_draft, kvs_reorder, and appends behind kvs_truncate or kvs_reset.  It reads the slot
+ *     lengths as they stand on the host at the call.
  *   device_status: device pointer to an int32 (4-byte aligned, else INVALID_ARG) that receives 0,
  *     KVS_ERR_TIMEOUT if a bounded wait inside the kernel ran out, or (only under KVS_OPT_REPLAY)
  *     KVS_ERR_CAPACITY if a replayed launch passed max_seq; may be NULL (the word inside the array

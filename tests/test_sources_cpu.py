@@ -29,3 +29,22 @@ def test_attention_kernels_wait_before_they_let_the_next_launch_start(source, na
     assert releases and len(waits) >= len(releases)
     for n, at in enumerate(releases):        # every role of the kernel waits, then releases
         assert sum(w < at for w in waits) > n, (source, text[at - 200:at])
+
+
+def header_before(declaration):
+    """The comment in front of a declaration of the C interface, as one line of words."""
+    with open(os.path.join(kbuild.CSRC, "..", "..", "include", "kvs.h")) as f:
+        text = f.read()
+    text = text[:text.index(declaration)]
+    return " ".join(text[text.rindex("/*"):].replace("\n *", " ").split())
+
+
+def test_static_attention_names_the_calls_that_must_wait_for_it():
+    """Every call that may move rows (rows_moved in its body)."""
+    with open(os.path.join(kbuild.CSRC, "kvs_api.cu")) as f:
+        parts = re.split(r"\nkvs_status (kvs_\w+)\(", f.read())
+    movers = {name for name, body in zip(parts[1::2], parts[2::2]) if "rows_moved(" in body}
+    assert {"kvs_evict", "kvs_accept_draft", "kvs_reorder"} <= movers
+    words = header_before("kvs_status kvs_decode_attention_static(")
+    waits = words[words.index("move or overwrite rows it reads"):]
+    assert all(name in waits for name in movers)
