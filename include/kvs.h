@@ -398,7 +398,7 @@ kvs_status kvs_read_rows(kvs_ctx* ctx, int32_t layer, int32_t first, int32_t n_r
  *   out_scores, out_tokens, out_parents: device, float32 / int32 [n_requests][n_out]; parents are sequence numbers of the batch,
  *                  as kvs_reorder takes them.  Where a request has fewer candidates: minus infinity, -1, its first sequence.
  *                  None may overlap an input.
- * n_beams and n_out are at most 64; n_requests * n_beams at most max_batch; n_beams * vocab below 2^31.  The cache is neither
+ * n_beams and n_out are at most 64; n_requests * n_beams at most max_batch and 65535; n_beams * vocab below 2^31.  The cache is neither
  * read nor changed.  Two launches.  The same call gives the same bits, and rows with equal bits equal scores.
  * Errors: STATE before bind; INVALID_ARG for the above. */
 kvs_status kvs_beam_select(kvs_ctx* ctx, const void* logits, int32_t logits_dtype, int64_t logits_stride, int32_t vocab,

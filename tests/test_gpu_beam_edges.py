@@ -4,7 +4,8 @@ import math
 import pytest
 import torch
 
-from paper_2410_18517_b200 import SharedKVCache
+from paper_2410_18517_b200 import KvsError, SharedKVCache
+from paper_2410_18517_b200 import binding as kb
 from paper_2410_18517_b200 import build as kbuild
 
 pytestmark = pytest.mark.gpu
@@ -71,4 +72,22 @@ def test_select_logits_that_differ_by_less_than_scores_show(dtype, V):
             assert got[K][1] == want[1]
         for r in range(2):
             assert got[K][r] == got[64][r][:K], (K, r)
+    assert cache.device_status() == 0
+
+
+def test_select_takes_as_many_rows_as_the_header_says():
+    """65535 rows, and not one more, though the cache has room for them."""
+    cache = SharedKVCache(1, 1, 1, 64, 65536, 1, "bf16")
+    x = torch.zeros(65536, 2, device="cuda")
+    x[:, 1] = torch.arange(65536, device="cuda") * 1e-4 - 3
+    scores = torch.zeros(65536, device="cuda")
+    s, t, p = cache.beam_select(x[:65535], scores[:65535], 1, 2)
+    want = x[:65535].double().log_softmax(-1).sort(dim=-1, descending=True, stable=True)
+    assert torch.equal(t.long(), want.indices) and torch.equal(p[:, 0], torch.arange(65535, device="cuda").int())
+    # one exponential below 1 (2^-22; its argument, at most 3.6, rounded twice: 7.2 * 2^-24), a sum (2^-24), and the rounding of
+    # the score, below 4.3 in size (4.3 * 2^-24)
+    assert float((s.double() - want.values).abs().max()) < 17 * 2.0 ** -24
+    with pytest.raises(KvsError) as e:
+        cache.beam_select(x, scores, 1, 2)
+    assert e.value.status == kb.KVS_ERR_INVALID_ARG
     assert cache.device_status() == 0

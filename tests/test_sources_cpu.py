@@ -48,3 +48,11 @@ def test_static_attention_names_the_calls_that_must_wait_for_it():
     words = header_before("kvs_status kvs_decode_attention_static(")
     waits = words[words.index("move or overwrite rows it reads"):]
     assert all(name in waits for name in movers)
+
+
+def test_header_states_the_rows_that_selection_takes():
+    words = header_before("kvs_status kvs_beam_select(")
+    with open(os.path.join(kbuild.CSRC, "kvs_api.cu")) as f:
+        body = re.split(r"\nkvs_status (?=kvs_\w+\()", f.read())
+    limit = re.search(r"n_requests \* n_beams > (\d+)\)", next(b for b in body if b.startswith("kvs_beam_select("))).group(1)
+    assert f"n_requests * n_beams at most max_batch and {limit}" in words
