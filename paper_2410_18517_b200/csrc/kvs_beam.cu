@@ -306,6 +306,12 @@ __global__ void __launch_bounds__(kBeamThreads, 5) beam_segments_kernel(const Be
     if (room && tid < a.K && tid >= s_count) out[tid] = 0;
 }
 
+// Blocks that start early settle where the first kernel's blocks leave room, several on an SM, and then wait for one another's
+// fp64 arithmetic.  Shared memory that nothing uses keeps them apart as long as each can have an SM (16 requests x 8 beams x
+// 131071 logits, 16 / 17 / 32 continuations: 21.9 / 29.4 / 34.4 us without, 20.3 / 24.8 / 28.7 with it; 148 requests x 4 x 32000
+// 18.4 and 18.1); with more requests they have to share (200 x 1 x 32000: 11.9 and 14.3, 1024 x 2 x 2000: 19.0 and 32.5).
+constexpr int kFinishApart = 80 * 1024;
+
 __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKernelArgs a) {
     __shared__ Wide s_list[kBeamRoom];
     __shared__ Wide s_keys[kBeamThreads];
@@ -350,24 +356,29 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
     }
     __syncthreads();
     const Wide lowest = {order_of(-(double)INFINITY), 0ull};      // scores of minus infinity and NaN are no candidates
-    auto candidate = [&](uint64_t k, int beam) {
-        Wide w = lowest;
-        if (k) {
-            const double score = s_base[beam] + ((double)value_of((uint32_t)(k >> 32)) - (double)s_top[beam]);
-            if (score > -(double)INFINITY)
-                w = {order_of(score), (uint64_t)(a.W - 1 - beam) << (32 + a.token_bits) | (k >> 32) << a.token_bits | ((uint32_t)a.vocab - 1 - ~(uint32_t)k)};
-        }
-        return w;
+    // an entry's score (as an order), and its key once that is known
+    auto score_of = [&](uint64_t k, int beam) {
+        if (k == 0) return lowest.v;
+        const double score = s_base[beam] + ((double)value_of((uint32_t)(k >> 32)) - (double)s_top[beam]);
+        return score > -(double)INFINITY ? order_of(score) : lowest.v;
+    };
+    auto key_of = [&](uint64_t v, uint64_t k, int beam) {
+        const uint32_t tokens_after = (uint32_t)a.vocab - 1 - ~(uint32_t)k;
+        return Wide{v, (uint64_t)(a.W - 1 - beam) << (32 + a.token_bits) | (k >> 32) << a.token_bits | tokens_after};
     };
     // The threads' best entries, in fp32 (whose rounding keeps the order), or the best of four threads each: what is below the
     // K-th largest of those is not among the K best.
     const int per = a.segs * a.K;                 // entries of a beam
-    auto entry = [&](int j, int e) { return candidate(j < AHEAD ? ahead[j] : __ldcg(list + e), e / per); };
     float most = -INFINITY;
+    uint64_t scores[AHEAD];
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j)
-        if (tid + j * kBeamThreads < entries) most = fmaxf(most, (float)value_of(entry(j, tid + j * kBeamThreads).v));
-    for (int e = tid + AHEAD * kBeamThreads; e < entries; e += kBeamThreads) most = fmaxf(most, (float)value_of(entry(AHEAD, e).v));
+    for (int j = 0; j < AHEAD; ++j) {
+        const int e = tid + j * kBeamThreads;
+        scores[j] = e < entries ? score_of(ahead[j], e / per) : lowest.v;
+        most = fmaxf(most, (float)value_of(scores[j]));
+    }
+    for (int e = tid + AHEAD * kBeamThreads; e < entries; e += kBeamThreads)
+        most = fmaxf(most, (float)value_of(score_of(__ldcg(list + e), e / per)));
     const bool quads = a.K <= 16;
     if (quads) {
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
@@ -377,17 +388,19 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
     __syncthreads();
     kth_of(s_head, quads ? kBeamThreads / 4 : kBeamThreads, s_head[quads ? tid % (kBeamThreads / 4) : tid], a.K, &s_cut);
     const float cut = value_of(s_cut);
-    auto reaches = [&](const Wide& w) { return above(w, lowest) && (float)value_of(w.v) >= cut; };
-    auto offer = [&](const Wide& w) {
-        if (reaches(w)) {
+    auto reaches = [&](uint64_t v) { return v > lowest.v && (float)value_of(v) >= cut; };
+    auto offer = [&](uint64_t v, uint64_t k, int e) {
+        if (reaches(v)) {
             const int at = atomicAdd(&s_count, 1);
-            if (at < kBeamRoom) s_list[at] = w;
+            if (at < kBeamRoom) s_list[at] = key_of(v, k, e / per);
         }
     };
 #pragma unroll
-    for (int j = 0; j < AHEAD; ++j)
-        if (tid + j * kBeamThreads < entries) offer(entry(j, tid + j * kBeamThreads));
-    for (int e = tid + AHEAD * kBeamThreads; e < entries; e += kBeamThreads) offer(entry(AHEAD, e));
+    for (int j = 0; j < AHEAD; ++j) offer(scores[j], ahead[j], tid + j * kBeamThreads);
+    for (int e = tid + AHEAD * kBeamThreads; e < entries; e += kBeamThreads) {
+        const uint64_t k = __ldcg(list + e);
+        offer(score_of(k, e / per), k, e);
+    }
     __syncthreads();
     if (s_count > kBeamRoom) {
         // more than there is room for (many equal scores): a row of entries of all threads at a time, keeping the best so far
@@ -397,8 +410,11 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
         int held = 0;
         Wide least = lowest;
         for (int e0 = 0; e0 < entries; e0 += kBeamThreads) {
-            const Wide w = e0 + tid < entries ? candidate(__ldcg(list + e0 + tid), (e0 + tid) / per) : lowest;
-            const bool in = reaches(w) && !above(least, w);
+            const int e = e0 + tid;
+            const uint64_t k = e < entries ? __ldcg(list + e) : 0;
+            Wide w = lowest;
+            if (k) w = key_of(score_of(k, e / per), k, e / per);
+            const bool in = reaches(w.v) && !above(least, w);
             if (in) s_list[atomicAdd(&s_count, 1)] = w;
             held += __syncthreads_count(in);
             if (held > kBeamRoom - kBeamThreads) {
@@ -555,6 +571,8 @@ size_t reorder_smem(int old_batch, int new_batch) { return kReorderBytes + 2ull 
 }  // namespace
 
 cudaError_t init_beam_kernels() {
+    const cudaError_t e = cudaFuncSetAttribute(beam_finish_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFinishApart);
+    if (e != cudaSuccess) return e;
     return cudaFuncSetAttribute(reorder_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)reorder_smem(kReorderMaxBatch, kReorderMaxBatch));
 }
 
@@ -589,7 +607,8 @@ cudaError_t launch_beam_select(const BeamArgs& p, cudaStream_t stream) {
     const cudaError_t err = p.dtype == 0 ? launch_kernel(beam_segments_kernel<__nv_bfloat16>, grid, dim3(kBeamThreads), 0, stream, p.programmatic, a)
                                          : launch_kernel(beam_segments_kernel<float>, grid, dim3(kBeamThreads), 0, stream, p.programmatic, a);
     if (err != cudaSuccess) return err;
-    return launch_kernel(beam_finish_kernel, dim3(p.requests), dim3(kBeamThreads), 0, stream, p.programmatic, a);
+    return launch_kernel(beam_finish_kernel, dim3(p.requests), dim3(kBeamThreads), p.requests <= p.sm_count ? kFinishApart : 0, stream,
+                         p.programmatic, a);
 }
 
 cudaError_t launch_reorder(const ReorderArgs& p, const ReorderRows& rows, cudaStream_t stream) {

@@ -91,3 +91,22 @@ def test_select_takes_as_many_rows_as_the_header_says():
         cache.beam_select(x, scores, 1, 2)
     assert e.value.status == kb.KVS_ERR_INVALID_ARG
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_select_of_as_many_requests_as_the_device_has_sms_and_more(dtype):
+    n = torch.cuda.get_device_properties(0).multi_processor_count
+    cache = SharedKVCache(1, 1, 1, 64, 2 * (2 * n + 1), 1, "bf16")
+    for R in (n - 1, n, n + 1, 2 * n + 1):
+        x = torch.randn(2 * R, 600, device="cuda", generator=torch.Generator(device="cuda").manual_seed(R)).to(DT[dtype])
+        x[:, 77] = x[:, 5]                       # a tie in every row
+        scores = -torch.rand(2 * R, device="cuda", generator=torch.Generator(device="cuda").manual_seed(R + 1))
+        s, t, p = cache.beam_select(x, scores, 2, 20)
+        total = (scores.double()[:, None] + x.double().log_softmax(-1)).view(R, -1)
+        want = total.sort(dim=-1, descending=True, stable=True)
+        assert float((s.double() - want.values[:, :20]).abs().max()) < 2.0 ** -22 + 32 * 2.0 ** -24 + 16 * 2.0 ** -24
+        # the order within a beam is exact; between beams scores may be as close as their error
+        chosen = total.gather(1, (t + 600 * (p - 2 * torch.arange(R, device="cuda").int()[:, None])).long())
+        assert float((chosen - want.values[:, :20]).abs().max()) < 2.0 ** -21 + 64 * 2.0 ** -24
+        assert all(len(set(zip(t[r].tolist(), p[r].tolist()))) == 20 for r in range(0, R, 37))
+    assert cache.device_status() == 0
