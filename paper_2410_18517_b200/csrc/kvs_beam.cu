@@ -26,6 +26,12 @@ constexpr int kBeamThreads = 256;
 constexpr int kBeamAhead = 4;                             // 16-byte pieces of logits a thread has in flight
 constexpr int kBeamRoom = 2048;                           // candidates a block has room for
 constexpr int kBeamRun = 8;                               // logits of a thread at a time where there are too many
+// Up to so many continuations the threshold is taken from the maxima of four threads each, a quarter of the numbers to rank; with
+// more it falls so low that too many logits reach it (16 x 8 beams x 131071 bf16, 4 / 16 / 24 / 32 continuations: 16.4 / 20.3 /
+// 22.5 / 28.0 us by fours, 22.0 / 24.8 / 26.4 / 28.9 by threads; 4 beams x 32000 fp32: 6.7 / 10.7 / 13.4 / 36.2 and 9.0 / 12.4 /
+// 14.9 / 18.4).
+constexpr int kBeamQuads = 24;
+static_assert(kBeamQuads <= kBeamThreads / 4 && kBeamMaxOut <= kBeamThreads, "at least as many maxima as continuations");
 static_assert(kBeamMaxOut * (kBeamRun + 1) * 2 <= kBeamRoom, "what is kept, and what a run adds");
 
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -213,7 +219,7 @@ __global__ void __launch_bounds__(kBeamThreads, 5) beam_segments_kernel(const Be
         m = top;
     }
     // the threshold; for few continuations the maxima of four threads each are enough of them
-    const bool quads = a.K <= 16;
+    const bool quads = a.K <= kBeamQuads;
     float most = m;
     if (quads) {
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
@@ -379,7 +385,7 @@ __global__ void __launch_bounds__(kBeamThreads) beam_finish_kernel(const BeamKer
     }
     for (int e = tid + AHEAD * kBeamThreads; e < entries; e += kBeamThreads)
         most = fmaxf(most, (float)value_of(score_of(__ldcg(list + e), e / per)));
-    const bool quads = a.K <= 16;
+    const bool quads = a.K <= kBeamQuads;
     if (quads) {
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));

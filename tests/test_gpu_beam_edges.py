@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from test_gpu_beam import check_select, logits_of
 from paper_2410_18517_b200 import KvsError, SharedKVCache
 from paper_2410_18517_b200 import binding as kb
 from paper_2410_18517_b200 import build as kbuild
@@ -110,3 +111,13 @@ def test_select_of_as_many_requests_as_the_device_has_sms_and_more(dtype):
         assert float((chosen - want.values[:, :20]).abs().max()) < 2.0 ** -21 + 64 * 2.0 ** -24
         assert all(len(set(zip(t[r].tolist(), p[r].tolist()))) == 20 for r in range(0, R, 37))
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [24, 25])
+def test_select_either_way_to_the_threshold(dtype, K):
+    """Up to 24 continuations the threshold comes from the maxima of four threads, above from each thread's."""
+    cache = SharedKVCache(1, 1, 1, 64, 6, 1, "bf16")
+    for V in (900, 40001):
+        check_select(cache, logits_of(V + K, dtype, 6, V), -torch.arange(6.0).cuda() / 3, 3, K)
+    check_select(cache, torch.full((6, 3000), 0.5, dtype=DT[dtype], device="cuda"), torch.zeros(6).cuda(), 3, K)
