@@ -57,8 +57,8 @@ struct Wide {
 __device__ __forceinline__ bool above(uint64_t a, uint64_t b) { return a > b; }
 __device__ __forceinline__ bool above(const Wide& a, const Wide& b) { return a.v > b.v || (a.v == b.v && a.t > b.t); }
 
-// The K-th largest of `n` numbers s_x[0 .. n-1] (n a multiple of four, at least 4), of which thread t < n holds `mine`, as
-// order_of: into *cut, which is to hold the highest order before.  n < K: minus infinity.  Ends with a barrier.
+// The K-th largest of `n` numbers s_x[0 .. n-1] (n a multiple of four, at least K), of which thread t < n holds `mine`, as
+// order_of: into *cut, which is to hold the highest order before.  Ends with a barrier.
 __device__ __forceinline__ void kth_of(const float* s_x, int n, float mine, int K, uint32_t* cut) {
     if ((int)threadIdx.x < n) {
         int rank = 0;
@@ -67,7 +67,7 @@ __device__ __forceinline__ void kth_of(const float* s_x, int n, float mine, int 
             const float4 x = *reinterpret_cast<const float4*>(s_x + j);
             rank += (x.x > mine) + (x.y > mine) + (x.z > mine) + (x.w > mine);
         }
-        if (rank < K) atomicMin(cut, order_of(n < K ? -INFINITY : mine));
+        if (rank < K) atomicMin(cut, order_of(mine));
     }
     __syncthreads();
 }

@@ -206,13 +206,6 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ uint64_t pair_of(float lo, float hi) { return (uint64_t)__float_as_uint(hi) << 32 | __float_as_uint(lo); }
 __device__ __forceinline__ float low_of(uint64_t x) { return __uint_as_float((uint32_t)x); }
 __device__ __forceinline__ float high_of(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
-
-// The values are made from the pieces anew wherever they are needed: eight floats a piece would not fit beside them.
-template <int NV>
-__device__ __forceinline__ void only_pieces(uint4 (&x)[NV]) {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) asm volatile("" : "+r"(x[j].x), "+r"(x[j].y), "+r"(x[j].z), "+r"(x[j].w));
-}
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     uint64_t r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));

@@ -56,3 +56,13 @@ def test_header_states_the_rows_that_selection_takes():
         body = re.split(r"\nkvs_status (?=kvs_\w+\()", f.read())
     limit = re.search(r"n_requests \* n_beams > (\d+)\)", next(b for b in body if b.startswith("kvs_beam_select("))).group(1)
     assert f"n_requests * n_beams at most max_batch and {limit}" in words
+
+
+def test_no_function_that_nothing_calls():
+    text = ""
+    for source in kbuild.SOURCES + kbuild.HEADERS:
+        with open(os.path.join(kbuild.CSRC, source)) as f:
+            text += re.sub(r"//[^\n]*|/\*.*?\*/", "", f.read(), flags=re.S)
+    names = set(re.findall(r"__(?:device|host)__ (?:__forceinline__|__noinline__|constexpr|__host__|__device__| )*[\w:&* ]*?\b(\w+)\(", text))
+    assert len(names) > 40
+    assert not [n for n in sorted(names) if len(re.findall(r"\b%s\b" % n, text)) < 2]
