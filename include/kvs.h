@@ -159,7 +159,10 @@ kvs_status kvs_set_share_map(kvs_ctx* ctx, const int32_t* share_map);
  *     s = (hi - lo) * (1/15) rounded up to bf16 (1/15: the nearest fp32),   b = lo - 16 s rounded to bf16,
  *     code c = clamp(rint((x - b) / s) - 16, 0, 15)  (ties to even; s = 0: c = 0),   value = s * (16 + c) + b
  * and the value, rounded once to the storage type, is what the cache holds of x: it differs from x by at most s/2, the
- * rounding of b (2^-8 |b|) and its own.  A group with an infinity or a NaN in it, or whose s or b overflows, has only NaN values
+ * rounding of b (2^-8 |b|) and its own.  The fp32 1/15 is a little above it and s is rounded up, so a range of exactly 15 steps of
+ * a bf16 number mostly gets the next larger step (109 of the 128 significands): values read from a 4-bit cache and stored in
+ * one again are in general not the same, but off by as much once more.  Move rows by kvs_reorder or as bytes where they are to
+ * stay.  A group with an infinity or a NaN in it, or whose s or b overflows, has only NaN values
  * (s = b = NaN, bits 0x7fc0, codes 0).
  * A row takes 16 + D/2 bytes (80 or 48): the pairs (s, b) of the groups as bf16, then the codes, element 8 w + i in bits
  * 4 i .. 4 i + 3 of word w; planes are [max_batch][n_kv_heads][row_stride] such rows.

@@ -5,7 +5,8 @@
 //   code c = clamp(rint((x - b) / s) - 16, 0, 15),  value = s * (16 + c) + b rounded once to the storage type
 // Why 16 + c and not c: four bits laid at bits 3..6 of a bf16 whose upper bits are those of 16.0 ARE the number 16 + c, so
 // one OR makes a factor of the code and one fused multiply-add the value.  Why s is rounded up: the largest element then has
-// a code of its own, and every element is off by at most s/2 plus the rounding of b (half a bf16 step).
+// a code of its own, and every element is off by at most s/2 plus the rounding of b (half a bf16 step).  The nearest fp32 of 1/15
+// is above 1/15, so a range of exactly 15 bf16 steps mostly gets the next larger step: rows' values are not stored as they are.
 // A group that holds an infinity or a NaN, or whose s or b overflows, gets NaN for both: all its values are NaN.
 //
 // Layout, 16 + D/2 bytes: four words s | b << 16 (bf16 each), one per group, then D/2 bytes of codes, element 8 w + i in

@@ -45,3 +45,15 @@ def test_groups_whose_range_is_near_the_largest_number(dtype, D):
     wide = x.float().unflatten(1, (4, -1))
     wide = (wide.amax(-1) - wide.amin(-1) > 1.7e38) & ~want.unflatten(1, (4, -1)).isnan().any(-1)
     assert int(wide.sum()) > 20                  # groups with values whose differences overflow
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_lie_on_sixteen_levels(dtype):
+    """Grids of every bf16 significand, and values read from such a cache: stored (again) as the definition says, bit for bit."""
+    steps = torch.arange(128).mul(2.0 ** -7).add(1.0).bfloat16().float()
+    grids = (torch.arange(16).repeat(4)[None] * steps[:, None]).to(DT[dtype])
+    for x in (grids, torch.randn(300, 64, generator=torch.Generator().manual_seed(3)).to(DT[dtype])):
+        for _ in range(3):
+            raw, values = stored(x, dtype)
+            assert torch.equal(raw, ref.row_bytes(x)) and torch.equal(values, ref.values(x))
+            x = values
