@@ -18,8 +18,11 @@ namespace {
 // more do, and only the logits of threads whose maximum does are read again (from L2, a warp for a thread's pieces).  Where
 // too many reach it (equal logits, sorted ones) the candidates become 64-bit keys - order of the value, then the lower index, all different - and the
 // threads' best of those bound them, a run of logits at a time: exactly K threads reach the K-th largest.
-// Second kernel, a block per request: lse in fp64 (a rounding of 1e-7 would decide between beams whose scores nearly tie), the
-// lists' entries by the same kind of threshold, and the K best in order.
+// Second kernel, a block per request: the segments' sums merged and scores formed in fp64 (the order within a beam is then the
+// logits', rows with equal bits tie exactly, and no rounding of a score near -20, 1e-6, decides between beams), the lists'
+// entries by the same kind of threshold, and the K best in order.  The sums themselves are of fp32 exponentials (ex2.approx, 2^-22)
+// added in fp32 within a segment: lse was off by 2.3e-7 at most over random rows of 1000 to 1000003 logits, and beams whose scores
+// are closer than that may come in either order.
 // Bound: HBM for the logits, once; small calls: two launches.
 // --------------------------------------------------------------------------------------
 constexpr int kBeamThreads = 256;

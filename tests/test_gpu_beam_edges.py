@@ -121,3 +121,21 @@ def test_select_either_way_to_the_threshold(dtype, K):
     for V in (900, 40001):
         check_select(cache, logits_of(V + K, dtype, 6, V), -torch.arange(6.0).cuda() / 3, 3, K)
     check_select(cache, torch.full((6, 3000), 0.5, dtype=DT[dtype], device="cuda"), torch.zeros(6).cuda(), 3, K)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,V", [(800, 1000), (800, 131072), (4, 1000003)])
+def test_select_logarithms_are_good_to_a_few_1e_7(dtype, rows, V):
+    """The scores of each row's best token against float64, beside the score's own rounding.  Bound: a term's exponential (2^-22),
+    and for each of the 8 levels at which partial sums meet within a block the rescaling of the smaller one, at most half of
+    the two (2^-22 of it), and the addition (2^-24).  A thread's own additions, up to 16 turns of 32, err either way and stay
+    below what the first term leaves; a sum in order over the row would not."""
+    cache = SharedKVCache(1, 1, 1, 64, rows, 1, "bf16")
+    x = (torch.randn(rows, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(V)) * 4).to(DT[dtype])
+    s, t, _ = cache.beam_select(x, torch.zeros(rows, device="cuda"), 1, 1)
+    for i in range(0, rows, 100):
+        exact = x[i:i + 100].double().log_softmax(-1).gather(1, t[i:i + 100].long())
+        off = (s[i:i + 100].double() - exact).abs() - 2.0 ** -24 * exact.abs()
+        assert float(off.max()) < 2.0 ** -22 + 8 * (2.0 ** -23 + 2.0 ** -24)
+        if dtype == "f32":                       # (bf16 logits tie)
+            assert torch.equal(t[i:i + 100, 0].long(), x[i:i + 100].argmax(-1))
