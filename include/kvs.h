@@ -255,8 +255,12 @@ kvs_status kvs_decode_step(kvs_ctx* ctx, int32_t layer, const void* q, const voi
  * chunk of it (n > n_q).
  *   q:   device, [batch][n_q][n_q_heads][head_dim], storage type, 16-byte aligned
  *   out: device, [batch][n_q][n_q_heads][head_dim], float32
- * bf16 storage: one 4-byte clear and one tcgen05 tensor-core kernel on `stream`.  fp32 storage (the
- * small configuration): one plain fp32 kernel, a warp per query.  A slot rows were evicted from:
+ * bf16 storage: one 4-byte clear and one tcgen05 tensor-core kernel on `stream`; the softmax weights enter
+ * its second product as two bf16 terms (off by at most 2^-16 of themselves, some 3e-6 of a result; its
+ * accumulators leave no room for a third, which single tokens over a 4-bit cache have: 2^-24).  fp32 storage
+ * (the small configuration): one plain fp32 kernel, a warp per query.  A 4-bit cache: its rows go to the
+ * workspace in the storage type first, as many sequences at a time as it has room for, a launch more for
+ * each time.  A slot rows were evicted from:
  * STATE.  Other errors as kvs_decode_attention; n_q > n: INVALID_ARG.                             */
 kvs_status kvs_prefill_attention(kvs_ctx* ctx, int32_t layer, const void* q, float* out,
                                  int32_t batch, int32_t n_q, void* stream);

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+import operators_reference as oref
 import pack4_reference as ref
 from paper_2410_18517_b200 import SharedKVCache
 from paper_2410_18517_b200 import build as kbuild
@@ -57,3 +58,22 @@ def test_values_that_lie_on_sixteen_levels(dtype):
             raw, values = stored(x, dtype)
             assert torch.equal(raw, ref.row_bytes(x)) and torch.equal(values, ref.values(x))
             x = values
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,n,T", [(8, 2, 128, 700, 700), (2, 2, 64, 1300, 5), (7, 1, 128, 150, 33)])
+def test_prompts_and_single_tokens_are_as_exact_as_the_header_says(Hq, Hkv, D, n, T):
+    """Weights of 2^-16 for prompts and 2^-24 for single tokens, over the values the cache stands for."""
+    g = torch.Generator().manual_seed(n)
+    cache = SharedKVCache(1, Hq, Hkv, D, 1, n, "bf16", cache_format="4bit")
+    cache.append(0, *(torch.randn(1, n, Hkv, D, generator=g).bfloat16().cuda() for _ in range(2)))
+    q = torch.randn(1, T, Hq, D, generator=g).bfloat16().cuda()
+    prompt, single = cache.prefill_attention(0, q), cache.decode_attention(0, q[:, -1].contiguous())
+    K, V = (x[0].cpu() for x in cache.read_rows(0))
+    sees = torch.arange(n) <= torch.arange(n - T, n)[:, None]
+    for h in range(Hq):
+        o, _, mass, d = oref.attend(q[0, :, h:h + 1].cpu(), K[:, h // (Hq // Hkv)], V[:, h // (Hq // Hkv)], sees)
+        rest = oref.weight_error(d, n) * mass + oref.U * o.abs()
+        # (the tensor cores' sums over the keys may be cut off instead of rounded: 2^-23 for each product of 16 keys)
+        assert ((prompt[0, :, h:h + 1].cpu().double() - o).abs() <= rest + (2.0 ** -16 + n / 16 * 2.0 ** -23) * mass).all()
+        assert ((single[0, h].cpu().double() - o[-1, 0]).abs() <= rest[-1, 0] + 2.0 ** -24 * mass[-1, 0]).all()
+    assert cache.device_status() == 0
