@@ -17,6 +17,21 @@ __all__ = ["binding", "SharedKVCache", "Rotary", "KvsError"]
 _unfinished = []        # caches closed while a graph was being recorded: (context, device, memory)
 
 
+def _finish():
+    """Ends the caches in ``_unfinished``, unless a graph is still being recorded."""
+    if not _unfinished:
+        return
+    import torch
+
+    while not torch.cuda.is_current_stream_capturing():
+        try:
+            ctx, device, _ = _unfinished.pop()
+        except IndexError:              # the last one, or another thread had it
+            return
+        torch.cuda.synchronize(device)
+        binding.kvs_destroy(ctx)
+
+
 class Rotary:
     """Rotary positions for ``append_rotary``: radians per position of every pair (``rotary_dim / 2`` numbers).
 
@@ -55,6 +70,7 @@ class SharedKVCache:
                  share_map=None, softmax_scale=0.0, device=0, cache_format="plain"):
         import torch
 
+        _finish()
         self._torch = torch
         self.device = torch.device("cuda", device)
         self._index = device
@@ -85,14 +101,11 @@ class SharedKVCache:
         return self._torch.empty(nbytes, dtype=self._torch.uint8, device=self.device)
 
     def close(self):
-        while _unfinished and not self._torch.cuda.is_current_stream_capturing():
-            ctx, device, _ = _unfinished.pop()
-            self._torch.cuda.synchronize(device)
-            binding.kvs_destroy(ctx)
+        _finish()
         if getattr(self, "ctx", None):
             if self._torch.cuda.is_current_stream_capturing():
                 # Python may collect a cache at any time, so also while a graph is being recorded, which waiting for the
-                # device would end: its memory is kept until the next cache is closed
+                # device would end: its memory is kept until the next cache is made or closed
                 _unfinished.append((self.ctx, self.device, (self.pool, self.workspace)))
             else:
                 self._torch.cuda.synchronize(self.device)
