@@ -106,7 +106,8 @@ typedef struct {
 /* Tuning knobs for kvs_set_option.  Defaults are chosen by the library. */
 typedef enum {
     KVS_OPT_MAX_CTAS = 0,   /* upper bound on thread blocks of the split-K kernel; 0 = auto  */
-    KVS_OPT_KERNEL = 1,     /* 0 = auto, 1 = scalar-FMA path, 2 = grouped tensor-core path   */
+    KVS_OPT_KERNEL = 1,     /* 0 = auto, 1 = scalar-FMA path, 2 = grouped tensor-core path (a 4-bit
+                               cache has one kernel per storage type whatever this says)    */
     KVS_OPT_EARLY_START = 2,/* 1 (default): kernels are launched so that they may start while
                                the previous kernel on the stream drains, and prefetch K/V rows
                                that nothing in flight writes; they wait for the previous kernel
@@ -596,7 +597,7 @@ kvs_status kvs_selftest_wait_timeout(kvs_ctx* ctx, uint32_t limit_us, uint64_t* 
  * consumers ended [20], the number of pieces [21], when the producer began to wait [22], and the SM the
  * block ran on [23]; rows 150 and
  * 151 hold entry [0], end of wait [1] and end [2] of the first and the last block of the combine kernel
- * (zero when the call launched none).  kvs_trace_end stops the recording and reports the calls recorded.   */
+ * (zero when the call launched none).  Over a 4-bit cache of fp32 storage only rows 150 and 151 are written.  kvs_trace_end stops the recording and reports the calls recorded.   */
 kvs_status kvs_trace_begin(kvs_ctx* ctx, void* buffer, size_t bytes);
 kvs_status kvs_trace_end(kvs_ctx* ctx, int32_t* launches_recorded);
 /* Self-test of the bounds-checking build (the library compiled with -DKVS_DEBUG_BOUNDS, in which every

@@ -66,3 +66,12 @@ def test_no_function_that_nothing_calls():
     names = set(re.findall(r"__(?:device|host)__ (?:__forceinline__|__noinline__|constexpr|__host__|__device__| )*[\w:&* ]*?\b(\w+)\(", text))
     assert len(names) > 40
     assert not [n for n in sorted(names) if len(re.findall(r"\b%s\b" % n, text)) < 2]
+
+
+def test_trace_and_kernel_choice_of_4bit_caches_are_as_the_header_says():
+    assert "Over a 4-bit cache of fp32 storage only rows 150 and 151" in header_before("kvs_status kvs_trace_begin(")
+    assert "KVS_TRACE_STAMP" not in kernel("kvs_pack4.cu", "decode_pack4_f32") and "KVS_TRACE_STAMP" in kernel("kvs_pack4_mma.cu", "decode_pack4_mma")
+    with open(os.path.join(kbuild.CSRC, "kvs_api.cu")) as f:
+        text = f.read()
+    plan = text[text.index("bool choose_plan("):]
+    assert plan.index("KVS_CACHE_4BIT") < plan.index("return false;") < plan.index("opt_kernel")
