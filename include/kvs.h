@@ -158,7 +158,7 @@ kvs_status kvs_set_share_map(kvs_ctx* ctx, const int32_t* share_map);
  * A 4-bit cache (nothing in the paper: it multiplies with the memory that sharing layers saves) cuts a row of D elements into
  * four groups of D/4.  With lo, hi the group's smallest and largest element, in fp32:
  *     s = (hi - lo) * (1/15) rounded up to bf16 (1/15: the nearest fp32),   b = lo - 16 s rounded to bf16,
- *     code c = clamp(rint((x - b) / s) - 16, 0, 15)  (ties to even; s = 0: c = 0),   value = s * (16 + c) + b
+ *     code c = clamp(rint((x - b) / s) - 16, 0, 15)  (of the exact quotient, ties to even; s = 0: c = 0),   value = s * (16 + c) + b
  * and the value, rounded once to the storage type, is what the cache holds of x: it differs from x by at most s/2, the
  * rounding of b (2^-8 |b|) and its own.  The fp32 1/15 is a little above it and s is rounded up, so a range of exactly 15 steps of
  * a bf16 number mostly gets the next larger step (109 of the 128 significands): values read from a 4-bit cache and stored in

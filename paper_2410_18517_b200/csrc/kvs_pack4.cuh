@@ -139,11 +139,12 @@ __device__ __forceinline__ void pack_group(const uint4 (&in)[Pack4Row<D>::GROUP 
     const float s = __uint_as_float((__float_as_uint(step) + 0xffffu) & 0xffff0000u);
     const float b = __bfloat162float(__float2bfloat16_rn(__fsub_rn(lo, 16.f * s)));
     const bool broken = !(finite(step) && finite(s) && finite(b));
-    const float inv = 1.f / s;
-    // What the two words say is not taken where the rounding of b (up to 2^-8 |b|) can bring a quotient past 15.5 or 31.5,
-    // and where fp32 steps do not carry: where s is tiny its reciprocal may overflow and products may lose bits, where it is
-    // huge x - b, up to 31 s, may overflow.
-    const bool carries = s >= 1e-30f && s <= 1e36f, plain = fabsf(b) <= 100.f * s && carries;
+    // Where s is tiny its reciprocal may overflow and products may lose bits, where it is huge x - b, up to 31 s, may overflow:
+    // code_of takes all of it times a power of two there (exact but for an element below 2^-147 beside a step above 1e36).
+    const float scale = s > 1e36f ? 0.25f : s < 1e-30f ? 18446744073709551616.f : 1.f;
+    const float inv = 1.f / (s * scale);
+    // What the two words say is not taken then, nor where the rounding of b (up to 2^-8 |b|) can bring a quotient past 15.5 or 31.5.
+    const bool plain = fabsf(b) <= 100.f * s && scale == 1.f;
     const uint64_t minus = pair_of(-b, -b), above = pair_of(inv * 1.000001f, inv * 1.000001f), under = pair_of(inv * 0.999999f, inv * 0.999999f);
     const uint64_t magic = pair_of(kRint, kRint);
 #pragma unroll
@@ -163,19 +164,12 @@ __device__ __forceinline__ void pack_group(const uint4 (&in)[Pack4Row<D>::GROUP 
         if (unsure && !broken) {
             if (s == 0.f) {
                 one = 0;
-            } else if (!carries) {
-                one = 0;
-#pragma unroll
-                for (int i = 7; i >= 0; --i) {
-                    const double q = rint(((double)x[i] - (double)b) / (double)s);
-                    one = one * 16 + (uint32_t)(fmin(fmax(q, 16.0), 31.0) - 16.0);
-                }
             } else {
                 while (unsure) {
                     const int i = (__ffs(unsure) - 1) / 4;
                     const float y0 = i & 1 ? x[1] : x[0], y1 = i & 1 ? x[3] : x[2], y2 = i & 1 ? x[5] : x[4], y3 = i & 1 ? x[7] : x[6];
                     const float y = i & 4 ? (i & 2 ? y3 : y2) : (i & 2 ? y1 : y0);
-                    one = (one & ~(15u << (4 * i))) | code_of(y, s, b, inv) << (4 * i);
+                    one = (one & ~(15u << (4 * i))) | code_of(y * scale, s * scale, b * scale, inv) << (4 * i);
                     unsure &= ~(15u << (4 * i));
                 }
             }

@@ -1,4 +1,8 @@
 """The 4-bit cache where its numbers are extreme."""
+import math
+import random
+from fractions import Fraction
+
 import pytest
 import torch
 
@@ -77,3 +81,34 @@ def test_prompts_and_single_tokens_are_as_exact_as_the_header_says(Hq, Hkv, D, n
         assert ((prompt[0, :, h:h + 1].cpu().double() - o).abs() <= rest + (2.0 ** -16 + n / 16 * 2.0 ** -23) * mass).all()
         assert ((single[0, h].cpu().double() - o[-1, 0]).abs() <= rest[-1, 0] + 2.0 ** -24 * mass[-1, 0]).all()
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("at", [-130, -110, -60, 0, 60, 123])
+def test_ties_that_a_tiny_element_decides(dtype, at):
+    """Elements that are next to nothing beside their group's step, where -b / s is a whole number and a half: their sign
+    decides between two codes, though x - b is b in fp64 too.  Against rationals, steps of every size."""
+    n, group = 400, 16
+    r = random.Random(at)
+    x = torch.zeros(n, 64, dtype=torch.float64)
+    for t in range(n):
+        for k in range(4):
+            # hi - lo is 15 s up to rounding, lo such that b = lo - 16 s lies on a half step
+            s = r.randint(128, 255) * 2.0 ** (at - 8)
+            lo = -s * (r.randint(0, 14) + 0.5)
+            x[t, 16 * k], x[t, 16 * k + 1] = lo, lo + 15 * s * (1 - 2.0 ** -6)
+            for i in range(2, group):
+                x[t, 16 * k + i] = r.choice((-1, 1)) * 2.0 ** max(-133, at - r.choice((20, 60, 100, 200)))
+    x = x.to(DT[dtype])
+    raw, _ = stored(x, dtype)
+    head = raw[:, :16].clone().view(torch.bfloat16).view(n, 4, 2)
+    codes = torch.stack((raw[:, 16:] & 15, raw[:, 16:] >> 4), -1).view(n, 4, group)
+    ties = 0
+    for t in range(n):
+        for k in range(4):
+            s, b = (Fraction(float(v)) for v in head[t, k])
+            for i in range(group):
+                q = (Fraction(float(x[t, group * k + i])) - b) / s
+                ties += abs(q - (math.floor(q) + Fraction(1, 2))) < Fraction(1, 2 ** 18)
+                assert int(codes[t, k, i]) == min(15, max(0, round(q) - 16)), (t, k, i, float(q))
+    assert ties > 50
