@@ -12,7 +12,7 @@ namespace {
 // Storing.  A lane takes a group of a row, four lanes a row, rows dealt out with the tokens of a head in a run, so that what a
 // warp writes is contiguous (see pack_group).
 // Bound: HBM, 2 D e bytes in and D + 32 out per token and head, once the instructions are few: 4 x 4096 tokens of 8 heads of 128 took
-// 67 us with 64-bit divisions and ties settled in fp64, 46 without, 24 with a group per lane (155 MB with the reading: 3.6 TB/s).
+// 67 us with 64-bit divisions and ties settled in fp64, 46 without, 24 with a group per lane, 22.8 without fp64 (88 MB: 3.9 TB/s).
 // --------------------------------------------------------------------------------------
 constexpr int kPackThreads = 256;
 

@@ -18,7 +18,10 @@
 //
 // What bounds it: the conversion.  A row of K and V together is D + 32 bytes, 7 cycles of an SM at 6.5 TB/s; its codes take 11 warp
 // instructions to become operands, 7 of them on the integer pipe and 4 on the heavy half of the FMA pipe, which take one every
-// other cycle and hardly overlap; the MMAs (1.5 a row) and the rest take as long again.
+// other cycle and hardly overlap; the MMAs (1.5 a row) and the rest take as long again.  And registers: ten warps put three on one SM
+// partition, which leaves a thread 168, and heads of 128 spill (32 bytes stored and 116 loaded a thread, with five to eight heads 68
+// and 240; what that costs is not measured).  13B shape, 16 x 40 heads x 8192 rows: 190 to 208 us over several GPUs, 8 x 8 kv-heads x
+// 32768 rows 83 to 88; 16 x 8 x 8192 rows with four heads each 48, with eight 61.
 //
 // Work decomposition (see DecodePlan), pieces, the hand-over between blocks and the combine kernel are those of the other
 // split-K kernels.  Rows of a tile are contiguous and come by two 1-D bulk copies, exactly as many as the unit holds.  A tile
