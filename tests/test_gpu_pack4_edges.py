@@ -8,7 +8,8 @@ import torch
 
 import operators_reference as oref
 import pack4_reference as ref
-from paper_2410_18517_b200 import SharedKVCache
+from paper_2410_18517_b200 import KVS_OPT_REPLAY, Rotary, SharedKVCache
+from paper_2410_18517_b200 import binding as kb
 from paper_2410_18517_b200 import build as kbuild
 
 pytestmark = pytest.mark.gpu
@@ -112,3 +113,72 @@ def test_ties_that_a_tiny_element_decides(dtype, at):
                 ties += abs(q - (math.floor(q) + Fraction(1, 2))) < Fraction(1, 2 ** 18)
                 assert int(codes[t, k, i]) == min(15, max(0, round(q) - 16)), (t, k, i, float(q))
     assert ties > 50
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_steps_recorded_and_replayed_to_the_end(dtype):
+    """Rotary append and attention over 4-bit rows, replayed until the slot is full: the rows of eager steps; one replay more
+    stores nothing and says so."""
+    Hq, Hkv, D, B, n, steps = 8, 2, 64, 3, 61, 5
+    g = torch.Generator().manual_seed(0)
+    new = lambda *s: torch.randn(*s, generator=g).to(DT[dtype]).cuda()  # noqa: E731
+    eager, graph = (SharedKVCache(2, Hq, Hkv, D, B, n + steps, dtype, share_map=[0, 0], cache_format="4bit") for _ in range(2))
+    k, v = new(B, n, Hkv, D), new(B, n, Hkv, D)
+    for c in (eager, graph):
+        c.append(0, k, v)
+    graph.set_option(KVS_OPT_REPLAY, 1)
+    rot, x = Rotary.from_theta(D), torch.zeros(B, 1, Hq + 2 * Hkv, D, dtype=DT[dtype], device="cuda")
+    pos = torch.zeros(B, 1, dtype=torch.int32, device="cuda")
+
+    def step(c, out):
+        q = c.append_rotary(0, x[:, :, :Hq], x[:, :, Hq:Hq + Hkv], x[:, :, Hq + Hkv:], pos, rot)
+        for l in range(2):
+            c.decode_attention(l, q[:, 0].contiguous(), out[l])
+
+    got, want = (torch.zeros(2, B, Hq, D, device="cuda") for _ in range(2))
+    rec = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(rec):
+        step(graph, got)
+        graph.replay_advance()
+    for t in range(steps):
+        x.copy_(new(*x.shape))
+        pos.fill_(n + t)
+        rec.replay()
+        step(eager, want)
+        # (tiles are dealt out for the recorded length: another order of the same fp32 sums of some 60 rows)
+        assert float((got - want).abs().max()) <= 70 * 2.0 ** -24 * 4
+    assert graph.device_status() == 0
+    before = [graph.plane(0, kv).clone() for kv in range(2)]
+    rec.replay()
+    torch.cuda.synchronize()
+    assert graph.device_status() == kb.KVS_ERR_CAPACITY
+    assert all(torch.equal(graph.plane(0, kv), before[kv]) for kv in range(2))
+    graph.clear_device_status()
+    graph.replay_commit(steps)
+    assert graph.seq_len(1) == n + steps
+    assert all(torch.equal(a, b) for a, b in zip(eager.read_rows(0), graph.read_rows(1)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rotary_tokens_behind_units_of_different_length(dtype):
+    """After an eviction every unit of a 4-bit cache takes the new tokens behind its own rows, as a plain cache's do."""
+    Hq, Hkv, D, B, n = 4, 2, 128, 3, 40
+    g = torch.Generator().manual_seed(1)
+    new = lambda *s: torch.randn(*s, generator=g).to(DT[dtype]).cuda()  # noqa: E731
+    packed, plain = (SharedKVCache(1, Hq, Hkv, D, B, n + 6, dtype, cache_format=f) for f in ("4bit", "plain"))
+    k, v = new(B, n, Hkv, D), new(B, n, Hkv, D)
+    keep = torch.arange(n, dtype=torch.int32).expand(B, Hkv, n).contiguous().cuda()
+    lens = [7, 40, 1, 23, 39, 16]
+    x, rot = new(B, 3, Hq + 2 * Hkv, D), Rotary.from_theta(D)
+    pos = torch.arange(n, n + 3, dtype=torch.int32).expand(B, 3).contiguous().cuda()
+    for c in (packed, plain):
+        c.append(0, k, v)
+        c.evict(0, keep, lens)
+        c.append_rotary(0, x[:, :, :Hq], x[:, :, Hq:Hq + Hkv], x[:, :, Hq + Hkv:], pos, rot)
+    assert packed.seq_len(0) == 43
+    for a, b in zip(plain.read_rows(0), packed.read_rows(0)):
+        for u, m in enumerate(lens):
+            i, h = divmod(u, Hkv)
+            assert packed.unit_len(0, i, h) == m + 3
+            assert torch.equal(b[i, :m + 3, h].cpu(), ref.values(a[i, :m + 3, h].cpu())) and not b[i, m + 3:, h].any()
+    assert packed.device_status() == 0
